@@ -236,6 +236,17 @@ int echo_score(echo_ctx *ctx, const int32_t *prompts, const int32_t *prompt_lens
                int32_t max_new_tokens, float temperature, const int32_t *tokens, float *out_logprobs,
                int64_t *out_versions);
 
+/* echo_score with what echo_token_logprobs gives beside the log-probability: per token of the given
+ * trajectories the entropy of the distribution it was taken from and its top_k most probable ids.
+ *   out_entropy       dev fp32  [P][G][T] or NULL
+ *   out_top_ids       dev int32 [P][G][T][top_k], out_top_logprobs dev fp32 [P][G][T][top_k]; NULL with
+ *                     top_k = 0; top_k <= 32
+ * Positions after a sequence's end token hold entropy 0, ids -1 and -inf.  Otherwise as echo_score. */
+int echo_score_detail(echo_ctx *ctx, const int32_t *prompts, const int32_t *prompt_lens, int32_t P, int32_t G,
+                      int32_t max_new_tokens, float temperature, const int32_t *tokens, int32_t top_k,
+                      float *out_logprobs, float *out_entropy, int32_t *out_top_ids, float *out_top_logprobs,
+                      int64_t *out_versions);
+
 /* Turn-aware response mask (Appendix F, "Turn-Aware Masking"): with u_t = [x_t == turn_start_id] and
  * c_t = u_0 + ... + u_t, m_t = [c_t > 1] * [c_t odd] selects the tokens of assistant turns after the
  * system prompt.  tokens dev int32 [n][T] -> out_mask dev uint8 [n][T].  With shift_to_targets != 0 the
@@ -285,6 +296,112 @@ int echo_grpo_surrogate(const float *logp_new, const float *logp_old, const floa
 int echo_grpo_objective(const float *logp_new, const float *logp_old, const float *logp_sampler,
                         const float *logp_ref, const float *adv, const uint8_t *mask, int32_t n,
                         int32_t T, float eps_clip, float C, float beta, float *out, void *cuda_stream);
+
+/* ---- the learner's step on what a rollout recorded ------------------------------------------
+ * From the learner's logits to the weights of the next snapshot: log-probabilities of the taken tokens
+ * (echo_token_logprobs), the objective and its gradient per token (echo_grpo_gradient), the gradient of the
+ * logits (echo_token_logprobs_backward), and, once the caller's own backward pass has made the weights'
+ * gradients, the update (echo_adamw_step), whose bf16 copies are what echo_load_policy installs.
+ * These calls need no context.  They are asynchronous on the stream, run on the current device, allocate
+ * no device memory, keep nothing between calls, use no atomics on results (equal inputs give equal
+ * outputs) and can be captured into a CUDA graph.
+ *
+ * Formats: 0 bf16, 1 IEEE half, 2 fp32. */
+
+/* Log-probability of one given token per row of logits (Appendix F: log pi_theta(y_t | x, y_<t)), the
+ * entropy of the row's distribution, and its most probable ids, in one pass over the logits.  With
+ * s_v = (z_v - max z) / temperature and l = sum_v exp(s_v):
+ *   out_logprobs[r] = s_y - log l, y = tokens[r];  out_entropy[r] = log l - sum_v exp(s_v) s_v / l;
+ *   out_stats[r] = (max z, log l);  out_top_ids[r][i], out_top_logprobs[r][i]: the top_k ids by logit,
+ *   largest first, equal logits by the lower id, with their log-probabilities.
+ *   logits        dev [R] rows of V elements, row_stride >= V elements apart (any stride, any alignment
+ *                 of the element type)
+ *   tokens        dev int32 [R]; < 0: the row has no token and scores 0.  An id >= V scores NaN.
+ *   top_k         0 .. 32 (more: ECHO_ERR_UNSUPPORTED)
+ *   out_*         dev fp32 [R], [R], [R][2] (8-byte aligned), int32 / fp32 [R][top_k]; each may be NULL
+ *                 (tokens and out_logprobs together; the top outputs only with top_k = 0)
+ * An id at -inf is masked: probability 0, never among the alternatives.  Places of a row that has fewer
+ * than top_k ids left hold id -1 and -inf.  A row with nothing left (all -inf) scores -inf (0 without a
+ * token), entropy 0, stats (-inf, -inf).  A NaN or +inf logit makes its row's log-probability, entropy
+ * and log l NaN; NaN is never an alternative.  V <= 2^30.  R = 0 does nothing. */
+int echo_token_logprobs(const void *logits, int32_t logits_format, int64_t row_stride, int32_t R, int32_t V,
+                        const int32_t *tokens, float temperature, int32_t top_k, float *out_logprobs,
+                        float *out_entropy, float *out_stats, int32_t *out_top_ids, float *out_top_logprobs,
+                        void *cuda_stream);
+
+/* Its gradient with respect to the logits.  For upstream gradients a of the log-probability and b of the
+ * entropy, with p = softmax(z / temperature) and the row's entropy H:
+ *   out_grad[r][v] = (a ([v = y] - p_v) - b p_v (log p_v + H)) / temperature, in the logits' format.
+ * logits, tokens, temperature as in the forward call, entropy and stats what it returned.
+ *   grad_logprobs  dev fp32 [R] or NULL (needs tokens; ignored in rows without a token)
+ *   grad_entropy   dev fp32 [R] or NULL (needs entropy); one of the two must be given
+ *   out_grad       dev [R] rows of V, grad_stride >= V elements apart.  It may be the logits themselves
+ *                  (same pointer and stride: they are overwritten) and may not overlap them otherwise.
+ * Rows that no gradient reaches (a = b = 0, or no token and b = 0) and rows with nothing left become
+ * zeros whatever their logits hold. */
+int echo_token_logprobs_backward(const void *logits, int32_t logits_format, int64_t row_stride, int32_t R, int32_t V,
+                                 const int32_t *tokens, float temperature, const float *entropy, const float *stats,
+                                 const float *grad_logprobs, const float *grad_entropy, void *out_grad,
+                                 int64_t grad_stride, void *cuda_stream);
+
+/* echo_grpo_objective with its gradient: out[i] as there (logp_ref NULL: without the KL term, as in
+ * echo_grpo_surrogate; beta is then unused), and with respect to logp_new
+ *   out_grad[i][t] = grad_out[i] m_t w_t (slope_t + beta (exp(d_t) - 1)) / sum_t m_t,  d = logp_ref - logp_new,
+ * slope_t = rho_t A_i where the minimum is its unclipped side (A_i > 0: rho_t <= 1 + eps_clip; A_i < 0:
+ * rho_t >= 1 - eps_clip) and 0 elsewhere.  w_t depends on the old and the sampler's policy only and is a
+ * constant.  Tokens that the mask leaves out have gradient 0 whatever their log-probabilities hold.
+ *   grad_out dev fp32 [n] or NULL (all ones), out dev fp32 [n] or NULL, out_grad dev fp32 [n][T]. */
+int echo_grpo_gradient(const float *logp_new, const float *logp_old, const float *logp_sampler, const float *logp_ref,
+                       const float *adv, const uint8_t *mask, const float *grad_out, int32_t n, int32_t T,
+                       float eps_clip, float C, float beta, float *out, float *out_grad, void *cuda_stream);
+
+/* One weight tensor of echo_adamw_step; every pointer is device memory and may have any alignment its
+ * element type allows (32-byte boundaries, 8 bytes for 8-bit moments, are fastest). */
+typedef struct echo_adamw_tensor {
+  float *param;               /* fp32 [n], updated                                                        */
+  const void *grad;           /* [n] in echo_adamw_options.grad_format                                    */
+  void *exp_avg;              /* first moment [n]: fp32, or int8 codes; updated                           */
+  void *exp_avg_sq;           /* second moment [n]: fp32, or uint8 codes; updated                         */
+  float *avg_scales;          /* 8-bit moments: fp32 [ceil(n / 256)], updated; else NULL                  */
+  float *sq_scales;           /* the same for the second moment                                           */
+  void *param_copy;           /* bf16 [n] or NULL: receives the updated weights rounded to bf16, which is
+                                 what echo_load_policy takes                                              */
+  int64_t n;                  /* elements; 0: the entry is passed over                                    */
+  double weight_decay;        /* >= 0, decoupled                                                          */
+} echo_adamw_tensor;
+
+typedef struct echo_adamw_options {
+  double lr, beta1, beta2, eps;   /* lr >= 0; beta1 and beta2 in [0, 1); eps > 0                          */
+  int64_t step;                   /* t >= 1, counts the updates including this one                        */
+  uint64_t seed;                  /* 8-bit moments: key of the rounding's random numbers                  */
+  const float *grad_scale;        /* dev fp32 [1] or NULL: every gradient is multiplied by it (clipping,
+                                     loss scale).  If it is not finite the call changes nothing.          */
+  int32_t grad_format;            /* of every tensor's gradient                                           */
+  int32_t state_bits;             /* 32 or 8                                                              */
+} echo_adamw_options;
+
+/* One AdamW step over a list of tensors in one launch (400 tensors a launch):
+ *   m <- beta1 m + (1 - beta1) g,  v <- beta2 v + (1 - beta2) g^2,
+ *   p <- p (1 - lr weight_decay) - lr m / (1 - beta1^t) / (sqrt(v / (1 - beta2^t)) + eps).
+ * 8-bit moments: blocks of 256 consecutive elements of a tensor share two scales, M the block's largest
+ * |m| and V its largest v as fp32; a first-moment code c in [-127, 127] stands for M (c/127) |c/127| and
+ * takes the nearest value on that axis, a second-moment code c in [0, 255] stands for V (c/255)^4 and takes
+ * the code below or above v at random so that the mean is kept (at least 1 for v > 0).  The random numbers
+ * are 16-bit halves of Philox4x32-10 words: key = seed, counter = (e/8 low, e/8 high, place of the tensor
+ * in the list, step) for element e, low half first.  A block whose largest value is below the smallest
+ * normal fp32 number is stored as zeros; codes 0 with scales 0 are the moments of step 0.  The update of p
+ * uses the moments before they are rounded.  A gradient that is not finite spoils its block's moments.
+ * tensors and opt are host memory, read before the call returns; no two arrays of which one is written may
+ * overlap (ECHO_ERR_INVALID: a tensor listed twice, for instance).  A captured call replays with the step,
+ * the rates and the seed it was captured with. */
+int echo_adamw_step(const echo_adamw_tensor *tensors, int32_t n_tensors, const echo_adamw_options *opt,
+                    void *cuda_stream);
+
+/* The fp32 values that 8-bit moments stand for: out_avg[i], out_avg_sq[i] dev fp32 [n] for every tensor of
+ * the list (host arrays of n_tensors pointers; entries of empty tensors are not read).  Only n and the
+ * moments' fields of the tensors are used. */
+int echo_adamw_unpack(const echo_adamw_tensor *tensors, int32_t n_tensors, float *const *out_avg,
+                      float *const *out_avg_sq, void *cuda_stream);
 
 /* Offset of this context's sequence ids in the noise streams: sequence (p, g) of later rollouts draws
  * from the Philox stream of id base + p*G + g.  Rollout workers are independent and share nothing but

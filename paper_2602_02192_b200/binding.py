@@ -60,6 +60,21 @@ class EchoStats(C.Structure):
     ]
 
 
+class EchoAdamWTensor(C.Structure):
+    _fields_ = [
+        ("param", C.c_void_p), ("grad", C.c_void_p), ("exp_avg", C.c_void_p), ("exp_avg_sq", C.c_void_p),
+        ("avg_scales", C.c_void_p), ("sq_scales", C.c_void_p), ("param_copy", C.c_void_p), ("n", C.c_int64),
+        ("weight_decay", C.c_double),
+    ]
+
+
+class EchoAdamWOptions(C.Structure):
+    _fields_ = [
+        ("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double), ("step", C.c_int64),
+        ("seed", C.c_uint64), ("grad_scale", C.c_void_p), ("grad_format", C.c_int32), ("state_bits", C.c_int32),
+    ]
+
+
 def _load() -> C.CDLL:
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"{LIB_PATH} is missing: build it with `python -m paper_2602_02192_b200.build` "
@@ -104,6 +119,15 @@ def _load() -> C.CDLL:
     lib.echo_grpo_surrogate.restype = C.c_int
     lib.echo_grpo_objective.argtypes = [vp, vp, vp, vp, vp, vp, i32, i32, f32, f32, f32, vp, vp]
     lib.echo_grpo_objective.restype = C.c_int
+    lib.echo_score_detail.argtypes = [vp, vp, vp, i32, i32, i32, f32, vp, i32, vp, vp, vp, vp, vp]
+    lib.echo_token_logprobs.argtypes = [vp, i32, i64, i32, i32, vp, f32, i32, vp, vp, vp, vp, vp, vp]
+    lib.echo_token_logprobs_backward.argtypes = [vp, i32, i64, i32, i32, vp, f32, vp, vp, vp, vp, vp, i64, vp]
+    lib.echo_grpo_gradient.argtypes = [vp, vp, vp, vp, vp, vp, vp, i32, i32, f32, f32, f32, vp, vp, vp]
+    lib.echo_adamw_step.argtypes = [C.POINTER(EchoAdamWTensor), i32, C.POINTER(EchoAdamWOptions), vp]
+    lib.echo_adamw_unpack.argtypes = [C.POINTER(EchoAdamWTensor), i32, C.POINTER(vp), C.POINTER(vp), vp]
+    for name in ("echo_score_detail", "echo_token_logprobs", "echo_token_logprobs_backward", "echo_grpo_gradient",
+                 "echo_adamw_step", "echo_adamw_unpack"):
+        getattr(lib, name).restype = C.c_int
     dbl = C.c_double
     lib.echo_mu_min.argtypes = [dbl, dbl, dbl, dbl, C.POINTER(dbl)]
     lib.echo_staleness_bound.argtypes = [i32, dbl, dbl, dbl, dbl, C.POINTER(i32)]
@@ -154,7 +178,8 @@ EXPORTED = ["echo_arena_bytes", "echo_create", "echo_destroy", "echo_load_policy
             "echo_mu_min", "echo_staleness_bound", "echo_greedy_provision", "echo_admissible",
             "echo_set_sequence_base", "echo_debug_capture", "echo_debug_wait_limit",
             "echo_gemm_bf16_noalloc_status", "echo_probe_read_bandwidth", "echo_peer_score", "echo_chain_assemble",
-            "echo_chain_arrival_time", "echo_score", "echo_turn_mask"]
+            "echo_chain_arrival_time", "echo_score", "echo_turn_mask", "echo_score_detail", "echo_token_logprobs",
+            "echo_token_logprobs_backward", "echo_grpo_gradient", "echo_adamw_step", "echo_adamw_unpack"]
 
 
 def _stream_ptr(stream: Optional[torch.cuda.Stream]) -> int:
@@ -315,6 +340,28 @@ class Engine:
                               tokens.data_ptr(), out_logprobs.data_ptr(), versions.ctypes.data), self._ctx)
         return out_logprobs, versions
 
+    def echo_score_detail(self, prompts: torch.Tensor, prompt_lens: Sequence[int], tokens: torch.Tensor,
+                          temperature: float, top_k: int = 0):
+        """echo_score with the entropy of every token's distribution and its top_k most probable ids: (logprobs
+        [P][G][T], entropy [P][G][T], top_ids int32 and top_logprobs [P][G][T][top_k] (None without), versions)."""
+        P, G, T = tokens.shape
+        assert prompts.dtype == torch.int32 and prompts.is_cuda and prompts.is_contiguous()
+        assert prompts.shape == (P, self.cfg.max_prompt_len)
+        assert tokens.dtype == torch.int32 and tokens.is_cuda and tokens.is_contiguous()
+        lens = np.ascontiguousarray(np.asarray(prompt_lens, dtype=np.int32))
+        assert lens.shape == (P,)
+        logprobs = torch.empty((P, G, T), dtype=torch.float32, device=self.device)
+        entropy = torch.empty_like(logprobs)
+        ids = torch.empty((P, G, T, top_k), dtype=torch.int32, device=self.device) if top_k > 0 else None
+        top = torch.empty((P, G, T, top_k), dtype=torch.float32, device=self.device) if top_k > 0 else None
+        versions = np.zeros((P, G), dtype=np.int64)
+        self.stream.wait_stream(torch.cuda.current_stream(self.device))
+        _check(lib.echo_score_detail(self._ctx, prompts.data_ptr(), lens.ctypes.data, P, G, T, float(temperature),
+                                     tokens.data_ptr(), int(top_k), logprobs.data_ptr(), entropy.data_ptr(),
+                                     ids.data_ptr() if ids is not None else None,
+                                     top.data_ptr() if top is not None else None, versions.ctypes.data), self._ctx)
+        return logprobs, entropy, ids, top, versions
+
     def echo_rollout_host(self, prompts: torch.Tensor, prompt_lens: Sequence[int], G: int, max_new_tokens: int,
                           temperature: float, seed: int, out_tokens: torch.Tensor, out_logprobs: torch.Tensor):
         """All buffers are host tensors (ideally pinned); returns versions.  Synchronous."""
@@ -430,6 +477,190 @@ def echo_grpo_surrogate(logp_new: torch.Tensor, logp_old: torch.Tensor, logp_sam
                                        adv.data_ptr(), mask.data_ptr() if mask is not None else None, n, T,
                                        float(eps_clip), float(C_trunc), out.data_ptr(), _stream_ptr(None)))
     return out
+
+
+# -- the learner's step -----------------------------------------------------------
+_FORMATS = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
+
+
+class _Here:
+    """The current device is already the tensor's."""
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        return False
+
+
+_HERE_DEVICE = _Here()
+
+
+def _on(device: torch.device):
+    """Context in which `device` is the current one (switching costs more than a small launch: only when it is not)."""
+    return _HERE_DEVICE if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+
+
+def _check_rows(logits: torch.Tensor, tokens: Optional[torch.Tensor]):
+    assert logits.is_cuda and logits.dim() == 2 and logits.dtype in _FORMATS
+    R, V = logits.shape
+    assert logits.stride(1) == 1 or V <= 1, "the elements of a row of logits lie side by side"
+    stride = logits.stride(0) if R > 1 else V
+    assert stride >= V, "rows of logits do not overlap"
+    if tokens is not None:
+        assert tokens.device == logits.device and tokens.dtype == torch.int32 and tokens.is_contiguous()
+        assert tokens.shape == (R,)
+    return R, V, stride
+
+
+def _check_vector(x: Optional[torch.Tensor], like: torch.Tensor, shape):
+    if x is None:
+        return None
+    assert x.device == like.device and x.dtype == torch.float32 and x.is_contiguous() and tuple(x.shape) == shape
+    return x.data_ptr()
+
+
+def echo_token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor], temperature: float = 1.0, top_k: int = 0):
+    """Log-probability of one token per row of logits [R][V] (bf16, float16 or fp32; rows may be strided), the row's
+    entropy, and its top_k (at most 32) most probable ids.  tokens int32 [R] (negative: none, scores 0) or None.
+    Returns (logprobs [R] or None, entropy [R], stats [R][2] for the backward call, top_ids int32 [R][top_k] or None,
+    top_logprobs [R][top_k] or None)."""
+    R, V, stride = _check_rows(logits, tokens)
+    dev = logits.device
+    logprobs = torch.empty(R, dtype=torch.float32, device=dev) if tokens is not None else None
+    entropy = torch.empty(R, dtype=torch.float32, device=dev)
+    stats = torch.empty((R, 2), dtype=torch.float32, device=dev)
+    ids = torch.empty((R, top_k), dtype=torch.int32, device=dev) if top_k > 0 else None
+    top = torch.empty((R, top_k), dtype=torch.float32, device=dev) if top_k > 0 else None
+    with _on(dev):
+        _check(lib.echo_token_logprobs(logits.data_ptr(), _FORMATS[logits.dtype], stride, R, V,
+                                       tokens.data_ptr() if tokens is not None else None, temperature, top_k,
+                                       logprobs.data_ptr() if tokens is not None else None, entropy.data_ptr(),
+                                       stats.data_ptr(), ids.data_ptr() if ids is not None else None,
+                                       top.data_ptr() if top is not None else None, _stream_ptr(None)))
+    return logprobs, entropy, stats, ids, top
+
+
+def echo_token_logprobs_backward(logits: torch.Tensor, tokens: Optional[torch.Tensor], entropy: Optional[torch.Tensor],
+                                 stats: torch.Tensor, grad_logprobs: Optional[torch.Tensor] = None,
+                                 grad_entropy: Optional[torch.Tensor] = None, temperature: float = 1.0,
+                                 out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Gradient of the logits from those of the log-probabilities and entropies ([R] each, or None), in the logits'
+    dtype; entropy and stats as echo_token_logprobs returned them.  out: where to (the logits themselves are allowed)."""
+    R, V, stride = _check_rows(logits, tokens)
+    if out is None:
+        out = torch.empty((R, V), dtype=logits.dtype, device=logits.device)
+    assert out.device == logits.device and out.dtype == logits.dtype and out.shape == logits.shape
+    _, _, out_stride = _check_rows(out, None)
+    with _on(logits.device):
+        _check(lib.echo_token_logprobs_backward(
+            logits.data_ptr(), _FORMATS[logits.dtype], stride, R, V, tokens.data_ptr() if tokens is not None else None,
+            temperature, _check_vector(entropy, logits, (R,)), _check_vector(stats, logits, (R, 2)),
+            _check_vector(grad_logprobs, logits, (R,)), _check_vector(grad_entropy, logits, (R,)), out.data_ptr(),
+            out_stride, _stream_ptr(None)))
+    return out
+
+
+def echo_grpo_gradient(logp_new: torch.Tensor, logp_old: torch.Tensor, logp_sampler: torch.Tensor,
+                       logp_ref: Optional[torch.Tensor], adv: torch.Tensor, mask: Optional[torch.Tensor],
+                       grad_out: Optional[torch.Tensor], eps_clip: float, C_trunc: float, beta: float):
+    """echo_grpo_objective (echo_grpo_surrogate where logp_ref is None) and its gradient with respect to logp_new:
+    (objective [n], gradient [n][T]).  grad_out [n] or None (ones): what arrives at the objective."""
+    assert logp_new.is_cuda and logp_new.dim() == 2
+    n, T = logp_new.shape
+    dev = logp_new.device
+    if mask is not None:
+        assert mask.device == dev and mask.dtype == torch.uint8 and mask.is_contiguous() and mask.shape == (n, T)
+    out = torch.empty(n, dtype=torch.float32, device=dev)
+    grad = torch.empty((n, T), dtype=torch.float32, device=dev)
+    with _on(dev):
+        _check(lib.echo_grpo_gradient(
+            _check_vector(logp_new, logp_new, (n, T)), _check_vector(logp_old, logp_new, (n, T)),
+            _check_vector(logp_sampler, logp_new, (n, T)), _check_vector(logp_ref, logp_new, (n, T)),
+            _check_vector(adv, logp_new, (n,)), mask.data_ptr() if mask is not None else None,
+            _check_vector(grad_out, logp_new, (n,)), n, T, eps_clip, C_trunc, beta, out.data_ptr(), grad.data_ptr(),
+            _stream_ptr(None)))
+    return out, grad
+
+
+class AdamWTensors:
+    """The tensors of an AdamW step, as the library's list of addresses (kept alive here).  params fp32, grads bf16,
+    float16 or fp32 (one dtype), exp_avg / exp_avg_sq both fp32, or int8 / uint8 codes with avg_scales and sq_scales
+    (fp32, one per 256 elements of a tensor); copies: bf16 tensors (or None) that receive the updated weights;
+    weight_decay: one number, or one per tensor.  All of them contiguous, on one GPU."""
+    BLOCK = 256
+
+    def __init__(self, params, grads, exp_avg, exp_avg_sq, copies=None, weight_decay=0.0, avg_scales=None, sq_scales=None):
+        n = len(params)
+        assert len(grads) == n and len(exp_avg) == n and len(exp_avg_sq) == n
+        self.device = params[0].device if n else torch.device("cuda", torch.cuda.current_device())
+        self.state_bits = 8 if n and exp_avg[0].dtype == torch.int8 else 32
+        self.grad_format = _FORMATS[grads[0].dtype] if n else 2
+        decay = list(weight_decay) if isinstance(weight_decay, (list, tuple)) else [weight_decay] * n
+        assert len(decay) == n and (copies is None or len(copies) == n)
+        self.sizes = [p.numel() for p in params]
+        self.table = (EchoAdamWTensor * max(n, 1))()
+        first, second = (torch.int8, torch.uint8) if self.state_bits == 8 else (torch.float32, torch.float32)
+
+        def address(x, numel, dtype):
+            assert x.is_cuda and x.device == self.device and x.dtype == dtype and x.is_contiguous() and x.numel() == numel
+            return x.data_ptr()
+
+        for i in range(n):
+            t, size = self.table[i], self.sizes[i]
+            t.param = address(params[i], size, torch.float32)
+            t.grad = address(grads[i], size, grads[0].dtype)
+            t.exp_avg = address(exp_avg[i], size, first)
+            t.exp_avg_sq = address(exp_avg_sq[i], size, second)
+            if self.state_bits == 8:
+                blocks = -(-size // self.BLOCK)
+                t.avg_scales = address(avg_scales[i], blocks, torch.float32)
+                t.sq_scales = address(sq_scales[i], blocks, torch.float32)
+            if copies is not None and copies[i] is not None:
+                t.param_copy = address(copies[i], size, torch.bfloat16)
+            t.n, t.weight_decay = size, decay[i]
+        self.count = n
+        self._keep = (params, grads, exp_avg, exp_avg_sq, copies, avg_scales, sq_scales)
+
+    @classmethod
+    def zeros(cls, params, grads, state_bits: int = 32, copies=None, weight_decay=0.0) -> "AdamWTensors":
+        """The list with moments of its own, all zero (attributes exp_avg, exp_avg_sq and, for 8 bits, avg_scales and
+        sq_scales)."""
+        assert state_bits in (8, 32)
+        first, second = (torch.int8, torch.uint8) if state_bits == 8 else (torch.float32, torch.float32)
+        m = [torch.zeros(p.numel(), dtype=first, device=p.device) for p in params]
+        v = [torch.zeros(p.numel(), dtype=second, device=p.device) for p in params]
+        scales = [None, None]
+        if state_bits == 8:
+            scales = [[torch.zeros(-(-p.numel() // cls.BLOCK), dtype=torch.float32, device=p.device) for p in params]
+                      for _ in range(2)]
+        self = cls(params, grads, m, v, copies, weight_decay, scales[0], scales[1])
+        self.exp_avg, self.exp_avg_sq, self.avg_scales, self.sq_scales = m, v, scales[0], scales[1]
+        return self
+
+
+def echo_adamw_step(tensors: AdamWTensors, step: int, lr: float, beta1: float = 0.9, beta2: float = 0.999,
+                    eps: float = 1e-8, grad_scale: Optional[torch.Tensor] = None, seed: int = 0):
+    """One AdamW step (number `step`, from 1) over every tensor of the list.  grad_scale: fp32 device tensor of one
+    element that multiplies the gradients (if it is not finite nothing changes).  seed: random numbers of the 8-bit
+    second moments."""
+    opt = EchoAdamWOptions(lr, beta1, beta2, eps, step, seed, None, tensors.grad_format, tensors.state_bits)
+    if grad_scale is not None:
+        assert grad_scale.device == tensors.device and grad_scale.dtype == torch.float32 and grad_scale.numel() == 1
+        opt.grad_scale = grad_scale.data_ptr()
+    with _on(tensors.device):
+        _check(lib.echo_adamw_step(tensors.table, tensors.count, C.byref(opt), _stream_ptr(None)))
+
+
+def echo_adamw_unpack(tensors: AdamWTensors, out_avg: Sequence[torch.Tensor], out_avg_sq: Sequence[torch.Tensor]):
+    """Writes the fp32 values that the 8-bit moments of the list stand for into the given tensors."""
+    assert tensors.state_bits == 8 and len(out_avg) == tensors.count and len(out_avg_sq) == tensors.count
+    addresses = []
+    for outs in (out_avg, out_avg_sq):
+        for x, size in zip(outs, tensors.sizes):
+            assert x.device == tensors.device and x.dtype == torch.float32 and x.is_contiguous() and x.numel() == size
+        addresses.append((C.c_void_p * max(tensors.count, 1))(*[x.data_ptr() for x in outs]))
+    with _on(tensors.device):
+        _check(lib.echo_adamw_unpack(tensors.table, tensors.count, addresses[0], addresses[1], _stream_ptr(None)))
 
 
 def echo_probe_read_bandwidth(n_bytes: int = 4 << 30, repeats: int = 10, device="cuda") -> float:

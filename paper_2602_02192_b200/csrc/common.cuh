@@ -258,6 +258,11 @@ cudaError_t first_end_launch(const int32_t *tokens, int B, int T, int eos_id, in
 cudaError_t logprob_rows_launch(const float *logits, int rows, int V, int rows_per_logit_row, float temperature,
                                 const int32_t *tokens, const int32_t *tok_idx, int T, const int32_t *first_end,
                                 float *out, int *status, cudaStream_t s);
+// the same with entropies and top alternatives (logprobs.cu)
+cudaError_t score_detail_launch(const float *logits, int rows, int V, int rows_per_logit_row, float temperature,
+                                const int32_t *tokens, const int32_t *tok_idx, int T, const int32_t *first_end,
+                                float *out, float *out_entropy, int top_k, int32_t *out_ids, float *out_top, int *status,
+                                cudaStream_t s);
 cudaError_t turn_mask_launch(const int32_t *tokens, int n, int T, int turn_start, int shift, uint8_t *out,
                              cudaStream_t s);
 // copies n floats (a multiple of 4) of x into slot (*d_step - 1) of dst

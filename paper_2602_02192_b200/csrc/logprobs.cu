@@ -1,0 +1,1006 @@
+// Log-probabilities of given tokens with entropy and top alternatives, the gradient back to the logits, and the
+// gradient of the clipped objective: the learner's row-wise operators on a [R][V] matrix of logits.
+//
+// With s_v = (z_v - zmax) / T, l = sum_v e^{s_v}:
+//   log p_y = s_y - log l,   H = log l - (1/l) sum_v e^{s_v} s_v,
+//   dL/dz_v = (1/T) [ a (1[v = y] - p_v) - b p_v (log p_v + H) ]   for upstream gradients a of log p_y and b of H.
+// Differences to the maximum are formed before anything is scaled, so a row may sit at any offset, and a row whose
+// every entry is the type's lowest value is an ordinary (uniform) row.  All sums are fp32.
+
+#include <cmath>
+#include <type_traits>
+
+#include "common.cuh"
+#include "ptx.cuh"
+
+namespace echo {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kFarBelow = -1e30f;          // stands for -inf where 0 * -inf would be formed
+
+// ---- element formats: 0 bf16, 1 IEEE half, 2 fp32 ----------------------------------------------
+template <int FMT> struct Fmt { static constexpr int kBytes = FMT == 2 ? 4 : 2, kPerVec = 16 / kBytes; };
+
+template <int FMT> __device__ __forceinline__ float load_elem(const void *p, size_t i) {
+  if (FMT == 2) return static_cast<const float *>(p)[i];
+  return widen16(static_cast<const uint16_t *>(p)[i], FMT == 1);
+}
+template <int FMT> __device__ __forceinline__ void store_elem(void *p, size_t i, float v) {
+  if (FMT == 2) static_cast<float *>(p)[i] = v;
+  else static_cast<uint16_t *>(p)[i] = cvt16(v, FMT == 1);
+}
+// -inf in every lane of a vector: the filling of loads past the end of a row
+template <int FMT> __device__ __forceinline__ uint4 neg_inf_vec() {
+  const uint32_t w = FMT == 2 ? 0xff800000u : FMT == 0 ? 0xff80ff80u : 0xfc00fc00u;
+  return make_uint4(w, w, w, w);
+}
+__device__ __forceinline__ uint4 load_stream(const uint4 *p) {
+  uint4 v;
+  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
+               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+               : "l"(p));
+  return v;
+}
+// the same for memory that this launch also writes (in place)
+__device__ __forceinline__ uint4 load_once(const uint4 *p) {
+  uint4 v;
+  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
+               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+               : "l"(p)
+               : "memory");
+  return v;
+}
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// two fp32 operations in one instruction
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("{.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tadd.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 d;
+  asm("{.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmul.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("{.reg .b64 a, b, c, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\t"
+      "fma.rn.f32x2 d, a, b, c;\n\tmov.b64 {%0, %1}, d;}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
+}
+// elements 2i and 2i+1 of a vector as fp32
+template <int FMT> __device__ __forceinline__ float2 pair_of(const uint4 &v, int i) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  if (FMT == 2) return make_float2(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
+  return widen16x2(w[i], FMT == 1);
+}
+template <int FMT> __device__ __forceinline__ uint32_t max_word(uint32_t a, uint32_t b) {
+  if (FMT == 0) {
+    const __nv_bfloat162 m = __hmax2(*reinterpret_cast<__nv_bfloat162 *>(&a), *reinterpret_cast<__nv_bfloat162 *>(&b));
+    return *reinterpret_cast<const uint32_t *>(&m);
+  }
+  const __half2 m = __hmax2(*reinterpret_cast<__half2 *>(&a), *reinterpret_cast<__half2 *>(&b));
+  return *reinterpret_cast<const uint32_t *>(&m);
+}
+// largest element of N vectors (NaN is passed over)
+template <int FMT, int N> __device__ __forceinline__ float max_of(const uint4 (&v)[N]) {
+  if (FMT == 2) {
+    float m = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      m = fmaxf(fmaxf(m, fmaxf(__uint_as_float(v[i].x), __uint_as_float(v[i].y))),
+                fmaxf(__uint_as_float(v[i].z), __uint_as_float(v[i].w)));
+    return m;
+  }
+  uint32_t m = neg_inf_vec<FMT>().x;
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+    m = max_word<FMT>(m, max_word<FMT>(max_word<FMT>(v[i].x, v[i].y), max_word<FMT>(v[i].z, v[i].w)));
+  const float2 f = widen16x2(m, FMT == 1);
+  return fmaxf(f.x, f.y);
+}
+
+// ---- running statistics of a row --------------------------------------------------------------
+// m: largest logit so far; l = sum 2^x, t = sum 2^x x over x = (z - m) c, c = log2(e) / T.
+struct RowStats {
+  float m, l, t;
+};
+__device__ __forceinline__ void merge(RowStats &a, const RowStats &b, float c) {
+  const float m = fmaxf(a.m, b.m);
+  // -inf - -inf and inf - inf give NaN, which fmaxf turns into "far below": both sums are 0 (or NaN) then
+  const float da = fmaxf((a.m - m) * c, kFarBelow), db = fmaxf((b.m - m) * c, kFarBelow);
+  const float fa = ex2(da), fb = ex2(db);
+  a.t = fa * fmaf(da, a.l, a.t) + fb * fmaf(db, b.l, b.t);
+  a.l = fa * a.l + fb * b.l;
+  a.m = m;
+}
+// moves the reference to a larger maximum
+__device__ __forceinline__ void raise(RowStats &a, float m, float c) {
+  const float d = fmaxf((a.m - m) * c, kFarBelow), f = ex2(d);
+  a.t = f * fmaf(d, a.l, a.t);
+  a.l *= f;
+  a.m = m;
+}
+__device__ __forceinline__ RowStats shfl_stats(const RowStats &a, int o) {
+  return RowStats{__shfl_xor_sync(0xffffffffu, a.m, o), __shfl_xor_sync(0xffffffffu, a.l, o),
+                  __shfl_xor_sync(0xffffffffu, a.t, o)};
+}
+
+// ---- order of the alternatives ----------------------------------------------------------------
+// One 64-bit number per entry: larger logit first, equal ones by the lower id.  0: no entry (-inf and NaN are none).
+__device__ __forceinline__ uint64_t entry_key(float z, uint32_t id) {
+  return (static_cast<uint64_t>(order_key(z + 0.0f)) << 32) | (0xffffffffu - id);      // + 0: -0 equals 0
+}
+__device__ __forceinline__ float key_value(uint64_t key) {
+  const uint32_t u = static_cast<uint32_t>(key >> 32);
+  return __uint_as_float((u & 0x80000000u) ? (u & 0x7fffffffu) : ~u);
+}
+__device__ __forceinline__ bool listable(float z) { return z > -INFINITY; }           // false for NaN
+
+__device__ __forceinline__ float sort_step(float v, int lane, int j, bool descending_block) {
+  const float o = __shfl_xor_sync(0xffffffffu, v, j);
+  const bool lower = (lane & j) == 0;
+  return (lower == descending_block) ? fmaxf(v, o) : fminf(v, o);
+}
+// 32 values of a warp, largest in lane 0
+__device__ __forceinline__ float sort32(float v, int lane) {
+#pragma unroll
+  for (int k = 2; k <= 32; k <<= 1)
+#pragma unroll
+    for (int j = k >> 1; j > 0; j >>= 1) v = sort_step(v, lane, j, (lane & k) == 0 || k == 32);
+  return v;
+}
+// the 32 largest of two descending lists, again descending (b is passed reversed)
+__device__ __forceinline__ float merge32(float a, float b_reversed, int lane) {
+  float v = fmaxf(a, b_reversed);
+#pragma unroll
+  for (int j = 16; j > 0; j >>= 1) v = sort_step(v, lane, j, true);
+  return v;
+}
+
+constexpr int kTopMax = 32;        // alternatives per row
+constexpr int kCandidates = 1024;  // candidates gathered per CTA before the exact selection takes over
+constexpr int kHotPieces = 128;
+constexpr int kUnroll = 4;         // 16-byte vectors per thread and step
+constexpr int kMaxSplit = 8;       // CTAs per row (one cluster)
+constexpr int kMaxVocab = 1 << 30; // element indexes of a row, plus a step, fit 32 bits
+
+struct TopShared {
+  float piece_max[2 * 512];
+  float lists[16][32];
+  uint64_t cand[kCandidates];
+  uint64_t best[kTopMax];                    // this CTA's alternatives, sorted
+  uint64_t gathered[kMaxSplit][kTopMax];     // first CTA of a cluster: everybody's
+  int hot[kHotPieces];
+  uint32_t hist[256];
+  int n_cand, n_hot, need, warp_count[16];
+  uint32_t prefix;
+};
+struct NoTop {};
+
+// What a row of the launch scores and where its results go.  Plain calls: row r of the logits, token tokens[r],
+// outputs at r.  Scoring whole trajectories (T > 0): the row's place in [sequences][T] is flat = tok_idx[r] + 1, or
+// r * T without tok_idx, rows_per_logit_row of them share a logits row, and places after a sequence's first end token
+// hold log-probability 0, entropy 0 and no alternatives.
+struct LogprobArgs {
+  const void *logits;
+  int64_t row_stride;
+  int R, V;
+  const int32_t *tokens;
+  float c, inv_temperature;
+  int top_k;
+  float *out_logprobs, *out_entropy;
+  float2 *out_stats;
+  int32_t *out_top_ids;
+  float *out_top_logprobs;
+  int T, rows_per_logit_row;
+  const int32_t *tok_idx, *first_end;
+  int *status;
+};
+
+// Exact selection of the k first entries of elements [begin, end) of a row, whatever their distribution: radix
+// selection of the k-th largest value, then everything above it and the lowest ids that equal it.  Reached when more
+// candidates than the buffer holds tie with, or sit above, the bound of the one-pass filter (constant rows, sorted
+// rows); it reads the elements six times out of L2.
+template <int FMT, int NT>
+__device__ void select_exact(const void *row, int begin, int end, int k, TopShared &sh) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  if (tid == 0) {
+    sh.n_cand = 0;
+    sh.prefix = 0;
+    sh.need = k;
+  }
+  __syncthreads();
+  bool all = false;                          // fewer than k entries: list them all
+  for (int shift = 24; shift >= 0 && !all; shift -= 8) {
+    for (int i = tid; i < 256; i += NT) sh.hist[i] = 0;
+    __syncthreads();
+    const uint32_t prefix = sh.prefix;
+    for (int base = begin; base < end; base += NT) {          // same trip count in every thread
+      const int i = base + tid;
+      const float z = i < end ? load_elem<FMT>(row, i) : -INFINITY;
+      const uint32_t key = order_key(z + 0.0f);
+      const bool in = listable(z) && (shift == 24 || (key >> (shift + 8)) == (prefix >> (shift + 8)));
+      const int bin = in ? static_cast<int>((key >> shift) & 255u) : -1;
+      const int bin0 = __shfl_sync(0xffffffffu, bin, 0);
+      if (__all_sync(0xffffffffu, bin == bin0)) {             // equal values: one addition for the warp
+        if (lane == 0 && bin0 >= 0) atomicAdd(&sh.hist[bin0], 32u);
+      } else if (bin >= 0) {
+        atomicAdd(&sh.hist[bin], 1u);
+      }
+    }
+    __syncthreads();
+    if (tid == 0) {
+      int need = sh.need, b = 255;
+      while (b >= 0 && static_cast<int>(sh.hist[b]) < need) need -= static_cast<int>(sh.hist[b--]);
+      if (b < 0) sh.need = 0;                                  // only possible in the first pass
+      else {
+        sh.need = need;
+        sh.prefix = prefix | (static_cast<uint32_t>(b) << shift);
+      }
+    }
+    __syncthreads();
+    all = sh.need == 0;
+  }
+  // sh.prefix is the k-th largest key, sh.need how many of the entries equal to it belong to the first k
+  const uint32_t cut = all ? 0u : sh.prefix;
+  const int need = sh.need;
+  int taken = 0;
+  for (int base = begin; base < end; base += NT) {
+    const int i = base + tid;
+    const float z = i < end ? load_elem<FMT>(row, i) : -INFINITY;
+    const uint32_t key = order_key(z + 0.0f);
+    if (listable(z) && key > cut) sh.cand[atomicAdd(&sh.n_cand, 1)] = entry_key(z, i);       // fewer than k <= 32
+    if (taken < need) {                                        // uniform: ids ascend with the thread index
+      const bool eq = listable(z) && key == cut;
+      const unsigned votes = __ballot_sync(0xffffffffu, eq);
+      if (lane == 0) sh.warp_count[warp] = __popc(votes);
+      __syncthreads();
+      int before = taken, total = 0;
+      for (int w = 0; w < NT / 32; ++w) {
+        if (w < warp) before += sh.warp_count[w];
+        total += sh.warp_count[w];
+      }
+      before += __popc(votes & ((1u << lane) - 1u));
+      if (eq && before < need) sh.cand[atomicAdd(&sh.n_cand, 1)] = entry_key(z, i);
+      taken += total;
+      __syncthreads();
+    }
+  }
+  __syncthreads();
+}
+
+// sorts n entries (n <= capacity of src) by counting how many precede each; the first kTopMax go to dst
+__device__ __forceinline__ void rank_entries(const uint64_t *src, int n, uint64_t *dst, int nt) {
+  for (int i = threadIdx.x; i < n; i += nt) {
+    const uint64_t mine = src[i];
+    if (!mine) continue;
+    int rank = 0;
+    for (int j = 0; j < n; ++j) rank += src[j] > mine ? 1 : 0;
+    if (rank < kTopMax) dst[rank] = mine;
+  }
+}
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ uint32_t map_to_first(const void *p) {
+  uint32_t a;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(a) : "r"(ptx::smem_u32(p)));
+  return a;
+}
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
+
+// One cluster of `split` CTAs per row (split = 1: one CTA), each with a contiguous share of the row, one pass.
+// A thread keeps (m, l, t) of its own elements and moves the reference only when a step of its vectors exceeds it.
+// Alternatives cost no second pass: a thread also keeps the maximum of each half of its elements ("pieces"); the k-th
+// largest of these is a lower bound of the k-th largest logit, and only the pieces that reach it, about k of 1024,
+// are looked at again for entries that reach it.
+template <int FMT, int NT, bool TOP>
+__global__ void __launch_bounds__(NT, 1024 / NT)
+token_logprobs_kernel(const __grid_constant__ LogprobArgs a, int split) {
+  constexpr int kPerVec = Fmt<FMT>::kPerVec, kBytes = Fmt<FMT>::kBytes, kWarps = NT / 32;
+  __shared__ RowStats warp_stats[kWarps];
+  __shared__ RowStats cta_stats[kMaxSplit];
+  __shared__ typename std::conditional<TOP, TopShared, NoTop>::type top_mem;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int r = static_cast<int>(blockIdx.x) / split;
+  const int rank = split > 1 ? static_cast<int>(cluster_rank()) : 0;
+  // ---- which token, where to
+  size_t flat = static_cast<size_t>(r);
+  if (a.T > 0) {
+    flat = a.tok_idx ? static_cast<size_t>(a.tok_idx[r]) + 1 : static_cast<size_t>(r) * a.T;
+    if (a.first_end && static_cast<int>(flat % a.T) > a.first_end[flat / a.T]) {
+      if (rank == 0) {                        // the whole cluster leaves here
+        if (tid == 0) {
+          if (a.out_logprobs) a.out_logprobs[flat] = 0.f;
+          if (a.out_entropy) a.out_entropy[flat] = 0.f;
+        }
+        if (TOP && tid < a.top_k) {
+          a.out_top_ids[flat * a.top_k + tid] = -1;
+          a.out_top_logprobs[flat * a.top_k + tid] = -INFINITY;
+        }
+      }
+      return;
+    }
+  }
+  const int token = a.tokens ? a.tokens[flat] : -1;
+  if (token < 0 && !TOP && !a.out_entropy && !a.out_stats) {
+    if (rank == 0 && tid == 0 && a.out_logprobs) a.out_logprobs[flat] = 0.f;
+    return;
+  }
+  if (split > 1) cluster_arrive();            // (waited for below: the first CTA's memory is written by the others)
+  const int zr = a.T > 0 ? r / a.rows_per_logit_row : r;
+  const char *row = static_cast<const char *>(a.logits) + static_cast<size_t>(zr) * a.row_stride * kBytes;
+  // ---- this CTA's share of the row
+  const int share = split > 1 ? ((a.V + split - 1) / split + 63) / 64 * 64 : a.V;
+  const int begin = min(rank * share, a.V), end = min(begin + share, a.V);
+  // elements before the first 16-byte boundary, whole vectors, the rest
+  const int lead = static_cast<int>((16 - (reinterpret_cast<uintptr_t>(row + static_cast<size_t>(begin) * kBytes) & 15)) & 15) / kBytes;
+  const int head = min(lead, end - begin);
+  const int n_vec = (end - begin - head) / kPerVec;
+  const int tail0 = begin + head + n_vec * kPerVec;
+  const uint4 *vec = reinterpret_cast<const uint4 *>(row + static_cast<size_t>(begin + head) * kBytes);
+  const float c = a.c;
+  RowStats st{-INFINITY, 0.f, 0.f};
+
+  auto absorb = [&](const uint4 (&v)[kUnroll]) -> float {
+    const float bm = max_of<FMT>(v);
+    if (bm > st.m) raise(st, bm, c);
+    const float ref = st.m == -INFINITY ? 0.f : st.m;        // nothing but -inf so far: any finite reference does
+    const float2 neg = make_float2(-ref, -ref), cc = make_float2(c, c);
+    float2 l0 = make_float2(st.l, 0.f), t0 = make_float2(st.t, 0.f);
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u)
+#pragma unroll
+      for (int i = 0; i < kPerVec / 2; ++i) {
+        float2 x = mul2(add2(pair_of<FMT>(v[u], i), neg), cc);
+        const float2 e = make_float2(ex2(x.x), ex2(x.y));
+        x.x = fmaxf(x.x, kFarBelow);
+        x.y = fmaxf(x.y, kFarBelow);
+        l0 = add2(l0, e);
+        t0 = fma2(e, x, t0);
+      }
+    st.l = l0.x + l0.y;
+    st.t = t0.x + t0.y;
+    return bm;
+  };
+  auto fetch = [&](uint4 (&v)[kUnroll], int step) {
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      const int i = (step * kUnroll + u) * NT + tid;
+      v[u] = i < n_vec ? load_stream(vec + i) : neg_inf_vec<FMT>();
+    }
+  };
+  auto absorb_one = [&](float z) {
+    if (z > st.m) raise(st, z, c);
+    const float x = (z - (st.m == -INFINITY ? 0.f : st.m)) * c, e = ex2(x);
+    st.l += e;
+    st.t = fmaf(e, fmaxf(x, kFarBelow), st.t);
+  };
+
+  const int steps = (n_vec + NT * kUnroll - 1) / (NT * kUnroll);
+  const int cross = ((steps + 1) / 2 + 1) / 2 * 2;           // first step of a thread's second piece (two steps a turn)
+  {
+    uint4 va[kUnroll], vb[kUnroll];
+    float piece = -INFINITY;
+    fetch(va, 0);
+    // the few elements outside whole vectors, under the first loads' latency
+    if (tid < head) absorb_one(load_elem<FMT>(row, begin + tid));
+    if (tail0 + tid < end) absorb_one(load_elem<FMT>(row, tail0 + tid));
+    for (int s = 0; s < steps; s += 2) {
+      if constexpr (TOP) {
+        if (s == cross) {
+          top_mem.piece_max[tid] = piece;
+          piece = -INFINITY;
+        }
+      }
+      fetch(vb, s + 1);
+      piece = fmaxf(piece, absorb(va));
+      fetch(va, s + 2);
+      if (s + 1 < steps) piece = fmaxf(piece, absorb(vb));
+    }
+    if constexpr (TOP) {
+      TopShared &sh = top_mem;
+      const bool crossed = cross < steps;                    // a second piece was begun
+      if (!crossed) sh.piece_max[tid] = piece;
+      sh.piece_max[NT + tid] = crossed ? piece : -INFINITY;
+    }
+  }
+  // ---- join the threads' statistics
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) merge(st, shfl_stats(st, o), c);
+  if (lane == 0) warp_stats[warp] = st;
+  __syncthreads();
+  if (warp == 0) {
+    st = lane < kWarps ? warp_stats[lane] : RowStats{-INFINITY, 0.f, 0.f};
+#pragma unroll
+    for (int o = kWarps / 2; o > 0; o >>= 1) merge(st, shfl_stats(st, o), c);
+  }
+  // ---- this CTA's alternatives
+  if constexpr (TOP) {
+    TopShared &sh = top_mem;
+    float v = merge32(sort32(sh.piece_max[tid], lane), __shfl_xor_sync(0xffffffffu, sort32(sh.piece_max[NT + tid], lane), 31), lane);
+    sh.lists[warp][lane] = v;
+    if (tid == 0) sh.n_cand = sh.n_hot = 0;
+    if (tid < kTopMax) sh.best[tid] = 0;
+    __syncthreads();
+    for (int d = 1; d < kWarps; d <<= 1) {
+      if ((warp & (2 * d - 1)) == 0) {
+        v = merge32(v, sh.lists[warp + d][31 - lane], lane);
+        sh.lists[warp][lane] = v;
+      }
+      __syncthreads();
+    }
+    const float bound = sh.lists[0][a.top_k - 1];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const float pm = sh.piece_max[h * NT + tid];
+      if (listable(pm) && pm >= bound) {
+        const int at = atomicAdd(&sh.n_hot, 1);
+        if (at < kHotPieces) sh.hot[at] = h * NT + tid;
+      }
+    }
+    __syncthreads();
+    const int n_hot = sh.n_hot;
+    if (n_hot <= kHotPieces) {
+      auto offer = [&](float z, int id) {
+        if (listable(z) && z >= bound) {
+          const int at = atomicAdd(&sh.n_cand, 1);
+          if (at < kCandidates) sh.cand[at] = entry_key(z, static_cast<uint32_t>(id));
+        }
+      };
+      if (tid < head) offer(load_elem<FMT>(row, begin + tid), begin + tid);
+      if (tail0 + tid < end) offer(load_elem<FMT>(row, tail0 + tid), tail0 + tid);
+      const int per = max(cross, steps - cross) * kUnroll;     // vectors of a piece, at most
+      for (int w = tid; w < n_hot * per; w += NT) {
+        const int piece = sh.hot[w / per], h = piece / NT, owner = piece % NT, j = w % per;
+        const int step = h * cross + j / kUnroll;
+        if (step >= (h ? steps : min(cross, steps))) continue;
+        const int i = (step * kUnroll + j % kUnroll) * NT + owner;
+        if (i >= n_vec) continue;
+        const uint4 q = load_stream(vec + i);
+        const int id0 = begin + head + i * kPerVec;
+#pragma unroll
+        for (int e = 0; e < kPerVec / 2; ++e) {
+          const float2 z = pair_of<FMT>(q, e);
+          offer(z.x, id0 + 2 * e);
+          offer(z.y, id0 + 2 * e + 1);
+        }
+      }
+      __syncthreads();
+    }
+    if (n_hot > kHotPieces || sh.n_cand > kCandidates) {
+      __syncthreads();
+      select_exact<FMT, NT>(row, begin, end, a.top_k, sh);
+    }
+    rank_entries(sh.cand, sh.n_cand, sh.best, NT);
+    __syncthreads();
+  }
+  // ---- join the CTAs of the row
+  if (split > 1) {
+    cluster_wait();                          // every CTA of the cluster runs: its shared memory may be written
+    if (tid == 0) {
+      const uint32_t dst = map_to_first(&cta_stats[rank]);
+      asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(dst), "f"(st.m) : "memory");
+      asm volatile("st.shared::cluster.f32 [%0 + 4], %1;" ::"r"(dst), "f"(st.l) : "memory");
+      asm volatile("st.shared::cluster.f32 [%0 + 8], %1;" ::"r"(dst), "f"(st.t) : "memory");
+    }
+    if constexpr (TOP) {
+      if (tid < kTopMax)
+        asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(map_to_first(&top_mem.gathered[rank][tid])),
+                     "l"(top_mem.best[tid])
+                     : "memory");
+    }
+    cluster_arrive();
+    cluster_wait();
+    if (rank != 0) return;
+    if constexpr (TOP) {
+      TopShared &sh = top_mem;
+      if (tid < kTopMax) sh.best[tid] = 0;
+      __syncthreads();
+      rank_entries(&sh.gathered[0][0], split * kTopMax, sh.best, NT);
+      __syncthreads();
+    }
+    if (warp == 0) {
+      st = lane < split ? cta_stats[lane] : RowStats{-INFINITY, 0.f, 0.f};
+#pragma unroll
+      for (int o = kMaxSplit / 2; o > 0; o >>= 1) merge(st, shfl_stats(st, o), c);
+    }
+  }
+  if (warp != 0) return;
+  st.m = __shfl_sync(0xffffffffu, st.m, 0);
+  st.l = __shfl_sync(0xffffffffu, st.l, 0);
+  st.t = __shfl_sync(0xffffffffu, st.t, 0);
+  const bool empty = st.l == 0.f;                             // nothing left in the row (all -inf)
+  const float log_l = logf(st.l);
+  if (lane == 0) {
+    if (a.out_logprobs) {
+      float lp = 0.f;
+      if (token >= a.V) {
+        lp = NAN;
+        if (a.status) atomicExch(a.status, STATUS_BAD_TOKEN);
+      } else if (token >= 0) {
+        lp = empty ? -INFINITY : (load_elem<FMT>(row, token) - st.m) * a.inv_temperature - log_l;
+      }
+      a.out_logprobs[flat] = lp;
+    }
+    if (a.out_entropy) a.out_entropy[flat] = empty ? 0.f : log_l - kLn2 * (st.t / st.l);
+    if (a.out_stats) a.out_stats[flat] = make_float2(st.m, log_l);
+  }
+  if constexpr (TOP) {
+    if (lane < a.top_k) {
+      const uint64_t key = top_mem.best[lane];
+      const size_t o = flat * a.top_k + lane;
+      a.out_top_ids[o] = key ? static_cast<int32_t>(0xffffffffu - static_cast<uint32_t>(key)) : -1;
+      a.out_top_logprobs[o] = key ? (key_value(key) - st.m) * a.inv_temperature - log_l : -INFINITY;
+    }
+  }
+}
+
+template <int FMT, int NT>
+cudaError_t launch_logprobs(const LogprobArgs &a, int split, cudaStream_t s) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>(a.R) * split);
+  cfg.blockDim = dim3(NT);
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = split;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = split > 1 ? 1 : 0;
+  return a.top_k > 0 ? cudaLaunchKernelEx(&cfg, token_logprobs_kernel<FMT, NT, true>, a, split)
+                     : cudaLaunchKernelEx(&cfg, token_logprobs_kernel<FMT, NT, false>, a, split);
+}
+template <int FMT>
+cudaError_t launch_logprobs_fmt(const LogprobArgs &a, int split, bool wide, cudaStream_t s) {
+  return wide ? launch_logprobs<FMT, 512>(a, split, s) : launch_logprobs<FMT, 128>(a, split, s);
+}
+
+cudaError_t logprobs_launch(const LogprobArgs &a, int format, cudaStream_t s) {
+  int dev = 0, sms = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+  if (e != cudaSuccess) return e;
+  const int64_t row_vecs = static_cast<int64_t>(a.V) * (format == 2 ? 4 : 2) / 16;
+  // 512 threads take 2048 vectors a step; rows of less than two steps of 128 threads leave most of them idle
+  const bool wide = row_vecs > 1024;
+  int split = 1;
+  while (split < kMaxSplit && static_cast<int64_t>(a.R) * split < 2 * sms && row_vecs / (2 * split) >= 512) split *= 2;
+  switch (format) {
+    case 0: return launch_logprobs_fmt<0>(a, split, wide, s);
+    case 1: return launch_logprobs_fmt<1>(a, split, wide, s);
+    default: return launch_logprobs_fmt<2>(a, split, wide, s);
+  }
+}
+
+// ---- gradient -----------------------------------------------------------------------------------
+struct BackwardArgs {
+  const void *logits;
+  int64_t row_stride;
+  int R, V;
+  const int32_t *tokens;
+  float c, inv_temperature;
+  const float *entropy;
+  const float2 *stats;
+  const float *grad_logprobs, *grad_entropy;
+  void *out;
+  int64_t out_stride;
+};
+// dz_v = -p_v (A + B log2 p_v) + [v = y] a / T, with A = (a + b H) / T, B = b ln 2 / T, log2 p = (z - m) c - log2 l.
+struct RowGrad {
+  float m, log2_l, A, B, hot;
+  int token;
+};
+template <bool ENT> __device__ __forceinline__ float2 grad_pair(float2 z, const RowGrad &g, float c) {
+  float2 x = mul2(add2(z, make_float2(-g.m, -g.m)), make_float2(c, c));
+  x = add2(x, make_float2(-g.log2_l, -g.log2_l));
+  const float2 p = make_float2(ex2(x.x), ex2(x.y));
+  if (!ENT) return mul2(p, make_float2(-g.A, -g.A));
+  x.x = fmaxf(x.x, kFarBelow);
+  x.y = fmaxf(x.y, kFarBelow);
+  return mul2(p, fma2(x, make_float2(-g.B, -g.B), make_float2(-g.A, -g.A)));
+}
+template <int FMT> __device__ __forceinline__ uint4 pack_vec(const float (&f)[Fmt<FMT>::kPerVec]) {
+  if constexpr (FMT == 2) {
+    return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+  } else {
+    return make_uint4(cvt16x2(f[0], f[1], FMT == 1), cvt16x2(f[2], f[3], FMT == 1), cvt16x2(f[4], f[5], FMT == 1),
+                      cvt16x2(f[6], f[7], FMT == 1));
+  }
+}
+// 16 bytes that start `bytes` (a multiple of 2) into the 32 bytes lo, hi
+__device__ __forceinline__ uint4 bytes_from(const uint4 &lo, const uint4 &hi, int bytes) {
+  const uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+  uint32_t o[4];
+  const int words = bytes >> 2, bits = (bytes & 3) * 8;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    uint32_t x = 0, y = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (words == j) {
+        x = w[i + j];
+        y = w[i + j + 1];
+      }
+    o[i] = __funnelshift_r(x, y, bits);
+  }
+  return make_uint4(o[0], o[1], o[2], o[3]);
+}
+
+constexpr int kBackThreads = 256, kBackUnroll = 4;
+
+template <int FMT, bool ENT>
+__device__ __forceinline__ void backward_row(const BackwardArgs &a, const RowGrad &g, const char *zrow, char *orow,
+                                             int begin, int end) {
+  constexpr int kPerVec = Fmt<FMT>::kPerVec, kBytes = Fmt<FMT>::kBytes;
+  const int tid = threadIdx.x;
+  const float c = a.c;
+  auto one = [&](int i) {
+    const float z = load_elem<FMT>(zrow, i);
+    float d = grad_pair<ENT>(make_float2(z, z), g, c).x;
+    if (i == g.token) d += g.hot;
+    store_elem<FMT>(orow, i, d);
+  };
+  // whole 16-byte vectors of the output; where the logits lie differently on 16-byte boundaries (a padded or offset
+  // row beside a dense output) a vector is cut out of the two aligned ones around it, both inside the row
+  const int off = static_cast<int>((reinterpret_cast<uintptr_t>(orow + static_cast<size_t>(begin) * kBytes)) & 15);
+  int head = min(((16 - off) & 15) / kBytes, end - begin);
+  int skew = static_cast<int>(reinterpret_cast<uintptr_t>(zrow + static_cast<size_t>(begin + head) * kBytes) & 15);
+  if (skew && begin + head - skew / kBytes < 0) {             // first aligned vector would begin before the row
+    head = min(head + kPerVec, end - begin);
+  }
+  int n_vec = (end - begin - head) / kPerVec;
+  if (skew && n_vec > 0 && begin + head + n_vec * kPerVec + kPerVec - skew / kBytes > a.V) --n_vec;
+  const int tail0 = begin + head + n_vec * kPerVec;
+  for (int i = begin + tid; i < begin + head; i += kBackThreads) one(i);
+  for (int i = tail0 + tid; i < end; i += kBackThreads) one(i);
+  const uint4 *zv = reinterpret_cast<const uint4 *>(zrow + static_cast<size_t>(begin + head) * kBytes - skew);
+  uint4 *ov = reinterpret_cast<uint4 *>(orow + static_cast<size_t>(begin + head) * kBytes);
+  for (int base = 0; base < n_vec; base += kBackThreads * kBackUnroll) {
+    uint4 q[kBackUnroll];
+#pragma unroll
+    for (int u = 0; u < kBackUnroll; ++u) {
+      const int i = base + u * kBackThreads + tid;
+      if (i >= n_vec) continue;
+      q[u] = load_once(zv + i);
+      if (skew) q[u] = bytes_from(q[u], load_once(zv + i + 1), skew);
+    }
+#pragma unroll
+    for (int u = 0; u < kBackUnroll; ++u) {
+      const int i = base + u * kBackThreads + tid;
+      if (i >= n_vec) continue;
+      float f[kPerVec];
+#pragma unroll
+      for (int e = 0; e < kPerVec / 2; ++e) {
+        const float2 d = grad_pair<ENT>(pair_of<FMT>(q[u], e), g, c);
+        f[2 * e] = d.x;
+        f[2 * e + 1] = d.y;
+      }
+      const int at = g.token - (begin + head + i * kPerVec);
+      if (at >= 0 && at < kPerVec) {
+#pragma unroll
+        for (int e = 0; e < kPerVec; ++e)
+          if (e == at) f[e] += g.hot;
+      }
+      __stcs(ov + i, pack_vec<FMT>(f));
+    }
+  }
+}
+
+// grid: (row, slice of the row); every thread of a CTA works on the same row
+template <int FMT>
+__global__ void __launch_bounds__(kBackThreads)
+token_logprobs_backward_kernel(const __grid_constant__ BackwardArgs a, int slices, int slice_elems) {
+  constexpr int kBytes = Fmt<FMT>::kBytes;
+  const int r = static_cast<int>(blockIdx.x / slices), slice = static_cast<int>(blockIdx.x % slices);
+  const int begin = slice * slice_elems, end = min(begin + slice_elems, a.V);
+  const char *zrow = static_cast<const char *>(a.logits) + static_cast<size_t>(r) * a.row_stride * kBytes;
+  char *orow = static_cast<char *>(a.out) + static_cast<size_t>(r) * a.out_stride * kBytes;
+  RowGrad g;
+  g.token = a.tokens ? a.tokens[r] : -1;
+  const float2 st = a.stats[r];
+  const float ga = (a.grad_logprobs && g.token >= 0) ? a.grad_logprobs[r] : 0.f;
+  const float gb = a.grad_entropy ? a.grad_entropy[r] : 0.f;
+  if ((ga == 0.f && gb == 0.f) || st.y == -INFINITY) {
+    // no gradient arrives, or nothing is left in the row: zeros, and the logits are not read
+    const int off = static_cast<int>(reinterpret_cast<uintptr_t>(orow + static_cast<size_t>(begin) * kBytes) & 15);
+    const int head = min(((16 - off) & 15) / kBytes, end - begin);
+    const int n_vec = (end - begin - head) / Fmt<FMT>::kPerVec;
+    for (int i = begin + threadIdx.x; i < begin + head; i += kBackThreads) store_elem<FMT>(orow, i, 0.f);
+    uint4 *ov = reinterpret_cast<uint4 *>(orow + static_cast<size_t>(begin + head) * kBytes);
+    for (int i = threadIdx.x; i < n_vec; i += kBackThreads) __stcs(ov + i, make_uint4(0u, 0u, 0u, 0u));
+    for (int i = begin + head + n_vec * Fmt<FMT>::kPerVec + threadIdx.x; i < end; i += kBackThreads)
+      store_elem<FMT>(orow, i, 0.f);
+    return;
+  }
+  g.m = st.x;
+  g.log2_l = st.y * kLog2e;
+  g.hot = ga * a.inv_temperature;
+  g.A = (gb != 0.f ? fmaf(gb, a.entropy[r], ga) : ga) * a.inv_temperature;
+  g.B = gb * kLn2 * a.inv_temperature;
+  if (gb != 0.f) backward_row<FMT, true>(a, g, zrow, orow, begin, end);
+  else backward_row<FMT, false>(a, g, zrow, orow, begin, end);
+}
+
+template <int FMT> cudaError_t launch_backward(const BackwardArgs &a, int slices, int slice_elems, cudaStream_t s) {
+  token_logprobs_backward_kernel<FMT><<<static_cast<unsigned>(a.R) * slices, kBackThreads, 0, s>>>(a, slices, slice_elems);
+  return cudaGetLastError();
+}
+
+// ---- gradient of the clipped objective ----------------------------------------------------------
+struct GrpoGradArgs {
+  const float *ln, *lo, *ls, *lr, *adv;
+  const uint8_t *mask;
+  const float *grad_out;
+  int n, T;
+  float eps_clip, C, beta;
+  double log_hi, log_lo;       // log(1 + eps), log(1 - eps) (-inf if eps >= 1)
+  float *out, *grad;
+};
+// sum over the NT threads that share a sequence (a warp, or the whole block)
+template <int NT> __device__ __forceinline__ float team_sum(float v, float *scratch) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  if (NT == 32) return v;
+  __syncthreads();
+  if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = v;
+  __syncthreads();
+  v = 0.f;
+#pragma unroll
+  for (int w = 0; w < NT / 32; ++w) v += scratch[w];
+  return v;
+}
+struct GrpoToken {
+  float term, slope;           // both times the truncated weight
+};
+// The clipped term's slope is rho A where the minimum is the unclipped side (A > 0: rho <= 1 + eps; A < 0:
+// rho >= 1 - eps), else 0; which side it is goes by the exact difference ln - lo, since the slope jumps there.
+__device__ __forceinline__ GrpoToken grpo_token(const GrpoGradArgs &a, float A, float ln, float lo, float ls, float lr) {
+  const float rho = expf(ln - lo);
+  const float w = fminf(expf(lo - ls), a.C);
+  const float clipped = fminf(fmaxf(rho, 1.0f - a.eps_clip), 1.0f + a.eps_clip);
+  const double x = static_cast<double>(ln) - static_cast<double>(lo);
+  const bool flat = A > 0.f ? x > a.log_hi : x < a.log_lo;
+  float term = fminf(rho * A, clipped * A);
+  float slope = flat ? 0.f : rho * A;
+  if (a.lr) {
+    const float d = lr - ln, k = expm1f(d);
+    term -= a.beta * (k - d);
+    slope = fmaf(a.beta, k, slope);
+  }
+  return {w * term, w * slope};
+}
+// NT threads per sequence: a warp (several sequences a block) or a block.  VEC: rows are read as float4 / uchar4.
+template <int NT, bool VEC>
+__global__ void __launch_bounds__(NT == 32 ? 128 : NT)
+grpo_gradient_kernel(const __grid_constant__ GrpoGradArgs a) {
+  __shared__ float scratch[32];
+  const int i = NT == 32 ? static_cast<int>(blockIdx.x) * 4 + (threadIdx.x >> 5) : static_cast<int>(blockIdx.x);
+  if (i >= a.n) return;
+  const int t0 = NT == 32 ? (threadIdx.x & 31) : threadIdx.x;
+  const size_t base = static_cast<size_t>(i) * a.T;
+  const float A = a.adv[i], up = a.grad_out ? a.grad_out[i] : 1.0f;
+  float count = static_cast<float>(a.T);
+  if (a.mask) {
+    int c = 0;
+    if (VEC) {
+      const uint32_t *m4 = reinterpret_cast<const uint32_t *>(a.mask + base);
+      for (int t = t0; t < a.T / 4; t += NT) c += __popc(__vcmpne4(m4[t], 0u)) >> 3;
+    } else {
+      for (int t = t0; t < a.T; t += NT) c += a.mask[base + t] ? 1 : 0;
+    }
+    count = team_sum<NT>(static_cast<float>(c), scratch);
+  }
+  const float share = count > 0.f ? 1.0f / count : 0.f, scale = up * share;
+  float value = 0.f;
+  if (VEC) {
+    for (int t = t0; t < a.T / 4; t += NT) {
+      const size_t q = base / 4 + t;
+      const uint32_t m = a.mask ? reinterpret_cast<const uint32_t *>(a.mask)[q] : 0x01010101u;
+      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (m) {
+        const float4 ln = reinterpret_cast<const float4 *>(a.ln)[q], lo = reinterpret_cast<const float4 *>(a.lo)[q],
+                     ls = reinterpret_cast<const float4 *>(a.ls)[q];
+        const float4 lr = a.lr ? reinterpret_cast<const float4 *>(a.lr)[q] : ln;
+        const float *pn = &ln.x, *po = &lo.x, *ps = &ls.x, *pr = &lr.x;
+        float *pg = &o.x;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if ((m >> (8 * e)) & 0xffu) {
+            const GrpoToken k = grpo_token(a, A, pn[e], po[e], ps[e], pr[e]);
+            value += k.term;
+            pg[e] = k.slope * scale;
+          }
+      }
+      reinterpret_cast<float4 *>(a.grad)[q] = o;
+    }
+  } else {
+    for (int t = t0; t < a.T; t += NT) {
+      float o = 0.f;
+      if (!a.mask || a.mask[base + t]) {
+        const float ln = a.ln[base + t];
+        const GrpoToken k = grpo_token(a, A, ln, a.lo[base + t], a.ls[base + t], a.lr ? a.lr[base + t] : ln);
+        value += k.term;
+        o = k.slope * scale;
+      }
+      a.grad[base + t] = o;
+    }
+  }
+  if (a.out) {
+    value = team_sum<NT>(value, scratch);
+    if (t0 == 0) a.out[i] = value * share;
+  }
+}
+
+bool aligned(const void *p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+
+}  // namespace
+
+cudaError_t score_detail_launch(const float *logits, int rows, int V, int rows_per_logit_row, float temperature,
+                                const int32_t *tokens, const int32_t *tok_idx, int T, const int32_t *first_end,
+                                float *out, float *out_entropy, int top_k, int32_t *out_ids, float *out_top, int *status,
+                                cudaStream_t s) {
+  if (rows <= 0) return cudaSuccess;
+  LogprobArgs a{};
+  a.logits = logits;
+  a.row_stride = V;
+  a.R = rows;
+  a.V = V;
+  a.tokens = tokens;
+  a.c = static_cast<float>(1.4426950408889634 / temperature);
+  a.inv_temperature = static_cast<float>(1.0 / temperature);
+  a.top_k = top_k;
+  a.out_logprobs = out;
+  a.out_entropy = out_entropy;
+  a.out_top_ids = out_ids;
+  a.out_top_logprobs = out_top;
+  a.T = T;
+  a.rows_per_logit_row = rows_per_logit_row;
+  a.tok_idx = tok_idx;
+  a.first_end = first_end;
+  a.status = status;
+  return logprobs_launch(a, 2, s);
+}
+
+}  // namespace echo
+
+// ============================================================================
+// C ABI
+// ============================================================================
+using namespace echo;
+
+namespace {
+int elem_bytes(int32_t format) { return format == 2 ? 4 : 2; }
+// logits shapes and temperature of both directions
+bool logits_ok(const void *logits, int32_t format, int64_t row_stride, int32_t R, int32_t V, float temperature) {
+  if (!logits || format < 0 || format > 2 || R < 0 || V < 1 || row_stride < V) return false;
+  if (reinterpret_cast<uintptr_t>(logits) % elem_bytes(format)) return false;
+  return temperature > 0.f && std::isfinite(temperature) && std::isfinite(static_cast<float>(1.4426950408889634 / temperature));
+}
+}  // namespace
+
+extern "C" {
+
+int echo_token_logprobs(const void *logits, int32_t logits_format, int64_t row_stride, int32_t R, int32_t V,
+                        const int32_t *tokens, float temperature, int32_t top_k, float *out_logprobs,
+                        float *out_entropy, float *out_stats, int32_t *out_top_ids, float *out_top_logprobs,
+                        void *cuda_stream) {
+  if (R == 0) return ECHO_OK;
+  if (!logits_ok(logits, logits_format, row_stride, R, V, temperature)) return ECHO_ERR_INVALID;
+  if ((tokens == nullptr) != (out_logprobs == nullptr)) return ECHO_ERR_INVALID;
+  if (top_k < 0 || (top_k > 0 && (!out_top_ids || !out_top_logprobs))) return ECHO_ERR_INVALID;
+  if (!out_logprobs && !out_entropy && !out_stats && top_k == 0) return ECHO_ERR_INVALID;
+  if (!aligned(out_stats, 8)) return ECHO_ERR_INVALID;
+  if (top_k > kTopMax || V > kMaxVocab || static_cast<int64_t>(R) * kMaxSplit > 0x7fffffffLL) return ECHO_ERR_UNSUPPORTED;
+  LogprobArgs a{};
+  a.logits = logits;
+  a.row_stride = row_stride;
+  a.R = R;
+  a.V = V;
+  a.tokens = tokens;
+  a.c = static_cast<float>(1.4426950408889634 / temperature);
+  a.inv_temperature = static_cast<float>(1.0 / temperature);
+  a.top_k = top_k;
+  a.out_logprobs = out_logprobs;
+  a.out_entropy = out_entropy;
+  a.out_stats = reinterpret_cast<float2 *>(out_stats);
+  a.out_top_ids = out_top_ids;
+  a.out_top_logprobs = out_top_logprobs;
+  return logprobs_launch(a, logits_format, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? ECHO_OK : ECHO_ERR_CUDA;
+}
+
+int echo_token_logprobs_backward(const void *logits, int32_t logits_format, int64_t row_stride, int32_t R, int32_t V,
+                                 const int32_t *tokens, float temperature, const float *entropy, const float *stats,
+                                 const float *grad_logprobs, const float *grad_entropy, void *out_grad,
+                                 int64_t grad_stride, void *cuda_stream) {
+  if (R == 0) return ECHO_OK;
+  if (!logits_ok(logits, logits_format, row_stride, R, V, temperature)) return ECHO_ERR_INVALID;
+  if (!out_grad || !stats || !aligned(stats, 8) || grad_stride < V) return ECHO_ERR_INVALID;
+  if (!grad_logprobs && !grad_entropy) return ECHO_ERR_INVALID;
+  if ((grad_logprobs && !tokens) || (grad_entropy && !entropy)) return ECHO_ERR_INVALID;
+  const size_t eb = elem_bytes(logits_format);
+  if (reinterpret_cast<uintptr_t>(out_grad) % eb) return ECHO_ERR_INVALID;
+  // in place (the same rows), or apart
+  const uintptr_t z0 = reinterpret_cast<uintptr_t>(logits), o0 = reinterpret_cast<uintptr_t>(out_grad);
+  const uintptr_t z1 = z0 + (static_cast<size_t>(R - 1) * row_stride + V) * eb, o1 = o0 + (static_cast<size_t>(R - 1) * grad_stride + V) * eb;
+  if (z0 < o1 && o0 < z1 && !(z0 == o0 && (row_stride == grad_stride || R == 1))) return ECHO_ERR_INVALID;
+  // a CTA takes two steps of its threads' vectors: long enough to cover its start, short enough to spread few rows
+  const int slice = kBackThreads * kBackUnroll * 2 * (16 / static_cast<int>(eb));
+  const int64_t slices = (static_cast<int64_t>(V) + slice - 1) / slice;
+  if (V > kMaxVocab || static_cast<int64_t>(R) * slices > 0x7fffffffLL) return ECHO_ERR_UNSUPPORTED;
+  BackwardArgs a{};
+  a.logits = logits;
+  a.row_stride = row_stride;
+  a.R = R;
+  a.V = V;
+  a.tokens = tokens;
+  a.c = static_cast<float>(1.4426950408889634 / temperature);
+  a.inv_temperature = static_cast<float>(1.0 / temperature);
+  a.entropy = entropy;
+  a.stats = reinterpret_cast<const float2 *>(stats);
+  a.grad_logprobs = grad_logprobs;
+  a.grad_entropy = grad_entropy;
+  a.out = out_grad;
+  a.out_stride = grad_stride;
+  cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+  cudaError_t e = logits_format == 0   ? launch_backward<0>(a, static_cast<int>(slices), slice, s)
+                  : logits_format == 1 ? launch_backward<1>(a, static_cast<int>(slices), slice, s)
+                                       : launch_backward<2>(a, static_cast<int>(slices), slice, s);
+  return e == cudaSuccess ? ECHO_OK : ECHO_ERR_CUDA;
+}
+
+int echo_grpo_gradient(const float *logp_new, const float *logp_old, const float *logp_sampler, const float *logp_ref,
+                       const float *adv, const uint8_t *mask, const float *grad_out, int32_t n, int32_t T,
+                       float eps_clip, float C, float beta, float *out, float *out_grad, void *cuda_stream) {
+  if (!logp_new || !logp_old || !logp_sampler || !adv || !out_grad || n < 0 || T < 1) return ECHO_ERR_INVALID;
+  if (!(eps_clip >= 0.f) || !(C > 0.f) || !(beta >= 0.f)) return ECHO_ERR_INVALID;
+  if (n == 0) return ECHO_OK;
+  GrpoGradArgs a{};
+  a.ln = logp_new;
+  a.lo = logp_old;
+  a.ls = logp_sampler;
+  a.lr = logp_ref;
+  a.adv = adv;
+  a.mask = mask;
+  a.grad_out = grad_out;
+  a.n = n;
+  a.T = T;
+  a.eps_clip = eps_clip;
+  a.C = C;
+  a.beta = beta;
+  a.log_hi = std::log1p(static_cast<double>(eps_clip));
+  a.log_lo = eps_clip < 1.f ? std::log1p(-static_cast<double>(eps_clip)) : -INFINITY;
+  a.out = out;
+  a.grad = out_grad;
+  const bool vec = T % 4 == 0 && aligned(logp_new, 16) && aligned(logp_old, 16) && aligned(logp_sampler, 16) &&
+                   aligned(logp_ref, 16) && aligned(out_grad, 16) && aligned(mask, 4);
+  cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+  if (T <= 256) {
+    const unsigned grid = (static_cast<unsigned>(n) + 3) / 4;
+    if (vec) grpo_gradient_kernel<32, true><<<grid, 128, 0, s>>>(a);
+    else grpo_gradient_kernel<32, false><<<grid, 128, 0, s>>>(a);
+  } else {
+    if (vec) grpo_gradient_kernel<512, true><<<n, 512, 0, s>>>(a);
+    else grpo_gradient_kernel<512, false><<<n, 512, 0, s>>>(a);
+  }
+  return cudaGetLastError() == cudaSuccess ? ECHO_OK : ECHO_ERR_CUDA;
+}
+
+}  // extern "C"

@@ -1394,8 +1394,16 @@ int rollout_queue_impl(echo_ctx *ctx, const int32_t *prompts, const int32_t *pro
 // every sequence's given tokens as rows of 2048-row chunks (sequence-major), each chunk through the
 // layers with causal attention over the paged cache, the lm_head and the log-probability kernel in
 // blocks of at most P*G rows (the logits buffer).
+// `detail`: entropies and top alternatives as well (the log-probabilities then come from the same kernel).
+struct ScoreDetail {
+  float *entropy;
+  int top_k;
+  int32_t *top_ids;
+  float *top_logprobs;
+};
 int score_impl(echo_ctx *ctx, const int32_t *prompts, const int32_t *prompt_lens, int P, int G, int T,
-               float temperature, const int32_t *tokens, float *out_logprobs, int64_t *out_versions) {
+               float temperature, const int32_t *tokens, float *out_logprobs, int64_t *out_versions,
+               const ScoreDetail *detail = nullptr) {
   if (!ctx || !prompts || !prompt_lens || !tokens || !out_logprobs || !out_versions) return ECHO_ERR_INVALID;
   const Limits &M = ctx->M;
   if (P < 1 || P > M.P || G < 1 || G > M.G || T < 1 || T > M.T) return ECHO_ERR_INVALID;
@@ -1430,8 +1438,15 @@ int score_impl(echo_ctx *ctx, const int32_t *prompts, const int32_t *prompt_lens
   TRY(run_prefill(ctx, w, pl, prompts));
   // token 0 of every sample: scored on the prompt's last logits row
   TRY(lm_head(ctx, w, ctx->ptr<float>(lo.xlast), P));
-  LAUNCH(logprob_rows_launch(logits, pl.B, D.V, G, temperature, tokens, nullptr, T, first_end, out_logprobs, status,
-                             ctx->stream));
+  auto score_rows = [&](int rows, int rows_per_logit_row, const int32_t *idx) {
+    if (detail)
+      return score_detail_launch(logits, rows, D.V, rows_per_logit_row, temperature, tokens, idx, T, first_end,
+                                 out_logprobs, detail->entropy, detail->top_k, detail->top_ids, detail->top_logprobs,
+                                 status, ctx->stream);
+    return logprob_rows_launch(logits, rows, D.V, rows_per_logit_row, temperature, tokens, idx, T, first_end,
+                               out_logprobs, status, ctx->stream);
+  };
+  LAUNCH(score_rows(pl.B, G, nullptr));
   CK(cudaEventRecord(ctx->ev_first, ctx->stream));
   // tokens 1..T-1: row (s, j) feeds given token j at position len0[s] + j and scores token j + 1
   const long n_rows = static_cast<long>(pl.B) * (T - 1);
@@ -1448,8 +1463,7 @@ int score_impl(echo_ctx *ctx, const int32_t *prompts, const int32_t *prompt_lens
     for (int sub = 0; sub < R; sub += pl.B) {
       const int rows = std::min(pl.B, R - sub);
       TRY(lm_head(ctx, w, x + static_cast<size_t>(sub) * D.d, rows));
-      LAUNCH(logprob_rows_launch(logits, rows, D.V, 1, temperature, tokens, tok_idx + sub, T, first_end, out_logprobs,
-                                 status, ctx->stream));
+      LAUNCH(score_rows(rows, 1, tok_idx + sub));
     }
   }
   CK(cudaEventRecord(ctx->ev_end, ctx->stream));
@@ -1756,6 +1770,16 @@ int echo_score(echo_ctx *ctx, const int32_t *prompts, const int32_t *prompt_lens
                int32_t max_new_tokens, float temperature, const int32_t *tokens, float *out_logprobs,
                int64_t *out_versions) {
   return score_impl(ctx, prompts, prompt_lens, P, G, max_new_tokens, temperature, tokens, out_logprobs, out_versions);
+}
+
+int echo_score_detail(echo_ctx *ctx, const int32_t *prompts, const int32_t *prompt_lens, int32_t P, int32_t G,
+                      int32_t max_new_tokens, float temperature, const int32_t *tokens, int32_t top_k,
+                      float *out_logprobs, float *out_entropy, int32_t *out_top_ids, float *out_top_logprobs,
+                      int64_t *out_versions) {
+  if (top_k < 0 || (top_k > 0 && (!out_top_ids || !out_top_logprobs))) return ECHO_ERR_INVALID;
+  if (top_k > 32) return ECHO_ERR_UNSUPPORTED;
+  const ScoreDetail d{out_entropy, top_k, out_top_ids, out_top_logprobs};
+  return score_impl(ctx, prompts, prompt_lens, P, G, max_new_tokens, temperature, tokens, out_logprobs, out_versions, &d);
 }
 
 int echo_turn_mask(const int32_t *tokens, int32_t n, int32_t T, int32_t turn_start_id, int32_t shift_to_targets,
