@@ -371,7 +371,8 @@ typedef struct echo_adamw_tensor {
 } echo_adamw_tensor;
 
 typedef struct echo_adamw_options {
-  double lr, beta1, beta2, eps;   /* lr >= 0; beta1 and beta2 in [0, 1); eps > 0                          */
+  double lr, beta1, beta2, eps;   /* lr >= 0; beta1 and beta2 in [0, 1); eps > 0, with 8-bit
+                                     moments at least 1e-12 (else ECHO_ERR_UNSUPPORTED)                    */
   int64_t step;                   /* t >= 1, counts the updates including this one                        */
   uint64_t seed;                  /* 8-bit moments: key of the rounding's random numbers                  */
   const float *grad_scale;        /* dev fp32 [1] or NULL: every gradient is multiplied by it (clipping,

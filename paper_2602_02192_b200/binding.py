@@ -483,21 +483,18 @@ def echo_grpo_surrogate(logp_new: torch.Tensor, logp_old: torch.Tensor, logp_sam
 _FORMATS = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
 
 
-class _Here:
-    """The current device is already the tensor's."""
-    def __enter__(self):
-        return self
-
-    def __exit__(self, *exc):
-        return False
-
-
-_HERE_DEVICE = _Here()
-
-
-def _on(device: torch.device):
-    """Context in which `device` is the current one (switching costs more than a small launch: only when it is not)."""
-    return _HERE_DEVICE if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+def _call(device: torch.device, fn, *args):
+    """fn(*args, current stream of `device`) with `device` current.  A small launch takes less time than entering a device
+    context or making a stream object, so neither is done where it is not needed."""
+    index = device.index
+    stream = torch._C._cuda_getCurrentRawStream(index)
+    if torch._C._cuda_getDevice() == index:
+        rc = fn(*args, stream)
+    else:
+        with torch.cuda.device(index):
+            rc = fn(*args, stream)
+    if rc != ECHO_OK:
+        raise EchoError(rc)
 
 
 def _check_rows(logits: torch.Tensor, tokens: Optional[torch.Tensor]):
@@ -515,7 +512,7 @@ def _check_rows(logits: torch.Tensor, tokens: Optional[torch.Tensor]):
 def _check_vector(x: Optional[torch.Tensor], like: torch.Tensor, shape):
     if x is None:
         return None
-    assert x.device == like.device and x.dtype == torch.float32 and x.is_contiguous() and tuple(x.shape) == shape
+    assert x.dtype == torch.float32 and x.shape == shape and x.is_contiguous() and x.device == like.device
     return x.data_ptr()
 
 
@@ -526,18 +523,17 @@ def echo_token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor], te
     top_logprobs [R][top_k] or None)."""
     R, V, stride = _check_rows(logits, tokens)
     dev = logits.device
-    logprobs = torch.empty(R, dtype=torch.float32, device=dev) if tokens is not None else None
-    entropy = torch.empty(R, dtype=torch.float32, device=dev)
-    stats = torch.empty((R, 2), dtype=torch.float32, device=dev)
-    ids = torch.empty((R, top_k), dtype=torch.int32, device=dev) if top_k > 0 else None
-    top = torch.empty((R, top_k), dtype=torch.float32, device=dev) if top_k > 0 else None
-    with _on(dev):
-        _check(lib.echo_token_logprobs(logits.data_ptr(), _FORMATS[logits.dtype], stride, R, V,
-                                       tokens.data_ptr() if tokens is not None else None, temperature, top_k,
-                                       logprobs.data_ptr() if tokens is not None else None, entropy.data_ptr(),
-                                       stats.data_ptr(), ids.data_ptr() if ids is not None else None,
-                                       top.data_ptr() if top is not None else None, _stream_ptr(None)))
-    return logprobs, entropy, stats, ids, top
+    # one allocation, cut: statistics, entropies, log-probabilities, alternatives' log-probabilities
+    n = R if tokens is not None else 0
+    k = top_k if top_k > 0 else 0
+    whole = torch.empty((3 + k) * R + n, dtype=torch.float32, device=dev)
+    stats, entropy, logprobs, top = whole.split_with_sizes((2 * R, R, n, k * R))
+    ids = torch.empty((R, k), dtype=torch.int32, device=dev) if k else None
+    base = stats.data_ptr()
+    _call(dev, lib.echo_token_logprobs, logits.data_ptr(), _FORMATS[logits.dtype], stride, R, V,
+          tokens.data_ptr() if n else None, temperature, top_k, base + 12 * R if n else None, base + 8 * R, base,
+          ids.data_ptr() if k else None, base + 12 * R + 4 * n if k else None)
+    return (logprobs if tokens is not None else None, entropy, stats.view(R, 2), ids, top.view(R, k) if k else None)
 
 
 def echo_token_logprobs_backward(logits: torch.Tensor, tokens: Optional[torch.Tensor], entropy: Optional[torch.Tensor],
@@ -551,12 +547,10 @@ def echo_token_logprobs_backward(logits: torch.Tensor, tokens: Optional[torch.Te
         out = torch.empty((R, V), dtype=logits.dtype, device=logits.device)
     assert out.device == logits.device and out.dtype == logits.dtype and out.shape == logits.shape
     _, _, out_stride = _check_rows(out, None)
-    with _on(logits.device):
-        _check(lib.echo_token_logprobs_backward(
-            logits.data_ptr(), _FORMATS[logits.dtype], stride, R, V, tokens.data_ptr() if tokens is not None else None,
-            temperature, _check_vector(entropy, logits, (R,)), _check_vector(stats, logits, (R, 2)),
-            _check_vector(grad_logprobs, logits, (R,)), _check_vector(grad_entropy, logits, (R,)), out.data_ptr(),
-            out_stride, _stream_ptr(None)))
+    _call(logits.device, lib.echo_token_logprobs_backward, logits.data_ptr(), _FORMATS[logits.dtype], stride, R, V,
+          tokens.data_ptr() if tokens is not None else None, temperature, _check_vector(entropy, logits, (R,)),
+          _check_vector(stats, logits, (R, 2)), _check_vector(grad_logprobs, logits, (R,)),
+          _check_vector(grad_entropy, logits, (R,)), out.data_ptr(), out_stride)
     return out
 
 
@@ -572,13 +566,10 @@ def echo_grpo_gradient(logp_new: torch.Tensor, logp_old: torch.Tensor, logp_samp
         assert mask.device == dev and mask.dtype == torch.uint8 and mask.is_contiguous() and mask.shape == (n, T)
     out = torch.empty(n, dtype=torch.float32, device=dev)
     grad = torch.empty((n, T), dtype=torch.float32, device=dev)
-    with _on(dev):
-        _check(lib.echo_grpo_gradient(
-            _check_vector(logp_new, logp_new, (n, T)), _check_vector(logp_old, logp_new, (n, T)),
-            _check_vector(logp_sampler, logp_new, (n, T)), _check_vector(logp_ref, logp_new, (n, T)),
-            _check_vector(adv, logp_new, (n,)), mask.data_ptr() if mask is not None else None,
-            _check_vector(grad_out, logp_new, (n,)), n, T, eps_clip, C_trunc, beta, out.data_ptr(), grad.data_ptr(),
-            _stream_ptr(None)))
+    _call(dev, lib.echo_grpo_gradient, _check_vector(logp_new, logp_new, (n, T)), _check_vector(logp_old, logp_new, (n, T)),
+          _check_vector(logp_sampler, logp_new, (n, T)), _check_vector(logp_ref, logp_new, (n, T)),
+          _check_vector(adv, logp_new, (n,)), mask.data_ptr() if mask is not None else None,
+          _check_vector(grad_out, logp_new, (n,)), n, T, eps_clip, C_trunc, beta, out.data_ptr(), grad.data_ptr())
     return out, grad
 
 
@@ -647,8 +638,7 @@ def echo_adamw_step(tensors: AdamWTensors, step: int, lr: float, beta1: float = 
     if grad_scale is not None:
         assert grad_scale.device == tensors.device and grad_scale.dtype == torch.float32 and grad_scale.numel() == 1
         opt.grad_scale = grad_scale.data_ptr()
-    with _on(tensors.device):
-        _check(lib.echo_adamw_step(tensors.table, tensors.count, C.byref(opt), _stream_ptr(None)))
+    _call(tensors.device, lib.echo_adamw_step, tensors.table, tensors.count, C.byref(opt))
 
 
 def echo_adamw_unpack(tensors: AdamWTensors, out_avg: Sequence[torch.Tensor], out_avg_sq: Sequence[torch.Tensor]):
@@ -656,11 +646,10 @@ def echo_adamw_unpack(tensors: AdamWTensors, out_avg: Sequence[torch.Tensor], ou
     assert tensors.state_bits == 8 and len(out_avg) == tensors.count and len(out_avg_sq) == tensors.count
     addresses = []
     for outs in (out_avg, out_avg_sq):
-        for x, size in zip(outs, tensors.sizes):
-            assert x.device == tensors.device and x.dtype == torch.float32 and x.is_contiguous() and x.numel() == size
+        assert [x.numel() for x in outs] == tensors.sizes
+        assert all(x.dtype == torch.float32 and x.is_contiguous() and x.device == tensors.device for x in outs)
         addresses.append((C.c_void_p * max(tensors.count, 1))(*[x.data_ptr() for x in outs]))
-    with _on(tensors.device):
-        _check(lib.echo_adamw_unpack(tensors.table, tensors.count, addresses[0], addresses[1], _stream_ptr(None)))
+    _call(tensors.device, lib.echo_adamw_unpack, tensors.table, tensors.count, addresses[0], addresses[1])
 
 
 def echo_probe_read_bandwidth(n_bytes: int = 4 << 30, repeats: int = 10, device="cuda") -> float:

@@ -25,7 +25,7 @@ namespace echo {
 namespace {
 
 constexpr int kBlock = 256;                  // elements that share the 8-bit scales; one warp, eight per lane
-constexpr int kThreads = 256;
+constexpr int kThreads = 256, kResident = 4;        // threads per CTA, CTAs per SM
 
 struct Entry {
   float *p;
@@ -107,27 +107,34 @@ template <bool WHOLE> __device__ __forceinline__ void put_copy(__nv_bfloat16 *c,
       if (j < left) c[j] = __float2bfloat16(x[j]);
   }
 }
-template <bool WHOLE> __device__ __forceinline__ uint2 get_codes(const void *c, size_t at, int left) {
+// the eight codes of a lane, element j in byte j
+template <bool WHOLE> __device__ __forceinline__ uint64_t get_codes(const void *c, size_t at, int left) {
   const uint8_t *b = static_cast<const uint8_t *>(c) + at;
-  if (WHOLE) return __ldcs(reinterpret_cast<const uint2 *>(b));
-  uint2 w = make_uint2(0u, 0u);
+  if (WHOLE) {
+    const uint2 w = __ldcs(reinterpret_cast<const uint2 *>(b));
+    return static_cast<uint64_t>(w.y) << 32 | w.x;
+  }
+  uint64_t w = 0;
 #pragma unroll
   for (int j = 0; j < 8; ++j)
-    if (j < left) (j < 4 ? w.x : w.y) |= static_cast<uint32_t>(b[j]) << (8 * (j & 3));
+    if (j < left) w |= static_cast<uint64_t>(b[j]) << (8 * j);
   return w;
 }
-template <bool WHOLE> __device__ __forceinline__ void put_codes(void *c, size_t at, int left, uint2 w) {
+template <bool WHOLE> __device__ __forceinline__ void put_codes(void *c, size_t at, int left, uint64_t w) {
   uint8_t *b = static_cast<uint8_t *>(c) + at;
   if (WHOLE) {
-    *reinterpret_cast<uint2 *>(b) = w;
+    *reinterpret_cast<uint2 *>(b) = make_uint2(static_cast<uint32_t>(w), static_cast<uint32_t>(w >> 32));
     return;
   }
 #pragma unroll
   for (int j = 0; j < 8; ++j)
-    if (j < left) b[j] = static_cast<uint8_t>((j < 4 ? w.x : w.y) >> (8 * (j & 3)));
+    if (j < left) b[j] = static_cast<uint8_t>(w >> (8 * j));
 }
-__device__ __forceinline__ uint32_t byte_of(uint2 w, int j) { return ((j < 4 ? w.x : w.y) >> (8 * (j & 3))) & 0xffu; }
-__device__ __forceinline__ int signed_byte(uint2 w, int j) { return static_cast<int>(static_cast<int8_t>(byte_of(w, j))); }
+__device__ __forceinline__ uint32_t byte_of(uint64_t w, int j) { return static_cast<uint32_t>(w >> (8 * j)) & 0xffu; }
+__device__ __forceinline__ int signed_byte(uint64_t w, int j) { return static_cast<int>(static_cast<int8_t>(byte_of(w, j))); }
+__device__ __forceinline__ void set_byte(uint64_t &w, int j, int code) {
+  w = (w & ~(0xffull << (8 * j))) | static_cast<uint64_t>(code & 0xff) << (8 * j);
+}
 __device__ __forceinline__ float sqrt_fast(float x) {
   float y;
   asm("sqrt.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -149,22 +156,68 @@ __device__ __forceinline__ uint4 philox(uint4 c, uint32_t k0, uint32_t k1) {
 
 // the moments in 64 bits
 __device__ __forceinline__ double exact_avg(const Scalars &s, int code, float scale, float g, float gs) {
-  const double q = code / 127.0;
+  const double q = code * (1.0 / 127.0);
   return s.b1_d * (q * fabs(q) * scale) + s.b1c_d * (static_cast<double>(g) * gs);
 }
 __device__ __forceinline__ double exact_sq(const Scalars &s, uint32_t code, float scale, float g, float gs) {
-  const double q = code / 255.0, h = static_cast<double>(g) * gs;
+  const double q = code * (1.0 / 255.0), h = static_cast<double>(g) * gs;
   return s.b2_d * (q * q * (q * q) * scale) + s.b2c_d * h * h;
 }
-// Largest of non-negative values by their bits, which order like the values; NaN is above infinity, so that it shows.
-__device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(fabsf(v)); }
-__device__ __forceinline__ float warp_max(uint32_t bits) { return __uint_as_float(__reduce_max_sync(0xffffffffu, bits)); }
+// Largest magnitude of three; NaN wins, so that it shows.  Across a warp by the bits of the (non-negative) values, which
+// order like the values, NaN above infinity.
+__device__ __forceinline__ float max_or_nan(float a, float b, float c) {
+  float d;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(fabsf(b)), "f"(fabsf(c)));
+  return d;
+}
+__device__ __forceinline__ float warp_max(float v) {
+  return __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(fabsf(v))));
+}
+// Whole numbers and floats without the conversion unit: a float 2^23 + n holds n in its low bits.
+constexpr float kTwo23 = 8388608.0f, kRound = 12582912.0f;      // 2^23, 1.5 * 2^23
+__device__ __forceinline__ float byte_plus_two23(uint32_t word, int byte) {
+  return __uint_as_float(__byte_perm(word, 0x4B000000u, 0x7440u | byte));
+}
+__device__ __forceinline__ float half_plus_two23(uint32_t word, int half) {
+  return __uint_as_float(__byte_perm(word, 0x4B000000u, half ? 0x7432u : 0x7410u));
+}
+// low bytes of eight registers
+__device__ __forceinline__ uint64_t low_bytes(const uint32_t (&r)[8]) {
+  const uint32_t lo = __byte_perm(__byte_perm(r[0], r[1], 0x0040), __byte_perm(r[2], r[3], 0x0040), 0x5410);
+  const uint32_t hi = __byte_perm(__byte_perm(r[4], r[5], 0x0040), __byte_perm(r[6], r[7], 0x0040), 0x5410);
+  return static_cast<uint64_t>(hi) << 32 | lo;
+}
+__device__ __forceinline__ float sqrt_ftz(float x) {
+  float y;
+  asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float rcp_ftz(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float rsqrt_ftz(float x) {
+  float y;
+  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+using ptx::add2;
+using ptx::fma2;
+using ptx::mul2;
+__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
 
 // relative error of the fp32 moments, generously: a handful of roundings of 2^-24 each
 constexpr float kMomentErr = 1e-6f;
 
+// a lane's elements, by number (each lane reads its own only)
+struct Stash {
+  float4 g[2][32];
+  uint64_t m[32], v[32];
+};
+
 template <int FMT, bool EIGHT, bool WHOLE>
-__device__ __forceinline__ void step_block(const Scalars &s, const Entry &e, int64_t block, int lane, float gs) {
+__device__ __forceinline__ void step_block(const Scalars &s, const Entry &e, int64_t block, int lane, float gs, Stash &stash) {
   const int64_t at = block * kBlock + lane * 8;
   const int left = WHOLE ? 8 : static_cast<int>(min(static_cast<int64_t>(8), max(static_cast<int64_t>(0), e.n - at)));
   float p[8], g[8];
@@ -184,80 +237,143 @@ __device__ __forceinline__ void step_block(const Scalars &s, const Entry &e, int
     }
     put_f32<WHOLE>(static_cast<float *>(e.m) + at, left, m);
     put_f32<WHOLE>(static_cast<float *>(e.v) + at, left, v);
+    put_f32<WHOLE>(e.p + at, left, p);
+    if (e.copy) put_copy<WHOLE>(e.copy + at, left, p);
   } else {
-    const uint2 mc = get_codes<WHOLE>(e.m, at, left), vc = get_codes<WHOLE>(e.v, at, left);
+    const uint64_t mc = get_codes<WHOLE>(e.m, at, left), vc = get_codes<WHOLE>(e.v, at, left);
     const float M0 = e.m_scale[block], V0 = e.v_scale[block];
-    float m[8], v[8], err[8];                  // err: how far m may be off
-    uint32_t top_m = 0, top_v = 0;
-    float sure_m = 0.f;
+    // (what the 64-bit parts below want of single elements by number is kept in shared memory, not in registers)
+    stash.g[0][lane] = make_float4(g[0], g[1], g[2], g[3]);
+    stash.g[1][lane] = make_float4(g[4], g[5], g[6], g[7]);
+    stash.m[lane] = mc;
+    stash.v[lane] = vc;
+    auto old_g = [&](int j) { return reinterpret_cast<const float *>(&stash.g[j >> 2][lane])[j & 3]; };
+    auto old_m = [&](int j) { return static_cast<int>(reinterpret_cast<const int8_t *>(&stash.m[lane])[j]); };
+    auto old_v = [&](int j) { return static_cast<uint32_t>(reinterpret_cast<const uint8_t *>(&stash.v[lane])[j]); };
+    float m[8], v[8];
+    float big_m = 0.f, big_b = 0.f, big_v = 0.f;
+    const uint64_t mb = mc ^ 0x8080808080808080ull;            // c + 128
+    const float km = s.b1 * M0 * (1.0f / 16129.0f), kv = s.b2 * V0 * (1.0f / 4228250625.0f);      // 127^2, 255^4
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) {
+      const uint32_t mw = static_cast<uint32_t>(i < 4 ? mb : mb >> 32), vw = static_cast<uint32_t>(i < 4 ? vc : vc >> 32);
+      const float2 c = add2(make_float2(byte_plus_two23(mw, i & 3), byte_plus_two23(mw, (i & 3) + 1)), both(-kTwo23 - 128.0f));
+      const float2 d = add2(make_float2(byte_plus_two23(vw, i & 3), byte_plus_two23(vw, (i & 3) + 1)), both(-kTwo23));
+      const float2 h = mul2(make_float2(g[i], g[i + 1]), both(gs)), b = mul2(h, both(s.b1c));
+      const float2 cc = make_float2(c.x * fabsf(c.x), c.y * fabsf(c.y));
+      const float2 mm = fma2(cc, both(km), b);
+      const float2 d2 = mul2(d, d), vv = fma2(mul2(d2, d2), both(kv), mul2(mul2(h, both(s.b2c)), h));
+      m[i] = mm.x;
+      m[i + 1] = mm.y;
+      v[i] = vv.x;
+      v[i + 1] = vv.y;
+      big_m = max_or_nan(big_m, mm.x, mm.y);
+      big_v = max_or_nan(big_v, vv.x, vv.y);
+      big_b = max_or_nan(big_b, b.x, b.y);
+      const float2 denom = fma2(make_float2(sqrt_ftz(vv.x), sqrt_ftz(vv.y)), both(s.root_corr), both(s.eps));
+      const float2 up = mul2(mm, make_float2(rcp_ftz(denom.x), rcp_ftz(denom.y)));        // (denom is at least eps)
+      const float2 pp = fma2(make_float2(p[i], p[i + 1]), both(e.decay), mul2(up, both(-s.rate)));
+      p[i] = pp.x;
+      p[i + 1] = pp.y;
+    }
+    put_f32<WHOLE>(e.p + at, left, p);
+    if (e.copy) put_copy<WHOLE>(e.copy + at, left, p);
+    // scales: the 64-bit maximum as fp32, found among the elements that fp32 cannot tell from it.  (The 64-bit parts
+    // are loops over bit masks: unrolled, their code would not fit the instruction cache.)
+    big_m = warp_max(big_m);
+    big_v = warp_max(big_v);
+    // b1 |m| is at most b1 M0 and (1 - b1) |g| at most its largest: their sum's kMomentErr-th part bounds the error of
+    // every m of the block
+    const float err_m = kMomentErr * fmaf(s.b1, M0, warp_max(big_b));
+    uint32_t near_m = 0, near_v = 0;
+    const float from_m = err_m > 0.f ? fmaf(err_m, -2.0f, big_m) : INFINITY;
+    const float from_v = big_v > 0.f ? big_v * (1.0f - 2.0f * kMomentErr) : INFINITY;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const float h = g[j] * gs;
-      const float q = static_cast<float>(signed_byte(mc, j)) * (1.0f / 127.0f);
-      const float a = s.b1 * (q * fabsf(q) * M0), b = s.b1c * h;
-      m[j] = a + b;
-      err[j] = kMomentErr * (fabsf(a) + fabsf(b));
-      float r = static_cast<float>(byte_of(vc, j)) * (1.0f / 255.0f);
-      r *= r;
-      v[j] = fmaf(s.b2, r * r * V0, s.b2c * h * h);
-      top_m = max(top_m, magnitude(m[j]));
-      sure_m = fmaxf(sure_m, fabsf(m[j]) - err[j]);
-      top_v = max(top_v, magnitude(v[j]));
-      const float denom = fmaf(sqrt_fast(v[j]), s.root_corr, s.eps);
-      p[j] = fmaf(p[j], e.decay, -s.rate * __fdividef(m[j], denom));
+      if (fabsf(m[j]) >= from_m) near_m |= 1u << j;
+      if (v[j] >= from_v) near_v |= 1u << j;
     }
-    // scales: the 64-bit maximum as fp32, found among the elements that fp32 cannot tell from it
-    const float big_m = warp_max(top_m), big_v = warp_max(top_v);
-    sure_m = warp_max(magnitude(sure_m));
     float M = 0.f, V = 0.f;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      if (fabsf(m[j]) + err[j] >= sure_m && err[j] > 0.f)
-        M = fmaxf(M, static_cast<float>(fabs(exact_avg(s, signed_byte(mc, j), M0, g[j], gs))));
-      if (v[j] >= big_v * (1.0f - 2.0f * kMomentErr) && v[j] != 0.f)
-        V = fmaxf(V, static_cast<float>(exact_sq(s, byte_of(vc, j), V0, g[j], gs)));
+#pragma unroll 1
+    for (; near_m; near_m &= near_m - 1) {
+      const int j = __ffs(near_m) - 1;
+      M = fmaxf(M, static_cast<float>(fabs(exact_avg(s, old_m(j), M0, old_g(j), gs))));
     }
-    M = isfinite(big_m) ? warp_max(magnitude(M)) : big_m;
-    V = isfinite(big_v) ? warp_max(magnitude(V)) : big_v;
+#pragma unroll 1
+    for (; near_v; near_v &= near_v - 1) {
+      const int j = __ffs(near_v) - 1;
+      V = fmaxf(V, static_cast<float>(exact_sq(s, old_v(j), V0, old_g(j), gs)));
+    }
+    M = isfinite(big_m) ? warp_max(M) : big_m;
+    V = isfinite(big_v) ? warp_max(V) : big_v;
     if (M < 1.17549435e-38f) M = 0.f;          // below the normal numbers: counts as 0
     if (V < 1.17549435e-38f) V = 0.f;
-    const float inv_m = M > 0.f ? 16129.0f / M : 0.f, inv_v = V > 0.f ? 4228250625.0f / V : 0.f;     // 127^2, 255^4
+    const float inv_m = M > 0.f ? 16129.0f / M : 0.f, inv_v = V > 0.f ? 4228250625.0f / V : 0.f;
     const uint64_t octet = static_cast<uint64_t>(block) * (kBlock / 8) + lane;
     const uint4 rnd = philox(make_uint4(static_cast<uint32_t>(octet), static_cast<uint32_t>(octet >> 32), e.id, s.step),
                              s.key0, s.key1);
     const uint32_t words[4] = {rnd.x, rnd.y, rnd.z, rnd.w};
-    uint2 mo = make_uint2(0u, 0u), vo = make_uint2(0u, 0u);
+    uint32_t mr[8], vr[8];                     // codes in the low bytes
+    uint32_t unsure_m = 0, unsure_v = 0;
+    const float err_y = 0.5f * err_m * inv_m;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      // ---- first moment: y = 127^2 |m| / M lies between the borders (c - 1/2)^2 and (c + 1/2)^2
-      const float y = fabsf(m[j]) * inv_m;
-      float c = rintf(sqrt_fast(y));
-      const float mid = fmaf(c, c, 0.25f);
-      const float up = (mid + c) - y, down = c > 0.f ? y - (mid - c) : 1e30f;
-      if (fminf(up, down) <= fmaf(err[j], inv_m, y * kMomentErr))
-        c = M > 0.f ? static_cast<float>(rint(sqrt(fabs(exact_avg(s, signed_byte(mc, j), M0, g[j], gs)) * 16129.0 / M))) : 0.f;
-      int code = static_cast<int>(c);
-      code = m[j] < 0.f ? -code : code;
-      (j < 4 ? mo.x : mo.y) |= (static_cast<uint32_t>(code) & 0xffu) << (8 * (j & 3));
-      // ---- second moment: w = 255^4 v / V lies between c^4 and (c + 1)^4
-      const float w = v[j] * inv_v;
-      float d = fminf(floorf(sqrt_fast(sqrt_fast(w))), 254.0f);
-      const float d2 = d * d, above = w - d2 * d2, width = fmaf(fmaf(fmaf(4.0f, d, 6.0f), d, 4.0f), d, 1.0f);
-      const uint32_t half16 = (words[j >> 1] >> (16 * (j & 1))) & 0xffffu;
-      const float u = static_cast<float>(half16) * 1.52587890625e-05f;
-      const float diff = above - u * width, err_w = w * (1.2f * kMomentErr);
-      uint32_t vcode = static_cast<uint32_t>(d) + (diff > 0.f ? 1u : 0u);
-      if (v[j] == big_v) {
-        vcode = 255u;                          // the block's largest
-      } else if (fminf(fminf(fabsf(diff), above), width - above) <= err_w) {
-        const double we = V > 0.f ? exact_sq(s, byte_of(vc, j), V0, g[j], gs) * (4228250625.0 / V) : 0.0;
-        const double dd = fmin(floor(sqrt(sqrt(we))), 254.0);
-        const double lo = dd * dd * (dd * dd), hi = (dd + 1.0) * (dd + 1.0) * ((dd + 1.0) * (dd + 1.0));
-        vcode = static_cast<uint32_t>(dd) + (half16 * 1.52587890625e-05 * (hi - lo) < we - lo ? 1u : 0u);
+    for (int i = 0; i < 8; i += 2) {
+      const float2 ym = mul2(make_float2(m[i], m[i + 1]), both(inv_m)), w = mul2(make_float2(v[i], v[i + 1]), both(inv_v));
+      // first moment: x = sqrt(y), y = 127^2 |m| / M, is off by (error of y) / (2 x) and, x being at most 127, less than
+      // 1e-4 of its own rounding.  (Below y = 1/1000 every code is 0, and so stands for the smaller ones.)
+      const float2 y = make_float2(fmaxf(fabsf(ym.x), 1e-3f), fmaxf(fabsf(ym.y), 1e-3f));
+      const float2 rs = make_float2(rsqrt_ftz(y.x), rsqrt_ftz(y.y)), x = mul2(y, rs);
+      const float2 xs = make_float2(copysignf(x.x, ym.x), copysignf(x.y, ym.y));
+      const float2 r = add2(xs, both(kRound)), dist = fma2(add2(r, both(-kRound)), both(-1.0f), xs);
+      const float2 clear = fma2(rs, both(-err_y), both(0.4999f));
+      mr[i] = __float_as_uint(r.x);
+      mr[i + 1] = __float_as_uint(r.y);
+      if (fabsf(dist.x) > clear.x) unsure_m |= 1u << i;
+      if (fabsf(dist.y) > clear.y) unsure_m |= 2u << i;
+      // second moment: w = 255^4 v / V lies between d^4 and (d + 1)^4 (d at most 254; 254.5 stands for all above it).
+      // Next to d^4 the rounded root may name the neighbouring interval, which gives the same code unless the random
+      // number u is within (error of the place in the interval) < 2.4e-4 of 0 or 1.  (A v that just decays with its
+      // block sits there step after step: only these u may cost anything.)
+      const bool some_x = w.x > 0.f, some_y = w.y > 0.f;
+      const float2 z = make_float2(fminf(sqrt_ftz(sqrt_ftz(w.x)), 254.5f), fminf(sqrt_ftz(sqrt_ftz(w.y)), 254.5f));
+      const float2 zr = make_float2(__fadd_rd(z.x, kTwo23), __fadd_rd(z.y, kTwo23)), d = add2(zr, both(-kTwo23));
+      const float2 d2 = mul2(d, d), above = fma2(mul2(d2, both(-1.0f)), d2, w);
+      const float2 width = fma2(fma2(fma2(d, both(4.0f), both(6.0f)), d, both(4.0f)), d, both(1.0f));
+      const float2 u = fma2(make_float2(half_plus_two23(words[i >> 1], 0), half_plus_two23(words[i >> 1], 1)),
+                            both(-1.52587890625e-05f), both(128.0f));          // minus the random number
+      const float2 diff = fma2(u, width, above), near = mul2(w, both(1.2f * kMomentErr)), mid = add2(u, both(0.5f));
+      vr[i] = max(__float_as_uint(zr.x) + (diff.x > 0.f ? 1u : 0u), some_x ? 0x4B000001u : 0x4B000000u);
+      vr[i + 1] = max(__float_as_uint(zr.y) + (diff.y > 0.f ? 1u : 0u), some_y ? 0x4B000001u : 0x4B000000u);
+      if (fabsf(diff.x) <= near.x || fabsf(mid.x) > 0.49976f) unsure_v |= 1u << i;
+      if (fabsf(diff.y) <= near.y || fabsf(mid.y) > 0.49976f) unsure_v |= 2u << i;
+    }
+    uint64_t mo = low_bytes(mr), vo = low_bytes(vr);
+    if (!(M > 0.f)) unsure_m = 0;
+    if (!(V > 0.f)) unsure_v = 0;
+    // The code that fp32 chose is right or next to it: compared with the borders around it in 64 bits.
+#pragma unroll 1
+    for (; unsure_m; unsure_m &= unsure_m - 1) {
+      const int j = __ffs(unsure_m) - 1;
+      const double x = exact_avg(s, old_m(j), M0, old_g(j), gs), y = fabs(x) * 16129.0;
+      int c = abs(signed_byte(mo, j));
+      const double up = c + 0.5, down = c - 0.5;
+      if (y > up * up * M) ++c;
+      else if (c > 0 && y < down * down * M) --c;
+      set_byte(mo, j, x < 0.0 ? -c : c);
+    }
+#pragma unroll 1
+    for (; unsure_v; unsure_v &= unsure_v - 1) {
+      const int j = __ffs(unsure_v) - 1;
+      const double y = exact_sq(s, old_v(j), V0, old_g(j), gs) * 4228250625.0;
+      double d = min(static_cast<int>(byte_of(vo, j)), 254), lo = d * d * (d * d) * V;
+      if (y < lo) {                            // the code is the upper one of its interval
+        d -= 1.0;
+        lo = d * d * (d * d) * V;
       }
-      if (vcode == 0u) vcode = 1u;
-      if (!(w > 0.f)) vcode = 0u;
-      (j < 4 ? vo.x : vo.y) |= vcode << (8 * (j & 3));
+      const double hi = (d + 1.0) * (d + 1.0) * ((d + 1.0) * (d + 1.0)) * V;
+      const uint64_t half = j < 4 ? static_cast<uint64_t>(words[1]) << 32 | words[0] : static_cast<uint64_t>(words[3]) << 32 | words[2];
+      const double u = static_cast<double>(static_cast<uint32_t>(half >> (16 * (j & 3))) & 0xffffu) * 1.52587890625e-05;
+      if (y > 0.0) set_byte(vo, j, max(static_cast<int>(d) + (u * (hi - lo) < y - lo ? 1 : 0), 1));
     }
     put_codes<WHOLE>(e.m, at, left, mo);
     put_codes<WHOLE>(e.v, at, left, vo);
@@ -266,8 +382,6 @@ __device__ __forceinline__ void step_block(const Scalars &s, const Entry &e, int
       e.v_scale[block] = V;
     }
   }
-  put_f32<WHOLE>(e.p + at, left, p);
-  if (e.copy) put_copy<WHOLE>(e.copy + at, left, p);
 }
 
 // A grid that fills the GPU; a warp takes every n-th block of 256 elements of the whole list.
@@ -291,13 +405,15 @@ template <int N, typename F> __device__ __forceinline__ void for_blocks(const Ta
 }
 
 template <int N, int FMT, bool EIGHT>
-__global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__ Table<N> t) {
+__global__ void __launch_bounds__(kThreads, kResident) adamw_kernel(const __grid_constant__ Table<N> t) {
   const float gs = t.s.grad_scale ? *t.s.grad_scale : 1.0f;
   if (!isfinite(gs)) return;                              // an overflowed step changes nothing
   const int lane = threadIdx.x & 31;
+  __shared__ Stash stashes[EIGHT ? kThreads / 32 : 1];
+  Stash &stash = stashes[EIGHT ? threadIdx.x >> 5 : 0];
   for_blocks(t, [&](const Entry &e, int64_t block, uint32_t) {
-    if (e.vec && (block + 1) * kBlock <= e.n) step_block<FMT, EIGHT, true>(t.s, e, block, lane, gs);
-    else step_block<FMT, EIGHT, false>(t.s, e, block, lane, gs);
+    if (e.vec && (block + 1) * kBlock <= e.n) step_block<FMT, EIGHT, true>(t.s, e, block, lane, gs, stash);
+    else step_block<FMT, EIGHT, false>(t.s, e, block, lane, gs, stash);
   });
 }
 
@@ -308,8 +424,8 @@ template <int N> __global__ void __launch_bounds__(kThreads) adamw_unpack_kernel
     const int64_t at = block * kBlock + lane * 8;
     const int left = static_cast<int>(min(static_cast<int64_t>(8), max(static_cast<int64_t>(0), e.n - at)));
     const bool whole = e.vec && left == 8;
-    const uint2 mc = whole ? get_codes<true>(e.m, at, left) : get_codes<false>(e.m, at, left);
-    const uint2 vc = whole ? get_codes<true>(e.v, at, left) : get_codes<false>(e.v, at, left);
+    const uint64_t mc = whole ? get_codes<true>(e.m, at, left) : get_codes<false>(e.m, at, left);
+    const uint64_t vc = whole ? get_codes<true>(e.v, at, left) : get_codes<false>(e.v, at, left);
     const float M = e.m_scale[block], V = e.v_scale[block];
     float m[8], v[8];
 #pragma unroll
@@ -380,7 +496,7 @@ cudaError_t launch_list(int n_tensors, const Scalars &base, int grad_format, int
     t.s.n_tensors = n;
     t.s.n_blocks = static_cast<uint32_t>(blocks);
     const uint64_t need = (blocks + kThreads / 32 - 1) / (kThreads / 32);
-    const int grid = static_cast<int>(std::min<uint64_t>(need, static_cast<uint64_t>(sms) * 8));
+    const int grid = static_cast<int>(std::min<uint64_t>(need, static_cast<uint64_t>(sms) * kResident));
     if (n <= kSmallTable) {
       Table<kSmallTable> small;
       small.s = t.s;
@@ -440,6 +556,8 @@ int echo_adamw_step(const echo_adamw_tensor *tensors, int32_t n_tensors, const e
   if (!(static_cast<float>(opt->eps) > 0.f) || !std::isfinite(static_cast<float>(opt->eps))) return ECHO_ERR_INVALID;
   if (opt->step < 1 || opt->step > 0xffffffffLL || !aligned(opt->grad_scale, 4)) return ECHO_ERR_INVALID;
   if (opt->grad_format < 0 || opt->grad_format > 2 || (opt->state_bits != 8 && opt->state_bits != 32)) return ECHO_ERR_INVALID;
+  // 8-bit moments: roots of denormal numbers count as 0 beside eps
+  if (opt->state_bits == 8 && opt->eps < 1e-12) return ECHO_ERR_UNSUPPORTED;
   const int bits = opt->state_bits, gb = elem_bytes(opt->grad_format);
   if (!list_ok(tensors, n_tensors, bits, opt->grad_format, true)) return ECHO_ERR_INVALID;
   for (int i = 0; i < n_tensors; ++i)

@@ -8,6 +8,7 @@
 // every entry is the type's lowest value is an ordinary (uniform) row.  All sums are fp32.
 
 #include <cmath>
+#include <algorithm>
 #include <type_traits>
 
 #include "common.cuh"
@@ -52,34 +53,10 @@ __device__ __forceinline__ uint4 load_once(const uint4 *p) {
                : "memory");
   return v;
 }
-__device__ __forceinline__ float ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-// two fp32 operations in one instruction
-__device__ __forceinline__ float2 add2(float2 a, float2 b) {
-  float2 d;
-  asm("{.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tadd.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;}"
-      : "=f"(d.x), "=f"(d.y)
-      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-  return d;
-}
-__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
-  float2 d;
-  asm("{.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmul.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;}"
-      : "=f"(d.x), "=f"(d.y)
-      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-  return d;
-}
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
-  float2 d;
-  asm("{.reg .b64 a, b, c, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\t"
-      "fma.rn.f32x2 d, a, b, c;\n\tmov.b64 {%0, %1}, d;}"
-      : "=f"(d.x), "=f"(d.y)
-      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
-  return d;
-}
+using ptx::add2;
+using ptx::ex2;
+using ptx::fma2;
+using ptx::mul2;
 // elements 2i and 2i+1 of a vector as fp32
 template <int FMT> __device__ __forceinline__ float2 pair_of(const uint4 &v, int i) {
   const uint32_t w[4] = {v.x, v.y, v.z, v.w};
@@ -149,40 +126,23 @@ __device__ __forceinline__ float key_value(uint64_t key) {
 }
 __device__ __forceinline__ bool listable(float z) { return z > -INFINITY; }           // false for NaN
 
-__device__ __forceinline__ float sort_step(float v, int lane, int j, bool descending_block) {
-  const float o = __shfl_xor_sync(0xffffffffu, v, j);
-  const bool lower = (lane & j) == 0;
-  return (lower == descending_block) ? fmaxf(v, o) : fminf(v, o);
-}
-// 32 values of a warp, largest in lane 0
-__device__ __forceinline__ float sort32(float v, int lane) {
-#pragma unroll
-  for (int k = 2; k <= 32; k <<= 1)
-#pragma unroll
-    for (int j = k >> 1; j > 0; j >>= 1) v = sort_step(v, lane, j, (lane & k) == 0 || k == 32);
-  return v;
-}
-// the 32 largest of two descending lists, again descending (b is passed reversed)
-__device__ __forceinline__ float merge32(float a, float b_reversed, int lane) {
-  float v = fmaxf(a, b_reversed);
-#pragma unroll
-  for (int j = 16; j > 0; j >>= 1) v = sort_step(v, lane, j, true);
-  return v;
-}
-
 constexpr int kTopMax = 32;        // alternatives per row
 constexpr int kCandidates = 1024;  // candidates gathered per CTA before the exact selection takes over
-constexpr int kHotPieces = 128;
+constexpr int kHotPieces = 512;
+constexpr int kRescan = 2;         // vectors per thread and turn there
 constexpr int kUnroll = 4;         // 16-byte vectors per thread and step
+template <int NT> constexpr int kPieces = 1024 / NT;       // parts of a thread's elements whose maxima are kept
+constexpr uint32_t kNoEntry = 0x007fffffu;         // order_key(-inf)
 constexpr int kMaxSplit = 8;       // CTAs per row (one cluster)
 constexpr int kMaxVocab = 1 << 30; // element indexes of a row, plus a step, fit 32 bits
 
 struct TopShared {
-  float piece_max[2 * 512];
-  float lists[16][32];
-  uint64_t cand[kCandidates];
+  uint32_t piece[1024];                      // order keys of the pieces' maxima
+  uint32_t sorted[8][32];                    // the threads' maxima, each warp's in descending order
+  uint32_t bound;
+  alignas(16) uint64_t cand[kCandidates + 2];
   uint64_t best[kTopMax];                    // this CTA's alternatives, sorted
-  uint64_t gathered[kMaxSplit][kTopMax];     // first CTA of a cluster: everybody's
+  alignas(16) uint64_t gathered[kMaxSplit * kTopMax + 2];      // first CTA of a cluster: everybody's
   int hot[kHotPieces];
   uint32_t hist[256];
   int n_cand, n_hot, need, warp_count[16];
@@ -215,7 +175,7 @@ struct LogprobArgs {
 // candidates than the buffer holds tie with, or sit above, the bound of the one-pass filter (constant rows, sorted
 // rows); it reads the elements six times out of L2.
 template <int FMT, int NT>
-__device__ void select_exact(const void *row, int begin, int end, int k, TopShared &sh) {
+__device__ __noinline__ void select_exact(const void *row, int begin, int end, int k, TopShared &sh) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   if (tid == 0) {
     sh.n_cand = 0;
@@ -282,13 +242,18 @@ __device__ void select_exact(const void *row, int begin, int end, int k, TopShar
   __syncthreads();
 }
 
-// sorts n entries (n <= capacity of src) by counting how many precede each; the first kTopMax go to dst
+// sorts n entries by counting how many precede each; the first kTopMax go to dst.  src[n] is 0 where n is odd.
 __device__ __forceinline__ void rank_entries(const uint64_t *src, int n, uint64_t *dst, int nt) {
+  const ulonglong2 *pairs = reinterpret_cast<const ulonglong2 *>(src);
   for (int i = threadIdx.x; i < n; i += nt) {
     const uint64_t mine = src[i];
     if (!mine) continue;
     int rank = 0;
-    for (int j = 0; j < n; ++j) rank += src[j] > mine ? 1 : 0;
+#pragma unroll 4
+    for (int j = 0; j < (n + 1) / 2; ++j) {
+      const ulonglong2 q = pairs[j];
+      rank += (q.x > mine ? 1 : 0) + (q.y > mine ? 1 : 0);
+    }
     if (rank < kTopMax) dst[rank] = mine;
   }
 }
@@ -306,10 +271,131 @@ __device__ __forceinline__ uint32_t map_to_first(const void *p) {
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
 
+// The CTA's alternatives, sorted, into sh.best.  (Not inlined: the registers of the streaming loop are worth more than
+// the call: 112 against 116 us for 8 alternatives at 2048 x 151936 bf16, where scoring alone takes 101.)
+template <int FMT, int NT>
+__device__ __noinline__ void find_alternatives(const void *row, const uint4 *vec, int begin, int end, int head, int n_vec,
+                                               int per, int k, TopShared &sh) {
+  constexpr int kPerVec = Fmt<FMT>::kPerVec, kWarps = NT / 32;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int tail0 = begin + head + n_vec * kPerVec;          // elements behind the whole vectors
+  // Lower bound of the k-th largest entry: the k-th largest of the threads' maxima (k entries reach it; not many more
+  // than k do).  Every warp sorts its 32, and an element of one list finds its place among all by bisecting the others.
+  uint32_t most = sh.piece[tid];
+#pragma unroll
+  for (int i = 1; i < kPieces<NT>; ++i) most = max(most, sh.piece[i * NT + tid]);
+#pragma unroll
+  for (int span = 2; span <= 32; span <<= 1)
+#pragma unroll
+    for (int o = span >> 1; o > 0; o >>= 1) {
+      const uint32_t other = __shfl_xor_sync(0xffffffffu, most, o);
+      most = ((lane & o) == 0) == ((lane & span) == 0 || span == 32) ? max(most, other) : min(most, other);
+    }
+  sh.sorted[warp][lane] = most;
+  if (tid == 0) sh.n_cand = sh.n_hot = 0;
+  if (tid < kTopMax) sh.best[tid] = 0;
+  __syncthreads();
+  if (lane < k) {
+    int before[kWarps];                                      // entries of each list that precede this one
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) before[w] = 0;
+#pragma unroll
+    for (int half = 16; half > 0; half >>= 1)
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) {
+        const uint32_t other = sh.sorted[w][before[w] + half - 1];
+        if (other > most || (other == most && w < warp)) before[w] += half;
+      }
+    int rank = lane;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w)
+      if (w != warp) {
+        const uint32_t other = sh.sorted[w][before[w]];      // (at most 31 so far: one more may precede)
+        rank += before[w] + (other > most || (other == most && w < warp) ? 1 : 0);
+      }
+    if (rank == k - 1) sh.bound = most;
+  }
+  __syncthreads();
+  const uint32_t bound_key = sh.bound;
+  const float bound = key_value(static_cast<uint64_t>(bound_key) << 32);
+#pragma unroll
+  for (int i = 0; i < kPieces<NT>; ++i) {
+    const uint32_t key = sh.piece[i * NT + tid];
+    if (key >= bound_key && key > kNoEntry) {
+      const int at = atomicAdd(&sh.n_hot, 1);
+      if (at < kHotPieces) sh.hot[at] = i * NT + tid;
+    }
+  }
+  __syncthreads();
+  const int n_hot = sh.n_hot;
+  if (n_hot <= kHotPieces) {
+    auto offer = [&](float z, int id) {
+      if (z >= bound && listable(z)) {
+        const int at = atomicAdd(&sh.n_cand, 1);
+        if (at < kCandidates) sh.cand[at] = entry_key(z, static_cast<uint32_t>(id));
+      }
+    };
+    if (tid < head) offer(load_elem<FMT>(row, begin + tid), begin + tid);
+    if (tail0 + tid < end) offer(load_elem<FMT>(row, tail0 + tid), tail0 + tid);
+    // a few vectors of the hot pieces per thread and turn, requested together
+    const float pieces_per_vec = 1.0f / static_cast<float>(per);
+    const int total = n_hot * per;                           // (at most 512 pieces: places below are exact in fp32)
+    for (int w0 = tid; w0 < total; w0 += kRescan * NT) {
+      uint4 q[kRescan];
+      int at[kRescan];
+#pragma unroll
+      for (int b = 0; b < kRescan; ++b) {
+        const int w = w0 + b * NT;
+        at[b] = n_vec;
+        if (w < total) {
+          const int p = static_cast<int>((static_cast<float>(w) + 0.5f) * pieces_per_vec), which = sh.hot[p];
+          at[b] = ((which / NT) * per + (w - p * per)) * NT + which % NT;
+        }
+        q[b] = at[b] < n_vec ? load_stream(vec + at[b]) : neg_inf_vec<FMT>();
+      }
+      // bit j: element j of the thread's vectors is an entry at or above the bound (few are)
+      uint32_t found = 0;
+#pragma unroll
+      for (int b = 0; b < kRescan; ++b)
+#pragma unroll
+        for (int e = 0; e < kPerVec / 2; ++e) {
+          const float2 z = pair_of<FMT>(q[b], e);
+          if (z.x >= bound && listable(z.x)) found |= 1u << (b * kPerVec + 2 * e);
+          if (z.y >= bound && listable(z.y)) found |= 2u << (b * kPerVec + 2 * e);
+        }
+      for (; found; found &= found - 1) {
+        const int which = __ffs(found) - 1;
+        float z = 0.f;
+        int id = 0;
+#pragma unroll
+        for (int b = 0; b < kRescan; ++b)
+#pragma unroll
+          for (int e = 0; e < kPerVec / 2; ++e)
+            if (which / 2 == (b * kPerVec + 2 * e) / 2) {
+              const float2 pair = pair_of<FMT>(q[b], e);
+              z = (which & 1) ? pair.y : pair.x;
+              id = begin + head + at[b] * kPerVec + 2 * e + (which & 1);
+            }
+        offer(z, id);
+      }
+    }
+    __syncthreads();
+  }
+  if (n_hot > kHotPieces || sh.n_cand > kCandidates) {
+    __syncthreads();
+    select_exact<FMT, NT>(row, begin, end, k, sh);
+  }
+  const int n_cand = sh.n_cand;
+  if (tid == 0) sh.cand[n_cand] = 0;
+  __syncthreads();
+  rank_entries(sh.cand, n_cand, sh.best, NT);
+  __syncthreads();
+}
+
 // One cluster of `split` CTAs per row (split = 1: one CTA), each with a contiguous share of the row, one pass.
 // A thread keeps (m, l, t) of its own elements and moves the reference only when a step of its vectors exceeds it.
-// Alternatives cost no second pass: a thread also keeps the maximum of each half of its elements ("pieces"); the k-th
-// largest of these is a lower bound of the k-th largest logit, and only the pieces that reach it, about k of 1024,
+// Alternatives cost no second pass: the threads also keep the maxima of 1024 parts of the CTA's elements ("pieces");
+// from these comes a lower bound of the k-th largest logit, and only the pieces that reach it, little more than k,
 // are looked at again for entries that reach it.
 template <int FMT, int NT, bool TOP>
 __global__ void __launch_bounds__(NT, 1024 / NT)
@@ -340,7 +426,7 @@ token_logprobs_kernel(const __grid_constant__ LogprobArgs a, int split) {
     }
   }
   const int token = a.tokens ? a.tokens[flat] : -1;
-  if (token < 0 && !TOP && !a.out_entropy && !a.out_stats) {
+  if (!TOP && !a.out_entropy && !a.out_stats && token < 0) {
     if (rank == 0 && tid == 0 && a.out_logprobs) a.out_logprobs[flat] = 0.f;
     return;
   }
@@ -371,7 +457,7 @@ token_logprobs_kernel(const __grid_constant__ LogprobArgs a, int split) {
       for (int i = 0; i < kPerVec / 2; ++i) {
         float2 x = mul2(add2(pair_of<FMT>(v[u], i), neg), cc);
         const float2 e = make_float2(ex2(x.x), ex2(x.y));
-        x.x = fmaxf(x.x, kFarBelow);
+        x.x = fmaxf(x.x, kFarBelow);                         // (-inf would make 0 * -inf)
         x.y = fmaxf(x.y, kFarBelow);
         l0 = add2(l0, e);
         t0 = fma2(e, x, t0);
@@ -395,31 +481,33 @@ token_logprobs_kernel(const __grid_constant__ LogprobArgs a, int split) {
   };
 
   const int steps = (n_vec + NT * kUnroll - 1) / (NT * kUnroll);
-  const int cross = ((steps + 1) / 2 + 1) / 2 * 2;           // first step of a thread's second piece (two steps a turn)
+  const int piece_steps = (steps + 2 * kPieces<NT> - 1) / (2 * kPieces<NT>) * 2;      // (whole turns of the loop below)
   {
     uint4 va[kUnroll], vb[kUnroll];
-    float piece = -INFINITY;
     fetch(va, 0);
     // the few elements outside whole vectors, under the first loads' latency
     if (tid < head) absorb_one(load_elem<FMT>(row, begin + tid));
     if (tail0 + tid < end) absorb_one(load_elem<FMT>(row, tail0 + tid));
-    for (int s = 0; s < steps; s += 2) {
-      if constexpr (TOP) {
-        if (s == cross) {
-          top_mem.piece_max[tid] = piece;
-          piece = -INFINITY;
-        }
-      }
-      fetch(vb, s + 1);
-      piece = fmaxf(piece, absorb(va));
-      fetch(va, s + 2);
-      if (s + 1 < steps) piece = fmaxf(piece, absorb(vb));
-    }
+    int s = 0;
     if constexpr (TOP) {
-      TopShared &sh = top_mem;
-      const bool crossed = cross < steps;                    // a second piece was begun
-      if (!crossed) sh.piece_max[tid] = piece;
-      sh.piece_max[NT + tid] = crossed ? piece : -INFINITY;
+#pragma unroll 1
+      for (int h = 0; h < kPieces<NT>; ++h) {
+        float most = -INFINITY;
+        for (const int until = min((h + 1) * piece_steps, steps); s < until; s += 2) {
+          fetch(vb, s + 1);
+          most = fmaxf(most, absorb(va));
+          fetch(va, s + 2);
+          if (s + 1 < steps) most = fmaxf(most, absorb(vb));
+        }
+        top_mem.piece[h * NT + tid] = order_key(most + 0.0f);          // (+ 0: -0 equals 0)
+      }
+    } else {
+      for (; s < steps; s += 2) {
+        fetch(vb, s + 1);
+        absorb(va);
+        fetch(va, s + 2);
+        if (s + 1 < steps) absorb(vb);
+      }
     }
   }
   // ---- join the threads' statistics
@@ -432,66 +520,7 @@ token_logprobs_kernel(const __grid_constant__ LogprobArgs a, int split) {
 #pragma unroll
     for (int o = kWarps / 2; o > 0; o >>= 1) merge(st, shfl_stats(st, o), c);
   }
-  // ---- this CTA's alternatives
-  if constexpr (TOP) {
-    TopShared &sh = top_mem;
-    float v = merge32(sort32(sh.piece_max[tid], lane), __shfl_xor_sync(0xffffffffu, sort32(sh.piece_max[NT + tid], lane), 31), lane);
-    sh.lists[warp][lane] = v;
-    if (tid == 0) sh.n_cand = sh.n_hot = 0;
-    if (tid < kTopMax) sh.best[tid] = 0;
-    __syncthreads();
-    for (int d = 1; d < kWarps; d <<= 1) {
-      if ((warp & (2 * d - 1)) == 0) {
-        v = merge32(v, sh.lists[warp + d][31 - lane], lane);
-        sh.lists[warp][lane] = v;
-      }
-      __syncthreads();
-    }
-    const float bound = sh.lists[0][a.top_k - 1];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const float pm = sh.piece_max[h * NT + tid];
-      if (listable(pm) && pm >= bound) {
-        const int at = atomicAdd(&sh.n_hot, 1);
-        if (at < kHotPieces) sh.hot[at] = h * NT + tid;
-      }
-    }
-    __syncthreads();
-    const int n_hot = sh.n_hot;
-    if (n_hot <= kHotPieces) {
-      auto offer = [&](float z, int id) {
-        if (listable(z) && z >= bound) {
-          const int at = atomicAdd(&sh.n_cand, 1);
-          if (at < kCandidates) sh.cand[at] = entry_key(z, static_cast<uint32_t>(id));
-        }
-      };
-      if (tid < head) offer(load_elem<FMT>(row, begin + tid), begin + tid);
-      if (tail0 + tid < end) offer(load_elem<FMT>(row, tail0 + tid), tail0 + tid);
-      const int per = max(cross, steps - cross) * kUnroll;     // vectors of a piece, at most
-      for (int w = tid; w < n_hot * per; w += NT) {
-        const int piece = sh.hot[w / per], h = piece / NT, owner = piece % NT, j = w % per;
-        const int step = h * cross + j / kUnroll;
-        if (step >= (h ? steps : min(cross, steps))) continue;
-        const int i = (step * kUnroll + j % kUnroll) * NT + owner;
-        if (i >= n_vec) continue;
-        const uint4 q = load_stream(vec + i);
-        const int id0 = begin + head + i * kPerVec;
-#pragma unroll
-        for (int e = 0; e < kPerVec / 2; ++e) {
-          const float2 z = pair_of<FMT>(q, e);
-          offer(z.x, id0 + 2 * e);
-          offer(z.y, id0 + 2 * e + 1);
-        }
-      }
-      __syncthreads();
-    }
-    if (n_hot > kHotPieces || sh.n_cand > kCandidates) {
-      __syncthreads();
-      select_exact<FMT, NT>(row, begin, end, a.top_k, sh);
-    }
-    rank_entries(sh.cand, sh.n_cand, sh.best, NT);
-    __syncthreads();
-  }
+  if constexpr (TOP) find_alternatives<FMT, NT>(row, vec, begin, end, head, n_vec, piece_steps * kUnroll, a.top_k, top_mem);
   // ---- join the CTAs of the row
   if (split > 1) {
     cluster_wait();                          // every CTA of the cluster runs: its shared memory may be written
@@ -502,8 +531,8 @@ token_logprobs_kernel(const __grid_constant__ LogprobArgs a, int split) {
       asm volatile("st.shared::cluster.f32 [%0 + 8], %1;" ::"r"(dst), "f"(st.t) : "memory");
     }
     if constexpr (TOP) {
-      if (tid < kTopMax)
-        asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(map_to_first(&top_mem.gathered[rank][tid])),
+      if (tid < a.top_k)
+        asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(map_to_first(&top_mem.gathered[rank * a.top_k + tid])),
                      "l"(top_mem.best[tid])
                      : "memory");
     }
@@ -513,8 +542,9 @@ token_logprobs_kernel(const __grid_constant__ LogprobArgs a, int split) {
     if constexpr (TOP) {
       TopShared &sh = top_mem;
       if (tid < kTopMax) sh.best[tid] = 0;
+      if (tid == kTopMax) sh.gathered[split * a.top_k] = 0;
       __syncthreads();
-      rank_entries(&sh.gathered[0][0], split * kTopMax, sh.best, NT);
+      rank_entries(sh.gathered, split * a.top_k, sh.best, NT);
       __syncthreads();
     }
     if (warp == 0) {
@@ -570,7 +600,7 @@ cudaError_t launch_logprobs(const LogprobArgs &a, int split, cudaStream_t s) {
 }
 template <int FMT>
 cudaError_t launch_logprobs_fmt(const LogprobArgs &a, int split, bool wide, cudaStream_t s) {
-  return wide ? launch_logprobs<FMT, 512>(a, split, s) : launch_logprobs<FMT, 128>(a, split, s);
+  return wide ? launch_logprobs<FMT, 256>(a, split, s) : launch_logprobs<FMT, 128>(a, split, s);
 }
 
 cudaError_t logprobs_launch(const LogprobArgs &a, int format, cudaStream_t s) {
@@ -579,10 +609,13 @@ cudaError_t logprobs_launch(const LogprobArgs &a, int format, cudaStream_t s) {
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
   if (e != cudaSuccess) return e;
   const int64_t row_vecs = static_cast<int64_t>(a.V) * (format == 2 ? 4 : 2) / 16;
-  // 512 threads take 2048 vectors a step; rows of less than two steps of 128 threads leave most of them idle
-  const bool wide = row_vecs > 1024;
   int split = 1;
   while (split < kMaxSplit && static_cast<int64_t>(a.R) * split < 2 * sms && row_vecs / (2 * split) >= 512) split *= 2;
+  // Four CTAs of 256 threads or eight of 128 fit an SM.  While the launch fits in one round the larger ones finish sooner
+  // (592 rows of 151936 half values: 33.0 against 37.5 us); in a launch of several rounds the smaller ones leave less
+  // idle at the end and overlap their beginnings and ends better (3000 x 20000 bf16: 26.0 against 33.4 us; 777 x 50263
+  // fp32: 22.8 against 29.2; 2048 x 151936 bf16: 101.0 against 101.8).
+  const bool wide = row_vecs > 1024 && static_cast<int64_t>(a.R) * split <= 4 * sms;
   switch (format) {
     case 0: return launch_logprobs_fmt<0>(a, split, wide, s);
     case 1: return launch_logprobs_fmt<1>(a, split, wide, s);
@@ -627,64 +660,91 @@ template <int FMT> __device__ __forceinline__ uint4 pack_vec(const float (&f)[Fm
 }
 // 16 bytes that start `bytes` (a multiple of 2) into the 32 bytes lo, hi
 __device__ __forceinline__ uint4 bytes_from(const uint4 &lo, const uint4 &hi, int bytes) {
-  const uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
-  uint32_t o[4];
-  const int words = bytes >> 2, bits = (bytes & 3) * 8;
+  uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+  if (bytes & 8) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    uint32_t x = 0, y = 0;
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (words == j) {
-        x = w[i + j];
-        y = w[i + j + 1];
-      }
-    o[i] = __funnelshift_r(x, y, bits);
+    for (int i = 0; i < 6; ++i) w[i] = w[i + 2];
   }
-  return make_uint4(o[0], o[1], o[2], o[3]);
+  if (bytes & 4) {
+#pragma unroll
+    for (int i = 0; i < 5; ++i) w[i] = w[i + 1];
+  }
+  const int bits = (bytes & 3) * 8;
+  return make_uint4(__funnelshift_r(w[0], w[1], bits), __funnelshift_r(w[1], w[2], bits), __funnelshift_r(w[2], w[3], bits),
+                    __funnelshift_r(w[3], w[4], bits));
 }
 
-constexpr int kBackThreads = 256, kBackUnroll = 4;
+constexpr int kBackThreads = 256, kBackUnroll = 2;
 
+// One CTA per slice of a row.  The first vectors are requested before the row's scalars, whose latency would otherwise
+// stand in front of every slice, and from then on a step's loads run under the step before it.  Bound by HBM, as many
+// bytes written as read: 2048 x 151936 bf16 in 213 us, 5.8 TB/s.  Two vectors a step and six CTAs an SM against four and
+// four: 219 against 226 us; ordinary stores against evict-first ones: 213 against 219.
 template <int FMT, bool ENT>
-__device__ __forceinline__ void backward_row(const BackwardArgs &a, const RowGrad &g, const char *zrow, char *orow,
-                                             int begin, int end) {
+__global__ void __launch_bounds__(kBackThreads, 6)
+token_logprobs_backward_kernel(const __grid_constant__ BackwardArgs a, int slices, int slice_elems) {
   constexpr int kPerVec = Fmt<FMT>::kPerVec, kBytes = Fmt<FMT>::kBytes;
   const int tid = threadIdx.x;
-  const float c = a.c;
-  auto one = [&](int i) {
-    const float z = load_elem<FMT>(zrow, i);
-    float d = grad_pair<ENT>(make_float2(z, z), g, c).x;
-    if (i == g.token) d += g.hot;
-    store_elem<FMT>(orow, i, d);
-  };
+  const int r = static_cast<int>(blockIdx.x / slices), slice = static_cast<int>(blockIdx.x % slices);
+  const int begin = slice * slice_elems, end = min(begin + slice_elems, a.V);
+  const char *zrow = static_cast<const char *>(a.logits) + static_cast<size_t>(r) * a.row_stride * kBytes;
+  char *orow = static_cast<char *>(a.out) + static_cast<size_t>(r) * a.out_stride * kBytes;
   // whole 16-byte vectors of the output; where the logits lie differently on 16-byte boundaries (a padded or offset
   // row beside a dense output) a vector is cut out of the two aligned ones around it, both inside the row
-  const int off = static_cast<int>((reinterpret_cast<uintptr_t>(orow + static_cast<size_t>(begin) * kBytes)) & 15);
+  const int off = static_cast<int>(reinterpret_cast<uintptr_t>(orow + static_cast<size_t>(begin) * kBytes) & 15);
   int head = min(((16 - off) & 15) / kBytes, end - begin);
-  int skew = static_cast<int>(reinterpret_cast<uintptr_t>(zrow + static_cast<size_t>(begin + head) * kBytes) & 15);
-  if (skew && begin + head - skew / kBytes < 0) {             // first aligned vector would begin before the row
-    head = min(head + kPerVec, end - begin);
-  }
+  const int skew = static_cast<int>(reinterpret_cast<uintptr_t>(zrow + static_cast<size_t>(begin + head) * kBytes) & 15);
+  if (skew && begin + head - skew / kBytes < 0) head = min(head + kPerVec, end - begin);       // would begin before the row
   int n_vec = (end - begin - head) / kPerVec;
-  if (skew && n_vec > 0 && begin + head + n_vec * kPerVec + kPerVec - skew / kBytes > a.V) --n_vec;
+  if (skew && n_vec > 0 && begin + head + n_vec * kPerVec + kPerVec - skew / kBytes > a.V) --n_vec;   // would end behind it
   const int tail0 = begin + head + n_vec * kPerVec;
-  for (int i = begin + tid; i < begin + head; i += kBackThreads) one(i);
-  for (int i = tail0 + tid; i < end; i += kBackThreads) one(i);
   const uint4 *zv = reinterpret_cast<const uint4 *>(zrow + static_cast<size_t>(begin + head) * kBytes - skew);
   uint4 *ov = reinterpret_cast<uint4 *>(orow + static_cast<size_t>(begin + head) * kBytes);
-  for (int base = 0; base < n_vec; base += kBackThreads * kBackUnroll) {
-    uint4 q[kBackUnroll];
+  auto fetch = [&](uint4 (&q)[kBackUnroll], int step) {
 #pragma unroll
     for (int u = 0; u < kBackUnroll; ++u) {
-      const int i = base + u * kBackThreads + tid;
-      if (i >= n_vec) continue;
-      q[u] = load_once(zv + i);
-      if (skew) q[u] = bytes_from(q[u], load_once(zv + i + 1), skew);
+      const int i = (step * kBackUnroll + u) * kBackThreads + tid;
+      if (i < n_vec) {
+        q[u] = load_once(zv + i);
+        if (skew) q[u] = bytes_from(q[u], load_once(zv + i + 1), skew);
+      }
     }
+  };
+  uint4 qa[kBackUnroll], qb[kBackUnroll];
+  fetch(qa, 0);
+  RowGrad g;
+  g.token = a.tokens ? a.tokens[r] : -1;
+  const float2 st = a.stats[r];
+  const float gl = a.grad_logprobs ? a.grad_logprobs[r] : 0.f;
+  const float gb = ENT ? a.grad_entropy[r] : 0.f, H = ENT ? a.entropy[r] : 0.f;
+  const float ga = g.token >= 0 ? gl : 0.f;
+  // no gradient arrives, or nothing is left in the row: zeros, whatever the logits hold
+  const bool zero = (ga == 0.f && gb == 0.f) || st.y == -INFINITY;
+  g.m = st.x;
+  g.log2_l = st.y * kLog2e;
+  g.hot = ga * a.inv_temperature;
+  g.A = (gb != 0.f ? fmaf(gb, H, ga) : ga) * a.inv_temperature;
+  g.B = gb * kLn2 * a.inv_temperature;
+  const float c = a.c;
+  auto one = [&](int i) {
+    float d = 0.f;
+    if (!zero) {
+      const float z = load_elem<FMT>(zrow, i);
+      d = grad_pair<ENT>(make_float2(z, z), g, c).x;
+      if (i == g.token) d += g.hot;
+    }
+    store_elem<FMT>(orow, i, d);
+  };
+  for (int i = begin + tid; i < begin + head; i += kBackThreads) one(i);
+  for (int i = tail0 + tid; i < end; i += kBackThreads) one(i);
+  if (zero) {
+    for (int i = tid; i < n_vec; i += kBackThreads) __stcs(ov + i, make_uint4(0u, 0u, 0u, 0u));
+    return;
+  }
+  auto finish = [&](const uint4 (&q)[kBackUnroll], int step) {
 #pragma unroll
     for (int u = 0; u < kBackUnroll; ++u) {
-      const int i = base + u * kBackThreads + tid;
+      const int i = (step * kBackUnroll + u) * kBackThreads + tid;
       if (i >= n_vec) continue;
       float f[kPerVec];
 #pragma unroll
@@ -699,48 +759,22 @@ __device__ __forceinline__ void backward_row(const BackwardArgs &a, const RowGra
         for (int e = 0; e < kPerVec; ++e)
           if (e == at) f[e] += g.hot;
       }
-      __stcs(ov + i, pack_vec<FMT>(f));
+      ov[i] = pack_vec<FMT>(f);
     }
+  };
+  const int steps = (n_vec + kBackThreads * kBackUnroll - 1) / (kBackThreads * kBackUnroll);
+  for (int s = 0; s < steps; s += 2) {
+    fetch(qb, s + 1);
+    finish(qa, s);
+    fetch(qa, s + 2);
+    finish(qb, s + 1);
   }
-}
-
-// grid: (row, slice of the row); every thread of a CTA works on the same row
-template <int FMT>
-__global__ void __launch_bounds__(kBackThreads)
-token_logprobs_backward_kernel(const __grid_constant__ BackwardArgs a, int slices, int slice_elems) {
-  constexpr int kBytes = Fmt<FMT>::kBytes;
-  const int r = static_cast<int>(blockIdx.x / slices), slice = static_cast<int>(blockIdx.x % slices);
-  const int begin = slice * slice_elems, end = min(begin + slice_elems, a.V);
-  const char *zrow = static_cast<const char *>(a.logits) + static_cast<size_t>(r) * a.row_stride * kBytes;
-  char *orow = static_cast<char *>(a.out) + static_cast<size_t>(r) * a.out_stride * kBytes;
-  RowGrad g;
-  g.token = a.tokens ? a.tokens[r] : -1;
-  const float2 st = a.stats[r];
-  const float ga = (a.grad_logprobs && g.token >= 0) ? a.grad_logprobs[r] : 0.f;
-  const float gb = a.grad_entropy ? a.grad_entropy[r] : 0.f;
-  if ((ga == 0.f && gb == 0.f) || st.y == -INFINITY) {
-    // no gradient arrives, or nothing is left in the row: zeros, and the logits are not read
-    const int off = static_cast<int>(reinterpret_cast<uintptr_t>(orow + static_cast<size_t>(begin) * kBytes) & 15);
-    const int head = min(((16 - off) & 15) / kBytes, end - begin);
-    const int n_vec = (end - begin - head) / Fmt<FMT>::kPerVec;
-    for (int i = begin + threadIdx.x; i < begin + head; i += kBackThreads) store_elem<FMT>(orow, i, 0.f);
-    uint4 *ov = reinterpret_cast<uint4 *>(orow + static_cast<size_t>(begin + head) * kBytes);
-    for (int i = threadIdx.x; i < n_vec; i += kBackThreads) __stcs(ov + i, make_uint4(0u, 0u, 0u, 0u));
-    for (int i = begin + head + n_vec * Fmt<FMT>::kPerVec + threadIdx.x; i < end; i += kBackThreads)
-      store_elem<FMT>(orow, i, 0.f);
-    return;
-  }
-  g.m = st.x;
-  g.log2_l = st.y * kLog2e;
-  g.hot = ga * a.inv_temperature;
-  g.A = (gb != 0.f ? fmaf(gb, a.entropy[r], ga) : ga) * a.inv_temperature;
-  g.B = gb * kLn2 * a.inv_temperature;
-  if (gb != 0.f) backward_row<FMT, true>(a, g, zrow, orow, begin, end);
-  else backward_row<FMT, false>(a, g, zrow, orow, begin, end);
 }
 
 template <int FMT> cudaError_t launch_backward(const BackwardArgs &a, int slices, int slice_elems, cudaStream_t s) {
-  token_logprobs_backward_kernel<FMT><<<static_cast<unsigned>(a.R) * slices, kBackThreads, 0, s>>>(a, slices, slice_elems);
+  const unsigned grid = static_cast<unsigned>(a.R) * slices;
+  if (a.grad_entropy) token_logprobs_backward_kernel<FMT, true><<<grid, kBackThreads, 0, s>>>(a, slices, slice_elems);
+  else token_logprobs_backward_kernel<FMT, false><<<grid, kBackThreads, 0, s>>>(a, slices, slice_elems);
   return cudaGetLastError();
 }
 
@@ -941,10 +975,17 @@ int echo_token_logprobs_backward(const void *logits, int32_t logits_format, int6
   const uintptr_t z0 = reinterpret_cast<uintptr_t>(logits), o0 = reinterpret_cast<uintptr_t>(out_grad);
   const uintptr_t z1 = z0 + (static_cast<size_t>(R - 1) * row_stride + V) * eb, o1 = o0 + (static_cast<size_t>(R - 1) * grad_stride + V) * eb;
   if (z0 < o1 && o0 < z1 && !(z0 == o0 && (row_stride == grad_stride || R == 1))) return ECHO_ERR_INVALID;
-  // a CTA takes two steps of its threads' vectors: long enough to cover its start, short enough to spread few rows
-  const int slice = kBackThreads * kBackUnroll * 2 * (16 / static_cast<int>(eb));
-  const int64_t slices = (static_cast<int64_t>(V) + slice - 1) / slice;
-  if (V > kMaxVocab || static_cast<int64_t>(R) * slices > 0x7fffffffLL) return ECHO_ERR_UNSUPPORTED;
+  if (V > kMaxVocab) return ECHO_ERR_UNSUPPORTED;
+  int dev = 0, sms = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
+    return ECHO_ERR_CUDA;
+  // slices of whole steps: as long as a row allows while the launch still has about six rounds of CTAs (few rows are
+  // cut finely, many rows into long runs whose start-up counts for little)
+  const int64_t step = kBackThreads * kBackUnroll * (16 / static_cast<int64_t>(eb)), steps = (V + step - 1) / step;
+  const int64_t wanted = std::min(steps, (24 * static_cast<int64_t>(sms) + R - 1) / R);
+  const int64_t per_slice = (steps + wanted - 1) / wanted, slices = (steps + per_slice - 1) / per_slice;
+  const int slice = static_cast<int>(per_slice * step);
+  if (static_cast<int64_t>(R) * slices > 0x7fffffffLL) return ECHO_ERR_UNSUPPORTED;
   BackwardArgs a{};
   a.logits = logits;
   a.row_stride = row_stride;
