@@ -498,21 +498,24 @@ def _call(device: torch.device, fn, *args):
 
 
 def _check_rows(logits: torch.Tensor, tokens: Optional[torch.Tensor]):
-    assert logits.is_cuda and logits.dim() == 2 and logits.dtype in _FORMATS
     R, V = logits.shape
-    assert logits.stride(1) == 1 or V <= 1, "the elements of a row of logits lie side by side"
-    stride = logits.stride(0) if R > 1 else V
+    stride, side = logits.stride()
+    assert logits.is_cuda and logits.dtype in _FORMATS
+    assert side == 1 or V <= 1, "the elements of a row of logits lie side by side"
+    if R <= 1:
+        stride = V
     assert stride >= V, "rows of logits do not overlap"
     if tokens is not None:
-        assert tokens.device == logits.device and tokens.dtype == torch.int32 and tokens.is_contiguous()
-        assert tokens.shape == (R,)
+        assert tokens.dtype is torch.int32 and tokens.shape == (R,) and tokens.is_contiguous()
+        assert tokens.get_device() == logits.get_device()
     return R, V, stride
 
 
-def _check_vector(x: Optional[torch.Tensor], like: torch.Tensor, shape):
+def _address(x: Optional[torch.Tensor], index: int, shape):
+    """Address of a contiguous fp32 tensor of the given shape on GPU `index` (None: none)."""
     if x is None:
         return None
-    assert x.dtype == torch.float32 and x.shape == shape and x.is_contiguous() and x.device == like.device
+    assert x.dtype is torch.float32 and x.shape == shape and x.is_contiguous() and x.get_device() == index
     return x.data_ptr()
 
 
@@ -543,14 +546,16 @@ def echo_token_logprobs_backward(logits: torch.Tensor, tokens: Optional[torch.Te
     """Gradient of the logits from those of the log-probabilities and entropies ([R] each, or None), in the logits'
     dtype; entropy and stats as echo_token_logprobs returned them.  out: where to (the logits themselves are allowed)."""
     R, V, stride = _check_rows(logits, tokens)
+    index = logits.get_device()
     if out is None:
-        out = torch.empty((R, V), dtype=logits.dtype, device=logits.device)
-    assert out.device == logits.device and out.dtype == logits.dtype and out.shape == logits.shape
-    _, _, out_stride = _check_rows(out, None)
+        out, out_stride = torch.empty((R, V), dtype=logits.dtype, device=logits.device), V
+    else:
+        assert out.get_device() == index and out.dtype is logits.dtype and out.shape == logits.shape
+        _, _, out_stride = _check_rows(out, None)
     _call(logits.device, lib.echo_token_logprobs_backward, logits.data_ptr(), _FORMATS[logits.dtype], stride, R, V,
-          tokens.data_ptr() if tokens is not None else None, temperature, _check_vector(entropy, logits, (R,)),
-          _check_vector(stats, logits, (R, 2)), _check_vector(grad_logprobs, logits, (R,)),
-          _check_vector(grad_entropy, logits, (R,)), out.data_ptr(), out_stride)
+          tokens.data_ptr() if tokens is not None else None, temperature, _address(entropy, index, (R,)),
+          _address(stats, index, (R, 2)), _address(grad_logprobs, index, (R,)), _address(grad_entropy, index, (R,)),
+          out.data_ptr(), out_stride)
     return out
 
 
@@ -559,17 +564,17 @@ def echo_grpo_gradient(logp_new: torch.Tensor, logp_old: torch.Tensor, logp_samp
                        grad_out: Optional[torch.Tensor], eps_clip: float, C_trunc: float, beta: float):
     """echo_grpo_objective (echo_grpo_surrogate where logp_ref is None) and its gradient with respect to logp_new:
     (objective [n], gradient [n][T]).  grad_out [n] or None (ones): what arrives at the objective."""
-    assert logp_new.is_cuda and logp_new.dim() == 2
-    n, T = logp_new.shape
-    dev = logp_new.device
+    assert logp_new.is_cuda
+    n, T = shape = logp_new.shape
+    index = logp_new.get_device()
     if mask is not None:
-        assert mask.device == dev and mask.dtype == torch.uint8 and mask.is_contiguous() and mask.shape == (n, T)
-    out = torch.empty(n, dtype=torch.float32, device=dev)
-    grad = torch.empty((n, T), dtype=torch.float32, device=dev)
-    _call(dev, lib.echo_grpo_gradient, _check_vector(logp_new, logp_new, (n, T)), _check_vector(logp_old, logp_new, (n, T)),
-          _check_vector(logp_sampler, logp_new, (n, T)), _check_vector(logp_ref, logp_new, (n, T)),
-          _check_vector(adv, logp_new, (n,)), mask.data_ptr() if mask is not None else None,
-          _check_vector(grad_out, logp_new, (n,)), n, T, eps_clip, C_trunc, beta, out.data_ptr(), grad.data_ptr())
+        assert mask.get_device() == index and mask.dtype is torch.uint8 and mask.is_contiguous() and mask.shape == shape
+    out = torch.empty(n, dtype=torch.float32, device=logp_new.device)
+    grad = torch.empty_like(logp_new)
+    _call(logp_new.device, lib.echo_grpo_gradient, _address(logp_new, index, shape), _address(logp_old, index, shape),
+          _address(logp_sampler, index, shape), _address(logp_ref, index, shape), _address(adv, index, (n,)),
+          mask.data_ptr() if mask is not None else None, _address(grad_out, index, (n,)), n, T, eps_clip, C_trunc, beta,
+          out.data_ptr(), grad.data_ptr())
     return out, grad
 
 
@@ -636,7 +641,7 @@ def echo_adamw_step(tensors: AdamWTensors, step: int, lr: float, beta1: float = 
     second moments."""
     opt = EchoAdamWOptions(lr, beta1, beta2, eps, step, seed, None, tensors.grad_format, tensors.state_bits)
     if grad_scale is not None:
-        assert grad_scale.device == tensors.device and grad_scale.dtype == torch.float32 and grad_scale.numel() == 1
+        assert grad_scale.get_device() == tensors.device.index and grad_scale.dtype is torch.float32 and grad_scale.numel() == 1
         opt.grad_scale = grad_scale.data_ptr()
     _call(tensors.device, lib.echo_adamw_step, tensors.table, tensors.count, C.byref(opt))
 
@@ -644,10 +649,10 @@ def echo_adamw_step(tensors: AdamWTensors, step: int, lr: float, beta1: float = 
 def echo_adamw_unpack(tensors: AdamWTensors, out_avg: Sequence[torch.Tensor], out_avg_sq: Sequence[torch.Tensor]):
     """Writes the fp32 values that the 8-bit moments of the list stand for into the given tensors."""
     assert tensors.state_bits == 8 and len(out_avg) == tensors.count and len(out_avg_sq) == tensors.count
-    addresses = []
+    index, addresses = tensors.device.index, []
     for outs in (out_avg, out_avg_sq):
-        assert [x.numel() for x in outs] == tensors.sizes
-        assert all(x.dtype == torch.float32 and x.is_contiguous() and x.device == tensors.device for x in outs)
+        for x, size in zip(outs, tensors.sizes):
+            assert x.dtype is torch.float32 and x.numel() == size and x.is_contiguous() and x.get_device() == index
         addresses.append((C.c_void_p * max(tensors.count, 1))(*[x.data_ptr() for x in outs]))
     _call(tensors.device, lib.echo_adamw_unpack, tensors.table, tensors.count, addresses[0], addresses[1])
 

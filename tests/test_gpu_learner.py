@@ -540,3 +540,130 @@ def test_repeats_are_equal_and_graphs_replay(B):
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(first, third))
         assert all(torch.equal(a, b) for a, b in zip(state, [x for k in d for x in d[k]]))
+
+
+def _engine(B, vocab, P, G, Lp, T, eos_id=-1, **more):
+    from paper_2602_02192_b200 import synth
+    shape = synth.DecoderShape("small", 2, 128, 2, 1, 64, 256, vocab)
+    w = synth.make_weights(shape, 3, device="cuda", std=0.08)
+    eng = B.Engine(B.make_config(shape, P, G, Lp, T, eos_id=eos_id, **more))
+    eng.echo_load_policy(w, 1)
+    eng.echo_wait_policy()
+    prompts = torch.from_numpy(synth.make_prompts(P, Lp, vocab, 5)).cuda()
+    return shape, w, eng, prompts
+
+
+@pytest.mark.parametrize("eos", [-1, 7])
+def test_score_detail(B, eos, monkeypatch):
+    """With as many alternatives as ids the whole distribution comes back: it has to hold the log-probability that
+    echo_score gives, sum to 1 and have the entropy that is reported.  (Fixed-order projections: both calls then see the
+    same logits, bit for bit.)"""
+    monkeypatch.setenv("ECHO_DETERMINISTIC", "1")
+    P, G, Lp, T, V = 3, 2, 9, 12, 32
+    shape, w, eng, prompts = _engine(B, V, P, G, Lp, T, eos)
+    lens = [9, 4, 1]
+    tok, lp, _ = eng.echo_rollout(prompts, lens, G, T, 0.8, 11)
+    if eos >= 0:
+        tok[0, 0, 3] = eos                               # ends early; what follows is not scored
+    want, _ = eng.echo_score(prompts, lens, tok, 0.8)
+    got, H, ids, top, ver = eng.echo_score_detail(prompts, lens, tok, 0.8, V)
+    _, H0, none_ids, none_top, _ = eng.echo_score_detail(prompts, lens, tok, 0.8)
+    _, _, ids5, top5, _ = eng.echo_score_detail(prompts, lens, tok, 0.8, 5)
+    eng.echo_sync()
+    assert none_ids is None and none_top is None and torch.equal(H, H0)
+    assert torch.equal(ids5, ids[..., :5]) and torch.equal(top5, top[..., :5]) and np.all(ver == 1)
+    want, got, H, ids, top, tk = (x.cpu().numpy() for x in (want, got, H, ids, top, tok))
+    assert np.all(np.abs(got - want) <= E * 64 * np.maximum(1, np.abs(want)))       # two kernels, one formula, 32 ids
+    live = np.ones((P, G, T), dtype=bool)
+    if eos >= 0:
+        for p in range(P):
+            for g in range(G):
+                at = np.nonzero(tk[p, g] == eos)[0]
+                if len(at):
+                    live[p, g, at[0] + 1:] = False
+        assert not live.all()
+        assert np.all(got[~live] == 0) and np.all(H[~live] == 0) and np.all(ids[~live] == -1) and np.isneginf(top[~live]).all()
+    assert np.all(np.sort(ids[live], axis=-1) == np.arange(V)) and np.all(np.diff(top[live], axis=-1) <= 0)
+    prob = np.exp(top[live].astype(np.float64))
+    assert np.abs(prob.sum(axis=-1) - 1).max() < E * 64 * 4
+    assert np.abs(-(prob * top[live]).sum(axis=-1) - H[live]).max() < E * 64 * 16
+    at = (ids == tk[..., None]) & live[..., None]
+    assert np.array_equal(at.sum(axis=-1), live.astype(int)) and np.array_equal(top[at], got[live])
+    eng.close()
+
+
+def test_score_detail_refuses_bad_tokens(B):
+    shape, w, eng, prompts = _engine(B, 64, 1, 1, 4, 3)
+    tok = torch.tensor([[[1, 64, 2]]], dtype=torch.int32, device="cuda")
+    eng.echo_score_detail(prompts, [4], tok, 1.0, 2)
+    with pytest.raises(B.EchoError) as e:
+        eng.echo_sync()
+    assert e.value.code == -7
+    eng.close()
+
+
+def test_one_learner_step(B):
+    """Rollout -> rewards -> log-probabilities of the learner's logits -> objective and gradient -> gradient of the
+    logits -> gradient of the lm_head -> AdamW -> next snapshot, as a trainer runs it."""
+    P, G, Lp, T, V = 4, 4, 8, 17, 500
+    shape, w, eng, prompts = _engine(B, V, P, G, Lp, T)
+    n, d = P * G, shape.d_model
+    hidden = torch.zeros((T - 1, n, d), device="cuda")
+    eng.echo_debug_capture(shape.n_layers - 1, dec_out=hidden)
+    tok, lp_sampler, ver = eng.echo_rollout(prompts, [Lp] * P, G, T, 1.0, 21)
+    eng.echo_sync()
+    eng.echo_debug_capture(-1)
+    adv = B.echo_group_advantage(torch.rand((P, G), generator=torch.Generator().manual_seed(0)).cuda()).view(n)
+    # the learner's own forward: tokens 1..T-1 from the last layer's output
+    h = hidden * torch.rsqrt(hidden.pow(2).mean(dim=-1, keepdim=True) + shape.rms_eps) * w["final_norm"].float()
+    h = h.transpose(0, 1).reshape(n * (T - 1), d).contiguous()
+    y = tok.view(n, T)[:, 1:].reshape(-1).contiguous()
+    sampler = lp_sampler.view(n, T)[:, 1:].contiguous()
+    master = w["lm_head"].float().contiguous()
+
+    def objective(weight):
+        logits = (h.double() @ weight.double().T).float()
+        lp, H, st, _, _ = B.echo_token_logprobs(logits, y)
+        value, g = B.echo_grpo_gradient(lp.view(n, T - 1), old, sampler, sampler, adv, None, None, 0.2, 2.0, 0.04)
+        return logits, lp, H, st, value, g
+
+    old = sampler
+    _, lp, _, _, _, _ = objective(master)
+    # the learner's logits are the sampler's up to the engine's 16-bit activations
+    assert float((lp.view(n, T - 1) - sampler).abs().max()) < 5e-2
+    old = lp.view(n, T - 1).clone()
+    logits, lp, H, st, value, g = objective(master)
+    bonus = torch.full((n * (T - 1),), 0.01, device="cuda")
+    dz = B.echo_token_logprobs_backward(logits, y, H, st, g.view(-1), bonus, out=logits)          # in place
+    dW = dz.T @ h
+    # the gradient against a difference along a random direction: J is smooth here up to the clipping borders at
+    # rho = 0.8 and 1.2, far from rho = 1; h = 2^-8 moves a logit by at most 0.03
+    step = torch.randn(master.shape, generator=torch.Generator(device="cuda").manual_seed(5), device="cuda")
+    s = 2.0 ** -8 / float((h @ step.T).abs().max())
+    values = []
+    for sign in (1.0, -1.0):
+        _, _, H2, _, v2, _ = objective(master + sign * s * step)
+        values.append(float(v2.double().sum() + (bonus.double() * H2.double()).sum()))
+    slope, want = (values[0] - values[1]) / (2 * s), float((dW.double() * step.double()).sum())
+    # values of ~n terms in fp32 (2^-24 each) over 2 s, and the third derivative's s^2
+    noise = 2.0 ** -22 * (float(value.abs().sum()) + 0.01 * float(H.sum())) / s
+    assert abs(slope - want) <= noise + 1e-3 * float(dz.abs().sum()) * float((h @ step.T).abs().max())
+    # update, snapshot, next version
+    copy = torch.empty_like(w["lm_head"])
+    plan = B.AdamWTensors.zeros([master], [(-dW).to(torch.bfloat16)], state_bits=8, copies=[copy])
+    norm = dW.norm()
+    before = master.clone()
+    B.echo_adamw_step(plan, 1, 1e-3, grad_scale=(1.0 / norm.clamp(min=1.0)).view(1), seed=1)
+    assert torch.equal(copy, master.to(torch.bfloat16)) and float((master - before).abs().max()) <= 1.01e-3
+    assert float(((master - before) * dW).sum()) > 0                       # uphill
+    w2 = dict(w)
+    w2["lm_head"] = copy
+    eng.echo_load_policy(w2, 2)
+    eng.echo_wait_policy()
+    lp2, ver2 = eng.echo_score(prompts, [Lp] * P, tok, 1.0)
+    eng.echo_sync()
+    assert np.all(ver == 1) and np.all(ver2 == 2)
+    _, lp_learner, *_ = objective(copy.float())
+    # hidden states are the same; the engine multiplies 16-bit activations
+    assert float((lp2.view(n, T)[:, 1:].reshape(-1) - lp_learner).abs().max()) < 5e-2
+    eng.close()
