@@ -609,8 +609,12 @@ cudaError_t logprobs_launch(const LogprobArgs &a, int format, cudaStream_t s) {
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
   if (e != cudaSuccess) return e;
   const int64_t row_vecs = static_cast<int64_t>(a.V) * (format == 2 ? 4 : 2) / 16;
+  // Few rows are cut over the CTAs of a cluster until the launch has about one CTA and a half per SM (two without
+  // alternatives, which cost less to join): 200 rows of 151936 fp32 values with 5 alternatives take 23.9 us in two parts
+  // and 28.3 in one, 64 rows 12.3 in four and 14.0 in eight, 256 rows bf16 24.2 in two and 21.2 in one.
   int split = 1;
-  while (split < kMaxSplit && static_cast<int64_t>(a.R) * split < 2 * sms && row_vecs / (2 * split) >= 512) split *= 2;
+  const int64_t enough = a.top_k > 0 ? 3 * sms / 2 : 2 * sms;
+  while (split < kMaxSplit && a.R * static_cast<int64_t>(split) < enough && row_vecs / (2 * split) >= 512) split *= 2;
   // Four CTAs of 256 threads or eight of 128 fit an SM.  While the launch fits in one round the larger ones finish sooner
   // (592 rows of 151936 half values: 33.0 against 37.5 us); in a launch of several rounds the smaller ones leave less
   // idle at the end and overlap their beginnings and ends better (3000 x 20000 bf16: 26.0 against 33.4 us; 777 x 50263
@@ -678,7 +682,7 @@ constexpr int kBackThreads = 256, kBackUnroll = 2;
 
 // One CTA per slice of a row.  The first vectors are requested before the row's scalars, whose latency would otherwise
 // stand in front of every slice, and from then on a step's loads run under the step before it.  Bound by HBM, as many
-// bytes written as read: 2048 x 151936 bf16 in 213 us, 5.8 TB/s.  Two vectors a step and six CTAs an SM against four and
+// bytes written as read: 2048 x 151936 bf16 in 207 us, 6.0 TB/s.  Two vectors a step and six CTAs an SM against four and
 // four: 219 against 226 us; ordinary stores against evict-first ones: 213 against 219.
 template <int FMT, bool ENT>
 __global__ void __launch_bounds__(kBackThreads, 6)
@@ -979,10 +983,10 @@ int echo_token_logprobs_backward(const void *logits, int32_t logits_format, int6
   int dev = 0, sms = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
     return ECHO_ERR_CUDA;
-  // slices of whole steps: as long as a row allows while the launch still has about six rounds of CTAs (few rows are
+  // slices of whole steps: as long as a row allows while the launch still has about eight rounds of CTAs (few rows are
   // cut finely, many rows into long runs whose start-up counts for little)
   const int64_t step = kBackThreads * kBackUnroll * (16 / static_cast<int64_t>(eb)), steps = (V + step - 1) / step;
-  const int64_t wanted = std::min(steps, (24 * static_cast<int64_t>(sms) + R - 1) / R);
+  const int64_t wanted = std::min(steps, (48 * static_cast<int64_t>(sms) + R - 1) / R);
   const int64_t per_slice = (steps + wanted - 1) / wanted, slices = (steps + per_slice - 1) / per_slice;
   const int slice = static_cast<int>(per_slice * step);
   if (static_cast<int64_t>(R) * slices > 0x7fffffffLL) return ECHO_ERR_UNSUPPORTED;
