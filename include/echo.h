@@ -323,7 +323,7 @@ int echo_grpo_objective(const float *logp_new, const float *logp_old, const floa
  * An id at -inf is masked: probability 0, never among the alternatives.  Places of a row that has fewer
  * than top_k ids left hold id -1 and -inf.  A row with nothing left (all -inf) scores -inf (0 without a
  * token), entropy 0, stats (-inf, -inf).  A NaN or +inf logit makes its row's log-probability, entropy
- * and log l NaN; NaN is never an alternative.  V <= 2^30.  R = 0 does nothing. */
+ * and log l NaN; NaN is never an alternative.  V <= 2^24.  R = 0 does nothing. */
 int echo_token_logprobs(const void *logits, int32_t logits_format, int64_t row_stride, int32_t R, int32_t V,
                         const int32_t *tokens, float temperature, int32_t top_k, float *out_logprobs,
                         float *out_entropy, float *out_stats, int32_t *out_top_ids, float *out_top_logprobs,

@@ -67,15 +67,21 @@ __device__ __forceinline__ void store8(float *p, const float (&x)[8]) {
 }
 // the eight elements of a lane: whole, or the first `left` of them one by one (the others read as 0)
 template <bool WHOLE> __device__ __forceinline__ void get_f32(const float *p, int left, float (&x)[8]) {
-  if (WHOLE) return load8(p, x);
+  if constexpr (WHOLE) {
+    load8(p, x);
+  } else {
 #pragma unroll
-  for (int j = 0; j < 8; ++j) x[j] = j < left ? p[j] : 0.f;
+    for (int j = 0; j < 8; ++j) x[j] = j < left ? p[j] : 0.f;
+  }
 }
 template <bool WHOLE> __device__ __forceinline__ void put_f32(float *p, int left, const float (&x)[8]) {
-  if (WHOLE) return store8(p, x);
+  if constexpr (WHOLE) {
+    store8(p, x);
+  } else {
 #pragma unroll
-  for (int j = 0; j < 8; ++j)
-    if (j < left) p[j] = x[j];
+    for (int j = 0; j < 8; ++j)
+      if (j < left) p[j] = x[j];
+  }
 }
 template <int FMT, bool WHOLE> __device__ __forceinline__ void get_grad(const void *g, size_t at, int left, float (&x)[8]) {
   if constexpr (FMT == 2) {
@@ -110,25 +116,26 @@ template <bool WHOLE> __device__ __forceinline__ void put_copy(__nv_bfloat16 *c,
 // the eight codes of a lane, element j in byte j
 template <bool WHOLE> __device__ __forceinline__ uint64_t get_codes(const void *c, size_t at, int left) {
   const uint8_t *b = static_cast<const uint8_t *>(c) + at;
-  if (WHOLE) {
+  if constexpr (WHOLE) {
     const uint2 w = __ldcs(reinterpret_cast<const uint2 *>(b));
     return static_cast<uint64_t>(w.y) << 32 | w.x;
-  }
-  uint64_t w = 0;
+  } else {
+    uint64_t w = 0;
 #pragma unroll
-  for (int j = 0; j < 8; ++j)
-    if (j < left) w |= static_cast<uint64_t>(b[j]) << (8 * j);
-  return w;
+    for (int j = 0; j < 8; ++j)
+      if (j < left) w |= static_cast<uint64_t>(b[j]) << (8 * j);
+    return w;
+  }
 }
 template <bool WHOLE> __device__ __forceinline__ void put_codes(void *c, size_t at, int left, uint64_t w) {
   uint8_t *b = static_cast<uint8_t *>(c) + at;
-  if (WHOLE) {
+  if constexpr (WHOLE) {
     *reinterpret_cast<uint2 *>(b) = make_uint2(static_cast<uint32_t>(w), static_cast<uint32_t>(w >> 32));
-    return;
-  }
+  } else {
 #pragma unroll
-  for (int j = 0; j < 8; ++j)
-    if (j < left) b[j] = static_cast<uint8_t>(w >> (8 * j));
+    for (int j = 0; j < 8; ++j)
+      if (j < left) b[j] = static_cast<uint8_t>(w >> (8 * j));
+  }
 }
 __device__ __forceinline__ uint32_t byte_of(uint64_t w, int j) { return static_cast<uint32_t>(w >> (8 * j)) & 0xffu; }
 __device__ __forceinline__ int signed_byte(uint64_t w, int j) { return static_cast<int>(static_cast<int8_t>(byte_of(w, j))); }
@@ -210,11 +217,59 @@ __device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
 // relative error of the fp32 moments, generously: a handful of roundings of 2^-24 each
 constexpr float kMomentErr = 1e-6f;
 
+// Below these a block's products of codes and scales may leave fp32's normal numbers (M / 127^2, V / 255^4).
+constexpr float kTinyAvg = 1e-32f, kTinySq = 1e-27f;
+// a largest value below the normal numbers counts as 0
+__device__ __forceinline__ float kept_scale(float largest) { return largest < 1.17549435e-38f ? 0.f : largest; }
+
 // a lane's elements, by number (each lane reads its own only)
 struct Stash {
   float4 g[2][32];
   uint64_t m[32], v[32];
+  __device__ float old_g(int lane, int j) const { return reinterpret_cast<const float *>(&g[j >> 2][lane])[j & 3]; }
+  __device__ int old_m(int lane, int j) const { return reinterpret_cast<const int8_t *>(&m[lane])[j]; }
+  __device__ uint32_t old_v(int lane, int j) const { return reinterpret_cast<const uint8_t *>(&v[lane])[j]; }
 };
+
+// the random numbers of eight elements, and the one of element j in [0, 1)
+__device__ __forceinline__ uint4 random_words(const Scalars &s, const Entry &e, uint64_t octet) {
+  return philox(make_uint4(static_cast<uint32_t>(octet), static_cast<uint32_t>(octet >> 32), e.id, s.step), s.key0, s.key1);
+}
+__device__ __forceinline__ double random_of(const uint4 &w, int j) {
+  const uint64_t half = j < 4 ? static_cast<uint64_t>(w.y) << 32 | w.x : static_cast<uint64_t>(w.w) << 32 | w.z;
+  return static_cast<double>(static_cast<uint32_t>(half >> (16 * (j & 3))) & 0xffffu) * 1.52587890625e-05;
+}
+
+// A block so small that fp32 products of its codes and scales leave the normal numbers: all of it in 64 bits.
+__device__ __noinline__ void quantise_tiny(const Scalars &s, const Entry &e, int64_t block, int lane, int left, float gs,
+                                           float M0, float V0, const Stash &stash) {
+  const uint4 words = random_words(s, e, static_cast<uint64_t>(block) * (kBlock / 8) + lane);
+  float M = 0.f, V = 0.f;
+  for (int j = 0; j < left; ++j) {
+    M = max_or_nan(M, static_cast<float>(exact_avg(s, stash.old_m(lane, j), M0, stash.old_g(lane, j), gs)), 0.f);
+    V = max_or_nan(V, static_cast<float>(exact_sq(s, stash.old_v(lane, j), V0, stash.old_g(lane, j), gs)), 0.f);
+  }
+  M = kept_scale(warp_max(M));
+  V = kept_scale(warp_max(V));
+  uint64_t mo = 0, vo = 0;
+  for (int j = 0; j < left; ++j) {
+    const double x = exact_avg(s, stash.old_m(lane, j), M0, stash.old_g(lane, j), gs);
+    const double y = exact_sq(s, stash.old_v(lane, j), V0, stash.old_g(lane, j), gs);
+    const int c = M > 0.f ? static_cast<int>(rint(127.0 * sqrt(fabs(x) / M))) : 0;
+    set_byte(mo, j, x < 0.0 ? -c : c);
+    if (V > 0.f && y > 0.0) {
+      const double w = y / V * 4228250625.0, d = fmin(floor(sqrt(sqrt(w))), 254.0), lo = d * d * (d * d);
+      const double hi = (d + 1.0) * (d + 1.0) * ((d + 1.0) * (d + 1.0));
+      set_byte(vo, j, max(static_cast<int>(d) + (random_of(words, j) * (hi - lo) < w - lo ? 1 : 0), 1));
+    }
+  }
+  put_codes<false>(e.m, block * kBlock + lane * 8, left, mo);
+  put_codes<false>(e.v, block * kBlock + lane * 8, left, vo);
+  if (lane == 0) {
+    e.m_scale[block] = M;
+    e.v_scale[block] = V;
+  }
+}
 
 template <int FMT, bool EIGHT, bool WHOLE>
 __device__ __forceinline__ void step_block(const Scalars &s, const Entry &e, int64_t block, int lane, float gs, Stash &stash) {
@@ -247,9 +302,9 @@ __device__ __forceinline__ void step_block(const Scalars &s, const Entry &e, int
     stash.g[1][lane] = make_float4(g[4], g[5], g[6], g[7]);
     stash.m[lane] = mc;
     stash.v[lane] = vc;
-    auto old_g = [&](int j) { return reinterpret_cast<const float *>(&stash.g[j >> 2][lane])[j & 3]; };
-    auto old_m = [&](int j) { return static_cast<int>(reinterpret_cast<const int8_t *>(&stash.m[lane])[j]); };
-    auto old_v = [&](int j) { return static_cast<uint32_t>(reinterpret_cast<const uint8_t *>(&stash.v[lane])[j]); };
+    auto old_g = [&](int j) { return stash.old_g(lane, j); };
+    auto old_m = [&](int j) { return stash.old_m(lane, j); };
+    auto old_v = [&](int j) { return stash.old_v(lane, j); };
     float m[8], v[8];
     float big_m = 0.f, big_b = 0.f, big_v = 0.f;
     const uint64_t mb = mc ^ 0x8080808080808080ull;            // c + 128
@@ -282,6 +337,8 @@ __device__ __forceinline__ void step_block(const Scalars &s, const Entry &e, int
     // are loops over bit masks: unrolled, their code would not fit the instruction cache.)
     big_m = warp_max(big_m);
     big_v = warp_max(big_v);
+    const bool tiny = (big_v > 0.f && big_v < kTinySq) || (V0 > 0.f && V0 < kTinySq) || (big_m > 0.f && big_m < kTinyAvg) ||
+                      (M0 > 0.f && M0 < kTinyAvg);
     // b1 |m| is at most b1 M0 and (1 - b1) |g| at most its largest: their sum's kMomentErr-th part bounds the error of
     // every m of the block
     const float err_m = kMomentErr * fmaf(s.b1, M0, warp_max(big_b));
@@ -304,15 +361,12 @@ __device__ __forceinline__ void step_block(const Scalars &s, const Entry &e, int
       const int j = __ffs(near_v) - 1;
       V = fmaxf(V, static_cast<float>(exact_sq(s, old_v(j), V0, old_g(j), gs)));
     }
-    M = isfinite(big_m) ? warp_max(M) : big_m;
-    V = isfinite(big_v) ? warp_max(V) : big_v;
-    if (M < 1.17549435e-38f) M = 0.f;          // below the normal numbers: counts as 0
-    if (V < 1.17549435e-38f) V = 0.f;
+    M = isfinite(big_m) ? kept_scale(warp_max(M)) : big_m;
+    V = isfinite(big_v) ? kept_scale(warp_max(V)) : big_v;
     const float inv_m = M > 0.f ? 16129.0f / M : 0.f, inv_v = V > 0.f ? 4228250625.0f / V : 0.f;
     const uint64_t octet = static_cast<uint64_t>(block) * (kBlock / 8) + lane;
-    const uint4 rnd = philox(make_uint4(static_cast<uint32_t>(octet), static_cast<uint32_t>(octet >> 32), e.id, s.step),
-                             s.key0, s.key1);
-    const uint32_t words[4] = {rnd.x, rnd.y, rnd.z, rnd.w};
+    const uint4 words4 = random_words(s, e, octet);
+    const uint32_t words[4] = {words4.x, words4.y, words4.z, words4.w};
     uint32_t mr[8], vr[8];                     // codes in the low bytes
     uint32_t unsure_m = 0, unsure_v = 0;
     const float err_y = 0.5f * err_m * inv_m;
@@ -350,12 +404,13 @@ __device__ __forceinline__ void step_block(const Scalars &s, const Entry &e, int
     uint64_t mo = low_bytes(mr), vo = low_bytes(vr);
     if (!(M > 0.f)) unsure_m = 0;
     if (!(V > 0.f)) unsure_v = 0;
-    // The code that fp32 chose is right or next to it: compared with the borders around it in 64 bits.
+    // A code from the 64-bit moment, rounded to fp32 only for the root, is right or next to it: it is compared with the
+    // borders around it in 64 bits.  (Of a second moment, a sum without cancellation, that holds for fp32's own code.)
 #pragma unroll 1
     for (; unsure_m; unsure_m &= unsure_m - 1) {
       const int j = __ffs(unsure_m) - 1;
       const double x = exact_avg(s, old_m(j), M0, old_g(j), gs), y = fabs(x) * 16129.0;
-      int c = abs(signed_byte(mo, j));
+      int c = static_cast<int>(rintf(sqrt_ftz(static_cast<float>(fabs(x)) * inv_m)));
       const double up = c + 0.5, down = c - 0.5;
       if (y > up * up * M) ++c;
       else if (c > 0 && y < down * down * M) --c;
@@ -371,9 +426,11 @@ __device__ __forceinline__ void step_block(const Scalars &s, const Entry &e, int
         lo = d * d * (d * d) * V;
       }
       const double hi = (d + 1.0) * (d + 1.0) * ((d + 1.0) * (d + 1.0)) * V;
-      const uint64_t half = j < 4 ? static_cast<uint64_t>(words[1]) << 32 | words[0] : static_cast<uint64_t>(words[3]) << 32 | words[2];
-      const double u = static_cast<double>(static_cast<uint32_t>(half >> (16 * (j & 3))) & 0xffffu) * 1.52587890625e-05;
-      if (y > 0.0) set_byte(vo, j, max(static_cast<int>(d) + (u * (hi - lo) < y - lo ? 1 : 0), 1));
+      if (y > 0.0) set_byte(vo, j, max(static_cast<int>(d) + (random_of(words4, j) * (hi - lo) < y - lo ? 1 : 0), 1));
+    }
+    if (tiny) {                                // (here few registers are live; the codes above mean nothing)
+      quantise_tiny(s, e, block, lane, left, gs, M0, V0, stash);
+      return;
     }
     put_codes<WHOLE>(e.m, at, left, mo);
     put_codes<WHOLE>(e.v, at, left, vo);

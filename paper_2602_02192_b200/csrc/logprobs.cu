@@ -134,7 +134,7 @@ constexpr int kUnroll = 4;         // 16-byte vectors per thread and step
 template <int NT> constexpr int kPieces = 1024 / NT;       // parts of a thread's elements whose maxima are kept
 constexpr uint32_t kNoEntry = 0x007fffffu;         // order_key(-inf)
 constexpr int kMaxSplit = 8;       // CTAs per row (one cluster)
-constexpr int kMaxVocab = 1 << 30; // element indexes of a row, plus a step, fit 32 bits
+constexpr int kMaxVocab = 1 << 24; // (find_alternatives divides places of a row in fp32)
 
 struct TopShared {
   uint32_t piece[1024];                      // order keys of the pieces' maxima
@@ -339,7 +339,9 @@ __device__ __noinline__ void find_alternatives(const void *row, const uint4 *vec
     if (tail0 + tid < end) offer(load_elem<FMT>(row, tail0 + tid), tail0 + tid);
     // a few vectors of the hot pieces per thread and turn, requested together
     const float pieces_per_vec = 1.0f / static_cast<float>(per);
-    const int total = n_hot * per;                           // (at most 512 pieces: places below are exact in fp32)
+    // at most 512 pieces of kMaxVocab / 4 / 1024 + 8 vectors: w + 1/2 is exact in fp32, and the quotient is off by less
+    // than 512 * 2^-23, half a vector's share of a piece being 1.2e-4
+    const int total = n_hot * per;
     for (int w0 = tid; w0 < total; w0 += kRescan * NT) {
       uint4 q[kRescan];
       int at[kRescan];
@@ -562,7 +564,7 @@ token_logprobs_kernel(const __grid_constant__ LogprobArgs a, int split) {
   if (lane == 0) {
     if (a.out_logprobs) {
       float lp = 0.f;
-      if (token >= a.V) {
+      if (token >= a.V || (a.T > 0 && token < 0)) {             // (a trajectory has no places without a token)
         lp = NAN;
         if (a.status) atomicExch(a.status, STATUS_BAD_TOKEN);
       } else if (token >= 0) {

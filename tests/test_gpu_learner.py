@@ -435,6 +435,30 @@ def test_adamw_8(B, gdtype, offset, seed, step, scale):
         assert np.all(np.abs(_host([out_v[i]])[0] - L.sq_values(cv, sv)) <= 10 * E * L.sq_values(cv, sv) + 1e-44)
 
 
+def test_adamw_8_where_everything_cancels(B):
+    """(1 - b1) g = -b1 m up to the last bits in a whole block: fp32's m is mostly rounding, the codes are the 64-bit
+    ones all the same.  And blocks that only decay, where every code stays next to itself; and tiny values."""
+    n = 256 * 4
+    rng = np.random.default_rng(12)
+    codes, scales = rng.integers(-127, 128, n).astype(np.int8), np.full(4, 1e-3, dtype=np.float32)
+    vcodes, vscales = rng.integers(1, 256, n).astype(np.uint8), np.array([1e-6, 1e-6, 1e-36, 1e-38], dtype=np.float32)
+    m, v = L.avg_values(codes, scales), L.sq_values(vcodes, vscales)
+    g = (-9.0 * m * (1 + 1e-6 * rng.normal(size=n))).astype(np.float32)
+    g[256:512] = 0
+    g[512:768] = rng.normal(size=256) * 1e-19
+    g[768:] = 0
+    dev = lambda x: torch.from_numpy(x.copy()).cuda()  # noqa: E731
+    tm, tv, sm, sv, p = dev(codes), dev(vcodes), dev(scales), dev(vscales), torch.zeros(n, device="cuda")
+    plan = B.AdamWTensors([p], [dev(g)], [tm], [tv], None, 0.0, [sm], [sv])
+    B.echo_adamw_step(plan, 5, 1e-3, seed=77)
+    _, wm, wv = L.adamw(np.zeros(n), g, m, v, 5, 1e-3, 0.9, 0.999, 1e-8, 0.0)
+    cm, csm = L.quantise_avg(wm)
+    cv, csv = L.quantise_sq(wv, L.halves(n, 0, 5, 77))
+    assert np.array_equal(sm.cpu().numpy(), csm) and np.array_equal(sv.cpu().numpy(), csv) and csv[3] == 0
+    assert np.array_equal(tm.cpu().numpy(), cm) and np.array_equal(tv.cpu().numpy(), cv)
+    assert bool(torch.isfinite(p).all())
+
+
 @pytest.mark.parametrize("bits", [32, 8])
 def test_adamw_overflowed_step_changes_nothing(B, bits):
     d = _adamw_inputs([1000, 3], bits, torch.float32, 7)
@@ -596,6 +620,13 @@ def test_score_detail_refuses_bad_tokens(B):
     shape, w, eng, prompts = _engine(B, 64, 1, 1, 4, 3)
     tok = torch.tensor([[[1, 64, 2]]], dtype=torch.int32, device="cuda")
     eng.echo_score_detail(prompts, [4], tok, 1.0, 2)
+    with pytest.raises(B.EchoError) as e:
+        eng.echo_sync()
+    assert e.value.code == -7
+    eng.close()
+    shape, w, eng, prompts = _engine(B, 64, 1, 1, 4, 3)
+    tok[0, 0, 1], tok[0, 0, 2] = 2, -1                   # the last token is never fed: only the scoring sees it
+    eng.echo_score_detail(prompts, [4], tok, 1.0)
     with pytest.raises(B.EchoError) as e:
         eng.echo_sync()
     assert e.value.code == -7

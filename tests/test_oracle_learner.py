@@ -136,7 +136,7 @@ def _forward(**over):
     (dict(lp=None), INVALID), (dict(k=-1), INVALID), (dict(k=5), INVALID), (dict(k=5, ids=P1), INVALID),
     (dict(k=33, ids=P1, top=P1), UNSUPPORTED), (dict(stats=P1 + 4), INVALID), (dict(logits=P0 + 1), INVALID),
     (dict(fmt=2, logits=P0 + 2), INVALID), (dict(tokens=None, lp=None, ent=None, stats=None), INVALID),
-    (dict(V=(1 << 30) + 1, stride=1 << 31), UNSUPPORTED), (dict(R=1 << 30), UNSUPPORTED)])
+    (dict(V=(1 << 24) + 1, stride=1 << 31), UNSUPPORTED), (dict(R=1 << 30), UNSUPPORTED)])
 def test_token_logprobs_refusals(over, code):
     assert _forward(**over) == code
 
@@ -204,6 +204,10 @@ def test_adamw_option_refusals(options):
     (dict(param_copy=P0 + 2000), 32), (dict(avg_scales=P0 + (5 << 16) + 12), 8)])
 def test_adamw_entry_refusals(entry, bits):
     assert _adamw(bits=bits, entry=entry) == INVALID
+
+
+def test_adamw_8_wants_an_ordinary_eps():
+    assert _adamw(bits=8, eps=1e-13) == UNSUPPORTED
 
 
 def test_adamw_refuses_a_tensor_listed_twice():
