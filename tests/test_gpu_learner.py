@@ -519,6 +519,52 @@ def test_adamw_8_follows_adamw_32(B):
     assert float((p8 - p32).norm() / p32.norm()) < 0.25
 
 
+@pytest.mark.parametrize("bits", [32, 8])
+def test_adamw_past_32_bit_offsets(B, bits):
+    """The end of one tensor of more than 2^32 elements (bytes of its fp32 arrays: 17 GB each)."""
+    n = (1 << 32) + 5 * 256 + 77 if bits == 8 else (1 << 31) + 300
+    tail = 256 * 3 + (77 if bits == 8 else 44)
+    rng = np.random.default_rng(4)
+    p, g = torch.zeros(n, device="cuda"), torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    p[-tail:] = torch.from_numpy(rng.normal(size=tail).astype(np.float32)).cuda()
+    g[-tail:] = torch.from_numpy(rng.normal(size=tail).astype(np.float32)).cuda().to(torch.bfloat16)
+    before = _host([p[-tail:], g[-tail:]])
+    plan = B.AdamWTensors.zeros([p], [g], state_bits=bits)
+    B.echo_adamw_step(plan, 1, 1e-2, seed=3)
+    wp, wm, wv = L.adamw(before[0], before[1], np.zeros(tail), np.zeros(tail), 1, 1e-2, 0.9, 0.999, 1e-8, 0.0)
+    # first step: p moves by lr times the sign of g, through a dozen roundings
+    assert np.abs(_host([p[-tail:]])[0] - wp).max() <= 3 * E * np.abs(before[0]).max() + 20 * E * 1e-2
+    if bits == 8:
+        cm, _ = L.quantise_avg(wm)
+        octet = (n - tail) // 8                          # the tail starts on a block
+        words = L.philox.philox4x32_10(np.arange(octet, octet + (tail + 7) // 8, dtype=np.uint64) & np.uint64(0xFFFFFFFF),
+                                       np.arange(octet, octet + (tail + 7) // 8, dtype=np.uint64) >> np.uint64(32), 0, 1, 3, 0)
+        half = np.empty((tail + 7) // 8 * 8, dtype=np.int64)
+        for j, w in enumerate(words):
+            half[2 * j::8], half[2 * j + 1::8] = w & 0xFFFF, w >> 16
+        cv, _ = L.quantise_sq(wv, half[:tail])
+        assert np.array_equal(plan.exp_avg[0][-tail:].cpu().numpy(), cm)
+        assert np.array_equal(plan.exp_avg_sq[0][-tail:].cpu().numpy(), cv)
+    else:
+        assert np.abs(_host([plan.exp_avg[0][-tail:]])[0] - wm).max() <= 5 * E
+    assert bool((p[:-tail][::4097] == 0).all()) and float(p[1 << 30]) == 0
+    del p, g, plan
+    torch.cuda.empty_cache()
+
+
+def test_grpo_past_32_bit_offsets(B):
+    n, T = 262160, 8200
+    x = torch.zeros((n, T), device="cuda")
+    adv = torch.randn(n, device="cuda")
+    v, grad = B.echo_grpo_gradient(x, x, x, None, adv, None, None, 0.2, 2.0, 0.0)
+    # equal policies: the objective is A (a sum of T equal terms in fp32), the gradient A / T
+    assert bool(((v - adv).abs() <= adv.abs() * E * (T / 16 + 16)).all())
+    for r in (0, n // 2, n - 1):
+        assert torch.allclose(grad[r], adv[r] / T, rtol=4 * E, atol=0)
+    del x, grad
+    torch.cuda.empty_cache()
+
+
 # ---- streams, graphs, the whole step --------------------------------------------------------------
 def test_repeats_are_equal_and_graphs_replay(B):
     z = _rows("few", 40, 30011, torch.bfloat16, 3)
