@@ -516,6 +516,8 @@ token_logprobs_kernel(const __grid_constant__ LogprobArgs a, int split) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) merge(st, shfl_stats(st, o), c);
   if (lane == 0) warp_stats[warp] = st;
+  // the token's own logit, wanted at the end: requested here, under the joins
+  const float taken = tid == 0 && rank == 0 && token >= 0 && token < a.V ? load_elem<FMT>(row, token) : 0.f;
   __syncthreads();
   if (warp == 0) {
     st = lane < kWarps ? warp_stats[lane] : RowStats{-INFINITY, 0.f, 0.f};
@@ -568,7 +570,7 @@ token_logprobs_kernel(const __grid_constant__ LogprobArgs a, int split) {
         lp = NAN;
         if (a.status) atomicExch(a.status, STATUS_BAD_TOKEN);
       } else if (token >= 0) {
-        lp = empty ? -INFINITY : (load_elem<FMT>(row, token) - st.m) * a.inv_temperature - log_l;
+        lp = empty ? -INFINITY : (taken - st.m) * a.inv_temperature - log_l;
       }
       a.out_logprobs[flat] = lp;
     }
@@ -613,12 +615,16 @@ cudaError_t logprobs_launch(const LogprobArgs &a, int format, cudaStream_t s) {
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
   if (e != cudaSuccess) return e;
   const int64_t row_vecs = static_cast<int64_t>(a.V) * (format == 2 ? 4 : 2) / 16;
-  // Few rows are cut over the CTAs of a cluster until the launch has about one CTA and a half per SM (two without
-  // alternatives, which cost less to join): 200 rows of 151936 fp32 values with 5 alternatives take 23.9 us in two parts
-  // and 28.3 in one, 64 rows 12.3 in four and 14.0 in eight, 256 rows bf16 24.2 in two and 21.2 in one.
+  // Few rows are cut over the CTAs of a cluster until the launch has two CTAs per SM.  With alternatives, which cost more
+  // to join, one and a half will do unless the parts stay long: 200 rows of 151936 fp32 values with 5 alternatives take
+  // 23.9 us in two parts and 28.3 in one, 256 rows 30.2 and 32.0, but bf16 24.2 and 21.4; 64 rows fp32 12.3 us in four and
+  // 14.0 in eight.
   int split = 1;
-  const int64_t enough = a.top_k > 0 ? 3 * sms / 2 : 2 * sms;
-  while (split < kMaxSplit && a.R * static_cast<int64_t>(split) < enough && row_vecs / (2 * split) >= 512) split *= 2;
+  auto more = [&] {
+    const int64_t ctas = a.R * static_cast<int64_t>(split), part = row_vecs / (2 * split);
+    return split < kMaxSplit && part >= 512 && (ctas < 3 * sms / 2 || (ctas < 2 * sms && (a.top_k == 0 || part >= 16384)));
+  };
+  while (more()) split *= 2;
   // Four CTAs of 256 threads or eight of 128 fit an SM.  While the launch fits in one round the larger ones finish sooner
   // (592 rows of 151936 half values: 33.0 against 37.5 us); in a launch of several rounds the smaller ones leave less
   // idle at the end and overlap their beginnings and ends better (3000 x 20000 bf16: 26.0 against 33.4 us; 777 x 50263
