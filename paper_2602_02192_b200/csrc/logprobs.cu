@@ -47,7 +47,7 @@ __device__ __forceinline__ uint4 load_stream(const uint4 *p) {
 // the same for memory that this launch also writes (in place)
 __device__ __forceinline__ uint4 load_once(const uint4 *p) {
   uint4 v;
-  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
+  asm volatile("ld.global.v4.u32 {%0, %1, %2, %3}, [%4];"
                : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
                : "l"(p)
                : "memory");
@@ -71,6 +71,29 @@ template <int FMT> __device__ __forceinline__ uint32_t max_word(uint32_t a, uint
   const __half2 m = __hmax2(*reinterpret_cast<__half2 *>(&a), *reinterpret_cast<__half2 *>(&b));
   return *reinterpret_cast<const uint32_t *>(&m);
 }
+// A value far below every logit that can matter (checked at the row's end), as a word of the format and as a float.
+template <int FMT> struct Floor;
+template <> struct Floor<0> { static constexpr uint32_t kWord = 0xf149f149u; static constexpr float kValue = -9.95e29f; };
+template <> struct Floor<1> { static constexpr uint32_t kWord = 0xfbfffbffu; static constexpr float kValue = -65504.f; };
+template <> struct Floor<2> { static constexpr uint32_t kWord = 0xf149f2cau; static constexpr float kValue = -1e30f; };
+// a vector with its elements raised to at least that (NaN stays)
+template <int FMT> __device__ __forceinline__ uint4 floored(const uint4 &v) {
+  uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    uint32_t lo = Floor<FMT>::kWord;
+    if constexpr (FMT == 2) {
+      asm("max.NaN.f32 %0, %1, %2;" : "=f"(reinterpret_cast<float &>(w[i])) : "f"(__uint_as_float(w[i])), "f"(__uint_as_float(lo)));
+    } else if constexpr (FMT == 0) {
+      const __nv_bfloat162 m = __hmax2_nan(*reinterpret_cast<__nv_bfloat162 *>(&w[i]), *reinterpret_cast<__nv_bfloat162 *>(&lo));
+      w[i] = *reinterpret_cast<const uint32_t *>(&m);
+    } else {
+      const __half2 m = __hmax2_nan(*reinterpret_cast<__half2 *>(&w[i]), *reinterpret_cast<__half2 *>(&lo));
+      w[i] = *reinterpret_cast<const uint32_t *>(&m);
+    }
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
 // largest element of N vectors (NaN is passed over)
 template <int FMT, int N> __device__ __forceinline__ float max_of(const uint4 (&v)[N]) {
   if (FMT == 2) {
@@ -90,22 +113,33 @@ template <int FMT, int N> __device__ __forceinline__ float max_of(const uint4 (&
 }
 
 // ---- running statistics of a row --------------------------------------------------------------
-// m: largest logit so far; l = sum 2^x, t = sum 2^x x over x = (z - m) c, c = log2(e) / T.
+// m: largest logit so far; l = sum 2^x, t = sum 2^x x over x = z c - K, c = log2(e) / T, K = max(fp32(m c), k_min).
+// One FMA an element: the reference is K itself, so that K's rounding is no error; m c - K enters once, at the end.
+// z is raised to the floor first, so that -inf makes no 0 * -inf.  k_min is at least -2^23 (below it K's rounding alone
+// would be more than 1: x could be large; such a maximum counts for nothing beside an ordinary one) and so far above
+// the floor's x that a floored element counts as 0.  A row whose own maximum is not ordinary (nothing left, everything
+// at some huge negative value, infinities, extreme temperatures) is found at its end and summed again by sum_plainly.
 struct RowStats {
   float m, l, t;
 };
-__device__ __forceinline__ void merge(RowStats &a, const RowStats &b, float c) {
-  const float m = fmaxf(a.m, b.m);
-  // -inf - -inf and inf - inf give NaN, which fmaxf turns into "far below": both sums are 0 (or NaN) then
-  const float da = fmaxf((a.m - m) * c, kFarBelow), db = fmaxf((b.m - m) * c, kFarBelow);
-  const float fa = ex2(da), fb = ex2(db);
+struct Scale {
+  float c, k_min;
+};
+__device__ __forceinline__ float reference(float m, const Scale &s) { return fmaxf(__fmul_rn(m, s.c), s.k_min); }
+__device__ __forceinline__ bool ordinary(float m, const Scale &s) {
+  const float k = __fmul_rn(m, s.c);
+  return k >= s.k_min && k <= 8388608.0f;
+}
+__device__ __forceinline__ void merge(RowStats &a, const RowStats &b, const Scale &s) {
+  const float m = fmaxf(a.m, b.m), k = reference(m, s);
+  const float da = reference(a.m, s) - k, db = reference(b.m, s) - k, fa = ex2(da), fb = ex2(db);
   a.t = fa * fmaf(da, a.l, a.t) + fb * fmaf(db, b.l, b.t);
   a.l = fa * a.l + fb * b.l;
   a.m = m;
 }
 // moves the reference to a larger maximum
-__device__ __forceinline__ void raise(RowStats &a, float m, float c) {
-  const float d = fmaxf((a.m - m) * c, kFarBelow), f = ex2(d);
+__device__ __forceinline__ void raise(RowStats &a, float m, const Scale &s) {
+  const float d = reference(a.m, s) - reference(m, s), f = ex2(d);
   a.t = f * fmaf(d, a.l, a.t);
   a.l *= f;
   a.m = m;
@@ -160,6 +194,7 @@ struct LogprobArgs {
   int R, V;
   const int32_t *tokens;
   float c, inv_temperature;
+  float k_min;                 // lowest reference (set by logprobs_launch)
   int top_k;
   float *out_logprobs, *out_entropy;
   float2 *out_stats;
@@ -240,6 +275,34 @@ __device__ __noinline__ void select_exact(const void *row, int begin, int end, i
     }
   }
   __syncthreads();
+}
+
+// The sums of a whole row about its maximum m with x = (z - m) c, which holds for any m and c: l and t in every thread.
+template <int FMT, int NT>
+__device__ __noinline__ float2 sum_plainly(const void *row, int V, float m, float c, float *scratch) {
+  const float ref = m == -INFINITY ? 0.f : m;
+  float l = 0.f, t = 0.f;
+  for (int i = threadIdx.x; i < V; i += NT) {
+    const float x = (load_elem<FMT>(row, i) - ref) * c, e = ex2(x);
+    l += e;
+    t = fmaf(e, fmaxf(x, kFarBelow), t);                       // (-inf would make 0 * -inf)
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    l += __shfl_xor_sync(0xffffffffu, l, o);
+    t += __shfl_xor_sync(0xffffffffu, t, o);
+  }
+  if ((threadIdx.x & 31) == 0) {
+    scratch[threadIdx.x >> 5] = l;
+    scratch[NT / 32 + (threadIdx.x >> 5)] = t;
+  }
+  __syncthreads();
+  l = t = 0.f;
+  for (int w = 0; w < NT / 32; ++w) {
+    l += scratch[w];
+    t += scratch[NT / 32 + w];
+  }
+  return make_float2(l, t);
 }
 
 // sorts n entries by counting how many precede each; the first kTopMax go to dst.  src[n] is 0 where n is odd.
@@ -445,25 +508,26 @@ token_logprobs_kernel(const __grid_constant__ LogprobArgs a, int split) {
   const int tail0 = begin + head + n_vec * kPerVec;
   const uint4 *vec = reinterpret_cast<const uint4 *>(row + static_cast<size_t>(begin + head) * kBytes);
   const float c = a.c;
+  const Scale scale{a.c, a.k_min};
   RowStats st{-INFINITY, 0.f, 0.f};
 
   auto absorb = [&](const uint4 (&v)[kUnroll]) -> float {
     const float bm = max_of<FMT>(v);
-    if (bm > st.m) raise(st, bm, c);
-    const float ref = st.m == -INFINITY ? 0.f : st.m;        // nothing but -inf so far: any finite reference does
-    const float2 neg = make_float2(-ref, -ref), cc = make_float2(c, c);
+    if (bm > st.m) raise(st, bm, scale);
+    const float k = -reference(st.m, scale);
+    const float2 kk = make_float2(k, k), cc = make_float2(c, c);
     float2 l0 = make_float2(st.l, 0.f), t0 = make_float2(st.t, 0.f);
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u)
+    for (int u = 0; u < kUnroll; ++u) {
+      const uint4 q = floored<FMT>(v[u]);
 #pragma unroll
       for (int i = 0; i < kPerVec / 2; ++i) {
-        float2 x = mul2(add2(pair_of<FMT>(v[u], i), neg), cc);
+        const float2 x = fma2(pair_of<FMT>(q, i), cc, kk);
         const float2 e = make_float2(ex2(x.x), ex2(x.y));
-        x.x = fmaxf(x.x, kFarBelow);                         // (-inf would make 0 * -inf)
-        x.y = fmaxf(x.y, kFarBelow);
         l0 = add2(l0, e);
         t0 = fma2(e, x, t0);
       }
+    }
     st.l = l0.x + l0.y;
     st.t = t0.x + t0.y;
     return bm;
@@ -476,10 +540,11 @@ token_logprobs_kernel(const __grid_constant__ LogprobArgs a, int split) {
     }
   };
   auto absorb_one = [&](float z) {
-    if (z > st.m) raise(st, z, c);
-    const float x = (z - (st.m == -INFINITY ? 0.f : st.m)) * c, e = ex2(x);
+    if (z > st.m) raise(st, z, scale);
+    const float raised = z < Floor<FMT>::kValue ? Floor<FMT>::kValue : z;      // (NaN stays)
+    const float x = fmaf(raised, c, -reference(st.m, scale)), e = ex2(x);
     st.l += e;
-    st.t = fmaf(e, fmaxf(x, kFarBelow), st.t);
+    st.t = fmaf(e, x, st.t);
   };
 
   const int steps = (n_vec + NT * kUnroll - 1) / (NT * kUnroll);
@@ -514,7 +579,7 @@ token_logprobs_kernel(const __grid_constant__ LogprobArgs a, int split) {
   }
   // ---- join the threads' statistics
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) merge(st, shfl_stats(st, o), c);
+  for (int o = 16; o > 0; o >>= 1) merge(st, shfl_stats(st, o), scale);
   if (lane == 0) warp_stats[warp] = st;
   // the token's own logit, wanted at the end: requested here, under the joins
   const float taken = tid == 0 && rank == 0 && token >= 0 && token < a.V ? load_elem<FMT>(row, token) : 0.f;
@@ -522,7 +587,7 @@ token_logprobs_kernel(const __grid_constant__ LogprobArgs a, int split) {
   if (warp == 0) {
     st = lane < kWarps ? warp_stats[lane] : RowStats{-INFINITY, 0.f, 0.f};
 #pragma unroll
-    for (int o = kWarps / 2; o > 0; o >>= 1) merge(st, shfl_stats(st, o), c);
+    for (int o = kWarps / 2; o > 0; o >>= 1) merge(st, shfl_stats(st, o), scale);
   }
   if constexpr (TOP) find_alternatives<FMT, NT>(row, vec, begin, end, head, n_vec, piece_steps * kUnroll, a.top_k, top_mem);
   // ---- join the CTAs of the row
@@ -554,15 +619,24 @@ token_logprobs_kernel(const __grid_constant__ LogprobArgs a, int split) {
     if (warp == 0) {
       st = lane < split ? cta_stats[lane] : RowStats{-INFINITY, 0.f, 0.f};
 #pragma unroll
-      for (int o = kMaxSplit / 2; o > 0; o >>= 1) merge(st, shfl_stats(st, o), c);
+      for (int o = kMaxSplit / 2; o > 0; o >>= 1) merge(st, shfl_stats(st, o), scale);
     }
   }
+  // ---- rows without an ordinary maximum (the CTA that holds the joined statistics decides)
+  if (tid == 0) cta_stats[0] = st;
+  __syncthreads();
+  st = cta_stats[0];
+  float log_l = logf(st.l);
+  if (ordinary(st.m, scale)) {
+    log_l -= kLn2 * fmaf(st.m, c, -reference(st.m, scale));
+  } else if (!(st.m == -INFINITY && st.l == 0.f)) {           // (nothing left: the sums are 0 already)
+    const float2 sums = sum_plainly<FMT, NT>(row, a.V, st.m, c, &warp_stats[0].m);
+    st.l = sums.x;
+    st.t = sums.y;
+    log_l = logf(st.l);
+  }
   if (warp != 0) return;
-  st.m = __shfl_sync(0xffffffffu, st.m, 0);
-  st.l = __shfl_sync(0xffffffffu, st.l, 0);
-  st.t = __shfl_sync(0xffffffffu, st.t, 0);
   const bool empty = st.l == 0.f;                             // nothing left in the row (all -inf)
-  const float log_l = logf(st.l);
   if (lane == 0) {
     if (a.out_logprobs) {
       float lp = 0.f;
@@ -574,7 +648,7 @@ token_logprobs_kernel(const __grid_constant__ LogprobArgs a, int split) {
       }
       a.out_logprobs[flat] = lp;
     }
-    if (a.out_entropy) a.out_entropy[flat] = empty ? 0.f : log_l - kLn2 * (st.t / st.l);
+    if (a.out_entropy) a.out_entropy[flat] = empty ? 0.f : logf(st.l) - kLn2 * (st.t / st.l);
     if (a.out_stats) a.out_stats[flat] = make_float2(st.m, log_l);
   }
   if constexpr (TOP) {
@@ -609,7 +683,16 @@ cudaError_t launch_logprobs_fmt(const LogprobArgs &a, int split, bool wide, cuda
   return wide ? launch_logprobs<FMT, 256>(a, split, s) : launch_logprobs<FMT, 128>(a, split, s);
 }
 
-cudaError_t logprobs_launch(const LogprobArgs &a, int format, cudaStream_t s) {
+// Half values reach down to -65504 only: their lowest reference lies halfway.  Where the floor's x would not vanish
+// beside it, or z c may overflow, no maximum is ordinary.
+float lowest_reference(int format, float c) {
+  const float floor = format == 1 ? Floor<1>::kValue : Floor<2>::kValue * 0.99f;
+  const float k_min = format == 1 ? fmaxf(-8388608.0f, -32000.0f * c) : -8388608.0f;
+  return c < 1e7f && floor * c < k_min - 200.0f ? k_min : INFINITY;
+}
+
+cudaError_t logprobs_launch(LogprobArgs a, int format, cudaStream_t s) {
+  a.k_min = lowest_reference(format, a.c);
   int dev = 0, sms = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);

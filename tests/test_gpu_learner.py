@@ -131,6 +131,38 @@ def test_undefined_rows(B):
     assert torch.isnan(g[:3]).all() and bool((g[3] == 0).all())
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, torch.float32])
+@pytest.mark.parametrize("temperature", [1e-9, 1e-5, 1e4, 1e9, 3e37])
+def test_extreme_temperatures_and_magnitudes(B, dtype, temperature):
+    """Sharp and flat distributions, rows of huge and of lowest values beside -inf: rows that the one-FMA form leaves."""
+    V, T = 2111, float(np.float32(temperature))
+    z = _rows("plain", 6, V, dtype, 21)
+    big = 6e4 if dtype == torch.float16 else 1e38
+    z[1] = z[1] * (big / 16)
+    z[2] = -big
+    z[2, 5:] = -math.inf
+    z[3] = torch.finfo(dtype).min
+    z[3, ::2] = -math.inf
+    z[4, :2000] = -math.inf
+    for r, mask in enumerate((-3e4, -1e4, -1e9, -1e10, -1e20, -1e30)):     # masks of every size, alone and beside logits
+        z = torch.cat([z, z[:1]])
+        z[-1, 7:] = max(mask, float(torch.finfo(dtype).min))
+        z = torch.cat([z, z[-1:]])
+        z[-1, :7] = z[-1, 7]
+    y = np.array([3, 4, 2, 1, 2100, -1] + [0, 9] * 6)
+    z64 = z.double().cpu().numpy()
+    lp, H, st, ids, top = (x.cpu().numpy() for x in B.echo_token_logprobs(z, torch.from_numpy(y.astype(np.int32)).cuda(), temperature, 5))
+    wlp, wH, wst, wids, wtop = L.token_logprobs(z64, y, T, 5)
+    s, d_logl, d_ent = _bounds(z64, T, V)
+    assert np.array_equal(ids, wids)
+    fin = np.abs(wlp) < 1e38
+    assert np.all(lp[~fin] < -1e38)
+    assert np.all(np.abs(lp - wlp)[fin] <= (d_logl + E * 6 * np.abs(wlp))[fin]) and np.all(np.abs(H - wH) <= d_ent)
+    assert np.all(np.abs(st[:, 1] - wst[:, 1]) <= d_logl)
+    fin = np.abs(wtop) < 1e38
+    assert np.all(np.abs(top - wtop)[fin] <= (d_logl[:, None] + E * 8 * np.abs(wtop))[fin]) and np.all(top[~fin] < -1e38)
+
+
 def test_statistics_without_tokens(B):
     z = _rows("plain", 6, 5000, torch.bfloat16, 1)
     lp, H, st, ids, top = B.echo_token_logprobs(z, None, 1.0, 3)
