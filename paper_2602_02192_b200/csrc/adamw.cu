@@ -12,8 +12,15 @@
 //                  1 - b2 a step, less than a code's width: rounding to the nearest would never let it fall), and never
 //                  0 for a v above 0, since a lost v beside a kept m would make a huge update.
 // Codes and scales are those of the 64-bit arithmetic: fp32 decides, and where fp32's own error could move a value
-// across a border between two codes the element is decided again in 64 bits (about one in ten thousand).  A scale is
+// across a border between two codes the element is decided again in 64 bits.  A scale is
 // the fp32 rounding of the 64-bit maximum.
+//
+// A warp takes a block of 256 elements, eight consecutive ones a lane, moved with 32-byte accesses.  fp32 moments: bound
+// by HBM (193 M elements with bf16 gradients and copies: 896 us, 6.0 TB/s).  8-bit moments: 757 us for the same step
+// against 471 of traffic at the copy rate; bound by instruction issue (69 % of the slots), about 98 instructions an
+// element.  Unpacking them: 321 us, 6.0 TB/s.  Bytes and whole numbers become floats, and back, through a float's low
+// bits, not the conversion unit.  Fetching the next 8-bit block into L2 ahead of time: 1134 against 1086 us for step and
+// unpack, so it is not done.
 #include <cmath>
 #include <new>
 #include <algorithm>
