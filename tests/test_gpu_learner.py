@@ -256,6 +256,17 @@ def test_token_logprobs_backward(B, kind, R, V, pad, offset, dtype, entropy, how
         assert bool((g[off] == 0).all())
 
 
+def test_entropy_gradient_at_the_smallest_temperatures(B):
+    """One id takes the whole mass: log p = 0 there, p = 0 elsewhere, so every gradient of the entropy is exactly 0, at -inf
+    too, however large 1 / temperature is."""
+    z = torch.full((2, 300), -1.0, device="cuda")
+    z[:, 17] = 0.0
+    z[1, 100:] = -math.inf
+    _, H, st, _, _ = B.echo_token_logprobs(z, None, 1e-9)
+    g = B.echo_token_logprobs_backward(z, None, H, st, None, torch.ones(2, device="cuda"), 1e-9)
+    assert bool((H == 0).all()) and bool((g == 0).all())
+
+
 def test_backward_leaves_padding_in_place(B):
     store = torch.full((5, 1100), 7.0, dtype=torch.bfloat16, device="cuda")
     z = store[:, 1:1004]
