@@ -495,7 +495,7 @@ token_logprobs_kernel(const __grid_constant__ LogprobArgs a, int split) {
     }
   }
   const int token = a.tokens ? a.tokens[flat] : -1;
-  if (!TOP && !a.out_entropy && !a.out_stats && token < 0) {
+  if (!TOP && !a.out_entropy && !a.out_stats && token < 0 && a.T == 0) {      // (a trajectory has no places without a token)
     if (rank == 0 && tid == 0 && a.out_logprobs) a.out_logprobs[flat] = 0.f;
     return;
   }
@@ -644,7 +644,7 @@ token_logprobs_kernel(const __grid_constant__ LogprobArgs a, int split) {
   if (lane == 0) {
     if (a.out_logprobs) {
       float lp = 0.f;
-      if (token >= a.V || (a.T > 0 && token < 0)) {             // (a trajectory has no places without a token)
+      if (token >= a.V || (a.T > 0 && token < 0)) {
         lp = NAN;
         if (a.status) atomicExch(a.status, STATUS_BAD_TOKEN);
       } else if (token >= 0) {

@@ -722,6 +722,20 @@ def test_score_detail_refuses_bad_tokens(B):
     eng.close()
 
 
+def test_score_detail_refuses_bad_tokens_when_nothing_else_is_wanted(B):
+    shape, w, eng, prompts = _engine(B, 64, 1, 1, 4, 3)
+    tok = torch.tensor([[[1, 2, -1]]], dtype=torch.int32, device="cuda")
+    lens, versions = np.array([4], dtype=np.int32), np.zeros(1, dtype=np.int64)
+    lp = torch.zeros(3, device="cuda")
+    torch.cuda.synchronize()
+    assert B.lib.echo_score_detail(eng._ctx, prompts.data_ptr(), lens.ctypes.data, 1, 1, 3, 1.0, tok.data_ptr(), 0,
+                                   lp.data_ptr(), None, None, None, versions.ctypes.data) == 0
+    with pytest.raises(B.EchoError) as e:
+        eng.echo_sync()
+    assert e.value.code == -7
+    eng.close()
+
+
 def test_one_learner_step(B):
     """Rollout -> rewards -> log-probabilities of the learner's logits -> objective and gradient -> gradient of the
     logits -> gradient of the lm_head -> AdamW -> next snapshot, as a trainer runs it."""
