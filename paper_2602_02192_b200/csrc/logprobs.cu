@@ -1114,9 +1114,10 @@ int echo_token_logprobs_backward(const void *logits, int32_t logits_format, int6
 int echo_grpo_gradient(const float *logp_new, const float *logp_old, const float *logp_sampler, const float *logp_ref,
                        const float *adv, const uint8_t *mask, const float *grad_out, int32_t n, int32_t T,
                        float eps_clip, float C, float beta, float *out, float *out_grad, void *cuda_stream) {
-  if (!logp_new || !logp_old || !logp_sampler || !adv || !out_grad || n < 0 || T < 1) return ECHO_ERR_INVALID;
-  if (!(eps_clip >= 0.f) || !(C > 0.f) || !(beta >= 0.f)) return ECHO_ERR_INVALID;
+  if (n < 0 || T < 1 || !(eps_clip >= 0.f) || !(C > 0.f) || !(beta >= 0.f)) return ECHO_ERR_INVALID;
   if (n == 0) return ECHO_OK;
+  if (!logp_new || !logp_old || !logp_sampler || !adv || !out_grad) return ECHO_ERR_INVALID;
+  if (T > (1 << 30)) return ECHO_ERR_UNSUPPORTED;             // (32-bit places within a sequence)
   GrpoGradArgs a{};
   a.ln = logp_new;
   a.lo = logp_old;

@@ -172,6 +172,13 @@ def test_grpo_gradient_refusals(change):
     assert lib.echo_grpo_gradient(*a.values(), None) == INVALID
 
 
+def test_grpo_gradient_lengths():
+    b, lib = _lib()
+    call = lambda p, n, T: lib.echo_grpo_gradient(p, p, p, None, p, None, None, n, T, 0.2, 1.0, 0.0, None, p, None)  # noqa: E731
+    assert call(None, 0, 5) == 0                          # empty tensors have no address
+    assert call(P0, 1, (1 << 30) + 1) == UNSUPPORTED
+
+
 def _adamw(bits=32, n_tensors=1, entry=None, second=None, **options):
     b, lib = _lib()
     o = dict(lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, step=1, seed=0, grad_scale=None, grad_format=2, state_bits=bits)
