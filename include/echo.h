@@ -304,7 +304,8 @@ int echo_grpo_objective(const float *logp_new, const float *logp_old, const floa
  * gradients, the update (echo_adamw_step), whose bf16 copies are what echo_load_policy installs.
  * These calls need no context.  They are asynchronous on the stream, run on the current device, allocate
  * no device memory, keep nothing between calls, use no atomics on results (equal inputs give equal
- * outputs) and can be captured into a CUDA graph.
+ * outputs; a row at another 16-byte boundary or in a launch of another size may differ in the last bits,
+ * since its sums run in another order) and can be captured into a CUDA graph.
  *
  * Formats: 0 bf16, 1 IEEE half, 2 fp32. */
 
@@ -401,7 +402,8 @@ int echo_adamw_step(const echo_adamw_tensor *tensors, int32_t n_tensors, const e
 
 /* The fp32 values that 8-bit moments stand for: out_avg[i], out_avg_sq[i] dev fp32 [n] for every tensor of
  * the list (host arrays of n_tensors pointers; entries of empty tensors are not read).  Only n and the
- * moments' fields of the tensors are used. */
+ * moments' fields of the tensors are used.  No output may overlap another array of the call
+ * (ECHO_ERR_INVALID). */
 int echo_adamw_unpack(const echo_adamw_tensor *tensors, int32_t n_tensors, float *const *out_avg,
                       float *const *out_avg_sq, void *cuda_stream);
 

@@ -701,6 +701,27 @@ int echo_adamw_unpack(const echo_adamw_tensor *tensors, int32_t n_tensors, float
     if (tensors[i].n > 0 && (!out_avg[i] || !out_avg_sq[i] || !aligned(out_avg[i], 4) || !aligned(out_avg_sq[i], 4)))
       return ECHO_ERR_INVALID;
   if (n_tensors == 0) return ECHO_OK;
+  Range *r = new (std::nothrow) Range[static_cast<size_t>(n_tensors) * 6];
+  if (!r) return ECHO_ERR_ARENA;
+  size_t n_ranges = 0;
+  auto range = [&](const void *p, int64_t bytes, bool written) {
+    const uintptr_t from = reinterpret_cast<uintptr_t>(p);
+    r[n_ranges++] = Range{from, from + static_cast<size_t>(bytes), written};
+  };
+  for (int i = 0; i < n_tensors; ++i) {
+    const echo_adamw_tensor &x = tensors[i];
+    if (x.n == 0) continue;
+    const int64_t blocks = (x.n + kBlock - 1) / kBlock;
+    range(out_avg[i], x.n * 4, true);
+    range(out_avg_sq[i], x.n * 4, true);
+    range(x.exp_avg, x.n, false);
+    range(x.exp_avg_sq, x.n, false);
+    range(x.avg_scales, blocks * 4, false);
+    range(x.sq_scales, blocks * 4, false);
+  }
+  const bool ok = apart(r, n_ranges);
+  delete[] r;
+  if (!ok) return ECHO_ERR_INVALID;
   auto make = [&](int i, Entry &e) {
     const echo_adamw_tensor &x = tensors[i];
     if (x.n == 0) return false;

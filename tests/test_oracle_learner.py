@@ -236,6 +236,15 @@ def test_adamw_unpack_refusals():
     assert lib.echo_adamw_unpack(table, 1, out, out, None) == INVALID
 
 
+def test_adamw_unpack_refuses_overlaps():
+    b, lib = _lib()
+    table = (b.EchoAdamWTensor * 1)()
+    table[0].n, table[0].exp_avg, table[0].exp_avg_sq, table[0].avg_scales, table[0].sq_scales = 10, P0, P0 + 64, P0 + 128, P0 + 192
+    call = lambda m, v: lib.echo_adamw_unpack(table, 1, (C.c_void_p * 1)(m), (C.c_void_p * 1)(v), None)  # noqa: E731
+    assert call(P1, P1) == INVALID and call(P1, P1 + 36) == INVALID           # the outputs with one another
+    assert call(P0 + 8, P1) == INVALID and call(P1, P0 + 192) == INVALID      # with the codes, with a scale
+
+
 def test_score_detail_refusals_come_first():
     b, lib = _lib()
     f = lambda k, ids, top: lib.echo_score_detail(None, P0, P0, 1, 1, 1, 1.0, P0, k, P1, None, ids, top, P1)  # noqa: E731
