@@ -461,7 +461,8 @@ __device__ __noinline__ void find_alternatives(const void *row, const uint4 *vec
 
 // One cluster of `split` CTAs per row (split = 1: one CTA), each with a contiguous share of the row, one pass.
 // Bound by HBM and, for 16-bit logits, almost as much by the exponentials (16 a cycle and SM): 2048 x 151936 bf16 in
-// 100 us, 6.2 TB/s, exponential unit 71 % busy (1024 such rows); 113 us under sustained load, where power holds the SM clock at 1.62 GHz.
+// 100 us, 6.2 TB/s, exponential unit 71 % busy (1024 such rows); 113 us under sustained load, where power holds the SM
+// clock at 1.62 GHz.
 // A thread keeps (m, l, t) of its own elements and moves the reference only when a step of its vectors exceeds it.
 // Alternatives cost no second pass: the threads also keep the maxima of 1024 parts of the CTA's elements ("pieces");
 // from these comes a lower bound of the k-th largest logit, and only the pieces that reach it, little more than k,
