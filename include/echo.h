@@ -349,8 +349,9 @@ int echo_token_logprobs_backward(const void *logits, int32_t logits_format, int6
  * echo_grpo_surrogate; beta is then unused), and with respect to logp_new
  *   out_grad[i][t] = grad_out[i] m_t w_t (slope_t + beta (exp(d_t) - 1)) / sum_t m_t,  d = logp_ref - logp_new,
  * slope_t = rho_t A_i where the minimum is its unclipped side (A_i > 0: rho_t <= 1 + eps_clip; A_i < 0:
- * rho_t >= 1 - eps_clip) and 0 elsewhere.  w_t depends on the old and the sampler's policy only and is a
- * constant.  Tokens that the mask leaves out have gradient 0 whatever their log-probabilities hold.
+ * rho_t >= 1 - eps_clip) and 0 elsewhere (A_i = 0: whatever rho_t, one that overflows too).  w_t depends on
+ * the old and the sampler's policy only and is a constant.  Tokens that the mask leaves out have gradient 0
+ * whatever their log-probabilities hold.
  *   grad_out dev fp32 [n] or NULL (all ones), out dev fp32 [n] or NULL, out_grad dev fp32 [n][T].
  * T <= 2^30.  n = 0 does nothing. */
 int echo_grpo_gradient(const float *logp_new, const float *logp_old, const float *logp_sampler, const float *logp_ref,

@@ -594,7 +594,8 @@ __global__ void grpo_surrogate_kernel(const float *__restrict__ ln, const float 
   float num = 0.f, den = 0.f;
   for (int t = lane; t < T; t += 32) {
     if (mask && !mask[base + t]) continue;
-    const float rho = expf(ln[base + t] - lo[base + t]);
+    float rho = expf(ln[base + t] - lo[base + t]);
+    if (a == 0.f && rho == INFINITY) rho = 1.0f;       // a zero advantage weighs nothing: no inf * 0
     const float w = fminf(expf(lo[base + t] - ls[base + t]), C);
     const float clipped = fminf(fmaxf(rho, 1.0f - eps_clip), 1.0f + eps_clip);
     float term = fminf(rho * a, clipped * a);

@@ -910,7 +910,8 @@ struct GrpoToken {
 // The clipped term's slope is rho A where the minimum is the unclipped side (A > 0: rho <= 1 + eps; A < 0:
 // rho >= 1 - eps), else 0; which side it is goes by the exact difference ln - lo, since the slope jumps there.
 __device__ __forceinline__ GrpoToken grpo_token(const GrpoGradArgs &a, float A, float ln, float lo, float ls, float lr) {
-  const float rho = expf(ln - lo);
+  float rho = expf(ln - lo);
+  if (A == 0.f && rho == INFINITY) rho = 1.0f;         // a zero advantage weighs nothing: no inf * 0
   const float w = fminf(expf(lo - ls), a.C);
   const float clipped = fminf(fmaxf(rho, 1.0f - a.eps_clip), 1.0f + a.eps_clip);
   const double x = static_cast<double>(ln) - static_cast<double>(lo);

@@ -1,0 +1,53 @@
+"""GPU tests of the learner's operators where their inputs leave the ordinary: overflowed ratios, undefined scores, ids
+outside the vocabulary, gradients far below their block's, decay below a weight's last bit, long runs of 8-bit moments."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import learner as L
+from oracle import objective as o_obj
+
+pytestmark = pytest.mark.gpu
+
+E = 2.0 ** -24
+
+
+@pytest.fixture(scope="module")
+def B():
+    from paper_2602_02192_b200 import binding
+    return binding
+
+
+def _dev(x):
+    return torch.from_numpy(np.ascontiguousarray(x, dtype=np.float32)).cuda()
+
+
+def _objective(B, ln, lo, ls, lr, adv, eps=0.2, C=2.0, beta=0.04):
+    """(value and gradient of the gradient call, value of the forward call), each [n] or [n][T] fp64."""
+    a = [_dev(x) for x in (ln, lo, ls)]
+    r = None if lr is None else _dev(lr)
+    value, grad = B.echo_grpo_gradient(*a, r, _dev(adv), None, None, eps, C, beta)
+    forward = B.echo_grpo_surrogate(*a, _dev(adv), None, eps, C) if r is None else B.echo_grpo_objective(*a, r, _dev(adv), None, eps, C, beta)
+    return (x.double().cpu().numpy() for x in (value, grad, forward))
+
+
+# ---- objective ----------------------------------------------------------------------------------
+@pytest.mark.parametrize("T", [1, 4, 300])               # one token, a vector of them; a warp or a CTA per sequence
+@pytest.mark.parametrize("kl", [False, True])
+def test_zero_advantage_beside_an_overflowed_ratio(B, T, kl):
+    """A = 0 makes the clipped term and its slope 0, whatever the ratio: what is left is the KL term, here -beta k and
+    beta expm1(d) with d = -1.5 under w = 1."""
+    lo = np.full((2, T), -101.0)
+    ln = np.full((2, T), -0.5)
+    ln[:, 1::2] = -101.5                                  # ordinary tokens among them
+    lr = ln - 1.5
+    value, grad, forward = _objective(B, ln, lo, lo, lr if kl else None, np.zeros(2))
+    beta = float(np.float32(0.04))
+    want = L.grpo_gradient(ln, lo, lo, lr if kl else None, np.zeros(2), None, None, float(np.float32(0.2)), 2.0, beta)
+    J = -beta * (math.exp(-1.5) + 1.5 - 1.0) if kl else 0.0
+    # expm1f is good to 2 steps (4 e), a handful of roundings beside; sums of T equal terms by at least 32 threads
+    assert np.all(np.abs(grad - want) <= 16 * E * np.abs(want))
+    assert np.all(np.abs(value - J) <= (16 + T / 32 + 16) * E * abs(J))
+    assert np.all(np.abs(forward - J) <= (16 + T / 32 + 16) * E * abs(J))
