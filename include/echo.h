@@ -275,7 +275,8 @@ int echo_group_advantage(const float *rewards, int32_t P, int32_t G, float eps,
  * sequence: with rho_t = exp(logp_new - logp_old), the truncated importance ratio
  * w_t = min(exp(logp_old - logp_sampler), C) and the response mask m_t,
  *   out[i] = sum_t m_t w_t min(rho_t A_i, clip(rho_t, 1 - eps_clip, 1 + eps_clip) A_i) / sum_t m_t
- * (0 for an empty mask; without the KL term: echo_grpo_objective adds it).
+ * (0 for an empty mask; without the KL term: echo_grpo_objective adds it).  NaN in a log-probability of a
+ * token that the mask keeps, or in a difference of infinite ones, makes out[i] NaN, here and below.
  * logp_* dev fp32 [n][T] are log-probabilities of the taken tokens (logp_sampler is what
  * echo_rollout recorded, the other two come from echo_rollout_forced under the respective
  * weights), adv dev fp32 [n] (echo_group_advantage), mask dev uint8 [n][T] or NULL (all ones),
@@ -351,7 +352,7 @@ int echo_token_logprobs_backward(const void *logits, int32_t logits_format, int6
  * slope_t = rho_t A_i where the minimum is its unclipped side (A_i > 0: rho_t <= 1 + eps_clip; A_i < 0:
  * rho_t >= 1 - eps_clip) and 0 elsewhere (A_i = 0: whatever rho_t, one that overflows too).  w_t depends on
  * the old and the sampler's policy only and is a constant.  Tokens that the mask leaves out have gradient 0
- * whatever their log-probabilities hold.
+ * whatever their log-probabilities hold; a kept one that is NaN, or whose differences are, has gradient NaN.
  *   grad_out dev fp32 [n] or NULL (all ones), out dev fp32 [n] or NULL, out_grad dev fp32 [n][T].
  * T <= 2^30.  n = 0 does nothing. */
 int echo_grpo_gradient(const float *logp_new, const float *logp_old, const float *logp_sampler, const float *logp_ref,

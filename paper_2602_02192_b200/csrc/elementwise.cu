@@ -582,7 +582,7 @@ __global__ void wait_probe_kernel(uint64_t limit_ns, int *status, unsigned long 
 
 // Clipped surrogate with truncated importance sampling, one warp per sequence (all in fp32):
 // J_i = sum_t m_t min(exp(lo - ls), C) (min(rho A, clip(rho, 1 - e, 1 + e) A) - beta k_t) / sum_t m_t,
-// rho = exp(ln - lo), k_t = exp(d) - d - 1 with d = lr - ln (lr may be null: no KL term).
+// rho = exp(ln - lo), k_t = exp(d) - d - 1 with d = lr - ln (lr may be null: no KL term).  NaN of an unmasked token shows.
 __global__ void grpo_surrogate_kernel(const float *__restrict__ ln, const float *__restrict__ lo,
                                       const float *__restrict__ ls, const float *__restrict__ lr,
                                       const float *__restrict__ adv, const uint8_t *__restrict__ mask, int n, int T,
@@ -596,9 +596,9 @@ __global__ void grpo_surrogate_kernel(const float *__restrict__ ln, const float 
     if (mask && !mask[base + t]) continue;
     float rho = expf(ln[base + t] - lo[base + t]);
     if (a == 0.f && rho == INFINITY) rho = 1.0f;       // a zero advantage weighs nothing: no inf * 0
-    const float w = fminf(expf(lo[base + t] - ls[base + t]), C);
-    const float clipped = fminf(fmaxf(rho, 1.0f - eps_clip), 1.0f + eps_clip);
-    float term = fminf(rho * a, clipped * a);
+    const float w = ptx::min_nan(expf(lo[base + t] - ls[base + t]), C);
+    const float clipped = ptx::min_nan(ptx::max_nan(rho, 1.0f - eps_clip), 1.0f + eps_clip);
+    float term = ptx::min_nan(rho * a, clipped * a);
     if (lr) {
       const float d = lr[base + t] - ln[base + t];
       term -= beta * (expm1f(d) - d);

@@ -909,14 +909,15 @@ struct GrpoToken {
 };
 // The clipped term's slope is rho A where the minimum is the unclipped side (A > 0: rho <= 1 + eps; A < 0:
 // rho >= 1 - eps), else 0; which side it is goes by the exact difference ln - lo, since the slope jumps there.
+// NaN in any of the log-probabilities, or in a difference of infinite ones, makes the token's value and slope NaN.
 __device__ __forceinline__ GrpoToken grpo_token(const GrpoGradArgs &a, float A, float ln, float lo, float ls, float lr) {
   float rho = expf(ln - lo);
   if (A == 0.f && rho == INFINITY) rho = 1.0f;         // a zero advantage weighs nothing: no inf * 0
-  const float w = fminf(expf(lo - ls), a.C);
-  const float clipped = fminf(fmaxf(rho, 1.0f - a.eps_clip), 1.0f + a.eps_clip);
+  const float w = ptx::min_nan(expf(lo - ls), a.C);
+  const float clipped = ptx::min_nan(ptx::max_nan(rho, 1.0f - a.eps_clip), 1.0f + a.eps_clip);
   const double x = static_cast<double>(ln) - static_cast<double>(lo);
   const bool flat = A > 0.f ? x > a.log_hi : x < a.log_lo;
-  float term = fminf(rho * A, clipped * A);
+  float term = ptx::min_nan(rho * A, clipped * A);
   float slope = flat ? 0.f : rho * A;
   if (a.lr) {
     const float d = lr - ln, k = expm1f(d);

@@ -51,3 +51,32 @@ def test_zero_advantage_beside_an_overflowed_ratio(B, T, kl):
     assert np.all(np.abs(grad - want) <= 16 * E * np.abs(want))
     assert np.all(np.abs(value - J) <= (16 + T / 32 + 16) * E * abs(J))
     assert np.all(np.abs(forward - J) <= (16 + T / 32 + 16) * E * abs(J))
+
+
+@pytest.mark.parametrize("T", [1, 8, 301])
+@pytest.mark.parametrize("kl", [False, True])
+@pytest.mark.parametrize("adv", [1.0, -0.5, 0.0])
+def test_undefined_log_probabilities_show(B, T, kl, adv):
+    """NaN in any log-probability of a token that counts, and -inf beside -inf (scores of rows with nothing left), reach
+    that sequence's value and that token's gradient, and no other; the forward calls agree."""
+    inf, nan = math.inf, math.nan
+    bad = [dict(ln=nan), dict(lo=nan), dict(ls=nan), dict(ln=-inf, lo=-inf), dict(lo=-inf, ls=-inf)]
+    if kl:
+        bad += [dict(lr=nan), dict(ln=-inf, lr=-inf)]
+    n, at = len(bad) + 1, T // 2
+    x = {k: np.full((n, T), v) for k, v in (("ln", -1.0), ("lo", -1.1), ("ls", -1.2), ("lr", -0.9))}
+    for i, change in enumerate(bad):
+        for k, v in change.items():
+            x[k][i, at] = v
+    args = x["ln"], x["lo"], x["ls"], x["lr"] if kl else None, np.full(n, adv)
+    value, grad, forward = _objective(B, *args)
+    want = np.zeros((n, T), dtype=bool)
+    want[:-1, at] = True
+    assert np.array_equal(np.isnan(grad), want) and np.isfinite(grad[~want]).all()
+    assert np.isnan(value[:-1]).all() and np.isfinite(value[-1]) and np.isnan(forward[:-1]).all() and np.isfinite(forward[-1])
+    mask = np.ones((n, T), np.uint8)
+    with np.errstate(invalid="ignore"):
+        oracle = L.grpo_gradient(*args, None, None, 0.2, 2.0, 0.04)
+        J = o_obj.grpo_objective(*args, mask, 0.2, 2.0, 0.04) if kl else o_obj.grpo_surrogate(*args[:3], args[4], mask, 0.2, 2.0)
+    assert np.array_equal(np.isnan(oracle), want)
+    assert np.isnan(J[:-1]).all() and np.isfinite(J[-1])
