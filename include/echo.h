@@ -293,7 +293,8 @@ int echo_grpo_surrogate(const float *logp_new, const float *logp_old, const floa
  * inside the masked mean and under the truncated ratio that multiplies the whole of J-bar:
  *   out[i] = sum_t m_t w_t (min(rho_t A_i, clip(rho_t) A_i) - beta k_t) / sum_t m_t.
  * logp_ref dev fp32 [n][T] (echo_score / echo_rollout_forced under the reference weights); the other
- * arguments as in echo_grpo_surrogate; beta >= 0.  Asynchronous on the stream. */
+ * arguments as in echo_grpo_surrogate; beta >= 0, and with beta = 0 logp_ref is not read.  Asynchronous on
+ * the stream. */
 int echo_grpo_objective(const float *logp_new, const float *logp_old, const float *logp_sampler,
                         const float *logp_ref, const float *adv, const uint8_t *mask, int32_t n,
                         int32_t T, float eps_clip, float C, float beta, float *out, void *cuda_stream);
@@ -347,7 +348,7 @@ int echo_token_logprobs_backward(const void *logits, int32_t logits_format, int6
                                  int64_t grad_stride, void *cuda_stream);
 
 /* echo_grpo_objective with its gradient: out[i] as there (logp_ref NULL: without the KL term, as in
- * echo_grpo_surrogate; beta is then unused), and with respect to logp_new
+ * echo_grpo_surrogate; beta is then unused; beta = 0: logp_ref is not read), and with respect to logp_new
  *   out_grad[i][t] = grad_out[i] m_t w_t (slope_t + beta (exp(d_t) - 1)) / sum_t m_t,  d = logp_ref - logp_new,
  * slope_t = rho_t A_i where the minimum is its unclipped side (A_i > 0: rho_t <= 1 + eps_clip; A_i < 0:
  * rho_t >= 1 - eps_clip) and 0 elsewhere (A_i = 0: whatever rho_t, one that overflows too).  w_t depends on

@@ -1125,7 +1125,7 @@ int echo_grpo_gradient(const float *logp_new, const float *logp_old, const float
   a.ln = logp_new;
   a.lo = logp_old;
   a.ls = logp_sampler;
-  a.lr = logp_ref;
+  a.lr = beta > 0.f ? logp_ref : nullptr;      // (no KL term, so that an estimate that overflows makes no 0 * inf)
   a.adv = adv;
   a.mask = mask;
   a.grad_out = grad_out;

@@ -1832,8 +1832,9 @@ int echo_grpo_objective(const float *logp_new, const float *logp_old, const floa
                         float beta, float *out, void *cuda_stream) {
   if (!logp_new || !logp_old || !logp_sampler || !logp_ref || !adv || !out || n < 0 || T < 1) return ECHO_ERR_INVALID;
   if (!(eps_clip >= 0.f) || !(C > 0.f) || !(beta >= 0.f)) return ECHO_ERR_INVALID;
-  cudaError_t e = grpo_surrogate_launch(logp_new, logp_old, logp_sampler, logp_ref, adv, mask, n, T, eps_clip, C,
-                                        beta, out, static_cast<cudaStream_t>(cuda_stream));
+  // (beta = 0: no KL term, so that an estimate that overflows makes no 0 * inf)
+  cudaError_t e = grpo_surrogate_launch(logp_new, logp_old, logp_sampler, beta > 0.f ? logp_ref : nullptr, adv, mask, n, T,
+                                        eps_clip, C, beta, out, static_cast<cudaStream_t>(cuda_stream));
   return e == cudaSuccess ? ECHO_OK : ECHO_ERR_CUDA;
 }
 

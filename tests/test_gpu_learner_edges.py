@@ -80,3 +80,15 @@ def test_undefined_log_probabilities_show(B, T, kl, adv):
         J = o_obj.grpo_objective(*args, mask, 0.2, 2.0, 0.04) if kl else o_obj.grpo_surrogate(*args[:3], args[4], mask, 0.2, 2.0)
     assert np.array_equal(np.isnan(oracle), want)
     assert np.isnan(J[:-1]).all() and np.isfinite(J[-1])
+
+
+def test_no_weight_on_the_reference_policy(B):
+    """beta = 0 is the objective without the KL term, also where exp(logp_ref - logp_new) overflows."""
+    rng = np.random.default_rng(8)
+    lo = -np.abs(rng.normal(size=(3, 40)))
+    ln, ls, adv = lo + 0.1 * rng.normal(size=lo.shape), lo + 0.1 * rng.normal(size=lo.shape), rng.normal(size=3)
+    lr = ln + 0.2
+    lr[:, ::3] = ln[:, ::3] + 100.0
+    with_ref = list(_objective(B, ln, lo, ls, lr, adv, beta=0.0))
+    without = list(_objective(B, ln, lo, ls, None, adv))
+    assert all(np.isfinite(a).all() and np.array_equal(a, b) for a, b in zip(with_ref, without))
