@@ -341,7 +341,7 @@ int echo_token_logprobs(const void *logits, int32_t logits_format, int64_t row_s
  *   out_grad       dev [R] rows of V, grad_stride >= V elements apart.  It may be the logits themselves
  *                  (same pointer and stride: they are overwritten) and may not overlap them otherwise.
  * Rows that no gradient reaches (a = b = 0, or no token and b = 0) and rows with nothing left become
- * zeros whatever their logits hold. */
+ * zeros whatever their logits hold.  A row whose id is >= V, which scores NaN, becomes NaN unless a = 0. */
 int echo_token_logprobs_backward(const void *logits, int32_t logits_format, int64_t row_stride, int32_t R, int32_t V,
                                  const int32_t *tokens, float temperature, const float *entropy, const float *stats,
                                  const float *grad_logprobs, const float *grad_entropy, void *out_grad,

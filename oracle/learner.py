@@ -74,9 +74,10 @@ def token_logprobs_backward(z: np.ndarray, tokens: np.ndarray, temperature: floa
         y = int(tokens[r])
         ar = float(a[r]) if a is not None and y >= 0 else 0.0
         br = float(b[r]) if b is not None else 0.0
-        if empty[r] or (ar == 0.0 and br == 0.0):
+        unknown = y >= V and ar != 0.0                   # scored NaN
+        if (empty[r] and not unknown) or (ar == 0.0 and br == 0.0):
             continue
-        if bad[r]:
+        if bad[r] or unknown:
             out[r] = np.nan
             continue
         plp = np.where(p[r] > 0, p[r] * np.where(p[r] > 0, logp[r], 0.0), 0.0)

@@ -821,9 +821,10 @@ token_logprobs_backward_kernel(const __grid_constant__ BackwardArgs a, int slice
   const float2 st = a.stats[r];
   const float gl = a.grad_logprobs ? a.grad_logprobs[r] : 0.f;
   const float gb = ENT ? a.grad_entropy[r] : 0.f, H = ENT ? a.entropy[r] : 0.f;
-  const float ga = g.token >= 0 ? gl : 0.f;
+  const bool unknown = g.token >= a.V && gl != 0.f;          // the forward call scored NaN: so is the row's gradient
+  const float ga = unknown ? NAN : g.token >= 0 ? gl : 0.f;
   // no gradient arrives, or nothing is left in the row: zeros, whatever the logits hold
-  const bool zero = (ga == 0.f && gb == 0.f) || st.y == -INFINITY;
+  const bool zero = (ga == 0.f && gb == 0.f) || (st.y == -INFINITY && !unknown);
   g.m = st.x;
   g.log2_l = st.y * kLog2e;
   g.hot = ga * a.inv_temperature;

@@ -92,3 +92,28 @@ def test_no_weight_on_the_reference_policy(B):
     with_ref = list(_objective(B, ln, lo, ls, lr, adv, beta=0.0))
     without = list(_objective(B, ln, lo, ls, None, adv))
     assert all(np.isfinite(a).all() and np.array_equal(a, b) for a, b in zip(with_ref, without))
+
+
+# ---- gradient of the logits ---------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, torch.float32])
+@pytest.mark.parametrize("how", ["dense", "in place", "strided"])
+@pytest.mark.parametrize("entropy", [False, True])
+def test_ids_outside_the_vocabulary_have_no_finite_gradient(B, dtype, how, entropy):
+    """The forward call scores them NaN; the gradient must not be an ordinary one that pushes the whole row down."""
+    R, V = 6, 1003
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    store = torch.randn((R, V + 5), generator=gen, device="cuda").to(dtype)
+    z = store[:, :V]
+    z[3] = -math.inf                                      # nothing left, and an id that is none
+    y = torch.tensor([V, 2 ** 31 - 1, V, V, 7, -1], dtype=torch.int32, device="cuda")
+    a = torch.tensor([1.0, -0.5, 0.0, 1.0, 1.0, 1.0], device="cuda")       # nothing arrives at row 2's score
+    b = torch.full((R,), 0.3, device="cuda") if entropy else None
+    lp, H, st, _, _ = B.echo_token_logprobs(z, y)
+    assert torch.isnan(lp).tolist() == [True] * 4 + [False] * 2
+    want = L.token_logprobs_backward(z.double().cpu().numpy(), y.cpu().numpy(), 1.0, a.cpu().numpy(),
+                                     b.cpu().numpy() if entropy else None)
+    out = {"dense": None, "in place": z, "strided": torch.zeros((R, V + 9), dtype=dtype, device="cuda")[:, 3:V + 3]}[how]
+    g = B.echo_token_logprobs_backward(z, y, H, st, a, b, out=out)
+    nan = torch.isnan(g).cpu().numpy()
+    assert np.array_equal(nan, np.isnan(want))
+    assert nan.all(axis=1).tolist() == [True, True, False, True, False, False] and not nan[[2, 4, 5]].any()
