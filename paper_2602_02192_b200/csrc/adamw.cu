@@ -409,6 +409,13 @@ __device__ __forceinline__ void step_block(const Scalars &s, const Entry &e, int
       if (fabsf(diff.y) <= near.y || fabsf(mid.y) > 0.49976f) unsure_v |= 2u << i;
     }
     uint64_t mo = low_bytes(mr), vo = low_bytes(vr);
+    // A gradient (or an old v) so far below its block's that fp32 does not hold its v still makes one above 0: 64 bits
+    // decide on codes 0 beside either.
+    if (__vcmpeq4(static_cast<uint32_t>(vo), 0u) | __vcmpeq4(static_cast<uint32_t>(vo >> 32), 0u)) {
+#pragma unroll 1
+      for (int j = 0; j < 8; ++j)
+        if (byte_of(vo, j) == 0 && (old_g(j) != 0.f || old_v(j) != 0)) unsure_v |= 1u << j;
+    }
     if (!(M > 0.f)) unsure_m = 0;
     if (!(V > 0.f)) unsure_v = 0;
     // A code from the 64-bit moment, rounded to fp32 only for the root, is right or next to it: it is compared with the

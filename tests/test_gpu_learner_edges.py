@@ -117,3 +117,38 @@ def test_ids_outside_the_vocabulary_have_no_finite_gradient(B, dtype, how, entro
     nan = torch.isnan(g).cpu().numpy()
     assert np.array_equal(nan, np.isnan(want))
     assert nan.all(axis=1).tolist() == [True, True, False, True, False, False] and not nan[[2, 4, 5]].any()
+
+
+# ---- AdamW --------------------------------------------------------------------------------------
+@pytest.mark.parametrize("gdtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("offset", [0, 1])
+def test_adamw_8_keeps_second_moments_far_below_their_block(B, gdtype, offset):
+    """(1 - beta2) g^2 of a gradient of 1e-23 is 0 in fp32 and 1e-49 in the definition: code 1 beside gradients of 1e-3,
+    code 0 only where there is no gradient.  The same for an old v beside a gradient of 1e16."""
+    n = 256 * 3 + 77
+    rng = np.random.default_rng(31)
+    g = rng.normal(size=n) * 1e-3
+    g[rng.random(n) < 0.3] = 0
+    small = rng.random(n) < 0.3
+    g[small] = rng.choice([-1e-23, 1e-23, 1e-30, 3e-22], size=small.sum())
+    codes, vcodes = rng.integers(-127, 128, n).astype(np.int8), rng.integers(0, 3, n).astype(np.uint8)
+    scales, vscales = np.full(4, 1e-3, np.float32), np.full(4, 1e-20, np.float32)
+    codes[:256], vcodes[:256], scales[0], vscales[0] = 0, 0, 0, 0           # nothing before
+    g[512] = 1e16
+
+    def dev(x, dtype):
+        store = torch.zeros(n + offset, dtype=dtype, device="cuda")[offset:]
+        store.copy_(torch.from_numpy(x))
+        return store
+
+    tg = dev(g, gdtype)
+    tm, tv, p = dev(codes, torch.int8), dev(vcodes, torch.uint8), dev(np.zeros(n), torch.float32)
+    sm, sv = _dev(scales), _dev(vscales)
+    B.echo_adamw_step(B.AdamWTensors([p], [tg], [tm], [tv], None, 0.0, [sm], [sv]), 5, 1e-3, seed=4)
+    g64 = tg.double().cpu().numpy()
+    _, wm, wv = L.adamw(np.zeros(n), g64, L.avg_values(codes, scales), L.sq_values(vcodes, vscales), 5, 1e-3, 0.9, 0.999, 1e-8, 0.0)
+    cv, csv = L.quantise_sq(wv, L.halves(n, 0, 5, 4))
+    cm, csm = L.quantise_avg(wm)
+    assert np.all((cv == 0) == (wv == 0)) and np.all(cv[512:768] >= (wv[512:768] > 0))
+    assert np.array_equal(sv.cpu().numpy(), csv) and np.array_equal(tv.cpu().numpy(), cv)
+    assert np.array_equal(sm.cpu().numpy(), csm) and np.array_equal(tm.cpu().numpy(), cm)
