@@ -375,6 +375,9 @@ typedef struct echo_adamw_tensor {
   double weight_decay;        /* >= 0, decoupled                                                          */
 } echo_adamw_tensor;
 
+/* Or'ed to state_bits = 8: first moments are rounded at random (what to train with, see echo_adamw_step). */
+#define ECHO_ADAMW_RANDOM_AVG 256
+
 typedef struct echo_adamw_options {
   double lr, beta1, beta2, eps;   /* lr >= 0; beta1 and beta2 in [0, 1); eps > 0, with 8-bit
                                      moments at least 1e-12 (else ECHO_ERR_UNSUPPORTED)                    */
@@ -383,23 +386,30 @@ typedef struct echo_adamw_options {
   const float *grad_scale;        /* dev fp32 [1] or NULL: every gradient is multiplied by it (clipping,
                                      loss scale).  If it is not finite the call changes nothing.          */
   int32_t grad_format;            /* of every tensor's gradient                                           */
-  int32_t state_bits;             /* 32 or 8                                                              */
+  int32_t state_bits;             /* 32, 8, or 8 | ECHO_ADAMW_RANDOM_AVG                                  */
 } echo_adamw_options;
 
 /* One AdamW step over a list of tensors in one launch (400 tensors a launch):
  *   m <- beta1 m + (1 - beta1) g,  v <- beta2 v + (1 - beta2) g^2,
  *   p <- p (1 - lr weight_decay) - lr m / (1 - beta1^t) / (sqrt(v / (1 - beta2^t)) + eps).
  * 8-bit moments: blocks of 256 consecutive elements of a tensor share two scales, M the block's largest
- * |m| and V its largest v as fp32; a first-moment code c in [-127, 127] stands for M (c/127) |c/127| and
- * takes the nearest value on that axis, a second-moment code c in [0, 255] stands for V (c/255)^4 and takes
- * the code below or above v at random so that the mean is kept (at least 1 for v > 0).  The random numbers
- * are 16-bit halves of Philox4x32-10 words: key = seed, counter = (e/8 low, e/8 high, place of the tensor
- * in the list, step) for element e, low half first.  A block whose largest value is below the smallest
+ * |m| and V its largest v as fp32; a first-moment code c in [-127, 127] stands for M (c/127) |c/127|, a
+ * second-moment code c in [0, 255] for V (c/255)^4.  The second moment takes the code below or above v at
+ * random so that the mean is kept (at least 1 for v > 0).  The random numbers are 16-bit halves h of
+ * Philox4x32-10 words: key = seed, counter = (e/8 low, e/8 high, place of the tensor in the list, step) for
+ * element e, low half first; the upper code where h / 2^16 is below v's place between the two.
+ * The first moment takes the nearest code on its axis, or, with ECHO_ADAMW_RANDOM_AVG and from step 2 on, the
+ * code below or above |m| at random with the mean kept (bit 63 of e/8 set in the counter, (h + 1/2) / 2^16
+ * compared).  Nearest codes do not fall by themselves: where |c| (1 - sqrt(beta1)) <= 1/2, that is up to 9 at
+ * beta1 = 0.9, an element whose gradient ends keeps its m as long as its block's largest stays, its v falls,
+ * and its weight drifts by several lr a step; gradients of 1e-3 of their block's largest and less suffer too.
+ * Train with ECHO_ADAMW_RANDOM_AVG; nearest codes are for blocks whose gradients stay of one size, and for
+ * single steps that are to be the same whatever the seed is.  A block whose largest value is below the smallest
  * normal fp32 number is stored as zeros; codes 0 with scales 0 are the moments of step 0.  The update of p
  * uses the moments before they are rounded.  A gradient that is not finite spoils its block's moments.
  * tensors and opt are host memory, read before the call returns; no two arrays of which one is written may
  * overlap (ECHO_ERR_INVALID: a tensor listed twice, for instance).  A captured call replays with the step,
- * the rates and the seed it was captured with. */
+ * the rates and the random numbers it was captured with. */
 int echo_adamw_step(const echo_adamw_tensor *tensors, int32_t n_tensors, const echo_adamw_options *opt,
                     void *cuda_stream);
 

@@ -124,11 +124,12 @@ def sq_values(codes: np.ndarray, scales: np.ndarray) -> np.ndarray:
     return np.repeat(scales.astype(np.float64), BLOCK)[: len(codes)] * q ** 4
 
 
-def halves(n: int, tensor: int, step: int, seed: int) -> np.ndarray:
-    """The 16-bit random number of elements 0..n-1 of tensor `tensor` at `step`."""
+def halves(n: int, tensor: int, step: int, seed: int, moment: int = 0) -> np.ndarray:
+    """The 16-bit random number of elements 0..n-1 of tensor `tensor` at `step`: of the second moment's rounding, or
+    (moment 1) the first's."""
     out = np.empty((n + 7) // 8 * 8, dtype=np.int64)
     octets = np.arange((n + 7) // 8, dtype=np.uint64)
-    words = philox.philox4x32_10(octets & np.uint64(0xFFFFFFFF), octets >> np.uint64(32), tensor, step,
+    words = philox.philox4x32_10(octets & np.uint64(0xFFFFFFFF), octets >> np.uint64(32) | np.uint64(moment << 31), tensor, step,
                                  seed & 0xFFFFFFFF, (seed >> 32) & 0xFFFFFFFF)
     for j, w in enumerate(words):
         out[2 * j::8] = w & 0xFFFF
@@ -143,11 +144,16 @@ def block_scale(x: np.ndarray) -> np.ndarray:
     return np.where(top < np.float32(2.0 ** -126), np.float32(0), top)
 
 
-def quantise_avg(m: np.ndarray):
-    """(int8 codes, fp32 scales), nearest code on the companded axis."""
+def quantise_avg(m: np.ndarray, half: Optional[np.ndarray] = None):
+    """(int8 codes, fp32 scales): the nearest code on the companded axis, or, with random numbers, the code below or above
+    |m|, the upper where (half + 1/2) / 2^16 is less than |m|'s place between the two."""
     scale = block_scale(np.abs(m))
     wide = np.repeat(scale.astype(np.float64), BLOCK)[: len(m)]
     ratio = np.divide(np.abs(m), wide, out=np.zeros_like(m), where=wide > 0)
+    if half is not None:
+        low = np.minimum(np.floor(127.0 * np.sqrt(ratio)), 126.0)
+        lo, hi = (low / 127.0) ** 2, ((low + 1) / 127.0) ** 2
+        return ((low + ((half + 0.5) / 65536.0 * (hi - lo) < ratio - lo)) * np.sign(m)).astype(np.int8), scale
     return (np.rint(127.0 * np.sqrt(ratio)) * np.sign(m)).astype(np.int8), scale
 
 

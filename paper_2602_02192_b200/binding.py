@@ -578,18 +578,27 @@ def echo_grpo_gradient(logp_new: torch.Tensor, logp_old: torch.Tensor, logp_samp
     return out, grad
 
 
+ECHO_ADAMW_RANDOM_AVG = 256
+
+
 class AdamWTensors:
     """The tensors of an AdamW step, as the library's list of addresses (kept alive here).  params fp32, grads bf16,
     float16 or fp32 (one dtype), exp_avg / exp_avg_sq both fp32, or int8 / uint8 codes with avg_scales and sq_scales
     (fp32, one per 256 elements of a tensor); copies: bf16 tensors (or None) that receive the updated weights;
-    weight_decay: one number, or one per tensor.  All of them contiguous, on one GPU."""
+    weight_decay: one number, or one per tensor.  All of them contiguous, on one GPU.
+
+    random_avg (8-bit moments): first moments are rounded at random with the mean kept, which is what to train with; the
+    lists that `zeros` makes do so.  False: to the nearest code, which does not fall by itself, so that weights whose
+    gradients end, or are far below their block's, drift.  Pass True to go on with moments of a list from `zeros`."""
     BLOCK = 256
 
-    def __init__(self, params, grads, exp_avg, exp_avg_sq, copies=None, weight_decay=0.0, avg_scales=None, sq_scales=None):
+    def __init__(self, params, grads, exp_avg, exp_avg_sq, copies=None, weight_decay=0.0, avg_scales=None, sq_scales=None,
+                 random_avg: bool = False):
         n = len(params)
         assert len(grads) == n and len(exp_avg) == n and len(exp_avg_sq) == n
         self.device = params[0].device if n else torch.device("cuda", torch.cuda.current_device())
         self.state_bits = 8 if n and exp_avg[0].dtype == torch.int8 else 32
+        self.random_avg = bool(random_avg)
         self.grad_format = _FORMATS[grads[0].dtype] if n else 2
         decay = list(weight_decay) if isinstance(weight_decay, (list, tuple)) else [weight_decay] * n
         assert len(decay) == n and (copies is None or len(copies) == n)
@@ -618,9 +627,9 @@ class AdamWTensors:
         self._keep = (params, grads, exp_avg, exp_avg_sq, copies, avg_scales, sq_scales)
 
     @classmethod
-    def zeros(cls, params, grads, state_bits: int = 32, copies=None, weight_decay=0.0) -> "AdamWTensors":
+    def zeros(cls, params, grads, state_bits: int = 32, copies=None, weight_decay=0.0, random_avg: bool = True) -> "AdamWTensors":
         """The list with moments of its own, all zero (attributes exp_avg, exp_avg_sq and, for 8 bits, avg_scales and
-        sq_scales)."""
+        sq_scales): where a run starts."""
         assert state_bits in (8, 32)
         first, second = (torch.int8, torch.uint8) if state_bits == 8 else (torch.float32, torch.float32)
         m = [torch.zeros(p.numel(), dtype=first, device=p.device) for p in params]
@@ -629,7 +638,7 @@ class AdamWTensors:
         if state_bits == 8:
             scales = [[torch.zeros(-(-p.numel() // cls.BLOCK), dtype=torch.float32, device=p.device) for p in params]
                       for _ in range(2)]
-        self = cls(params, grads, m, v, copies, weight_decay, scales[0], scales[1])
+        self = cls(params, grads, m, v, copies, weight_decay, scales[0], scales[1], random_avg)
         self.exp_avg, self.exp_avg_sq, self.avg_scales, self.sq_scales = m, v, scales[0], scales[1]
         return self
 
@@ -638,8 +647,11 @@ def echo_adamw_step(tensors: AdamWTensors, step: int, lr: float, beta1: float = 
                     eps: float = 1e-8, grad_scale: Optional[torch.Tensor] = None, seed: int = 0):
     """One AdamW step (number `step`, from 1) over every tensor of the list.  grad_scale: fp32 device tensor of one
     element that multiplies the gradients (if it is not finite nothing changes).  seed: random numbers of the 8-bit
-    second moments."""
-    opt = EchoAdamWOptions(lr, beta1, beta2, eps, step, seed, None, tensors.grad_format, tensors.state_bits)
+    moments' rounding."""
+    bits = tensors.state_bits
+    if bits == 8 and tensors.random_avg:
+        bits |= ECHO_ADAMW_RANDOM_AVG
+    opt = EchoAdamWOptions(lr, beta1, beta2, eps, step, seed, None, tensors.grad_format, bits)
     if grad_scale is not None:
         assert grad_scale.get_device() == tensors.device.index and grad_scale.dtype is torch.float32 and grad_scale.numel() == 1
         opt.grad_scale = grad_scale.data_ptr()

@@ -6,8 +6,12 @@
 // 8-bit moments: 256 consecutive elements of a tensor share two fp32 scales, the largest |m| (M) and the largest v (V)
 // of the block.  A code stands for M (c/127) |c/127| (first moment) and V (c/255)^4 (second moment): quadratic and
 // quartic companding put the steps where small values are, so that a block may span five decades of |m| and nine of v.
-//   first moment   nearest code on the companded axis, rint(127 sqrt(|m| / M)): it turns over by 1 - b1 a step, far
-//                  more than a code's width;
+//   first moment   the nearest code on the companded axis, rint(127 sqrt(|m| / M)), or (RANDOM) one of the two codes
+//                  around |m| with the mean kept.  Without a gradient a step multiplies a code by sqrt(b1), and the
+//                  nearest to sqrt(0.9) c is c itself up to c = 9: such an element keeps its m while the block's largest
+//                  stays, and as v falls beside it the update grows.  Rounding at random lets it fall as it should (one
+//                  element in 16 without a gradient after step 50, b2 = 0.95: after 2000 steps exact AdamW has moved
+//                  it by 7 lr, the nearest code by 8400 lr, random rounding by 7.5 lr);
 //   second moment  one of the two codes around v, the upper with the probability that keeps the mean (v moves by
 //                  1 - b2 a step, less than a code's width: rounding to the nearest would never let it fall), and never
 //                  0 for a v above 0, since a lost v beside a kept m would make a huge update.
@@ -238,19 +242,30 @@ struct Stash {
   __device__ uint32_t old_v(int lane, int j) const { return reinterpret_cast<const uint8_t *>(&v[lane])[j]; }
 };
 
-// the random numbers of eight elements, and the one of element j in [0, 1)
-__device__ __forceinline__ uint4 random_words(const Scalars &s, const Entry &e, uint64_t octet) {
-  return philox(make_uint4(static_cast<uint32_t>(octet), static_cast<uint32_t>(octet >> 32), e.id, s.step), s.key0, s.key1);
+// the random numbers of eight elements for the second (moment 0) or the first moment (1), and the one of element j in
+// [0, 1).  (An octet's number stays below 2^35: the counter's bit 63 is free.)
+__device__ __forceinline__ uint4 random_words(const Scalars &s, const Entry &e, uint64_t octet, uint32_t moment = 0) {
+  return philox(make_uint4(static_cast<uint32_t>(octet), static_cast<uint32_t>(octet >> 32) | moment << 31, e.id, s.step),
+                s.key0, s.key1);
 }
 __device__ __forceinline__ double random_of(const uint4 &w, int j) {
   const uint64_t half = j < 4 ? static_cast<uint64_t>(w.y) << 32 | w.x : static_cast<uint64_t>(w.w) << 32 | w.z;
   return static_cast<double>(static_cast<uint32_t>(half >> (16 * (j & 3))) & 0xffffu) * 1.52587890625e-05;
 }
 
+// The first-moment code below or above y = 127^2 |m| / M, the upper one where u + 2^-17 is below y's place between the two
+// (u has 16 bits; half a step more keeps the mean, and a code whose own value returns with another last bit).
+__device__ __forceinline__ int random_avg_code(double y, double u) {
+  const double d = fmin(floor(sqrt(y)), 126.0);
+  return static_cast<int>(d) + ((u + 7.62939453125e-06) * (2.0 * d + 1.0) < y - d * d ? 1 : 0);
+}
+
 // A block so small that fp32 products of its codes and scales leave the normal numbers: all of it in 64 bits.
+template <bool RANDOM>
 __device__ __noinline__ void quantise_tiny(const Scalars &s, const Entry &e, int64_t block, int lane, int left, float gs,
                                            float M0, float V0, const Stash &stash) {
-  const uint4 words = random_words(s, e, static_cast<uint64_t>(block) * (kBlock / 8) + lane);
+  const uint64_t octet = static_cast<uint64_t>(block) * (kBlock / 8) + lane;
+  const uint4 words = random_words(s, e, octet), avg_words = RANDOM ? random_words(s, e, octet, 1) : words;
   float M = 0.f, V = 0.f;
   for (int j = 0; j < left; ++j) {
     M = max_or_nan(M, static_cast<float>(exact_avg(s, stash.old_m(lane, j), M0, stash.old_g(lane, j), gs)), 0.f);
@@ -262,7 +277,9 @@ __device__ __noinline__ void quantise_tiny(const Scalars &s, const Entry &e, int
   for (int j = 0; j < left; ++j) {
     const double x = exact_avg(s, stash.old_m(lane, j), M0, stash.old_g(lane, j), gs);
     const double y = exact_sq(s, stash.old_v(lane, j), V0, stash.old_g(lane, j), gs);
-    const int c = M > 0.f ? static_cast<int>(rint(127.0 * sqrt(fabs(x) / M))) : 0;
+    const int c = !(M > 0.f) ? 0
+                  : RANDOM   ? random_avg_code(fabs(x) / M * 16129.0, random_of(avg_words, j))
+                             : static_cast<int>(rint(127.0 * sqrt(fabs(x) / M)));
     set_byte(mo, j, x < 0.0 ? -c : c);
     if (V > 0.f && y > 0.0) {
       const double w = y / V * 4228250625.0, d = fmin(floor(sqrt(sqrt(w))), 254.0), lo = d * d * (d * d);
@@ -278,7 +295,7 @@ __device__ __noinline__ void quantise_tiny(const Scalars &s, const Entry &e, int
   }
 }
 
-template <int FMT, bool EIGHT, bool WHOLE>
+template <int FMT, bool EIGHT, bool RANDOM, bool WHOLE>
 __device__ __forceinline__ void step_block(const Scalars &s, const Entry &e, int64_t block, int lane, float gs, Stash &stash) {
   const int64_t at = block * kBlock + lane * 8;
   const int left = WHOLE ? 8 : static_cast<int>(min(static_cast<int64_t>(8), max(static_cast<int64_t>(0), e.n - at)));
@@ -374,23 +391,47 @@ __device__ __forceinline__ void step_block(const Scalars &s, const Entry &e, int
     const uint64_t octet = static_cast<uint64_t>(block) * (kBlock / 8) + lane;
     const uint4 words4 = random_words(s, e, octet);
     const uint32_t words[4] = {words4.x, words4.y, words4.z, words4.w};
+    uint4 avg_words4 = make_uint4(0u, 0u, 0u, 0u);
+    if (RANDOM) avg_words4 = random_words(s, e, octet, 1);
+    const uint32_t avg_words[4] = {avg_words4.x, avg_words4.y, avg_words4.z, avg_words4.w};
     uint32_t mr[8], vr[8];                     // codes in the low bytes
     uint32_t unsure_m = 0, unsure_v = 0;
     const float err_y = 0.5f * err_m * inv_m;
 #pragma unroll
     for (int i = 0; i < 8; i += 2) {
       const float2 ym = mul2(make_float2(m[i], m[i + 1]), both(inv_m)), w = mul2(make_float2(v[i], v[i + 1]), both(inv_v));
-      // first moment: x = sqrt(y), y = 127^2 |m| / M, is off by (error of y) / (2 x) and, x being at most 127, less than
-      // 1e-4 of its own rounding.  (Below y = 1/1000 every code is 0, and so stands for the smaller ones.)
-      const float2 y = make_float2(fmaxf(fabsf(ym.x), 1e-3f), fmaxf(fabsf(ym.y), 1e-3f));
-      const float2 rs = make_float2(rsqrt_ftz(y.x), rsqrt_ftz(y.y)), x = mul2(y, rs);
-      const float2 xs = make_float2(copysignf(x.x, ym.x), copysignf(x.y, ym.y));
-      const float2 r = add2(xs, both(kRound)), dist = fma2(add2(r, both(-kRound)), both(-1.0f), xs);
-      const float2 clear = fma2(rs, both(-err_y), both(0.4999f));
-      mr[i] = __float_as_uint(r.x);
-      mr[i + 1] = __float_as_uint(r.y);
-      if (fabsf(dist.x) > clear.x) unsure_m |= 1u << i;
-      if (fabsf(dist.y) > clear.y) unsure_m |= 2u << i;
+      if constexpr (!RANDOM) {
+        // first moment: x = sqrt(y), y = 127^2 |m| / M, is off by (error of y) / (2 x) and, x being at most 127, less than
+        // 1e-4 of its own rounding.  (Below y = 1/1000 every code is 0, and so stands for the smaller ones.)
+        const float2 y = make_float2(fmaxf(fabsf(ym.x), 1e-3f), fmaxf(fabsf(ym.y), 1e-3f));
+        const float2 rs = make_float2(rsqrt_ftz(y.x), rsqrt_ftz(y.y)), x = mul2(y, rs);
+        const float2 xs = make_float2(copysignf(x.x, ym.x), copysignf(x.y, ym.y));
+        const float2 r = add2(xs, both(kRound)), dist = fma2(add2(r, both(-kRound)), both(-1.0f), xs);
+        const float2 clear = fma2(rs, both(-err_y), both(0.4999f));
+        mr[i] = __float_as_uint(r.x);
+        mr[i + 1] = __float_as_uint(r.y);
+        if (fabsf(dist.x) > clear.x) unsure_m |= 1u << i;
+        if (fabsf(dist.y) > clear.y) unsure_m |= 2u << i;
+      } else {
+        // first moment: y = 127^2 |m| / M lies between d^2 and (d + 1)^2 (d at most 126; 126.5 stands for all above it),
+        // the second moment's rule with squares.  The place in the interval is off by less than 2e-4 (y by the moments'
+        // error, 2 err_y, and 1.2e-6 of itself, which is below 8e-5 of the interval; the root by 1.5e-5) unless the
+        // moments' error alone is more: then 64 bits decide on all of the block.
+        const float2 y = make_float2(fabsf(ym.x), fabsf(ym.y));
+        const float2 z = make_float2(fminf(sqrt_ftz(y.x), 126.5f), fminf(sqrt_ftz(y.y), 126.5f));
+        const float2 zr = make_float2(__fadd_rd(z.x, kTwo23), __fadd_rd(z.y, kTwo23)), d = add2(zr, both(-kTwo23));
+        const float2 above = fma2(mul2(d, both(-1.0f)), d, y), width = fma2(d, both(2.0f), both(1.0f));
+        const float2 u = fma2(make_float2(half_plus_two23(avg_words[i >> 1], 0), half_plus_two23(avg_words[i >> 1], 1)),
+                              both(-1.52587890625e-05f), both(128.0f - 7.62939453125e-06f));   // minus the random number
+        const float2 diff = fma2(u, width, above), mid = add2(u, both(0.5f));
+        const float2 near = fma2(y, both(1.2f * kMomentErr), both(2.0f * err_y));
+        const uint32_t cx = __float_as_uint(zr.x) + (diff.x > 0.f ? 1u : 0u), cy = __float_as_uint(zr.y) + (diff.y > 0.f ? 1u : 0u);
+        mr[i] = ym.x < 0.f ? 0u - cx : cx;
+        mr[i + 1] = ym.y < 0.f ? 0u - cy : cy;
+        const bool all = !(err_y <= 5e-5f);
+        if (all || fabsf(diff.x) <= near.x || fabsf(mid.x) > 0.49976f) unsure_m |= 1u << i;
+        if (all || fabsf(diff.y) <= near.y || fabsf(mid.y) > 0.49976f) unsure_m |= 2u << i;
+      }
       // second moment: w = 255^4 v / V lies between d^4 and (d + 1)^4 (d at most 254; 254.5 stands for all above it).
       // Next to d^4 the rounded root may name the neighbouring interval, which gives the same code unless the random
       // number u is within (error of the place in the interval) < 2.4e-4 of 0 or 1.  (A v that just decays with its
@@ -424,10 +465,15 @@ __device__ __forceinline__ void step_block(const Scalars &s, const Entry &e, int
     for (; unsure_m; unsure_m &= unsure_m - 1) {
       const int j = __ffs(unsure_m) - 1;
       const double x = exact_avg(s, old_m(j), M0, old_g(j), gs), y = fabs(x) * 16129.0;
-      int c = static_cast<int>(rintf(sqrt_ftz(static_cast<float>(fabs(x)) * inv_m)));
-      const double up = c + 0.5, down = c - 0.5;
-      if (y > up * up * M) ++c;
-      else if (c > 0 && y < down * down * M) --c;
+      int c;
+      if (RANDOM) {
+        c = random_avg_code(y / M, random_of(avg_words4, j));
+      } else {
+        c = static_cast<int>(rintf(sqrt_ftz(static_cast<float>(fabs(x)) * inv_m)));
+        const double up = c + 0.5, down = c - 0.5;
+        if (y > up * up * M) ++c;
+        else if (c > 0 && y < down * down * M) --c;
+      }
       set_byte(mo, j, x < 0.0 ? -c : c);
     }
 #pragma unroll 1
@@ -443,7 +489,7 @@ __device__ __forceinline__ void step_block(const Scalars &s, const Entry &e, int
       if (y > 0.0) set_byte(vo, j, max(static_cast<int>(d) + (random_of(words4, j) * (hi - lo) < y - lo ? 1 : 0), 1));
     }
     if (tiny) {                                // (here few registers are live; the codes above mean nothing)
-      quantise_tiny(s, e, block, lane, left, gs, M0, V0, stash);
+      quantise_tiny<RANDOM>(s, e, block, lane, left, gs, M0, V0, stash);
       return;
     }
     put_codes<WHOLE>(e.m, at, left, mo);
@@ -475,7 +521,7 @@ template <int N, typename F> __device__ __forceinline__ void for_blocks(const Ta
   }
 }
 
-template <int N, int FMT, bool EIGHT>
+template <int N, int FMT, bool EIGHT, bool RANDOM>
 __global__ void __launch_bounds__(kThreads, kResident) adamw_kernel(const __grid_constant__ Table<N> t) {
   const float gs = t.s.grad_scale ? *t.s.grad_scale : 1.0f;
   if (!isfinite(gs)) return;                              // an overflowed step changes nothing
@@ -483,8 +529,8 @@ __global__ void __launch_bounds__(kThreads, kResident) adamw_kernel(const __grid
   __shared__ Stash stashes[EIGHT ? kThreads / 32 : 1];
   Stash &stash = stashes[EIGHT ? threadIdx.x >> 5 : 0];
   for_blocks(t, [&](const Entry &e, int64_t block, uint32_t) {
-    if (e.vec && (block + 1) * kBlock <= e.n) step_block<FMT, EIGHT, true>(t.s, e, block, lane, gs, stash);
-    else step_block<FMT, EIGHT, false>(t.s, e, block, lane, gs, stash);
+    if (e.vec && (block + 1) * kBlock <= e.n) step_block<FMT, EIGHT, RANDOM, true>(t.s, e, block, lane, gs, stash);
+    else step_block<FMT, EIGHT, RANDOM, false>(t.s, e, block, lane, gs, stash);
   });
 }
 
@@ -520,28 +566,28 @@ template <int N> __global__ void __launch_bounds__(kThreads) adamw_unpack_kernel
 
 bool aligned(const void *p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 
-template <int N, int FMT, bool EIGHT> cudaError_t launch_step(const Table<N> &t, int grid, cudaStream_t s) {
-  adamw_kernel<N, FMT, EIGHT><<<grid, kThreads, 0, s>>>(t);
+template <int N, int FMT> cudaError_t launch_step(const Table<N> &t, int state_bits, bool random_avg, int grid, cudaStream_t s) {
+  if (state_bits == 32) adamw_kernel<N, FMT, false, false><<<grid, kThreads, 0, s>>>(t);
+  else if (random_avg) adamw_kernel<N, FMT, true, true><<<grid, kThreads, 0, s>>>(t);
+  else adamw_kernel<N, FMT, true, false><<<grid, kThreads, 0, s>>>(t);
   return cudaGetLastError();
 }
-template <int N> cudaError_t launch_any(const Table<N> &t, int grad_format, int state_bits, int grid, cudaStream_t s) {
+template <int N>
+cudaError_t launch_any(const Table<N> &t, int grad_format, int state_bits, bool random_avg, int grid, cudaStream_t s) {
   if (state_bits == 0) {
     adamw_unpack_kernel<N><<<grid, kThreads, 0, s>>>(t);
     return cudaGetLastError();
   }
-  if (state_bits == 32)
-    return grad_format == 0   ? launch_step<N, 0, false>(t, grid, s)
-           : grad_format == 1 ? launch_step<N, 1, false>(t, grid, s)
-                              : launch_step<N, 2, false>(t, grid, s);
-  return grad_format == 0   ? launch_step<N, 0, true>(t, grid, s)
-         : grad_format == 1 ? launch_step<N, 1, true>(t, grid, s)
-                            : launch_step<N, 2, true>(t, grid, s);
+  return grad_format == 0   ? launch_step<N, 0>(t, state_bits, random_avg, grid, s)
+         : grad_format == 1 ? launch_step<N, 1>(t, state_bits, random_avg, grid, s)
+                            : launch_step<N, 2>(t, state_bits, random_avg, grid, s);
 }
 
 // Launches over the entries that make(i, entry) fills (false: nothing to do for tensor i), as many per launch as the
 // kernel parameters hold.  state_bits 0: unpack.
 template <typename Make>
-cudaError_t launch_list(int n_tensors, const Scalars &base, int grad_format, int state_bits, Make make, cudaStream_t s) {
+cudaError_t launch_list(int n_tensors, const Scalars &base, int grad_format, int state_bits, bool random_avg, Make make,
+                        cudaStream_t s) {
   int dev = 0, sms = 0;
   cudaError_t err = cudaGetDevice(&dev);
   if (err == cudaSuccess) err = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
@@ -572,9 +618,9 @@ cudaError_t launch_list(int n_tensors, const Scalars &base, int grad_format, int
       Table<kSmallTable> small;
       small.s = t.s;
       std::copy(t.e, t.e + n, small.e);
-      err = launch_any(small, grad_format, state_bits, grid, s);
+      err = launch_any(small, grad_format, state_bits, random_avg, grid, s);
     } else {
-      err = launch_any(t, grad_format, state_bits, grid, s);
+      err = launch_any(t, grad_format, state_bits, random_avg, grid, s);
     }
     if (err != cudaSuccess) return err;
   }
@@ -626,10 +672,13 @@ int echo_adamw_step(const echo_adamw_tensor *tensors, int32_t n_tensors, const e
   if (!fraction(opt->beta1) || !fraction(opt->beta2) || !(opt->lr >= 0.0) || !std::isfinite(opt->lr)) return ECHO_ERR_INVALID;
   if (!(static_cast<float>(opt->eps) > 0.f) || !std::isfinite(static_cast<float>(opt->eps))) return ECHO_ERR_INVALID;
   if (opt->step < 1 || opt->step > 0xffffffffLL || !aligned(opt->grad_scale, 4)) return ECHO_ERR_INVALID;
-  if (opt->grad_format < 0 || opt->grad_format > 2 || (opt->state_bits != 8 && opt->state_bits != 32)) return ECHO_ERR_INVALID;
+  // (the first step's moments come from zeros: nothing is there to fall, and the nearest code is the better one)
+  const bool random_avg = opt->state_bits == (8 | ECHO_ADAMW_RANDOM_AVG) && opt->step > 1;
+  const int bits = opt->state_bits == (8 | ECHO_ADAMW_RANDOM_AVG) ? 8 : opt->state_bits;
+  if (opt->grad_format < 0 || opt->grad_format > 2 || (bits != 8 && bits != 32)) return ECHO_ERR_INVALID;
   // 8-bit moments: roots of denormal numbers count as 0 beside eps
-  if (opt->state_bits == 8 && opt->eps < 1e-12) return ECHO_ERR_UNSUPPORTED;
-  const int bits = opt->state_bits, gb = elem_bytes(opt->grad_format);
+  if (bits == 8 && opt->eps < 1e-12) return ECHO_ERR_UNSUPPORTED;
+  const int gb = elem_bytes(opt->grad_format);
   if (!list_ok(tensors, n_tensors, bits, opt->grad_format, true)) return ECHO_ERR_INVALID;
   for (int i = 0; i < n_tensors; ++i)
     if (!(tensors[i].weight_decay >= 0.0) || !std::isfinite(tensors[i].weight_decay)) return ECHO_ERR_INVALID;
@@ -695,7 +744,8 @@ int echo_adamw_step(const echo_adamw_tensor *tensors, int32_t n_tensors, const e
             aligned(x.param_copy, 16);
     return true;
   };
-  return launch_list(n_tensors, s, opt->grad_format, bits, make, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess
+  return launch_list(n_tensors, s, opt->grad_format, bits, random_avg, make, static_cast<cudaStream_t>(cuda_stream)) ==
+                 cudaSuccess
              ? ECHO_OK
              : ECHO_ERR_CUDA;
 }
@@ -742,8 +792,9 @@ int echo_adamw_unpack(const echo_adamw_tensor *tensors, int32_t n_tensors, float
     e.vec = aligned(out_avg[i], 32) && aligned(out_avg_sq[i], 32) && aligned(x.exp_avg, 8) && aligned(x.exp_avg_sq, 8);
     return true;
   };
-  return launch_list(n_tensors, Scalars{}, 2, 0, make, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? ECHO_OK
-                                                                                                              : ECHO_ERR_CUDA;
+  return launch_list(n_tensors, Scalars{}, 2, 0, false, make, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess
+             ? ECHO_OK
+             : ECHO_ERR_CUDA;
 }
 
 }  // extern "C"
