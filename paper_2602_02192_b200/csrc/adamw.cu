@@ -45,10 +45,14 @@ struct Entry {
   float *m_scale, *v_scale;
   __nv_bfloat16 *copy;
   int64_t n;
-  float decay;                               // 1 - lr wd
+  // 1 - lr wd in two parts, the larger rounded towards zero: fp32's nearest number alone is off by up to 2^-25, which is
+  // 0.7 % of a decay of 3e-6 and all of one of 1e-8.  (Both have one sign, so that an infinite weight stays what it is.)
+  float decay, decay_rest;
   uint32_t first;                            // blocks of the launch before this tensor's
-  uint32_t id;                               // place in the caller's list (keys the random numbers)
-  uint32_t vec;                              // every array starts on a boundary of its 8-element pieces
+  uint32_t id_vec;                           // place in the caller's list (keys the random numbers); bit 31: every array
+                                             // starts on a boundary of its 8-element pieces
+  __device__ uint32_t id() const { return id_vec & 0x7fffffffu; }
+  __device__ bool vec() const { return (id_vec >> 31) != 0; }
 };
 struct Scalars {
   const float *grad_scale;
@@ -245,7 +249,7 @@ struct Stash {
 // the random numbers of eight elements for the second (moment 0) or the first moment (1), and the one of element j in
 // [0, 1).  (An octet's number stays below 2^35: the counter's bit 63 is free.)
 __device__ __forceinline__ uint4 random_words(const Scalars &s, const Entry &e, uint64_t octet, uint32_t moment = 0) {
-  return philox(make_uint4(static_cast<uint32_t>(octet), static_cast<uint32_t>(octet >> 32) | moment << 31, e.id, s.step),
+  return philox(make_uint4(static_cast<uint32_t>(octet), static_cast<uint32_t>(octet >> 32) | moment << 31, e.id(), s.step),
                 s.key0, s.key1);
 }
 __device__ __forceinline__ double random_of(const uint4 &w, int j) {
@@ -312,7 +316,9 @@ __device__ __forceinline__ void step_block(const Scalars &s, const Entry &e, int
       m[j] = fmaf(s.b1, m[j], s.b1c * h);
       v[j] = fmaf(s.b2, v[j], s.b2c * h * h);
       const float denom = fmaf(sqrt_fast(v[j]), s.root_corr, s.eps);
-      p[j] = fmaf(p[j], e.decay, -s.rate * __fdividef(m[j], denom));
+      float change = -s.rate * __fdividef(m[j], denom);
+      if (e.decay_rest != 0.f) change = fmaf(p[j], e.decay_rest, change);
+      p[j] = fmaf(p[j], e.decay, change);
     }
     put_f32<WHOLE>(static_cast<float *>(e.m) + at, left, m);
     put_f32<WHOLE>(static_cast<float *>(e.v) + at, left, v);
@@ -351,7 +357,9 @@ __device__ __forceinline__ void step_block(const Scalars &s, const Entry &e, int
       big_b = max_or_nan(big_b, b.x, b.y);
       const float2 denom = fma2(make_float2(sqrt_ftz(vv.x), sqrt_ftz(vv.y)), both(s.root_corr), both(s.eps));
       const float2 up = mul2(mm, make_float2(rcp_ftz(denom.x), rcp_ftz(denom.y)));        // (denom is at least eps)
-      const float2 pp = fma2(make_float2(p[i], p[i + 1]), both(e.decay), mul2(up, both(-s.rate)));
+      float2 change = mul2(up, both(-s.rate));
+      if (e.decay_rest != 0.f) change = fma2(make_float2(p[i], p[i + 1]), both(e.decay_rest), change);
+      const float2 pp = fma2(make_float2(p[i], p[i + 1]), both(e.decay), change);
       p[i] = pp.x;
       p[i + 1] = pp.y;
     }
@@ -529,7 +537,7 @@ __global__ void __launch_bounds__(kThreads, kResident) adamw_kernel(const __grid
   __shared__ Stash stashes[EIGHT ? kThreads / 32 : 1];
   Stash &stash = stashes[EIGHT ? threadIdx.x >> 5 : 0];
   for_blocks(t, [&](const Entry &e, int64_t block, uint32_t) {
-    if (e.vec && (block + 1) * kBlock <= e.n) step_block<FMT, EIGHT, RANDOM, true>(t.s, e, block, lane, gs, stash);
+    if (e.vec() && (block + 1) * kBlock <= e.n) step_block<FMT, EIGHT, RANDOM, true>(t.s, e, block, lane, gs, stash);
     else step_block<FMT, EIGHT, RANDOM, false>(t.s, e, block, lane, gs, stash);
   });
 }
@@ -540,7 +548,7 @@ template <int N> __global__ void __launch_bounds__(kThreads) adamw_unpack_kernel
   for_blocks(t, [&](const Entry &e, int64_t block, uint32_t) {
     const int64_t at = block * kBlock + lane * 8;
     const int left = static_cast<int>(min(static_cast<int64_t>(8), max(static_cast<int64_t>(0), e.n - at)));
-    const bool whole = e.vec && left == 8;
+    const bool whole = e.vec() && left == 8;
     const uint64_t mc = whole ? get_codes<true>(e.m, at, left) : get_codes<false>(e.m, at, left);
     const uint64_t vc = whole ? get_codes<true>(e.v, at, left) : get_codes<false>(e.v, at, left);
     const float M = e.m_scale[block], V = e.v_scale[block];
@@ -738,10 +746,13 @@ int echo_adamw_step(const echo_adamw_tensor *tensors, int32_t n_tensors, const e
     e.v_scale = x.sq_scales;
     e.copy = static_cast<__nv_bfloat16 *>(x.param_copy);
     e.n = x.n;
-    e.decay = static_cast<float>(1.0 - opt->lr * x.weight_decay);
-    e.id = static_cast<uint32_t>(i);
-    e.vec = aligned(x.param, 32) && aligned(x.grad, 8 * gb) && aligned(x.exp_avg, bits) && aligned(x.exp_avg_sq, bits) &&
-            aligned(x.param_copy, 16);
+    const double decay = 1.0 - opt->lr * x.weight_decay;
+    e.decay = static_cast<float>(decay);
+    if (std::fabs(static_cast<double>(e.decay)) > std::fabs(decay)) e.decay = std::nextafter(e.decay, 0.0f);
+    e.decay_rest = static_cast<float>(decay - e.decay);
+    const bool vec = aligned(x.param, 32) && aligned(x.grad, 8 * gb) && aligned(x.exp_avg, bits) &&
+                     aligned(x.exp_avg_sq, bits) && aligned(x.param_copy, 16);
+    e.id_vec = static_cast<uint32_t>(i) | static_cast<uint32_t>(vec) << 31;
     return true;
   };
   return launch_list(n_tensors, s, opt->grad_format, bits, random_avg, make, static_cast<cudaStream_t>(cuda_stream)) ==
@@ -789,7 +800,8 @@ int echo_adamw_unpack(const echo_adamw_tensor *tensors, int32_t n_tensors, float
     e.m_scale = x.avg_scales;
     e.v_scale = x.sq_scales;
     e.n = x.n;
-    e.vec = aligned(out_avg[i], 32) && aligned(out_avg_sq[i], 32) && aligned(x.exp_avg, 8) && aligned(x.exp_avg_sq, 8);
+    const bool vec = aligned(out_avg[i], 32) && aligned(out_avg_sq[i], 32) && aligned(x.exp_avg, 8) && aligned(x.exp_avg_sq, 8);
+    e.id_vec = static_cast<uint32_t>(i) | static_cast<uint32_t>(vec) << 31;
     return true;
   };
   return launch_list(n_tensors, Scalars{}, 2, 0, false, make, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess

@@ -261,3 +261,41 @@ def test_adamw_8_small_gradients_beside_large_ones(B):
     at random is noise without a drift, nearest codes keep whatever once reached one."""
     assert _drift(B, True, 2000, 0.999, 1e-4) < _drift(B, False, 2000, 0.999, 1e-4)
     assert _drift(B, True, 2000, 0.999, 3e-4) < _drift(B, False, 2000, 0.999, 3e-4)
+
+
+@pytest.mark.parametrize("bits,gdtype", [(32, torch.float32), (32, torch.bfloat16), (8, torch.float32)])
+@pytest.mark.parametrize("lr,decay", [(1e-6, 0.01), (1e-6, 0.1), (3e-5, 0.1), (1e-3, 0.0), (0.4, 7.0)])
+@pytest.mark.parametrize("offset", [0, 1])
+def test_adamw_decay_below_a_weights_last_bit(B, bits, gdtype, lr, decay, offset):
+    """lr * weight_decay = 1e-8 is a twelfth of the last bit of a weight in [1, 2).  Every weight is the fp32 number next to
+    its exact value, up to what comes before that rounding: the update's 20 roundings (of m relative to the sum of its
+    terms), one of its sum with the decay's second part, which is at most 2^-24 of the weight, and one of that part."""
+    n = 1 << 20
+    gen = torch.Generator(device="cuda").manual_seed(17)
+    rand = lambda: torch.rand(n + offset, generator=gen, device="cuda")  # noqa: E731
+    p, g = (1 + rand())[offset:], (rand() - 0.5).to(gdtype)[offset:]
+    if bits == 32:
+        m, v, scales = (rand() - 0.5)[offset:], (0.1 + rand())[offset:], ()
+        m64, v64 = m.double(), v.double()
+    else:
+        m = torch.randint(-127, 128, (n + offset,), generator=gen, device="cuda").to(torch.int8)[offset:]
+        v = torch.randint(128, 256, (n + offset,), generator=gen, device="cuda").to(torch.uint8)[offset:]
+        scales = [torch.full((n // 256,), 0.5, device="cuda")], [torch.full((n // 256,), 1.0, device="cuda")]
+        m64, v64 = 0.5 * (m.double() / 127) * (m.double() / 127).abs(), (v.double() / 255) ** 4
+    p64, g64 = p.double(), g.double()
+    B.echo_adamw_step(B.AdamWTensors([p], [g], [m], [v], None, decay, *scales), 9, lr)
+    v64 = 0.999 * v64 + (1 - 0.999) * g64 * g64
+    rate = lr / (1 - 0.9 ** 9) / ((v64 / (1 - 0.999 ** 9)).sqrt() + 1e-8)
+    want = p64 * (1 - lr * decay) - rate * (0.9 * m64 + (1 - 0.9) * g64)
+    before_rounding = 21 * E * rate * (0.9 * m64.abs() + (1 - 0.9) * g64.abs()) + 2 * E * E * p64
+    half_step = torch.ldexp(torch.full_like(want, E), torch.frexp(p.double())[1] - 1)
+    assert bool(((p.double() - want).abs() <= half_step + before_rounding).all())
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("decay", [0.0, 0.1])
+def test_adamw_leaves_infinite_weights(B, bits, decay):
+    p = torch.tensor([math.inf, -math.inf, 1.0] * 100, device="cuda")
+    before, g = p.clone(), torch.zeros(300, device="cuda")
+    B.echo_adamw_step(B.AdamWTensors.zeros([p], [g], state_bits=bits, weight_decay=decay), 1, 3e-5)
+    assert torch.equal(p[0::3], before[0::3]) and torch.equal(p[1::3], before[1::3]) and torch.isfinite(p[2::3]).all()
