@@ -46,7 +46,8 @@ struct Entry {
   __nv_bfloat16 *copy;
   int64_t n;
   // 1 - lr wd in two parts, the larger rounded towards zero: fp32's nearest number alone is off by up to 2^-25, which is
-  // 0.7 % of a decay of 3e-6 and all of one of 1e-8.  (Both have one sign, so that an infinite weight stays what it is.)
+  // 0.7 % of a decay of 3e-6 and all of one of 1e-8.  (Both have one sign and, where there is a weight left, neither is
+  // 0, so that an infinite weight stays what it is without a branch: 1 is 1 - 2^-24 and 2^-24.)
   float decay, decay_rest;
   uint32_t first;                            // blocks of the launch before this tensor's
   uint32_t id_vec;                           // place in the caller's list (keys the random numbers); bit 31: every array
@@ -316,9 +317,7 @@ __device__ __forceinline__ void step_block(const Scalars &s, const Entry &e, int
       m[j] = fmaf(s.b1, m[j], s.b1c * h);
       v[j] = fmaf(s.b2, v[j], s.b2c * h * h);
       const float denom = fmaf(sqrt_fast(v[j]), s.root_corr, s.eps);
-      float change = -s.rate * __fdividef(m[j], denom);
-      if (e.decay_rest != 0.f) change = fmaf(p[j], e.decay_rest, change);
-      p[j] = fmaf(p[j], e.decay, change);
+      p[j] = fmaf(p[j], e.decay, fmaf(p[j], e.decay_rest, -s.rate * __fdividef(m[j], denom)));
     }
     put_f32<WHOLE>(static_cast<float *>(e.m) + at, left, m);
     put_f32<WHOLE>(static_cast<float *>(e.v) + at, left, v);
@@ -357,9 +356,8 @@ __device__ __forceinline__ void step_block(const Scalars &s, const Entry &e, int
       big_b = max_or_nan(big_b, b.x, b.y);
       const float2 denom = fma2(make_float2(sqrt_ftz(vv.x), sqrt_ftz(vv.y)), both(s.root_corr), both(s.eps));
       const float2 up = mul2(mm, make_float2(rcp_ftz(denom.x), rcp_ftz(denom.y)));        // (denom is at least eps)
-      float2 change = mul2(up, both(-s.rate));
-      if (e.decay_rest != 0.f) change = fma2(make_float2(p[i], p[i + 1]), both(e.decay_rest), change);
-      const float2 pp = fma2(make_float2(p[i], p[i + 1]), both(e.decay), change);
+      const float2 old = make_float2(p[i], p[i + 1]);
+      const float2 pp = fma2(old, both(e.decay), fma2(old, both(e.decay_rest), mul2(up, both(-s.rate))));
       p[i] = pp.x;
       p[i + 1] = pp.y;
     }
@@ -748,7 +746,7 @@ int echo_adamw_step(const echo_adamw_tensor *tensors, int32_t n_tensors, const e
     e.n = x.n;
     const double decay = 1.0 - opt->lr * x.weight_decay;
     e.decay = static_cast<float>(decay);
-    if (std::fabs(static_cast<double>(e.decay)) > std::fabs(decay)) e.decay = std::nextafter(e.decay, 0.0f);
+    if (std::fabs(static_cast<double>(e.decay)) >= std::fabs(decay)) e.decay = std::nextafter(e.decay, 0.0f);
     e.decay_rest = static_cast<float>(decay - e.decay);
     const bool vec = aligned(x.param, 32) && aligned(x.grad, 8 * gb) && aligned(x.exp_avg, bits) &&
                      aligned(x.exp_avg_sq, bits) && aligned(x.param_copy, 16);
