@@ -624,7 +624,9 @@ class AdamWTensors:
                 t.param_copy = address(copies[i], size, torch.bfloat16)
             t.n, t.weight_decay = size, decay[i]
         self.count = n
-        self._keep = (params, grads, exp_avg, exp_avg_sq, copies, avg_scales, sq_scales)
+        # tensors and their memory, not the caller's lists: those may change, the addresses in the table do not
+        kept = [x for xs in (params, grads, exp_avg, exp_avg_sq, copies, avg_scales, sq_scales) if xs is not None for x in xs]
+        self._keep = [(x, x.untyped_storage()) for x in kept if x is not None]
 
     @classmethod
     def zeros(cls, params, grads, state_bits: int = 32, copies=None, weight_decay=0.0, random_avg: bool = True) -> "AdamWTensors":

@@ -333,3 +333,48 @@ def test_adamw_state_bits():
     with open(header) as f:
         assert f"#define ECHO_ADAMW_RANDOM_AVG {random_avg}" in f.read()
     assert _lib()[0].ECHO_ADAMW_RANDOM_AVG == random_avg
+
+
+# ---- the handle of an AdamW step (no GPU: stand-ins for device tensors) ----------------------------
+class _Memory:
+    pass
+
+
+class _Tensor:
+    is_cuda, is_leaf, grad, device = True, True, None, "cuda:0"
+
+    def __init__(self, address, numel=10, dtype=None):
+        import torch
+        self.address, self.n, self.dtype, self.memory = address, numel, dtype or torch.float32, _Memory()
+
+    def numel(self):
+        return self.n
+
+    def data_ptr(self):
+        return self.address
+
+    def is_contiguous(self):
+        return True
+
+    def untyped_storage(self):
+        return self.memory
+
+
+def test_adamw_handle_keeps_what_its_addresses_point_to():
+    import gc
+    import weakref
+    b, _ = _lib()
+    lists = [[_Tensor(P0 + 4096 * (2 * i + j)) for j in range(2)] for i in range(4)]
+    tensors = [weakref.ref(x) for xs in lists for x in xs]
+    memory = [weakref.ref(x.memory) for xs in lists for x in xs]
+    plan = b.AdamWTensors(*lists)
+    for xs in lists:                                      # the caller's lists move on, and so does a tensor's memory
+        xs[1].memory = _Memory()
+        xs.clear()
+    del lists, xs
+    gc.collect()
+    assert all(r() is not None for r in tensors) and all(r() is not None for r in memory)
+    assert plan.table[1].grad == P0 + 4096 * 3
+    del plan
+    gc.collect()
+    assert all(r() is None for r in tensors) and all(r() is None for r in memory)
