@@ -587,6 +587,10 @@ class AdamWTensors:
     (fp32, one per 256 elements of a tensor); copies: bf16 tensors (or None) that receive the updated weights;
     weight_decay: one number, or one per tensor.  All of them contiguous, on one GPU.
 
+    The list steps on the gradient tensors it was given, so a backward pass has to write into these (zero_grad with
+    set_to_none=False), or set_grads has to name the new ones.  Where the gradients given are the params' own .grad,
+    echo_adamw_step refuses to run once these have become other tensors.
+
     random_avg (8-bit moments): first moments are rounded at random with the mean kept, which is what to train with; the
     lists that `zeros` makes do so.  False: to the nearest code, which does not fall by itself, so that weights whose
     gradients end, or are far below their block's, drift.  Pass True to go on with moments of a list from `zeros`."""
@@ -625,8 +629,35 @@ class AdamWTensors:
             t.n, t.weight_decay = size, decay[i]
         self.count = n
         # tensors and their memory, not the caller's lists: those may change, the addresses in the table do not
-        kept = [x for xs in (params, grads, exp_avg, exp_avg_sq, copies, avg_scales, sq_scales) if xs is not None for x in xs]
+        kept = [x for xs in (params, exp_avg, exp_avg_sq, copies, avg_scales, sq_scales) if xs is not None for x in xs]
         self._keep = [(x, x.untyped_storage()) for x in kept if x is not None]
+        self._params = list(params)
+        self._grads = list(grads)
+        self._watch()
+
+    def _watch(self):
+        self._keep_grads = [x.untyped_storage() for x in self._grads]
+        # the gradients that are their params' own: what the next backward pass may replace
+        self._own = [(p, g) for p, g in zip(self._params, self._grads) if p.is_leaf and p.grad is g]
+
+    def set_grads(self, grads):
+        """The list steps on these gradients from now on: one per param, of the dtype and sizes of the first ones."""
+        grads = list(grads)
+        assert len(grads) == self.count
+        for g, size in zip(grads, self.sizes):
+            assert g.is_cuda and g.device == self.device and _FORMATS.get(g.dtype) == self.grad_format
+            assert g.is_contiguous() and g.numel() == size
+        for i, g in enumerate(grads):
+            self.table[i].grad = g.data_ptr()
+        self._grads = grads
+        self._watch()
+
+    def check_grads(self):
+        """Raises where a param's .grad is no longer the tensor that the list steps on."""
+        for p, g in self._own:
+            if p.grad is not g:
+                raise RuntimeError("a param's .grad is another tensor than the one this list steps on: call set_grads, or "
+                                   "keep the gradients with zero_grad(set_to_none=False)")
 
     @classmethod
     def zeros(cls, params, grads, state_bits: int = 32, copies=None, weight_decay=0.0, random_avg: bool = True) -> "AdamWTensors":
@@ -650,6 +681,8 @@ def echo_adamw_step(tensors: AdamWTensors, step: int, lr: float, beta1: float = 
     """One AdamW step (number `step`, from 1) over every tensor of the list.  grad_scale: fp32 device tensor of one
     element that multiplies the gradients (if it is not finite nothing changes).  seed: random numbers of the 8-bit
     moments' rounding."""
+    if tensors._own:
+        tensors.check_grads()
     bits = tensors.state_bits
     if bits == 8 and tensors.random_avg:
         bits |= ECHO_ADAMW_RANDOM_AVG

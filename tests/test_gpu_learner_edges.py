@@ -299,3 +299,33 @@ def test_adamw_leaves_infinite_weights(B, bits, decay):
     before, g = p.clone(), torch.zeros(300, device="cuda")
     B.echo_adamw_step(B.AdamWTensors.zeros([p], [g], state_bits=bits, weight_decay=decay), 1, 3e-5)
     assert torch.equal(p[0::3], before[0::3]) and torch.equal(p[1::3], before[1::3]) and torch.isfinite(p[2::3]).all()
+
+
+def test_adamw_handle_with_autograd(B):
+    """The usual loop: gradients that autograd makes anew every step."""
+    torch.manual_seed(4)
+    model = torch.nn.Linear(64, 8, bias=False, device="cuda")
+    p = model.weight
+    x = torch.randn(32, 64, device="cuda")
+
+    def backward():
+        model.zero_grad()                                  # (set_to_none)
+        model(x).pow(2).sum().backward()
+
+    backward()
+    plan = B.AdamWTensors.zeros([p], [p.grad])
+    w, m, v = p.detach().double().cpu().numpy().ravel(), np.zeros(512), np.zeros(512)
+    for t in range(1, 4):
+        if t > 1:
+            old = p.grad
+            backward()
+            if p.grad is not old:
+                with pytest.raises(RuntimeError):
+                    B.echo_adamw_step(plan, t, 1e-2)
+            plan.set_grads([p.grad])
+        g = p.grad.double().cpu().numpy().ravel()
+        B.echo_adamw_step(plan, t, 1e-2)
+        w, m, v = L.adamw(w, g, m, v, t, 1e-2, 0.9, 0.999, 1e-8, 0.0)
+        got = p.detach().double().cpu().numpy().ravel()
+        # moments: 8 e of terms of one size; the update: 14 e more; both at most 10 lr here; three steps
+        assert np.abs(got - w).max() <= t * (30 * E * 1e-2 * 10 + E * np.abs(w).max())

@@ -378,3 +378,41 @@ def test_adamw_handle_keeps_what_its_addresses_point_to():
     del plan
     gc.collect()
     assert all(r() is None for r in tensors) and all(r() is None for r in memory)
+
+
+def test_adamw_handle_notices_other_gradients(monkeypatch):
+    """A backward pass after zero_grad(set_to_none=True) makes new gradients: the step must not apply the old ones again."""
+    b, _ = _lib()
+    params = [_Tensor(P0 + 4096 * i) for i in range(2)]
+    grads = [_Tensor(P1 + 4096 * i) for i in range(2)]
+    moments = [[_Tensor(P1 + (k << 16) + 4096 * i) for i in range(2)] for k in (1, 2)]
+    for p, g in zip(params, grads):
+        p.grad = g
+    plan = b.AdamWTensors(params, grads, *moments)
+    launched = []
+    monkeypatch.setattr(b, "_call", lambda *a: launched.append([plan.table[i].grad for i in range(2)]))
+    plan.device = type("Device", (), {"index": 0})()
+    b.echo_adamw_step(plan, 1, 1e-3)
+    params[1].grad = None                                  # zero_grad
+    with pytest.raises(RuntimeError):
+        b.echo_adamw_step(plan, 2, 1e-3)
+    fresh = params[1].grad = _Tensor(P1 + (9 << 16))       # the next backward pass
+    with pytest.raises(RuntimeError):
+        b.echo_adamw_step(plan, 2, 1e-3)
+    plan.device = "cuda:0"
+    plan.set_grads([p.grad for p in params])
+    plan.device = type("Device", (), {"index": 0})()
+    b.echo_adamw_step(plan, 2, 1e-3)
+    assert launched == [[P1, P1 + 4096], [P1, fresh.address]]
+    plan.device = "cuda:0"
+    import torch
+    for bad in ([grads[0]], [grads[0], _Tensor(P1, 11)], [grads[0], _Tensor(P1, dtype=torch.bfloat16)], [grads[0], _Tensor(P1, dtype=torch.int32)]):
+        with pytest.raises(AssertionError):
+            plan.set_grads(bad)
+    assert [plan.table[i].grad for i in range(2)] == [P1, fresh.address]
+    # gradients that are not the params' own (pieces of a flat buffer, say) are the caller's to keep up to date
+    params[0].grad = None
+    plan.set_grads([_Tensor(P1), _Tensor(P1 + 4096)])
+    plan.device = type("Device", (), {"index": 0})()
+    b.echo_adamw_step(plan, 3, 1e-3)
+    assert launched[-1] == [P1, P1 + 4096]
