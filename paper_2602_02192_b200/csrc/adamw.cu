@@ -403,6 +403,8 @@ __device__ __forceinline__ void step_block(const Scalars &s, const Entry &e, int
     uint32_t mr[8], vr[8];                     // codes in the low bytes
     uint32_t unsure_m = 0, unsure_v = 0;
     const float err_y = 0.5f * err_m * inv_m;
+    const float of_g = 2.0f * kMomentErr * s.b1c * fabsf(gs) * inv_m;
+    const float4 ga = RANDOM ? stash.g[0][lane] : float4{}, gb = RANDOM ? stash.g[1][lane] : float4{};
 #pragma unroll
     for (int i = 0; i < 8; i += 2) {
       const float2 ym = mul2(make_float2(m[i], m[i + 1]), both(inv_m)), w = mul2(make_float2(v[i], v[i + 1]), both(inv_v));
@@ -420,9 +422,9 @@ __device__ __forceinline__ void step_block(const Scalars &s, const Entry &e, int
         if (fabsf(dist.y) > clear.y) unsure_m |= 2u << i;
       } else {
         // first moment: y = 127^2 |m| / M lies between d^2 and (d + 1)^2 (d at most 126; 126.5 stands for all above it),
-        // the second moment's rule with squares.  The place in the interval is off by less than 2e-4 (y by the moments'
-        // error, 2 err_y, and 1.2e-6 of itself, which is below 8e-5 of the interval; the root by 1.5e-5) unless the
-        // moments' error alone is more: then 64 bits decide on all of the block.
+        // the second moment's rule with squares.  m is off by kMomentErr of its terms, |b1 m0| + |(1 - b1) g|, at most
+        // |m| + 2 |(1 - b1) g|: `near` in y.  The root's error may name the neighbouring interval where y's place is
+        // within near / width + 1.5e-5 of 0 or 1: that matters only for random numbers as near to them.
         const float2 y = make_float2(fabsf(ym.x), fabsf(ym.y));
         const float2 z = make_float2(fminf(sqrt_ftz(y.x), 126.5f), fminf(sqrt_ftz(y.y), 126.5f));
         const float2 zr = make_float2(__fadd_rd(z.x, kTwo23), __fadd_rd(z.y, kTwo23)), d = add2(zr, both(-kTwo23));
@@ -430,13 +432,15 @@ __device__ __forceinline__ void step_block(const Scalars &s, const Entry &e, int
         const float2 u = fma2(make_float2(half_plus_two23(avg_words[i >> 1], 0), half_plus_two23(avg_words[i >> 1], 1)),
                               both(-1.52587890625e-05f), both(128.0f - 7.62939453125e-06f));   // minus the random number
         const float2 diff = fma2(u, width, above), mid = add2(u, both(0.5f));
-        const float2 near = fma2(y, both(1.2f * kMomentErr), both(2.0f * err_y));
+        const float2 h = i < 4 ? (i & 2 ? make_float2(ga.z, ga.w) : make_float2(ga.x, ga.y))
+                               : (i & 2 ? make_float2(gb.z, gb.w) : make_float2(gb.x, gb.y));
+        const float2 near = fma2(make_float2(fabsf(h.x), fabsf(h.y)), both(of_g), mul2(y, both(1.2f * kMomentErr)));
+        const float2 edge = fma2(make_float2(fabsf(mid.x), fabsf(mid.y)), width, near), from = mul2(width, both(0.4999f));
         const uint32_t cx = __float_as_uint(zr.x) + (diff.x > 0.f ? 1u : 0u), cy = __float_as_uint(zr.y) + (diff.y > 0.f ? 1u : 0u);
         mr[i] = ym.x < 0.f ? 0u - cx : cx;
         mr[i + 1] = ym.y < 0.f ? 0u - cy : cy;
-        const bool all = !(err_y <= 5e-5f);
-        if (all || fabsf(diff.x) <= near.x || fabsf(mid.x) > 0.49976f) unsure_m |= 1u << i;
-        if (all || fabsf(diff.y) <= near.y || fabsf(mid.y) > 0.49976f) unsure_m |= 2u << i;
+        if (fabsf(diff.x) <= near.x || edge.x > from.x) unsure_m |= 1u << i;
+        if (fabsf(diff.y) <= near.y || edge.y > from.y) unsure_m |= 2u << i;
       }
       // second moment: w = 255^4 v / V lies between d^4 and (d + 1)^4 (d at most 254; 254.5 stands for all above it).
       // Next to d^4 the rounded root may name the neighbouring interval, which gives the same code unless the random
