@@ -204,6 +204,7 @@ __device__ __forceinline__ float byte_plus_two23(uint32_t word, int byte) {
 __device__ __forceinline__ float half_plus_two23(uint32_t word, int half) {
   return __uint_as_float(__byte_perm(word, 0x4B000000u, half ? 0x7432u : 0x7410u));
 }
+__device__ __forceinline__ bool has_zero_byte(uint32_t x) { return ((x - 0x01010101u) & ~x & 0x80808080u) != 0; }
 // low bytes of eight registers
 __device__ __forceinline__ uint64_t low_bytes(const uint32_t (&r)[8]) {
   const uint32_t lo = __byte_perm(__byte_perm(r[0], r[1], 0x0040), __byte_perm(r[2], r[3], 0x0040), 0x5410);
@@ -462,7 +463,7 @@ __device__ __forceinline__ void step_block(const Scalars &s, const Entry &e, int
     uint64_t mo = low_bytes(mr), vo = low_bytes(vr);
     // A gradient (or an old v) so far below its block's that fp32 does not hold its v still makes one above 0: 64 bits
     // decide on codes 0 beside either.
-    if (__vcmpeq4(static_cast<uint32_t>(vo), 0u) | __vcmpeq4(static_cast<uint32_t>(vo >> 32), 0u)) {
+    if (has_zero_byte(static_cast<uint32_t>(vo)) || has_zero_byte(static_cast<uint32_t>(vo >> 32))) {
 #pragma unroll 1
       for (int j = 0; j < 8; ++j)
         if (byte_of(vo, j) == 0 && (old_g(j) != 0.f || old_v(j) != 0)) unsure_v |= 1u << j;
