@@ -329,3 +329,58 @@ def test_adamw_handle_with_autograd(B):
         got = p.detach().double().cpu().numpy().ravel()
         # moments: 8 e of terms of one size; the update: 14 e more; both at most 10 lr here; three steps
         assert np.abs(got - w).max() <= t * (30 * E * 1e-2 * 10 + E * np.abs(w).max())
+
+
+def test_adamw_random_first_moments_on_a_stream_and_in_a_graph(B):
+    """Three steps, eager on the current stream, on another, and replayed from a graph, end in the same state."""
+    sizes = [5000, 1, 300]
+    d = _state8(sizes, torch.bfloat16, 2, 0)
+    start = {k: [x.clone() for x in d[k]] for k in d}
+    plan = B.AdamWTensors(d["p"], d["g"], d["m"], d["v"], None, 0.1, d["ms"], d["vs"], random_avg=True)
+
+    def run():
+        for t in (4, 5, 6):
+            B.echo_adamw_step(plan, t, 1e-3, seed=9)
+
+    def reset():
+        for k in d:
+            for x, s in zip(d[k], start[k]):
+                x.copy_(s)
+
+    def state():
+        torch.cuda.synchronize()
+        return [x.clone() for k in d for x in d[k]]
+
+    run()
+    want = state()
+    reset()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        run()
+    assert all(torch.equal(a, b) for a, b in zip(want, state()))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run()
+    for _ in range(2):
+        reset()
+        graph.replay()
+        assert all(torch.equal(a, b) for a, b in zip(want, state()))
+
+
+def test_objective_with_undefined_scores_reaches_the_weights_as_nan(B):
+    """A token that the scoring call cannot score (an id outside the vocabulary) shows in every step after it, in its own
+    sequence alone."""
+    V, n, T = 500, 4, 8
+    gen = torch.Generator(device="cuda").manual_seed(6)
+    z = torch.randn((n * T, V), generator=gen, device="cuda")
+    y = torch.randint(0, V, (n * T,), generator=gen, device="cuda", dtype=torch.int32)
+    y[2 * T + 3] = V
+    lp, H, st, _, _ = B.echo_token_logprobs(z, y)
+    old = torch.where(torch.isnan(lp), torch.zeros_like(lp), lp).view(n, T)
+    value, g = B.echo_grpo_gradient(lp.view(n, T), old, old, None, torch.ones(n, device="cuda"), None, None, 0.2, 2.0, 0.0)
+    dz = B.echo_token_logprobs_backward(z, y, H, st, g.view(-1))
+    row = torch.zeros(n * T, dtype=torch.bool, device="cuda")
+    row[2 * T + 3] = True
+    assert torch.isnan(value).tolist() == [False, False, True, False]
+    assert torch.equal(torch.isnan(dz).all(dim=1), row) and torch.equal(torch.isnan(dz).any(dim=1), row)
