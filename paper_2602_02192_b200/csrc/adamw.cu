@@ -481,9 +481,10 @@ __device__ __forceinline__ void step_block(const Scalars &s, const Entry &e, int
         c = random_avg_code(y / M, random_of(avg_words4, j));
       } else {
         c = static_cast<int>(rintf(sqrt_ftz(static_cast<float>(fabs(x)) * inv_m)));
-        const double up = c + 0.5, down = c - 0.5;
-        if (y > up * up * M) ++c;
-        else if (c > 0 && y < down * down * M) --c;
+        const double up = (c + 0.5) * (c + 0.5) * M, down = (c - 0.5) * (c - 0.5) * M;
+        const bool odd = (c & 1) != 0;                          // (y on the border: the even code, as rint has it)
+        if (odd ? y >= up : y > up) ++c;
+        else if (c > 0 && (odd ? y <= down : y < down)) --c;
       }
       set_byte(mo, j, x < 0.0 ? -c : c);
     }

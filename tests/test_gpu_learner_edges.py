@@ -384,3 +384,24 @@ def test_objective_with_undefined_scores_reaches_the_weights_as_nan(B):
     row[2 * T + 3] = True
     assert torch.isnan(value).tolist() == [False, False, True, False]
     assert torch.equal(torch.isnan(dz).all(dim=1), row) and torch.equal(torch.isnan(dz).any(dim=1), row)
+
+
+@pytest.mark.parametrize("offset", [0, 1])
+def test_adamw_8_on_the_border_between_two_codes(B, offset):
+    """|m| a quarter of the block's largest is 127 / 2 on the codes' axis: the even one, 64, is taken (as by rint), for
+    blocks of every 8-bit mantissa (in fp32 one over some of them falls short), and beside neighbours one fp32 step away."""
+    n = 128 * 256
+    largest = np.repeat(1 + np.arange(128) / 128, 256).astype(np.float32)
+    g = largest.copy()
+    g[1::4] *= np.float32(-0.25)
+    g[2::4] = np.nextafter(g[2::4] / 4, np.float32(0))
+    g[3::4] = np.nextafter(g[3::4] / 4, np.float32(9))
+    store = torch.zeros(n + offset, device="cuda")[offset:]
+    store.copy_(torch.from_numpy(g))
+    tm, tv = torch.zeros(n, dtype=torch.int8, device="cuda"), torch.zeros(n, dtype=torch.uint8, device="cuda")
+    sm, sv, p = torch.zeros(128, device="cuda"), torch.zeros(128, device="cuda"), torch.zeros(n, device="cuda")
+    B.echo_adamw_step(B.AdamWTensors([p], [store], [tm], [tv], None, 0.0, [sm], [sv]), 1, 1e-3, beta1=0.0)
+    want, scale = L.quantise_avg(g.astype(np.float64))
+    assert np.array_equal(sm.cpu().numpy(), largest[::256]) and np.array_equal(scale, largest[::256])
+    assert np.array_equal(tm.cpu().numpy(), want)
+    assert want.reshape(-1, 4).min(axis=0).tolist() == [127, -64, 63, 64] == want.reshape(-1, 4).max(axis=0).tolist()
