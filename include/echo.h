@@ -276,7 +276,8 @@ int echo_group_advantage(const float *rewards, int32_t P, int32_t G, float eps,
  * w_t = min(exp(logp_old - logp_sampler), C) and the response mask m_t,
  *   out[i] = sum_t m_t w_t min(rho_t A_i, clip(rho_t, 1 - eps_clip, 1 + eps_clip) A_i) / sum_t m_t
  * (0 for an empty mask; without the KL term: echo_grpo_objective adds it).  NaN in a log-probability of a
- * token that the mask keeps, or in a difference of infinite ones, makes out[i] NaN, here and below.
+ * token that the mask keeps, or in a difference of infinite ones, makes out[i] NaN, here and below.  A ratio
+ * that overflows beside a weight that underflows is no NaN: w_t rho_t is then exp(logp_new - logp_sampler).
  * logp_* dev fp32 [n][T] are log-probabilities of the taken tokens (logp_sampler is what
  * echo_rollout recorded, the other two come from echo_rollout_forced under the respective
  * weights), adv dev fp32 [n] (echo_group_advantage), mask dev uint8 [n][T] or NULL (all ones),

@@ -11,7 +11,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libecho_b200.so")
 SOURCES = ["gemm.cu", "gemm_pair.cu", "elementwise.cu", "nucleus.cu", "attention.cu", "runtime.cu", "control.cu",
            "logprobs.cu", "adamw.cu"]
-HEADERS = ["common.cuh", "ptx.cuh", os.path.join("..", "..", "include", "echo.h")]
+HEADERS = ["common.cuh", "objective.cuh", "ptx.cuh", os.path.join("..", "..", "include", "echo.h")]
 
 
 def _nvcc() -> str:

@@ -3,6 +3,7 @@
 // group advantage, and the small bookkeeping kernels a decode step needs.
 
 #include "common.cuh"
+#include "objective.cuh"
 #include "ptx.cuh"
 
 namespace echo {
@@ -586,7 +587,7 @@ __global__ void wait_probe_kernel(uint64_t limit_ns, int *status, unsigned long 
 __global__ void grpo_surrogate_kernel(const float *__restrict__ ln, const float *__restrict__ lo,
                                       const float *__restrict__ ls, const float *__restrict__ lr,
                                       const float *__restrict__ adv, const uint8_t *__restrict__ mask, int n, int T,
-                                      float eps_clip, float C, float beta, float *__restrict__ out) {
+                                      const GrpoRule rule, float *__restrict__ out) {
   const int i = blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5), lane = threadIdx.x & 31;
   if (i >= n) return;
   const size_t base = static_cast<size_t>(i) * T;
@@ -594,16 +595,8 @@ __global__ void grpo_surrogate_kernel(const float *__restrict__ ln, const float 
   float num = 0.f, den = 0.f;
   for (int t = lane; t < T; t += 32) {
     if (mask && !mask[base + t]) continue;
-    float rho = expf(ln[base + t] - lo[base + t]);
-    if (a == 0.f && rho == INFINITY) rho = 1.0f;       // a zero advantage weighs nothing: no inf * 0
-    const float w = ptx::min_nan(expf(lo[base + t] - ls[base + t]), C);
-    const float clipped = ptx::min_nan(ptx::max_nan(rho, 1.0f - eps_clip), 1.0f + eps_clip);
-    float term = ptx::min_nan(rho * a, clipped * a);
-    if (lr) {
-      const float d = lr[base + t] - ln[base + t];
-      term -= beta * (expm1f(d) - d);
-    }
-    num += w * term;
+    const GrpoToken k = grpo_token(rule, a, ln[base + t], lo[base + t], ls[base + t], lr ? lr[base + t] : 0.f);
+    num += k.w * k.term;
     den += 1.0f;
   }
 #pragma unroll
@@ -893,7 +886,8 @@ cudaError_t grpo_surrogate_launch(const float *ln, const float *lo, const float 
                                   const float *adv, const uint8_t *mask, int n, int T, float eps_clip, float C,
                                   float beta, float *out, cudaStream_t s) {
   if (n == 0) return cudaSuccess;
-  grpo_surrogate_kernel<<<(n + 7) / 8, 256, 0, s>>>(ln, lo, ls, lr, adv, mask, n, T, eps_clip, C, beta, out);
+  const GrpoRule rule{eps_clip, C, lr ? beta : 0.f, 0.0, 0.0};       // (the borders of the slope are not used)
+  grpo_surrogate_kernel<<<(n + 7) / 8, 256, 0, s>>>(ln, lo, ls, lr, adv, mask, n, T, rule, out);
   return cudaGetLastError();
 }
 cudaError_t score_rows_launch(int r0, int R, int T, const int32_t *seq_len0, int32_t *row_pt, int32_t *row_pos,

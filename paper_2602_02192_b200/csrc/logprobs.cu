@@ -14,6 +14,7 @@
 #include <type_traits>
 
 #include "common.cuh"
+#include "objective.cuh"
 #include "ptx.cuh"
 
 namespace echo {
@@ -888,8 +889,7 @@ struct GrpoGradArgs {
   const uint8_t *mask;
   const float *grad_out;
   int n, T;
-  float eps_clip, C, beta;
-  double log_hi, log_lo;       // log(1 + eps), log(1 - eps) (-inf if eps >= 1)
+  GrpoRule rule;
   float *out, *grad;
 };
 // sum over the NT threads that share a sequence (a warp, or the whole block)
@@ -904,28 +904,6 @@ template <int NT> __device__ __forceinline__ float team_sum(float v, float *scra
 #pragma unroll
   for (int w = 0; w < NT / 32; ++w) v += scratch[w];
   return v;
-}
-struct GrpoToken {
-  float term, slope;           // both times the truncated weight
-};
-// The clipped term's slope is rho A where the minimum is the unclipped side (A > 0: rho <= 1 + eps; A < 0:
-// rho >= 1 - eps), else 0; which side it is goes by the exact difference ln - lo, since the slope jumps there.
-// NaN in any of the log-probabilities, or in a difference of infinite ones, makes the token's value and slope NaN.
-__device__ __forceinline__ GrpoToken grpo_token(const GrpoGradArgs &a, float A, float ln, float lo, float ls, float lr) {
-  float rho = expf(ln - lo);
-  if (A == 0.f && rho == INFINITY) rho = 1.0f;         // a zero advantage weighs nothing: no inf * 0
-  const float w = ptx::min_nan(expf(lo - ls), a.C);
-  const float clipped = ptx::min_nan(ptx::max_nan(rho, 1.0f - a.eps_clip), 1.0f + a.eps_clip);
-  const double x = static_cast<double>(ln) - static_cast<double>(lo);
-  const bool flat = A > 0.f ? x > a.log_hi : x < a.log_lo;
-  float term = ptx::min_nan(rho * A, clipped * A);
-  float slope = flat ? 0.f : rho * A;
-  if (a.lr) {
-    const float d = lr - ln, k = expm1f(d);
-    term -= a.beta * (k - d);
-    slope = fmaf(a.beta, k, slope);
-  }
-  return {w * term, w * slope};
 }
 // NT threads per sequence: a warp (several sequences a block) or a block.  VEC: rows are read as float4 / uchar4.
 // Latency: the mask is counted before the first gradient can be written (256 x 2048 tokens: 4.2 us, 16 x 32: 2.0 us).
@@ -966,9 +944,9 @@ grpo_gradient_kernel(const __grid_constant__ GrpoGradArgs a) {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
           if ((m >> (8 * e)) & 0xffu) {
-            const GrpoToken k = grpo_token(a, A, pn[e], po[e], ps[e], pr[e]);
-            value += k.term;
-            pg[e] = k.slope * scale;
+            const GrpoToken k = grpo_token(a.rule, A, pn[e], po[e], ps[e], pr[e]);
+            value += k.w * k.term;
+            pg[e] = k.w * k.slope * scale;
           }
       }
       reinterpret_cast<float4 *>(a.grad)[q] = o;
@@ -978,9 +956,9 @@ grpo_gradient_kernel(const __grid_constant__ GrpoGradArgs a) {
       float o = 0.f;
       if (!a.mask || a.mask[base + t]) {
         const float ln = a.ln[base + t];
-        const GrpoToken k = grpo_token(a, A, ln, a.lo[base + t], a.ls[base + t], a.lr ? a.lr[base + t] : ln);
-        value += k.term;
-        o = k.slope * scale;
+        const GrpoToken k = grpo_token(a.rule, A, ln, a.lo[base + t], a.ls[base + t], a.lr ? a.lr[base + t] : ln);
+        value += k.w * k.term;
+        o = k.w * k.slope * scale;
       }
       a.grad[base + t] = o;
     }
@@ -1132,11 +1110,8 @@ int echo_grpo_gradient(const float *logp_new, const float *logp_old, const float
   a.grad_out = grad_out;
   a.n = n;
   a.T = T;
-  a.eps_clip = eps_clip;
-  a.C = C;
-  a.beta = beta;
-  a.log_hi = std::log1p(static_cast<double>(eps_clip));
-  a.log_lo = eps_clip < 1.f ? std::log1p(-static_cast<double>(eps_clip)) : -INFINITY;
+  a.rule = {eps_clip, C, a.lr ? beta : 0.f, std::log1p(static_cast<double>(eps_clip)),
+            eps_clip < 1.f ? std::log1p(-static_cast<double>(eps_clip)) : -INFINITY};
   a.out = out;
   a.grad = out_grad;
   const bool vec = T % 4 == 0 && aligned(logp_new, 16) && aligned(logp_old, 16) && aligned(logp_sampler, 16) &&

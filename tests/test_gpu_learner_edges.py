@@ -405,3 +405,49 @@ def test_adamw_8_on_the_border_between_two_codes(B, offset):
     assert np.array_equal(sm.cpu().numpy(), largest[::256]) and np.array_equal(scale, largest[::256])
     assert np.array_equal(tm.cpu().numpy(), want)
     assert want.reshape(-1, 4).min(axis=0).tolist() == [127, -64, 63, 64] == want.reshape(-1, 4).max(axis=0).tolist()
+
+
+@pytest.mark.parametrize("T", [1, 4, 300])
+@pytest.mark.parametrize("adv", [-1.0, 0.7, 0.0])
+def test_ratios_that_overflow_beside_weights_that_underflow(B, T, adv):
+    """An old policy that all but rules a token out: rho = exp(ln - lo) overflows, w = exp(lo - ls) underflows, and w rho is
+    exp(ln - ls).  The same for the estimate's exp(lr - ln) beside w.  Against the formula with its products formed from
+    sums of exponents, in 64 bits; the kernel's exponents are off by 2 e of each difference where it multiplies."""
+    cases = [(-1.0, -120.0, -2.0, -1.5), (-1.0, -90.0, -2.0, -1.5), (-0.5, -81.0, -1.0, -0.7), (-0.5, -79.0, -1.0, -0.7),
+             (-0.1, -1e4, -3.0, -0.2), (-120.0, -120.5, -2.0, -1.0), (-100.0, -190.0, -3.0, -2.0), (-1.0, -1.1, -1.2, -0.9),
+             (-1.0, -120.0, -121.0, -1.1), (-95.0, -1.0, -1.0, -94.0)]
+    x = np.array([[c] * T for c in cases], dtype=np.float32).astype(np.float64)          # [cases][T][4]
+    ln, lo, ls, lr = (x[..., i] for i in range(4))
+    eps, C, beta = float(np.float32(0.2)), 2.0, float(np.float32(0.04))
+    lw = np.minimum(lo - ls, math.log(C))
+    a, w = np.full(ln.shape, adv), np.exp(lw)
+    with np.errstate(over="ignore", invalid="ignore"):
+        w_rho, clip = np.exp(ln - lo + lw), np.clip(np.exp(ln - lo), 1 - eps, 1 + eps)
+        policy = np.where(a == 0, 0.0, np.minimum(w_rho * a, w * clip * a))
+        flat = np.where(a > 0, ln - lo > math.log1p(eps), ln - lo < math.log1p(-eps))
+        slope = np.where(flat | (a == 0), 0.0, w_rho * a)
+        w_k = np.exp(lr - ln + lw) - w
+    for kl in (False, True):
+        term = policy - (beta * (w_k - w * (lr - ln)) if kl else 0.0)
+        d = slope + (beta * w_k if kl else 0.0)
+        size = np.abs(policy) + np.abs(slope) + (beta * (np.abs(w_k) + w * (np.abs(lr - ln) + 1)) if kl else 0.0)
+        exponents = np.minimum(np.abs(ln - lo), 80) + np.minimum(np.abs(lo - ls), 100) + np.minimum(np.abs(lr - ln), 80)
+        tol = E * (24 + 2 * exponents) * size + 1e-37
+        over = (np.abs(term) > 3.4e38) | (np.abs(d) > 3.4e38)                              # what fp32 cannot hold
+        value, grad, forward = _objective(B, ln, lo, ls, lr if kl else None, np.full(len(cases), adv))
+        assert not np.isnan(grad).any() and not np.isnan(value).any() and not np.isnan(forward).any()
+        assert np.all((np.abs(grad * T - d) <= tol + 2 * E * np.abs(d))[~over])
+        rows = ~over.any(axis=1)
+        mean, mean_tol = term.mean(axis=1), tol.mean(axis=1) + E * (T / 32 + 20) * size.mean(axis=1)
+        assert np.all((np.abs(value - mean) <= mean_tol)[rows]) and np.all((np.abs(forward - mean) <= mean_tol)[rows])
+        assert rows.sum() >= 8
+
+
+@pytest.mark.parametrize("adv", [0.7, 0.0])
+def test_tokens_that_the_old_policy_rules_out(B, adv):
+    """logp_old = -inf: the weight is 0, and so are the clipped term (0.7: at the border) and the KL term, however large."""
+    one = np.ones((1, 1))
+    for ln, lr in ((-90.0, -0.5), (-120.0, -0.5), (-1.0, -2.0)):
+        for ref in (None, lr * one):
+            value, grad, forward = _objective(B, ln * one, -math.inf * one, -one, ref, np.array([adv]))
+            assert value[0] == 0 and grad[0, 0] == 0 and forward[0] == 0
