@@ -324,7 +324,9 @@ int echo_grpo_objective(const float *logp_new, const float *logp_old, const floa
  *   top_k         0 .. 32 (more: ECHO_ERR_UNSUPPORTED)
  *   out_*         dev fp32 [R], [R], [R][2] (8-byte aligned), int32 / fp32 [R][top_k]; each may be NULL
  *                 (tokens and out_logprobs together; the top outputs only with top_k = 0)
- * An id at -inf is masked: probability 0, never among the alternatives.  Places of a row that has fewer
+ * An id at -inf is masked: probability 0, never among the alternatives.  (Ids at a finite value are ordinary
+ * ones: where most of a row shares one, such as the type's lowest, with fewer than top_k ids above it, the
+ * alternatives take tens of times longer than with -inf there.)  Places of a row that has fewer
  * than top_k ids left hold id -1 and -inf.  A row with nothing left (all -inf) scores -inf (0 without a
  * token), entropy 0, stats (-inf, -inf).  A NaN or +inf logit makes its row's log-probability, entropy
  * and log l NaN; NaN is never an alternative.  V <= 2^24.  R = 0 does nothing. */

@@ -19,10 +19,15 @@
 // across a border between two codes the element is decided again in 64 bits.  A scale is
 // the fp32 rounding of the 64-bit maximum.
 //
+// The weight's update is formed in fp32 from the moments before they are rounded, with approximate roots and reciprocals
+// (2^-23 each): some fifteen roundings of an update that is itself a small part of the weight, which is rounded once.
+//
 // A warp takes a block of 256 elements, eight consecutive ones a lane, moved with 32-byte accesses.  fp32 moments: bound
-// by HBM (193 M elements with bf16 gradients and copies: 896 us, 6.0 TB/s).  8-bit moments: 757 us for the same step
-// against 471 of traffic at the copy rate; bound by instruction issue (69 % of the slots), about 98 instructions an
-// element.  Unpacking them: 321 us, 6.0 TB/s.  Bytes and whole numbers become floats, and back, through a float's low
+// by HBM (193 M elements with bf16 gradients and copies: 893 to 902 us, 6.0 TB/s).  8-bit moments, the same step against
+// 471 us of traffic at the copy rate: 776 us with nearest codes, about 100 instructions an element, and 934 us with
+// random first moments, 120 (a second Philox and the squares' rule); instructions issue in 69 % of the slots.  Unpacking
+// them: 322 us, 6.0 TB/s.  Tensors off the 8-element boundaries go element by element: 40 M elements with fp32 moments in
+// 287 us instead of 176, with 8-bit random ones in 255 instead of 196.  Bytes and whole numbers become floats, and back, through a float's low
 // bits, not the conversion unit.  Fetching the next 8-bit block into L2 ahead of time: 1134 against 1086 us for step and
 // unpack, so it is not done.
 #include <cmath>

@@ -210,8 +210,10 @@ struct LogprobArgs {
 
 // Exact selection of the k first entries of elements [begin, end) of a row, whatever their distribution: radix
 // selection of the k-th largest value, then everything above it and the lowest ids that equal it.  Reached when more
-// candidates than the buffer holds tie with, or sit above, the bound of the one-pass filter (constant rows, sorted
-// rows); it reads the elements six times out of L2.
+// candidates than the buffer holds tie with, or sit above, the bound of the one-pass filter (constant rows, sorted rows,
+// rows whose masked ids share a finite value with fewer than k ids above it).  It reads the elements five times out of
+// L2 (four digits, then the entries), one element a thread and turn, and is slow: eight ids above the type's lowest
+// value and 20 alternatives, 256 x 151936 bf16 in 1094 us and 2048 rows in 6580, against 31 and 123 with -inf instead.
 template <int FMT, int NT>
 __device__ __noinline__ void select_exact(const void *row, int begin, int end, int k, TopShared &sh) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -462,8 +464,8 @@ __device__ __noinline__ void find_alternatives(const void *row, const uint4 *vec
 
 // One cluster of `split` CTAs per row (split = 1: one CTA), each with a contiguous share of the row, one pass.
 // Bound by HBM and, for 16-bit logits, almost as much by the exponentials (16 a cycle and SM): 2048 x 151936 bf16 in
-// 100 us, 6.2 TB/s, exponential unit 71 % busy (1024 such rows); 113 us under sustained load, where power holds the SM
-// clock at 1.62 GHz.
+// 112 to 115 us under sustained load, 5.4 to 5.6 TB/s, where power holds the SM clock at 1.62 GHz; 100 us, 6.2 TB/s, in
+// short bursts (exponential unit 71 % busy at 1024 such rows).
 // A thread keeps (m, l, t) of its own elements and moves the reference only when a step of its vectors exceeds it.
 // Alternatives cost no second pass: the threads also keep the maxima of 1024 parts of the CTA's elements ("pieces");
 // from these comes a lower bound of the k-th largest logit, and only the pieces that reach it, little more than k,
@@ -707,7 +709,8 @@ cudaError_t logprobs_launch(LogprobArgs a, int format, cudaStream_t s) {
   // Few rows are cut over the CTAs of a cluster until the launch has two CTAs per SM.  With alternatives, which cost more
   // to join, one and a half will do unless the parts stay long: 200 rows of 151936 fp32 values with 5 alternatives take
   // 23.9 us in two parts and 28.3 in one, 256 rows 30.2 and 32.0, but bf16 24.2 and 21.4; 64 rows fp32 12.3 us in four and
-  // 14.0 in eight.
+  // 14.0 in eight.  (Parts of 9496 vectors stay whole and parts of 18992 are cut there; the border of 16384 lies between
+  // and was not measured at other vocabularies.)
   int split = 1;
   auto more = [&] {
     const int64_t ctas = a.R * static_cast<int64_t>(split), part = row_vecs / (2 * split);
@@ -781,7 +784,8 @@ constexpr int kBackThreads = 256, kBackUnroll = 2;
 
 // One CTA per slice of a row.  The first vectors are requested before the row's scalars, whose latency would otherwise
 // stand in front of every slice, and from then on a step's loads run under the step before it.  Bound by HBM, as many
-// bytes written as read: 2048 x 151936 bf16 in 198 us (205 under sustained load), 6.1 TB/s.  Two vectors a step and six
+// bytes written as read: 2048 x 151936 bf16 in 198 us, 6.3 TB/s (205 under sustained load, 6.1 TB/s).  Logits on another
+// 16-byte boundary than the output cost a second load a vector: 1024 x 151936 bf16 in 123 us, not 107.  Two vectors a step and six
 // CTAs an SM against four and four: 219 against 226 us; ordinary stores against evict-first ones: 213 against 219; eight
 // rounds of CTAs against four: 207 against 211; ordinary loads against L1::no_allocate: 198 against 205.
 template <int FMT, bool ENT>
@@ -906,7 +910,7 @@ template <int NT> __device__ __forceinline__ float team_sum(float v, float *scra
   return v;
 }
 // NT threads per sequence: a warp (several sequences a block) or a block.  VEC: rows are read as float4 / uchar4.
-// Latency: the mask is counted before the first gradient can be written (256 x 2048 tokens: 4.2 us, 16 x 32: 2.0 us).
+// Latency: the mask is counted before the first gradient can be written (256 x 2048 tokens: 4.4 us, 16 x 32: 2.1 us).
 template <int NT, bool VEC>
 __global__ void __launch_bounds__(NT == 32 ? 128 : NT)
 grpo_gradient_kernel(const __grid_constant__ GrpoGradArgs a) {
