@@ -423,6 +423,64 @@ int echo_adamw_step(const echo_adamw_tensor *tensors, int32_t n_tensors, const e
 int echo_adamw_unpack(const echo_adamw_tensor *tensors, int32_t n_tensors, float *const *out_avg,
                       float *const *out_avg_sq, void *cuda_stream);
 
+/* ---- a caller's own paged cache -------------------------------------------------------------
+ * For callers that drive a model layer by layer: a reply that goes on after a tool's answer (Appendix F's turns), a
+ * prompt taken in pieces, a draft that is checked, one token for each of many sequences.  A batch is ragged: every
+ * sequence brings a chunk of new tokens (none, one or many), whose rows lie one behind the other.  Cache layout as in
+ * echo_decode_attention: a layer's pool is [n_pages][Hkv][2][16][hd], per page and kv head 16 K rows, then 16 V rows.
+ * These calls need no context.  They are asynchronous on the stream, run on the current device, allocate nothing, keep
+ * nothing between calls, and can be captured into a CUDA graph (a replay reads the tables anew).  Equal inputs give
+ * equal outputs. */
+typedef struct echo_kv_chunks {
+  const int32_t *row_starts;  /* dev int32 [n_seqs + 1]: rows row_starts[s] .. row_starts[s + 1] - 1 are sequence s's
+                                 new tokens; ascending, from 0 on or later, at most n_rows                    */
+  const int32_t *kv_lens;     /* dev int32 [n_seqs]: keys of the sequence once its chunk has been appended; row i of
+                                 a chunk of n rows has position kv_lens[s] - n + i                            */
+  const int32_t *page_table;  /* dev int32 [n_seqs][pt_width]: page of each 16 positions; entries behind the
+                                 sequence's last page are not read                                            */
+  int32_t *status;            /* dev int32, zeroed by the caller: the largest code that a kernel found (0: none;
+                                 1 a page id outside the pool, 3 a bounded wait ran out, 4 lengths outside the
+                                 limits: the batch's, or more than 16 pt_width keys)                          */
+  int32_t n_seqs;             /* 0: nothing is done                                                           */
+  int32_t n_rows;             /* rows of the arrays; those of no sequence are left as they are                */
+  int32_t pt_width;           /* at most 2^26                                                                 */
+  int32_t max_chunk;          /* no chunk is longer (sizes workspaces, chooses tiles)                         */
+} echo_kv_chunks;
+
+/* Appends the chunks' keys and values, with the position rotation on the way (rotate-half pairs (j, j + hd/2), angle
+ * position * theta^(-2j/hd)), and rotates the queries:
+ *   q, k, v     dev rows of [Hq][hd], [Hkv][hd], [Hkv][hd] in in_format (0 bf16, 1 IEEE half, 2 fp32), *_stride elements
+ *               from row to row (cuts of one projection's output, for instance), of any alignment of the type (16-byte
+ *               boundaries are fastest); strides up to 2^30.  q and out_q may both be NULL.
+ *   kv_pool     dev, in kv_format (0 bf16, 1 half), 16-byte aligned: rotated keys and plain values, rounded once
+ *   out_q       dev [n_rows][Hq][hd] in kv_format, 16-byte aligned.  It may be q itself (same format, contiguous rows);
+ *               otherwise nothing that is written may overlap anything else (ECHO_ERR_INVALID).
+ * hd 64 or 128.  A chunk that is longer than its cache, or has other lengths outside the limits, is passed over (status
+ * 4); a row whose page id is outside the pool is not appended (status 1), its query is rotated all the same.  Two rows
+ * that the tables send to one place of the pool leave one of the two there, either one. */
+int echo_append_kv(const void *q, const void *k, const void *v, int32_t in_format, int64_t q_stride, int64_t k_stride,
+                   int64_t v_stride, const echo_kv_chunks *chunks, int32_t Hq, int32_t Hkv, int32_t hd, float rope_theta,
+                   void *kv_pool, int32_t n_pages, int32_t kv_format, void *out_q, void *cuda_stream);
+
+/* Attention of the chunks' rows over the caches: with t the row's position, per query head and its kv head
+ *   out = sum_{u <= t} exp(q . k_u / sqrt(hd)) v_u / sum_{u <= t} exp(q . k_u / sqrt(hd))
+ * (the row's own key is among them: append first).  A row with t < 0 (a chunk longer than its cache) sees nothing: 0.
+ * Keys and values behind a row's position have no part in it, whatever they hold.  Fp32 softmax and accumulation;
+ * probabilities enter the products in the cache's format.
+ *   q           dev rows of [Hq][hd] in `format` (0 bf16, 1 half; the cache's), q_stride elements from row to row (a
+ *               multiple of 8, up to 2^30), 16-byte aligned; rotated (echo_append_kv)
+ *   kv_pool     dev, 16-byte aligned
+ *   out         dev [n_rows][Hq][hd] in `format`, 16-byte aligned; may not overlap q, the pool or the workspace
+ *   workspace   dev, echo_chunk_attention_workspace_bytes(...) bytes, 16-byte aligned: partial results of long caches.
+ *               Only this call's kernels use it: calls that may overlap on the GPU need one each.
+ * hd 64 or 128, at most 128 query heads to a kv head, n_pages Hkv at most 2^26 (else ECHO_ERR_UNSUPPORTED).  Sequences
+ * with lengths outside the limits are passed over (status 4); rows that need a page whose id is outside the pool become
+ * NaN (status 1). */
+size_t echo_chunk_attention_workspace_bytes(int32_t max_chunk, int32_t Hq, int32_t Hkv, int32_t hd);
+int echo_chunk_attention(const void *q, int64_t q_stride, const void *kv_pool, int32_t n_pages, int32_t format,
+                         const echo_kv_chunks *chunks, int32_t Hq, int32_t Hkv, int32_t hd, void *workspace,
+                         size_t workspace_bytes, void *out, void *cuda_stream);
+
 /* Offset of this context's sequence ids in the noise streams: sequence (p, g) of later rollouts draws
  * from the Philox stream of id base + p*G + g.  Rollout workers are independent and share nothing but
  * the snapshot and the buffer (Section 4.1), so a set of prompts can be cut by prompt over several

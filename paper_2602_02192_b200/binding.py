@@ -75,6 +75,13 @@ class EchoAdamWOptions(C.Structure):
     ]
 
 
+class EchoKVChunks(C.Structure):
+    _fields_ = [
+        ("row_starts", C.c_void_p), ("kv_lens", C.c_void_p), ("page_table", C.c_void_p), ("status", C.c_void_p),
+        ("n_seqs", C.c_int32), ("n_rows", C.c_int32), ("pt_width", C.c_int32), ("max_chunk", C.c_int32),
+    ]
+
+
 def _load() -> C.CDLL:
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"{LIB_PATH} is missing: build it with `python -m paper_2602_02192_b200.build` "
@@ -125,8 +132,13 @@ def _load() -> C.CDLL:
     lib.echo_grpo_gradient.argtypes = [vp, vp, vp, vp, vp, vp, vp, i32, i32, f32, f32, f32, vp, vp, vp]
     lib.echo_adamw_step.argtypes = [C.POINTER(EchoAdamWTensor), i32, C.POINTER(EchoAdamWOptions), vp]
     lib.echo_adamw_unpack.argtypes = [C.POINTER(EchoAdamWTensor), i32, C.POINTER(vp), C.POINTER(vp), vp]
+    chunks = C.POINTER(EchoKVChunks)
+    lib.echo_append_kv.argtypes = [vp, vp, vp, i32, i64, i64, i64, chunks, i32, i32, i32, f32, vp, i32, i32, vp, vp]
+    lib.echo_chunk_attention_workspace_bytes.restype = C.c_size_t
+    lib.echo_chunk_attention_workspace_bytes.argtypes = [i32, i32, i32, i32]
+    lib.echo_chunk_attention.argtypes = [vp, i64, vp, i32, i32, chunks, i32, i32, i32, vp, C.c_size_t, vp, vp]
     for name in ("echo_score_detail", "echo_token_logprobs", "echo_token_logprobs_backward", "echo_grpo_gradient",
-                 "echo_adamw_step", "echo_adamw_unpack"):
+                 "echo_adamw_step", "echo_adamw_unpack", "echo_append_kv", "echo_chunk_attention"):
         getattr(lib, name).restype = C.c_int
     dbl = C.c_double
     lib.echo_mu_min.argtypes = [dbl, dbl, dbl, dbl, C.POINTER(dbl)]
@@ -179,7 +191,8 @@ EXPORTED = ["echo_arena_bytes", "echo_create", "echo_destroy", "echo_load_policy
             "echo_set_sequence_base", "echo_debug_capture", "echo_debug_wait_limit",
             "echo_gemm_bf16_noalloc_status", "echo_probe_read_bandwidth", "echo_peer_score", "echo_chain_assemble",
             "echo_chain_arrival_time", "echo_score", "echo_turn_mask", "echo_score_detail", "echo_token_logprobs",
-            "echo_token_logprobs_backward", "echo_grpo_gradient", "echo_adamw_step", "echo_adamw_unpack"]
+            "echo_token_logprobs_backward", "echo_grpo_gradient", "echo_adamw_step", "echo_adamw_unpack", "echo_append_kv",
+            "echo_chunk_attention_workspace_bytes", "echo_chunk_attention"]
 
 
 def _stream_ptr(stream: Optional[torch.cuda.Stream]) -> int:
@@ -702,6 +715,105 @@ def echo_adamw_unpack(tensors: AdamWTensors, out_avg: Sequence[torch.Tensor], ou
             assert x.dtype is torch.float32 and x.numel() == size and x.is_contiguous() and x.get_device() == index
         addresses.append((C.c_void_p * max(tensors.count, 1))(*[x.data_ptr() for x in outs]))
     _call(tensors.device, lib.echo_adamw_unpack, tensors.table, tensors.count, addresses[0], addresses[1])
+
+
+# -- a caller's own paged cache -----------------------------------------------------
+class KVChunks:
+    """A ragged batch of new tokens over paged caches, named once for all layers of a step.
+
+    row_starts int32 [n_seqs + 1], kv_lens int32 [n_seqs] (keys once the new tokens are appended), page_table int32
+    [n_seqs][width]: contiguous tensors of one GPU, read by the kernels when they run, so that a captured step follows
+    what is written into them.  n_rows: rows of q, k, v and the outputs (those behind the last sequence are left as they
+    are); max_chunk: no sequence brings more new tokens.  status: int32 tensor of one element that receives what the
+    kernels find (its own, zeroed, by default): see check()."""
+
+    def __init__(self, row_starts: torch.Tensor, kv_lens: torch.Tensor, page_table: torch.Tensor, n_rows: int, max_chunk: int,
+                 status: Optional[torch.Tensor] = None):
+        n = kv_lens.shape[0]
+        if status is None:
+            status = torch.zeros(1, dtype=torch.int32, device=kv_lens.device)
+        assert row_starts.shape == (n + 1,) and kv_lens.shape == (n,) and status.numel() == 1
+        assert page_table.dim() == 2 and page_table.shape[0] == n
+        for x in (row_starts, kv_lens, page_table, status):
+            assert x.is_cuda and x.device == kv_lens.device and x.dtype is torch.int32 and x.is_contiguous()
+        self.device, self.n_rows, self.max_chunk, self.status = kv_lens.device, int(n_rows), int(max_chunk), status
+        self._keep = (row_starts, kv_lens, page_table)
+        self.table = EchoKVChunks(row_starts.data_ptr(), kv_lens.data_ptr(), page_table.data_ptr(), status.data_ptr(), n,
+                                  self.n_rows, page_table.shape[1], self.max_chunk)
+        self._ref = C.byref(self.table)
+
+    def check(self):
+        """Waits for the GPU; raises where a kernel found page ids or lengths out of range (EchoError -7) or gave up
+        waiting (-8) since the status was last zero, and zeroes it."""
+        found = int(self.status.item())
+        if found:
+            self.status.zero_()
+            raise EchoError(-8 if found == 3 else -7, {1: "a page id outside the pool", 4: "lengths outside the limits"}.get(found, ""))
+
+
+def _check_heads(x: torch.Tensor, chunks: KVChunks, hd: int):
+    """Rows of heads [n_rows][H][hd], one head behind the other: (H, elements from row to row)."""
+    rows, H, size = x.shape
+    assert x.get_device() == chunks.device.index and rows == chunks.n_rows and size == hd
+    stride, head, side = x.stride()
+    assert (side == 1 or hd <= 1) and (head == hd or H <= 1), "a row's heads lie one behind the other"
+    return H, stride if rows > 1 else H * hd
+
+
+def _check_pool(kv_pool: torch.Tensor, chunks: KVChunks):
+    n_pages, Hkv, two, page, hd = kv_pool.shape
+    assert two == 2 and page == 16 and kv_pool.is_contiguous() and kv_pool.get_device() == chunks.device.index
+    assert kv_pool.dtype is torch.bfloat16 or kv_pool.dtype is torch.float16
+    return n_pages, Hkv, hd, 1 if kv_pool.dtype is torch.float16 else 0
+
+
+def _check_out(out: Optional[torch.Tensor], shape, dtype, chunks: KVChunks) -> torch.Tensor:
+    if out is None:
+        return torch.empty(shape, dtype=dtype, device=chunks.device)
+    assert out.shape == shape and out.dtype is dtype and out.is_contiguous() and out.get_device() == chunks.device.index
+    return out
+
+
+def echo_append_kv(chunks: KVChunks, q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, kv_pool: torch.Tensor,
+                   rope_theta: float = 1e4, out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+    """Appends k, v [n_rows][Hkv][hd] to kv_pool [n_pages][Hkv][2][16][hd] (bf16 or float16) at the chunks' positions, keys
+    rotated, and returns q [n_rows][Hq][hd] rotated, in the pool's dtype (None without q).  q, k, v: one dtype (bf16,
+    float16, fp32), rows may be strided (cuts of one projection's output).  out: where the queries go (q itself is
+    allowed); without it the rows of no sequence come back undefined."""
+    n_pages, Hkv, hd, kv_format = _check_pool(kv_pool, chunks)
+    k_heads, k_stride = _check_heads(k, chunks, hd)
+    v_heads, v_stride = _check_heads(v, chunks, hd)
+    assert k_heads == Hkv and v_heads == Hkv and v.dtype is k.dtype
+    Hq, q_stride = 0, 0
+    if q is not None:
+        Hq, q_stride = _check_heads(q, chunks, hd)
+        assert q.dtype is k.dtype
+        out = _check_out(out, q.shape, kv_pool.dtype, chunks)
+    else:
+        assert out is None
+    _call(chunks.device, lib.echo_append_kv, q.data_ptr() if q is not None else None, k.data_ptr(), v.data_ptr(),
+          _FORMATS[k.dtype], q_stride, k_stride, v_stride, chunks._ref, Hq, Hkv, hd, rope_theta, kv_pool.data_ptr(), n_pages,
+          kv_format, out.data_ptr() if out is not None else None)
+    return out
+
+
+def echo_chunk_attention(chunks: KVChunks, q: torch.Tensor, kv_pool: torch.Tensor, out: Optional[torch.Tensor] = None,
+                         workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Attention of the chunks' rows q [n_rows][Hq][hd] (rotated, the pool's dtype, rows may be strided by a multiple of 8)
+    over kv_pool [n_pages][Hkv][2][16][hd], causal by position.  out: where to; without it the rows of no sequence come
+    back undefined.  workspace: a uint8 tensor to use instead of one allocated here (calls that may run at the same time
+    need one each)."""
+    n_pages, Hkv, hd, kv_format = _check_pool(kv_pool, chunks)
+    Hq, q_stride = _check_heads(q, chunks, hd)
+    assert q.dtype is kv_pool.dtype
+    out = _check_out(out, q.shape, kv_pool.dtype, chunks)
+    need = lib.echo_chunk_attention_workspace_bytes(chunks.max_chunk, Hq, Hkv, hd)
+    if workspace is None:
+        workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=chunks.device)
+    assert workspace.get_device() == chunks.device.index and workspace.is_contiguous()
+    _call(chunks.device, lib.echo_chunk_attention, q.data_ptr(), q_stride, kv_pool.data_ptr(), n_pages, kv_format, chunks._ref,
+          Hq, Hkv, hd, workspace.data_ptr(), workspace.numel() * workspace.element_size(), out.data_ptr())
+    return out
 
 
 def echo_probe_read_bandwidth(n_bytes: int = 4 << 30, repeats: int = 10, device="cuda") -> float:

@@ -10,8 +10,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libecho_b200.so")
 SOURCES = ["gemm.cu", "gemm_pair.cu", "elementwise.cu", "nucleus.cu", "attention.cu", "runtime.cu", "control.cu",
-           "logprobs.cu", "adamw.cu"]
-HEADERS = ["common.cuh", "objective.cuh", "ptx.cuh", os.path.join("..", "..", "include", "echo.h")]
+           "logprobs.cu", "adamw.cu", "append.cu", "chunk_attention.cu"]
+HEADERS = ["chunks.cuh", "common.cuh", "objective.cuh", "ptx.cuh", os.path.join("..", "..", "include", "echo.h")]
 
 
 def _nvcc() -> str:
