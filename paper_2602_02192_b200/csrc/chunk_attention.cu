@@ -1,72 +1,955 @@
 // Attention of a ragged batch of new tokens over a caller's paged caches.
 //
-// One warp per (row, query head): lanes share the head's elements, keys go by one at a time with a running maximum and
-// sum.  Right for every shape; nothing in it is fast.
+//   o_i = sum_{u <= t_i} exp(q_i . k_u / sqrt(hd)) v_u / sum_{u <= t_i} exp(q_i . k_u / sqrt(hd)),   t_i = L - n + i
+//
+// Tiles.  The query heads of a kv head read the same keys, so a row of a tile is a (token, query head) pair: 128 rows are
+// 128 / (Hq / Hkv) tokens.  Keys come in tiles of 128 (eight pages).  S = Q K^T (128 x 128) and O += P V (128 x hd) run on
+// the tcgen05 tensor cores: Q, K, V in shared memory as TMA leaves them (128-byte swizzle; K is the K-major operand, V the
+// same bytes read as an MN-major one), S, P and O in tensor memory, P over the columns that held S.  A thread owns a row:
+// it finds the row's maximum and sum without a shuffle.
+//
+// Two streams of tiles are in flight in a CTA, each with its own warpgroup, S and O, so that the tensor cores work on one
+// while the other's probabilities are formed:
+//   paired items   two row tiles share each K and V tile (long chunks: keys are read once per 256 rows)
+//   single items   one row tile; its key tiles alternate between the streams, whose two partial results are joined at
+//                  the end (few rows: what counts is to keep the copies running)
+//
+// Work.  An item is (sequence, kv head, pair of row tiles or last single one) with its keys.  Items have very different
+// lengths and the lengths are in device memory, so every CTA (one to an SM) adds up all items' costs, takes its equal share
+// of the total, and walks the items in it; an item that crosses a border is cut between two key tiles.  Cut items leave
+// fp32 partial results (unnormalised O, maximum, sum) in the workspace, in places that only depend on the CTA, and a second
+// launch joins them in key order: no atomics, equal inputs give equal outputs.
+//
+// A row's reference (the maximum that its exponents are relative to) moves only when the maximum has grown by more than
+// 2^8, so that O is hardly ever rescaled; probabilities then reach 256, which both formats hold.
+//
+// What a row does not see has no part in it: masked scores are replaced, not added to.  A masked probability is 0, but
+// 0 times an undefined value would not be: where a tile has keys that only some of its rows see, their values are looked
+// at, and a tile with an infinity or a NaN among them is accumulated by the threads instead (slow, and nothing else).
+//
+// Roles: warps 0-3 and 4-7 the two streams' softmax, warp 8 issues the MMAs, warp 9 walks the items and loads.
 
+#include <algorithm>
 #include <cmath>
 
 #include "chunks.cuh"
+#include "ptx.cuh"
 
 namespace echo {
+
+using namespace ptx;
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
+                                  const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
+                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
 namespace {
 
-struct AttendArgs {
-  const uint16_t *q;
-  int64_t q_stride;
-  const uint16_t *pool;
-  uint16_t *out;
-  int Hq, Hkv, hd, n_pages, half_io;
-  float scale;
-  ChunkArgs c;
+constexpr int kKeys = 128;                     // keys of a tile
+constexpr int kPages = kKeys / kChunkPage;
+constexpr int kAttThreads = 384;
+constexpr int kMaxCtas = 148;                  // CTAs of a launch: sizes the workspace
+constexpr int kItemRing = 4;
+constexpr float kMoveReference = 8.0f;         // log2 of how far a maximum may run ahead of the reference
+
+// Costs that the shares are cut by, in keys of a single item.  A paired item's tile keeps the tensor cores twice as long.
+constexpr int kSingleStart = 256, kPairWeight = 2, kPairStart = 512;
+constexpr int kLeastPart = 1;                  // key tiles
+
+template <int HD> struct AttSmem {
+  static constexpr int kQTile = 128 * HD * 2;
+  static constexpr int kStage = kKeys * HD * 2;
+  static constexpr int kStages = HD == 128 ? 5 : 8;
+  static constexpr int kQ = 0, kKV = 2 * kQTile, kBars = kKV + kStages * kStage;
+  static constexpr int kTotal = kBars + 3072;
+  static_assert(kTotal <= 227 * 1024, "shared memory");
 };
 
-__global__ void __launch_bounds__(128) attend_rows_kernel(const __grid_constant__ AttendArgs a) {
+struct Item {
+  int row0, n_tok, head, pos0;      // first row and tokens of the item, its kv head, position of the first token
+  int t0, t1, seen_end, flags;      // key tiles [t0, t1); no row sees key seen_end or a later one
+};
+constexpr int kPaired = 1, kEnd = 2, kPartLater = 4, kPartFirst = 8;      // parts of a cut item: a later one, the first
+
+// What a CTA says of its (at most two) partial results to the joining launch.
+struct PartRecord {
+  int first, later;                 // partial result present: of the first tiles of an item; of later ones
+  int later_ends;                   // the later one reaches the item's last tile
+  Item item;                        // of `first`
+};
+constexpr int kRecordBytes = 64;
+static_assert(sizeof(PartRecord) <= kRecordBytes, "record");
+
+struct AttendArgs {
+  ChunkArgs c;
+  uint16_t *out;
+  float *part_o;                    // [cta][2][rows_cap][hd]
+  float2 *part_ml;                  // [cta][2][rows_cap]: reference in log2 units, sum
+  PartRecord *records;
+  int Hq, Hkv, group, tile_tok, n_pages, rows_cap;
+  float scale_log2;
+};
+
+// ---- tensor memory and descriptors -----------------------------------------------------------------
+__device__ __forceinline__ void tc_st32(uint32_t taddr, const uint32_t (&r)[32]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};"
+      ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+        "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
+        "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
+        "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ uint32_t tc_ld1(uint32_t taddr) {
+  uint32_t v;
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];\n\ttcgen05.wait::ld.sync.aligned;" : "=r"(v) : "r"(taddr) : "memory");
+  return v;
+}
+// ties a loaded block of registers to the wait before it
+__device__ __forceinline__ void after_wait(uint32_t (&r)[32]) {
+#pragma unroll
+  for (int i = 0; i < 32; ++i) asm volatile("" : "+r"(r[i]));
+}
+// D += A B with A in tensor memory (16-bit pairs of one row in a 32-bit column)
+__device__ __forceinline__ void tc_mma_ts(uint32_t tmem_d, uint32_t tmem_a, uint64_t desc_b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+      ::"r"(tmem_d), "r"(tmem_a), "l"(desc_b), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+// shared-memory matrix descriptor, 128-byte swizzle: atoms of 8 rows x 128 bytes.  K-major: sbo between 8-row groups.
+// MN-major (a row of 128 bytes holds 64 elements of the MN dimension at one k): lbo between atoms along MN, sbo along K.
+__device__ __forceinline__ uint64_t smem_desc(uint32_t saddr, uint32_t lbo, uint32_t sbo) {
+  return static_cast<uint64_t>((saddr & 0x3FFFFu) >> 4) | (static_cast<uint64_t>(lbo >> 4) << 16) |
+         (static_cast<uint64_t>(sbo >> 4) << 32) | (static_cast<uint64_t>(1) << 46) | (static_cast<uint64_t>(2) << 61);
+}
+constexpr uint32_t kIdescBMajorMN = 1u << 16;
+
+__device__ __forceinline__ void tma_load_3d(const CUtensorMap *map, uint64_t *bar, uint32_t dst, int c0, int c1, int c2) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+      ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(smem_u32(bar)), "r"(c0), "r"(c1), "r"(c2)
+      : "memory");
+}
+__device__ __forceinline__ void tma_load_4d(const CUtensorMap *map, uint64_t *bar, uint32_t dst, int c0, int c1, int c2, int c3) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
+      ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(smem_u32(bar)), "r"(c0), "r"(c1), "r"(c2), "r"(c3)
+      : "memory");
+}
+
+// ---- costs -------------------------------------------------------------------------------------------
+// Items of one kv head of a sequence: n_items of up to 2 tile_tok tokens, the last one single if its tokens fit one tile.
+struct SeqCost {
+  int n_items, base, n, step;       // base = L - n: keys in front of the chunk (below 0: the first rows see nothing)
+  bool last_single;
+  // keys that item i's last token sees
+  __device__ __forceinline__ int seen(int i) const { return max(0, base + min(n, (i + 1) * step)); }
+  __device__ __forceinline__ bool single(int i) const { return i == n_items - 1 && last_single; }
+  __device__ __forceinline__ long long cost(int i) const {
+    return single(i) ? kSingleStart + static_cast<long long>(seen(i)) : kPairStart + static_cast<long long>(kPairWeight) * seen(i);
+  }
+  // cost of the items before i
+  __device__ __forceinline__ long long before(int i) const {
+    const int full = min(i, n_items - 1), dead = base < 0 ? min(full, -base / step) : 0;      // items 0 .. dead - 1 see nothing
+    const long long m = full - dead;
+    long long c = static_cast<long long>(full) * kPairStart +
+                  kPairWeight * (m * base + static_cast<long long>(step) * (m * (dead + 1) + m * (m - 1) / 2));
+    if (i == n_items) c += cost(n_items - 1);
+    return c;
+  }
+  __device__ __forceinline__ long long head() const { return n_items ? before(n_items) : 0; }
+};
+__device__ __forceinline__ SeqCost seq_cost(const SeqSpan &p, int tile_tok) {
+  SeqCost k;
+  k.step = 2 * tile_tok;
+  k.n = p.ok ? p.n : 0;
+  k.base = p.kv - p.n;
+  k.n_items = (k.n + k.step - 1) / k.step;
+  const int rest = k.n - (k.n_items - 1) * k.step;
+  k.last_single = k.n_items && rest <= tile_tok;
+  return k;
+}
+// key tile at which an item is cut, x into its cost
+__device__ __forceinline__ int cut_tile(long long x, bool single, int seen) {
+  const int tiles = (seen + kKeys - 1) / kKeys;
+  const long long y = x - (single ? kSingleStart : kPairStart), per = single ? kKeys : kPairWeight * kKeys;
+  const int t = y <= 0 ? 0 : static_cast<int>(min(static_cast<long long>(tiles), (y + per - 1) / per));
+  return t < kLeastPart ? 0 : tiles - t < kLeastPart ? tiles : t;
+}
+
+// ---- the kernel ----------------------------------------------------------------------------------------
+template <int HD> struct Shared {
+  uint64_t q_full[2], q_empty[2], kv_full[AttSmem<HD>::kStages], kv_empty[AttSmem<HD>::kStages];
+  uint64_t s_full[2], p_ready[2], pv_done[2], item_full[kItemRing], item_empty[kItemRing];
+  uint64_t look[2], join[2], drain;
+  Item items[kItemRing];
+  int bad_page[kItemRing];
+  int bad_value[2];                 // step (+ 1) of a stream whose P V the threads add themselves
+  uint32_t tmem;
+  int abort_flag;
+  long long total, start;           // plan: cost of everything; cost in front of the CTA's first sequence
+  int first_seq;
+  long long warp_sum[kAttThreads / 32];
+  float2 ml[2][128];
+};
+
+template <bool HALF> __device__ __forceinline__ bool any_undefined(uint4 v) {
+  const uint32_t m = HALF ? 0x7c007c00u : 0x7f807f80u;
+  return (__vcmpeq2(v.x & m, m) | __vcmpeq2(v.y & m, m) | __vcmpeq2(v.z & m, m) | __vcmpeq2(v.w & m, m)) != 0;
+}
+// byte of 16-byte unit c of key `key` in a K or V stage: [8-row group][64-element half][row][128 bytes], swizzled
+template <int HD> __device__ __forceinline__ uint32_t kv_unit(int key, int c) {
+  return (key >> 3) * (HD * 16) + (c >> 3) * 1024 + (key & 7) * 128 + (((c & 7) ^ (key & 7)) << 4);
+}
+
+// The total cost, and where this CTA's share begins.
+template <int HD> __device__ __forceinline__ void make_plan(const AttendArgs &a, Shared<HD> &sh) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  constexpr int kWarps = kAttThreads / 32;
+  auto cost_of = [&](int s, bool report) -> long long {
+    if (s >= a.c.S) return 0;
+    const SeqSpan p = seq_span(a.c, s);
+    if (report && !p.ok) atomicMax(a.c.status, STATUS_BAD_CHUNK);
+    return seq_cost(p, a.tile_tok).head() * a.Hkv;
+  };
+  long long mine = 0, first = 0;
+  for (int s = threadIdx.x; s < a.c.S; s += kAttThreads) {
+    const long long c = cost_of(s, blockIdx.x == 0);
+    if (s < kAttThreads) first = c;
+    mine += c;
+  }
+#pragma unroll
+  for (int o = 16; o; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
+  if (lane == 0) sh.warp_sum[warp] = mine;
+  if (threadIdx.x == 0) sh.first_seq = -1;
+  __syncthreads();
+  long long total = 0;
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) total += sh.warp_sum[w];
+  const long long x0 = total * blockIdx.x / gridDim.x, x1 = total * (blockIdx.x + 1) / gridDim.x;
+  if (threadIdx.x == 0) sh.total = total;
+  __syncthreads();
+  if (x0 == x1) return;                          // nothing to do (first_seq stays -1)
+  long long before = 0;
+  for (int s0 = 0; s0 < a.c.S; s0 += kAttThreads) {
+    const int s = s0 + threadIdx.x;
+    const long long c = s0 == 0 ? first : cost_of(s, false);
+    long long run = c;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long up = __shfl_up_sync(0xffffffffu, run, o);
+      if (lane >= o) run += up;
+    }
+    if (lane == 31) sh.warp_sum[warp] = run;
+    __syncthreads();
+    long long mine_before = before;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+      if (w < warp) mine_before += sh.warp_sum[w];
+      before += sh.warp_sum[w];
+    }
+    mine_before += run - c;
+    if (c > 0 && x0 >= mine_before && x0 < mine_before + c) {
+      sh.first_seq = s;
+      sh.start = mine_before;
+    }
+    __syncthreads();
+    if (sh.first_seq >= 0) break;
+  }
+}
+
+template <int HD, bool HALF>
+__global__ void __launch_bounds__(kAttThreads, 1)
+chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_kv,
+                       const __grid_constant__ AttendArgs a) {
+  using M = AttSmem<HD>;
+  extern __shared__ __align__(1024) uint8_t smem[];
+  Shared<HD> &sh = *reinterpret_cast<Shared<HD> *>(smem + M::kBars);
+  static_assert(sizeof(Shared<HD>) <= 3072, "barriers");
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  volatile int *abort_flag = &sh.abort_flag;
+  if (smem_u32(smem) & 1023) {                 // (swizzled tiles need it; a dynamic array alone begins there)
+    if (threadIdx.x == 0) atomicMax(a.c.status, STATUS_WAIT_TIMEOUT);
+    return;
+  }
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&sh.q_full[i], 1);
+      mbar_init(&sh.q_empty[i], 1);
+      mbar_init(&sh.s_full[i], 1);
+      mbar_init(&sh.p_ready[i], 4);
+      mbar_init(&sh.pv_done[i], 1);
+      mbar_init(&sh.look[i], 4);
+      mbar_init(&sh.join[i], 8);
+      sh.bad_value[i] = 0;
+    }
+    for (int i = 0; i < M::kStages; ++i) {
+      mbar_init(&sh.kv_full[i], 1);
+      mbar_init(&sh.kv_empty[i], 1);
+    }
+    for (int i = 0; i < kItemRing; ++i) {
+      mbar_init(&sh.item_full[i], 1);
+      mbar_init(&sh.item_empty[i], 9);
+    }
+    mbar_init(&sh.drain, 1);
+    sh.abort_flag = 0;
+    mbar_fence_init();
+  }
+  if (warp == 8) tc_alloc(&sh.tmem, 512);
   early_start_sync();
-  const int lane = threadIdx.x & 31, head = blockIdx.y * 4 + (threadIdx.x >> 5), row = blockIdx.x;
-  const bool h16 = a.half_io != 0;
-  if (blockIdx.x == 0 && blockIdx.y == 0)
-    for (int s = threadIdx.x; s < a.c.S; s += blockDim.x)
-      if (!seq_span(a.c, s).ok) atomicMax(a.c.status, STATUS_BAD_CHUNK);
-  if (head >= a.Hq) return;
-  int seq = -1;
-  SeqSpan p;
-  for (int s0 = 0; s0 < a.c.S && seq < 0; s0 += 32) {
-    const int s = s0 + lane;
-    bool mine = false;
-    if (s < a.c.S) {
-      p = seq_span(a.c, s);
-      mine = p.ok && row >= p.row0 && row < p.row0 + p.n;
+  make_plan<HD>(a, sh);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = sh.tmem;               // S of the streams at columns 0 and 128, O at 256 and 384
+  const long long x_begin = sh.total * blockIdx.x / gridDim.x, x_end = sh.total * (blockIdx.x + 1) / gridDim.x;
+
+  // 168 registers a thread at launch (64512 in all): 208 for the two softmax warpgroups, 80 for the third
+  if (warp >= 8) asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+  else asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+  // waits of a whole warp, whose lanes go on or give up together
+  auto wait = [&](uint64_t *bar, int parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity & 1, abort_flag)) != 0; };
+
+  if (warp == 9) {
+    // ---------------------------------------------------------------- items and copies
+    PartRecord rec = {};
+    int n_items = 0;                            // published
+    int q_uses[2] = {0, 0}, next_slot = 0;
+    int kv_at = 0;                              // position in the ring: stage kv_at % kStages
+    bool ok = true;
+    const uint32_t q_s = smem_u32(smem + M::kQ), kv_s = smem_u32(smem + M::kKV);
+    const int q_bytes = 2 * HD * a.group * a.tile_tok;
+    auto publish = [&](const Item &it) {
+      const int slot = n_items % kItemRing;
+      if (n_items >= kItemRing) ok = wait(&sh.item_empty[slot], (n_items / kItemRing) - 1);
+      if (!ok) return;
+      if (lane == 0) {
+        sh.items[slot] = it;
+        sh.bad_page[slot] = 0;
+        mbar_arrive(&sh.item_full[slot]);
+      }
+      __syncwarp();
+      ++n_items;
+    };
+    auto load_q = [&](const Item &it, int slot, int tile) {
+      if (ok && q_uses[slot] > 0) ok = wait(&sh.q_empty[slot], q_uses[slot] - 1);
+      if (!ok) return;
+      if (lane == 0) {
+        mbar_expect_tx(&sh.q_full[slot], q_bytes);
+#pragma unroll
+        for (int h = 0; h < HD / 64; ++h)
+          tma_load_3d(&tm_q, &sh.q_full[slot], q_s + slot * M::kQTile + h * 16384, 64 * h, it.head * a.group,
+                      it.row0 + tile * a.tile_tok);
+      }
+      __syncwarp();
+      ++q_uses[slot];
+    };
+    if (sh.first_seq >= 0) {
+      long long left = x_end - x_begin, y = x_begin - sh.start;      // cost left to do; place within the sequence
+      int window = sh.first_seq & ~31;
+      SeqSpan span = {};
+      int seq = sh.first_seq;
+      bool load_window = true;
+      while (left > 0 && seq < a.c.S && ok) {
+        if (load_window || seq >= window + 32) {
+          window = seq & ~31;
+          span.ok = false;
+          if (window + lane < a.c.S) span = seq_span(a.c, window + lane);
+          load_window = false;
+        }
+        SeqSpan p;
+        p.row0 = __shfl_sync(0xffffffffu, span.row0, seq - window);
+        p.n = __shfl_sync(0xffffffffu, span.n, seq - window);
+        p.kv = __shfl_sync(0xffffffffu, span.kv, seq - window);
+        p.ok = __shfl_sync(0xffffffffu, span.ok ? 1 : 0, seq - window) != 0;
+        const SeqCost k = seq_cost(p, a.tile_tok);
+        if (k.n_items == 0) {
+          ++seq;
+          y = 0;
+          continue;
+        }
+        const long long head_cost = k.head();
+        int head = static_cast<int>(y / head_cost);
+        y -= head * head_cost;
+        // last item that starts at or before y
+        int lo = 0, hi = k.n_items;
+        while (hi - lo > 1) {
+          const int step = (hi - lo + 31) / 32, at = lo + lane * step;
+          const unsigned m = __ballot_sync(0xffffffffu, at < hi && k.before(at) <= y);
+          lo += (31 - __clz(m)) * step;
+          hi = min(hi, lo + step);
+        }
+        y -= k.before(lo);
+        const int32_t *pages = a.c.page_table + static_cast<int64_t>(seq) * a.c.pt_width;
+        for (int i = lo; head < a.Hkv && left > 0 && ok;) {
+          const bool single = k.single(i);
+          const long long cost = k.cost(i), take = min(left, cost - y);
+          const int seen = k.seen(i), tiles = (seen + kKeys - 1) / kKeys;
+          Item it;
+          it.t0 = cut_tile(y, single, seen);
+          it.t1 = cut_tile(y + take, single, seen);
+          it.row0 = p.row0 + i * k.step;
+          it.n_tok = min(k.step, p.n - i * k.step);
+          it.head = head;
+          it.pos0 = k.base + i * k.step;
+          it.seen_end = seen;
+          it.flags = single ? 0 : kPaired;
+          if (it.t0 > 0) it.flags |= kPartLater;
+          else if (it.t1 < tiles) it.flags |= kPartFirst;
+          const bool none = tiles == 0 && y == 0;                    // rows that see nothing: zeros
+          if (it.t0 < it.t1 || none) {
+            if (it.flags & kPartLater) {
+              rec.later = 1;
+              rec.later_ends = it.t1 == tiles;
+            }
+            if (it.flags & kPartFirst) {
+              rec.first = 1;
+              rec.item = it;
+            }
+            const int slot = n_items % kItemRing;
+            publish(it);
+            if (!ok) break;
+            if (it.t0 < it.t1) {
+              if (single) {
+                load_q(it, next_slot, 0);
+                next_slot ^= 1;
+              } else {
+                load_q(it, 0, 0);
+                load_q(it, 1, 1);
+              }
+              int ids = 0, ids_next = 0, block = -1;
+              const int n_need = (seen + kChunkPage - 1) / kChunkPage;
+              auto fetch = [&](int b) { return 32 * b + lane < n_need ? pages[32 * b + lane] : -1; };
+              for (int t = it.t0; t < it.t1 && ok; ++t) {
+                if (block != t / 4) {
+                  ids = block < 0 ? fetch(t / 4) : ids_next;
+                  block = t / 4;
+                  ids_next = fetch(block + 1);
+                }
+                const int id = __shfl_sync(0xffffffffu, ids, (t & 3) * 8 + (lane & 7));
+                const bool need = t * kPages + (lane & 7) < n_need, valid = need && id >= 0 && id < a.n_pages;
+                if (lane < 8 && need && !valid) {
+                  sh.bad_page[slot] = 1;
+                  atomicMax(a.c.status, STATUS_BAD_PAGE);
+                }
+                // a page that nothing sees, or that does not exist, reads as zeros
+                const int unit = valid ? (id * a.Hkv + it.head) * 4 : a.n_pages * a.Hkv * 4;
+#pragma unroll
+                for (int kv = 0; kv < 2; ++kv) {
+                  const int stage = kv_at % M::kStages, use = kv_at / M::kStages;
+                  if (use > 0) ok = wait(&sh.kv_empty[stage], use - 1);
+                  if (!ok) break;
+                  if (lane == 0) mbar_expect_tx(&sh.kv_full[stage], M::kStage);
+                  __syncwarp();
+                  if (lane < 8)
+                    tma_load_4d(&tm_kv, &sh.kv_full[stage], kv_s + stage * M::kStage + lane * (M::kStage / kPages), 0, 0, 0,
+                                unit + 2 * kv);
+                  __syncwarp();
+                  ++kv_at;
+                }
+              }
+            }
+          }
+          left -= take;
+          y = 0;
+          if (++i == k.n_items) {
+            i = 0;
+            ++head;
+          }
+        }
+        ++seq;
+        y = 0;
+      }
     }
-    const unsigned any = __ballot_sync(0xffffffffu, mine);
-    if (any) seq = s0 + __ffs(any) - 1;
-  }
-  if (seq < 0) return;
-  p = seq_span(a.c, seq);
-  const int pos = p.kv - p.n + (row - p.row0), per = a.hd / 32, kvh = head / (a.Hq / a.Hkv);
-  float q[4], o[4] = {0.f, 0.f, 0.f, 0.f}, m = -INFINITY, l = 0.f;
-  bool bad = false;
-  for (int e = 0; e < per; ++e) q[e] = widen16(a.q[row * a.q_stride + head * a.hd + lane + 32 * e], h16);
-  for (int u = 0; u <= pos; ++u) {
-    const int page = a.c.page_table[static_cast<int64_t>(seq) * a.c.pt_width + u / kChunkPage];
-    if (page < 0 || page >= a.n_pages) {
-      bad = true;
-      break;
+    if (ok) {
+      Item end = {};
+      end.flags = kEnd;
+      publish(end);
     }
-    const uint16_t *k = a.pool + ((static_cast<int64_t>(page) * a.Hkv + kvh) * 2 * kChunkPage + u % kChunkPage) * a.hd + lane;
-    const uint16_t *v = k + kChunkPage * a.hd;
-    float s = 0.f;
-    for (int e = 0; e < per; ++e) s += q[e] * widen16(k[32 * e], h16);
-    for (int d = 16; d > 0; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
-    s *= a.scale;
-    const float top = fmaxf(m, s), fix = m == -INFINITY ? 0.f : expf(m - top), w = top == -INFINITY ? 0.f : expf(s - top);
-    l = l * fix + w;
-    for (int e = 0; e < per; ++e) o[e] = o[e] * fix + w * widen16(v[32 * e], h16);
-    m = top;
+    if (lane == 0) a.records[blockIdx.x] = rec;
+    if (!ok) {
+      // give up: let the copies that are under way land before the shared memory goes
+      if (lane == 0) {
+        for (int i = 0; i < 2; ++i)
+          if (q_uses[i] > 0) mbar_drain(&sh.q_full[i], (q_uses[i] - 1) & 1);
+        for (int i = max(0, kv_at - M::kStages); i < kv_at; ++i) mbar_drain(&sh.kv_full[i % M::kStages], (i / M::kStages) & 1);
+      }
+      __syncwarp();
+    }
+  } else if (warp >= 8) {
+    // ---------------------------------------------------------------- MMA issue
+    if (warp == 8 && lane == 0) {
+      const uint32_t idesc_s = idesc_operands(instr_desc_bf16(kKeys), HALF);
+      const uint32_t idesc_o = idesc_operands(instr_desc_bf16(HD), HALF) | kIdescBMajorMN;
+      const uint32_t q_s = smem_u32(smem + M::kQ), kv_s = smem_u32(smem + M::kKV);
+      int q_item = -1, q_step = 0, q_steps = 0, q_tile0 = 0, q_tiles = 0, q_slot = 0, next_slot = 0;      // S = Q K^T
+      int p_item = -1, p_step = 0, p_steps = 0, p_tile0 = 0, p_tiles = 0;                                 // O += P V
+      bool q_paired = false, p_paired = false, q_end = false, ok = true;
+      int q_uses[2] = {0, 0};
+      int gq = 0, gp = 0, stream_steps[2] = {0, 0};
+      int first_of[2] = {0, 0};                                       // streams that have begun the item
+      // Waits without blocking where there is other work to issue.
+      auto ready = [&](uint64_t *bar, uint32_t parity, bool block) {
+        if (mbar_try_wait(bar, parity)) return true;
+        if (!block) return false;
+        if (!mbar_wait(bar, parity, abort_flag)) ok = false;
+        return ok;
+      };
+      // the items whose S has been begun, as far as they have no steps left
+      auto next_p = [&]() {
+        while (p_step == p_steps && p_item < q_item) {
+          p_tile0 += p_tiles;
+          ++p_item;
+          const Item &it = sh.items[p_item % kItemRing];
+          p_step = 0;
+          p_paired = it.flags & kPaired;
+          p_tiles = it.t1 - it.t0;
+          p_steps = p_paired ? 2 * p_tiles : p_tiles;
+          first_of[0] = first_of[1] = 1;
+          if (p_steps == 0) mbar_arrive(&sh.item_empty[p_item % kItemRing]);
+        }
+      };
+      while (ok) {
+        next_p();
+        if (!q_end && gq < gp + 2) {
+          const bool block = gq == gp;
+          bool go = true;
+          while (go && q_step == q_steps) {                           // next item
+            const int n = q_item + 1, slot = n % kItemRing;
+            if (!ready(&sh.item_full[slot], (n / kItemRing) & 1, block)) {
+              go = false;
+              break;
+            }
+            const int flags = sh.items[slot].flags;
+            if (flags & kEnd) {
+              q_end = true;
+              break;
+            }
+            q_tile0 += q_tiles;
+            q_item = n;
+            q_step = 0;
+            q_paired = flags & kPaired;
+            q_tiles = sh.items[slot].t1 - sh.items[slot].t0;
+            q_steps = q_paired ? 2 * q_tiles : q_tiles;
+            next_p();
+            if (q_steps == 0) continue;
+            q_slot = 0;
+            if (!q_paired) {
+              q_slot = next_slot;
+              next_slot ^= 1;
+            }
+          }
+          if (!ok) break;
+          if (go && !q_end) {
+            const int row_tile = q_paired ? q_step & 1 : 0, tile = q_paired ? q_step >> 1 : q_step;
+            const int qs = q_paired ? row_tile : q_slot;
+            const int at = 2 * (q_tile0 + tile), stage = at % M::kStages;
+            const bool first_use = !q_paired || row_tile == 0, last_use = !q_paired || row_tile == 1;
+            if (q_step < (q_paired ? 2 : 1)) go = ready(&sh.q_full[qs], q_uses[qs] & 1, block);
+            if (go && first_use) go = ready(&sh.kv_full[stage], (at / M::kStages) & 1, block);
+            if (!ok) break;
+            if (go) {
+              const int w = gq & 1;
+              tc_fence_after();
+#pragma unroll
+              for (int k = 0; k < HD / 16; ++k) {
+                const uint64_t da = smem_desc(q_s + qs * M::kQTile + (k >> 2) * 16384 + (k & 3) * 32, 16, 1024);
+                const uint64_t db = smem_desc(kv_s + stage * M::kStage + (k >> 2) * 1024 + (k & 3) * 32, 16, HD * 16);
+                tc_mma_bf16(tmem + w * 128, da, db, idesc_s, k > 0);
+              }
+              tc_commit(&sh.s_full[w]);
+              if (last_use) tc_commit(&sh.kv_empty[stage]);
+              if (q_step >= q_steps - (q_paired ? 2 : 1)) {
+                tc_commit(&sh.q_empty[qs]);
+                ++q_uses[qs];
+              }
+              ++q_step;
+              ++gq;
+              continue;
+            }
+          }
+        }
+        if (gp == gq) {
+          if (q_end) break;
+          continue;
+        }
+        {
+          const int w = gp & 1, tile = p_paired ? p_step >> 1 : p_step;
+          const int at = 2 * (p_tile0 + tile) + 1, stage = at % M::kStages;
+          const bool first_use = !p_paired || (p_step & 1) == 0, last_use = !p_paired || (p_step & 1) == 1;
+          if (first_use && !ready(&sh.kv_full[stage], (at / M::kStages) & 1, true)) break;
+          if (!ready(&sh.p_ready[w], stream_steps[w] & 1, true)) break;
+          tc_fence_after();
+          if (*const_cast<volatile int *>(&sh.bad_value[w]) != stream_steps[w] + 1) {
+#pragma unroll
+            for (int k = 0; k < kKeys / 16; ++k) {
+              const uint64_t db = smem_desc(kv_s + stage * M::kStage + k * (HD * 32), 1024, HD * 16);
+              tc_mma_ts(tmem + 256 + w * 128, tmem + w * 128 + k * 8, db, idesc_o, !(first_of[w] && k == 0));
+            }
+          }
+          first_of[w] = 0;
+          tc_commit(&sh.pv_done[w]);
+          if (last_use) tc_commit(&sh.kv_empty[stage]);
+          ++stream_steps[w];
+          ++gp;
+          if (++p_step == p_steps) mbar_arrive(&sh.item_empty[p_item % kItemRing]);
+        }
+      }
+      if (!ok) {
+        *abort_flag = 1;
+        tc_commit(&sh.drain);                    // everything issued has ended before tensor memory is freed
+        mbar_drain(&sh.drain, 0);
+      }
+    }
+    __syncwarp();
+  } else {
+    // ---------------------------------------------------------------- softmax and results
+    const int w = warp >> 2, row = (warp & 3) * 32 + lane, wg_tid = threadIdx.x & 127;
+    const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
+    const uint32_t t_s = tmem + lanes + w * 128, t_o = tmem + lanes + 256 + w * 128;
+    const float c = a.scale_log2;
+    const int tok = row / a.group, rep = row % a.group;
+    int n_item = 0, steps_done = 0 /* of this stream */, g0 = 0 /* steps of both before the item */, tile0 = 0, looks = 0, joins = 0;
+    bool ok = true;
+    while (ok) {
+      const int slot = n_item % kItemRing;
+      ok = wait(&sh.item_full[slot], n_item / kItemRing);
+      if (!ok) break;
+      const Item it = sh.items[slot];
+      if (it.flags & kEnd) break;
+      const bool paired = it.flags & kPaired;
+      const int tiles = it.t1 - it.t0, n_steps = paired ? 2 * tiles : tiles, i0 = (w - g0) & 1;
+      const int row_tile = paired ? i0 : 0;
+      const int tok0 = row_tile * a.tile_tok, n_tok = min(a.tile_tok, it.n_tok - tok0);      // (may be <= 0: no rows)
+      const int pos_first = it.pos0 + tok0, pos = pos_first + tok;
+      const bool mine = row < n_tok * a.group, warp_mine = (warp & 3) * 32 < n_tok * a.group;
+      float m = -INFINITY, l = 0.f;              // reference (score units) and sum
+      for (int i = i0; i < n_steps; i += 2) {
+        const int t = it.t0 + (paired ? i >> 1 : i), key0 = t * kKeys;
+        ok = wait(&sh.s_full[w], steps_done);
+        if (!ok) break;
+        tc_fence_after();
+        const bool masked = key0 + kKeys > pos_first + 1;             // some row does not see all of the tile
+        if (warp_mine) {
+          uint32_t s[4][32];
+#pragma unroll
+          for (int b = 0; b < 4; ++b) tc_ld32(t_s + b * 32, s[b]);
+          tc_wait_ld();
+#pragma unroll
+          for (int b = 0; b < 4; ++b) after_wait(s[b]);
+          if (masked) {
+            const int last = pos - key0;
+#pragma unroll
+            for (int b = 0; b < 4; ++b)
+#pragma unroll
+              for (int e = 0; e < 32; ++e)
+                if (b * 32 + e > last) s[b][e] = 0xff800000u;
+          }
+          float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+          for (int e = 0; e < 32; ++e)
+#pragma unroll
+            for (int b = 0; b < 4; ++b) top[b] = fmaxf(top[b], __uint_as_float(s[b][e]));
+          const float now = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+          const bool move = mine && now > m && !((now - m) * c <= kMoveReference);
+          if (__any_sync(0xffffffffu, move)) {
+            const float to = fmaxf(m, now);
+            const float fix = to == m ? 1.0f : ex2((m - to) * c);     // (m = -inf: 0)
+            m = to;
+            l *= fix;
+            if (i != i0) {
+              ok = wait(&sh.pv_done[w], steps_done - 1);
+              if (!ok) break;
+              tc_fence_after();
+#pragma unroll
+              for (int b = 0; b < HD / 32; ++b) {
+                uint32_t o[32];
+                tc_ld32(t_o + b * 32, o);
+                tc_wait_ld();
+                after_wait(o);
+#pragma unroll
+                for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * fix);
+                tc_st32(t_o + b * 32, o);
+              }
+            }
+          }
+          const float base = m == -INFINITY ? 0.f : -m * c;
+          const float2 c2 = make_float2(c, c), b2 = make_float2(base, base);
+          float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            uint32_t p[32];
+#pragma unroll
+            for (int e = 0; e < 32; ++e) {
+              const int b = 2 * h + (e >> 4), j = 2 * (e & 15);
+              const float2 x = fma2(make_float2(__uint_as_float(s[b][j]), __uint_as_float(s[b][j + 1])), c2, b2);
+              const float2 y = make_float2(ex2(x.x), ex2(x.y));
+              sum[e & 1] = add2(sum[e & 1], y);
+              p[e] = cvt16x2(y.x, y.y, HALF);
+            }
+            tc_st32(t_s + h * 32, p);
+          }
+          l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
+          tc_wait_st();
+        }
+        // keys that some row of the tile does not see: their values must be finite, or kept out of the products
+        const int ks = max(0, pos_first + 1 - key0), ke = min(kKeys, it.seen_end - key0);
+        const int ke16 = (ke + 15) & ~15;
+        bool slow = false;
+        if (masked && (ks < ke || ke < ke16)) {
+          const int at = 2 * (tile0 + t - it.t0) + 1, stage = at % M::kStages;
+          ok = wait(&sh.kv_full[stage], at / M::kStages);
+          if (!ok) break;
+          uint8_t *v = smem + M::kKV + stage * M::kStage;
+          const int u0 = min(ks, ke) * (HD / 8), u1 = ke16 * (HD / 8);
+          bool bad = false;
+          for (int u = u0 + wg_tid; u < u1; u += 128) {
+            uint4 *unit = reinterpret_cast<uint4 *>(v + kv_unit<HD>(u / (HD / 8), u % (HD / 8)));
+            if (u / (HD / 8) < ke) bad |= any_undefined<HALF>(*unit);
+            else *unit = make_uint4(0u, 0u, 0u, 0u);                  // no row of the item sees it
+          }
+          fence_proxy_async();
+          if (ks < ke) {
+            if (bad) *const_cast<volatile int *>(&sh.bad_value[w]) = steps_done + 1;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sh.look[w]);
+            ok = wait(&sh.look[w], looks);
+            if (!ok) break;
+            ++looks;
+            slow = *const_cast<volatile int *>(&sh.bad_value[w]) == steps_done + 1;
+          }
+          if (slow && warp_mine) {
+            if (i != i0) ok = wait(&sh.pv_done[w], steps_done - 1);
+            if (!ok) break;
+            tc_fence_after();
+            const int last = min(pos - key0, kKeys - 1);
+#pragma unroll 1
+            for (int b = 0; b < HD / 32; ++b) {
+              uint32_t o[32];
+              tc_ld32(t_o + b * 32, o);
+              tc_wait_ld();
+              after_wait(o);
+              if (i == i0)
+#pragma unroll
+                for (int e = 0; e < 32; ++e) o[e] = 0u;
+#pragma unroll 1
+              for (int key = 0; key < kKeys; ++key) {
+                const float2 pp = widen16x2(tc_ld1(t_s + (key >> 1)), HALF);
+                const float p = (key & 1) ? pp.y : pp.x;
+                __syncwarp();
+#pragma unroll
+                for (int u = 0; u < 4 && key <= last; ++u) {
+                  const uint4 q = *reinterpret_cast<const uint4 *>(v + kv_unit<HD>(key, b * 4 + u));
+                  const uint32_t words[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+                  for (int e = 0; e < 4; ++e) {
+                    const float2 f = widen16x2(words[e], HALF);
+                    o[u * 8 + 2 * e] = __float_as_uint(fmaf(p, f.x, __uint_as_float(o[u * 8 + 2 * e])));
+                    o[u * 8 + 2 * e + 1] = __float_as_uint(fmaf(p, f.y, __uint_as_float(o[u * 8 + 2 * e + 1])));
+                  }
+                }
+              }
+              __syncwarp();
+              tc_st32(t_o + b * 32, o);
+            }
+            tc_wait_st();
+          }
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sh.p_ready[w]);
+        ++steps_done;
+      }
+      if (!ok) break;
+      // ---- the item's result: whole rows, or a part for the joining launch
+      if (i0 < n_steps) {
+        ok = wait(&sh.pv_done[w], steps_done - 1);
+        if (!ok) break;
+      }
+      tc_fence_after();
+      const bool spoiled = *const_cast<volatile int *>(&sh.bad_page[slot]) != 0;
+      float my_ref = m == -INFINITY ? -INFINITY : m * c, scale0 = 1.f, scale1 = 0.f;
+      int col0 = 0, col1 = HD;
+      uint32_t o_main = t_o, o_other = t_o;
+      bool has_main = i0 < n_steps, has_other = false;
+      if (!paired) {
+        // both streams hold a share of the keys: each warpgroup joins half of the columns
+        sh.ml[w][row] = make_float2(my_ref, l);
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sh.join[0]);
+        ok = wait(&sh.join[0], joins);
+        if (!ok) break;
+        tc_fence_after();
+        const float2 m0 = sh.ml[0][row], m1 = sh.ml[1][row];
+        const float ref = fmaxf(m0.x, m1.x);
+        scale0 = m0.x == -INFINITY ? 0.f : ex2(m0.x - ref);
+        scale1 = m1.x == -INFINITY ? 0.f : ex2(m1.x - ref);
+        l = m0.y * scale0 + m1.y * scale1;
+        my_ref = ref;
+        o_main = tmem + lanes + 256;
+        o_other = o_main + 128;
+        has_main = ((0 - g0) & 1) < n_steps;
+        has_other = ((1 - g0) & 1) < n_steps;
+        col0 = w * (HD / 2);
+        col1 = col0 + HD / 2;
+      }
+      if (warp_mine) {
+        const bool part = it.flags & (kPartFirst | kPartLater);
+        const int part_row = row_tile * 128 + row;
+        const int64_t part_at = (static_cast<int64_t>(blockIdx.x) * 2 + (it.flags & kPartFirst ? 1 : 0)) * a.rows_cap + part_row;
+        if (spoiled) l = NAN;
+        if (part && mine && col0 == 0) a.part_ml[part_at] = make_float2(spoiled ? 0.f : my_ref, l);
+        const float norm = part ? 1.f : spoiled ? NAN : pos < 0 ? 0.f : 1.0f / l;
+        uint16_t *dst = a.out + (static_cast<int64_t>(it.row0 + tok0 + tok) * a.Hq + it.head * a.group + rep) * HD;
+#pragma unroll 1
+        for (int col = col0; col < col1; col += 32) {
+          float f[32];
+#pragma unroll
+          for (int e = 0; e < 32; ++e) f[e] = 0.f;
+          if (has_main) {
+            uint32_t o[32];
+            tc_ld32(o_main + col, o);
+            tc_wait_ld();
+            after_wait(o);
+#pragma unroll
+            for (int e = 0; e < 32; ++e) f[e] = __uint_as_float(o[e]) * scale0;
+          }
+          if (has_other) {
+            uint32_t o[32];
+            tc_ld32(o_other + col, o);
+            tc_wait_ld();
+            after_wait(o);
+#pragma unroll
+            for (int e = 0; e < 32; ++e) f[e] = fmaf(__uint_as_float(o[e]), scale1, f[e]);
+          }
+          if (mine && part) {
+            float4 *q = reinterpret_cast<float4 *>(a.part_o + part_at * HD + col);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) q[e] = make_float4(f[4 * e], f[4 * e + 1], f[4 * e + 2], f[4 * e + 3]);
+          } else if (mine) {
+            uint4 *q = reinterpret_cast<uint4 *>(dst + col);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              uint32_t pk[4];
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                const float x = f[8 * e + 2 * k], y = f[8 * e + 2 * k + 1];
+                pk[k] = pos < 0 ? 0u : cvt16x2(x * norm, y * norm, HALF);
+              }
+              q[e] = make_uint4(pk[0], pk[1], pk[2], pk[3]);
+            }
+          }
+          __syncwarp();
+        }
+      }
+      if (!paired) {
+        // the other warpgroup has read this stream's O before it is written again
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sh.join[1]);
+        ok = wait(&sh.join[1], joins);
+        if (!ok) break;
+        ++joins;
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sh.item_empty[slot]);
+      ++n_item;
+      g0 += n_steps;
+      tile0 += tiles;
+    }
+    if (!ok) *abort_flag = 1;
   }
-  if (bad && lane == 0) atomicMax(a.c.status, STATUS_BAD_PAGE);
-  for (int e = 0; e < per; ++e)
-    a.out[(static_cast<int64_t>(row) * a.Hq + head) * a.hd + lane + 32 * e] =
-        cvt16(bad ? NAN : pos < 0 ? 0.f : o[e] / l, h16);
+  __syncthreads();
+  if (threadIdx.x == 0 && sh.abort_flag) atomicMax(a.c.status, STATUS_WAIT_TIMEOUT);
+  if (warp == 8) {
+    tc_fence_after();
+    tc_dealloc(tmem, 512);
+  }
+}
+
+// Joins the parts of the items that were cut, in key order: CTA (b, g) the item whose first part CTA b left, rows g * 8 ..
+// A warp to a row.
+template <int HD, bool HALF>
+__global__ void __launch_bounds__(256) join_parts_kernel(const __grid_constant__ AttendArgs a, int n_ctas) {
+  early_start_sync();
+  const int b = blockIdx.x, lane = threadIdx.x & 31;
+  if (!a.records[b].first) return;
+  const Item it = a.records[b].item;
+  const int row = blockIdx.y * 8 + (threadIdx.x >> 5);
+  const int tile = row >> 7, r = row & 127, tok = tile * a.tile_tok + r / a.group;
+  if (r >= a.tile_tok * a.group || tok >= it.n_tok) return;
+  // the reference of all parts, then their sums
+  const int64_t stride = 2 * static_cast<int64_t>(a.rows_cap), at0 = b * stride + a.rows_cap + row;
+  float ref = a.part_ml[at0].x;
+  int end = b + 1;                               // CTAs b + 1 .. end - 1 hold the later parts
+  for (bool more = true; more && end < n_ctas; ++end) {
+    const PartRecord &rec = a.records[end];
+    if (!rec.later) continue;
+    ref = fmaxf(ref, a.part_ml[end * stride + row].x);
+    more = !rec.later_ends;
+  }
+  float l = 0.f, o[HD / 32];
+#pragma unroll
+  for (int e = 0; e < HD / 32; ++e) o[e] = 0.f;
+  for (int k = b; k < end; ++k) {
+    if (k > b && !a.records[k].later) continue;
+    const int64_t at = k == b ? at0 : k * stride + row;
+    const float2 ml = a.part_ml[at];
+    const float scale = ml.x == -INFINITY ? 0.f : ex2(ml.x - ref);
+    l += ml.y * scale;
+#pragma unroll
+    for (int e = 0; e < HD / 32; ++e) o[e] += a.part_o[at * HD + lane * (HD / 32) + e] * scale;
+  }
+  const float norm = it.pos0 + tok < 0 ? 0.f : 1.0f / l;
+  uint16_t *dst = a.out + (static_cast<int64_t>(it.row0 + tok) * a.Hq + it.head * a.group + r % a.group) * HD + lane * (HD / 32);
+#pragma unroll
+  for (int e = 0; e < HD / 32; e += 2)
+    *reinterpret_cast<uint32_t *>(dst + e) = it.pos0 + tok < 0 ? 0u : cvt16x2(o[e] * norm, o[e + 1] * norm, HALF);
+}
+
+// ---- host ------------------------------------------------------------------------------------------------
+EncodeTiledFn encode_fn() {
+  static const EncodeTiledFn fn = [] {
+    void *p = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) != cudaSuccess ||
+        q != cudaDriverEntryPointSuccess)
+      p = nullptr;
+    return reinterpret_cast<EncodeTiledFn>(p);
+  }();
+  return fn;
+}
+bool make_map(CUtensorMap *out, int rank, const void *base, bool half, const cuuint64_t *dims, const cuuint64_t *strides,
+              const cuuint32_t *box) {
+  const EncodeTiledFn fn = encode_fn();
+  const cuuint32_t ones[4] = {1, 1, 1, 1};
+  return fn && fn(out, half ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, const_cast<void *>(base),
+                  dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                  CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// rows of an item's partial result
+int rows_cap(int max_chunk, int group) {
+  const int tile_tok = 128 / group;
+  return max_chunk > tile_tok ? 256 : (max_chunk * group + 7) / 8 * 8;
+}
+
+template <int HD, bool HALF>
+cudaError_t launch_attend(const CUtensorMap &tm_q, const CUtensorMap &tm_kv, const AttendArgs &a, int ctas, cudaStream_t s) {
+  cudaError_t e = cudaFuncSetAttribute(chunk_attention_kernel<HD, HALF>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                       AttSmem<HD>::kTotal);
+  if (e != cudaSuccess) return e;
+  e = launch_early(chunk_attention_kernel<HD, HALF>, dim3(ctas), dim3(kAttThreads), AttSmem<HD>::kTotal, s, tm_q, tm_kv, a);
+  if (e != cudaSuccess) return e;
+  return launch_early(join_parts_kernel<HD, HALF>, dim3(ctas, a.rows_cap / 8), dim3(256), 0, s, a, ctas);
 }
 
 }  // namespace
@@ -77,8 +960,9 @@ using namespace echo;
 extern "C" {
 
 size_t echo_chunk_attention_workspace_bytes(int32_t max_chunk, int32_t Hq, int32_t Hkv, int32_t hd) {
-  if (max_chunk < 1 || Hq < 1 || Hkv < 1 || Hq % Hkv || (hd != 64 && hd != 128)) return 0;
-  return 16;
+  if (max_chunk < 1 || Hq < 1 || Hkv < 1 || Hq % Hkv || Hq / Hkv > 128 || (hd != 64 && hd != 128)) return 0;
+  const size_t rows = static_cast<size_t>(kMaxCtas) * 2 * rows_cap(max_chunk, Hq / Hkv);
+  return kMaxCtas * kRecordBytes + rows * (hd * sizeof(float) + sizeof(float2));
 }
 
 int echo_chunk_attention(const void *q, int64_t q_stride, const void *kv_pool, int32_t n_pages, int32_t format,
@@ -91,27 +975,47 @@ int echo_chunk_attention(const void *q, int64_t q_stride, const void *kv_pool, i
   if (!q || !out || Hq < 1 || q_stride < width || q_stride % 8 || q_stride > (1 << 30)) return ECHO_ERR_INVALID;
   for (const void *p : {q, const_cast<const void *>(out), const_cast<const void *>(workspace)})
     if (reinterpret_cast<uintptr_t>(p) & 15) return ECHO_ERR_INVALID;
+  if (Hq / Hkv > 128 || static_cast<int64_t>(n_pages) * Hkv > (1 << 26)) return ECHO_ERR_UNSUPPORTED;
   const size_t need = echo_chunk_attention_workspace_bytes(a.c.max_chunk, Hq, Hkv, hd);
   if (!workspace || workspace_bytes < need) return ECHO_ERR_INVALID;
-  if (Hq / Hkv > 128 || static_cast<int64_t>(n_pages) * Hkv > (1 << 26)) return ECHO_ERR_UNSUPPORTED;
   if (a.c.S == 0 || a.c.n_rows == 0) return ECHO_OK;
   const uint64_t qs = (static_cast<uint64_t>(a.c.n_rows - 1) * q_stride + width) * 2, outs = a.c.n_rows * static_cast<uint64_t>(width) * 2;
   if (ranges_meet(out, outs, q, qs) || ranges_meet(out, outs, kv_pool, pool_bytes(n_pages, Hkv, hd)) ||
       ranges_meet(out, outs, workspace, need) || ranges_meet(workspace, need, q, qs) ||
       ranges_meet(workspace, need, kv_pool, pool_bytes(n_pages, Hkv, hd)))
     return ECHO_ERR_INVALID;
-  a.q = static_cast<const uint16_t *>(q);
-  a.q_stride = q_stride;
-  a.pool = static_cast<const uint16_t *>(kv_pool);
   a.out = static_cast<uint16_t *>(out);
   a.Hq = Hq;
   a.Hkv = Hkv;
-  a.hd = hd;
+  a.group = Hq / Hkv;
+  a.tile_tok = 128 / a.group;
   a.n_pages = n_pages;
-  a.half_io = format == 1;
-  a.scale = 1.0f / std::sqrt(static_cast<float>(hd));
-  const cudaError_t e = launch_early(attend_rows_kernel, dim3(a.c.n_rows, (Hq + 3) / 4), dim3(128), 0,
-                                     static_cast<cudaStream_t>(cuda_stream), a);
+  a.rows_cap = rows_cap(a.c.max_chunk, a.group);
+  a.scale_log2 = 1.4426950408889634f / std::sqrt(static_cast<float>(hd));
+  uint8_t *ws = static_cast<uint8_t *>(workspace);
+  a.records = reinterpret_cast<PartRecord *>(ws);
+  ws += kMaxCtas * kRecordBytes;
+  a.part_o = reinterpret_cast<float *>(ws);
+  a.part_ml = reinterpret_cast<float2 *>(ws + static_cast<size_t>(kMaxCtas) * 2 * a.rows_cap * hd * sizeof(float));
+  int dev = 0, sms = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
+    return ECHO_ERR_CUDA;
+  const bool half = format == 1;
+  CUtensorMap tm_q, tm_kv;
+  // queries: 64 elements of a head x the heads of a group x the tokens of a tile
+  const cuuint64_t qd[3] = {static_cast<cuuint64_t>(hd), static_cast<cuuint64_t>(Hq), static_cast<cuuint64_t>(a.c.n_rows)};
+  const cuuint64_t qst[2] = {static_cast<cuuint64_t>(hd) * 2, static_cast<cuuint64_t>(q_stride) * 2};
+  const cuuint32_t qb[3] = {64, static_cast<cuuint32_t>(a.group), static_cast<cuuint32_t>(a.tile_tok)};
+  // the pool in groups of eight rows, each read as 64-element halves: 64 elements x 8 rows x halves x the two groups of a
+  // page's K (or V) lie in shared memory as [group][half][row], so that operands have one stride from group to group
+  const cuuint64_t kd[4] = {64, 8, static_cast<cuuint64_t>(hd / 64), static_cast<cuuint64_t>(n_pages) * Hkv * 4};
+  const cuuint64_t kst[3] = {static_cast<cuuint64_t>(hd) * 2, 128, static_cast<cuuint64_t>(hd) * 16};
+  const cuuint32_t kb[4] = {64, 8, static_cast<cuuint32_t>(hd / 64), 2};
+  if (!make_map(&tm_q, 3, q, half, qd, qst, qb) || !make_map(&tm_kv, 4, kv_pool, half, kd, kst, kb)) return ECHO_ERR_CUDA;
+  const int ctas = std::min(sms, kMaxCtas);
+  cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+  const cudaError_t e = hd == 128 ? (half ? launch_attend<128, true>(tm_q, tm_kv, a, ctas, s) : launch_attend<128, false>(tm_q, tm_kv, a, ctas, s))
+                                  : (half ? launch_attend<64, true>(tm_q, tm_kv, a, ctas, s) : launch_attend<64, false>(tm_q, tm_kv, a, ctas, s));
   return e == cudaSuccess ? ECHO_OK : ECHO_ERR_CUDA;
 }
 
