@@ -11,8 +11,10 @@
 // Two streams of tiles are in flight in a CTA, each with its own warpgroup, S and O, so that the tensor cores work on one
 // while the other's probabilities are formed:
 //   paired items   two row tiles share each K and V tile (long chunks: keys are read once per 256 rows)
-//   single items   one row tile; its key tiles alternate between the streams, whose two partial results are joined at
-//                  the end (few rows: what counts is to keep the copies running)
+//   single items   one row tile; the streams take 64 keys each of every tile, and their two results are joined at the end
+//                  (few rows: what counts is to keep the copies running)
+// Either way both streams take every key tile in order, so that a barrier's phase is never more than one away from what is
+// waited for.
 //
 // Work.  An item is (sequence, kv head, pair of row tiles or last single one) with its keys.  Items have very different
 // lengths and the lengths are in device memory, so every CTA (one to an SM) adds up all items' costs, takes its equal share
@@ -27,7 +29,7 @@
 // 0 times an undefined value would not be: where a tile has keys that only some of its rows see, their values are looked
 // at, and a tile with an infinity or a NaN among them is accumulated by the threads instead (slow, and nothing else).
 //
-// Roles: warps 0-3 and 4-7 the two streams' softmax, warp 8 issues the MMAs, warp 9 walks the items and loads.
+// Roles: warps 0-3 and 4-7 the two streams' softmax, warps 8 and 10 issue their MMAs, warp 9 walks the items and loads.
 
 #include <algorithm>
 #include <cmath>
@@ -50,6 +52,7 @@ constexpr int kPages = kKeys / kChunkPage;
 constexpr int kAttThreads = 384;
 constexpr int kMaxCtas = 148;                  // CTAs of a launch: sizes the workspace
 constexpr int kItemRing = 4;
+constexpr int kFmaShare = 3;                   // of 8 pairs of exponentials, those that the FMA units compute
 constexpr float kMoveReference = 8.0f;         // log2 of how far a maximum may run ahead of the reference
 
 // Costs that the shares are cut by, in keys of a single item.  A paired item's tile keeps the tensor cores twice as long.
@@ -102,6 +105,22 @@ __device__ __forceinline__ void tc_st32(uint32_t taddr, const uint32_t (&r)[32])
         "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(taddr)
       : "memory");
 }
+__device__ __forceinline__ void tc_ld16(uint32_t taddr, uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr));
+}
+__device__ __forceinline__ void tc_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};"
+      ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+        "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(taddr)
+      : "memory");
+}
 __device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ uint32_t tc_ld1(uint32_t taddr) {
   uint32_t v;
@@ -109,9 +128,38 @@ __device__ __forceinline__ uint32_t tc_ld1(uint32_t taddr) {
   return v;
 }
 // ties a loaded block of registers to the wait before it
-__device__ __forceinline__ void after_wait(uint32_t (&r)[32]) {
+template <int N> __device__ __forceinline__ void after_wait(uint32_t (&r)[N]) {
 #pragma unroll
-  for (int i = 0; i < 32; ++i) asm volatile("" : "+r"(r[i]));
+  for (int i = 0; i < N; ++i) asm volatile("" : "+r"(r[i]));
+}
+// largest of three; NaN wins
+__device__ __forceinline__ float max3_nan(float a, float b, float c) {
+  float d;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+// 2^x of two numbers on the fused multiply-add units: whole part by adding 1.5 2^23, which rounds it into the low bits of the
+// sum; 2^f on [-1/2, 1/2] by a polynomial of degree 4 with constant term 1, fitted here to the least largest relative error
+// (2^-18.4); the whole part goes to the exponent.  Exactly 0 from 2^-127 down; x up to 127.
+__device__ __forceinline__ float2 exp2_by_fma(float2 x) {
+  x = make_float2(max_nan(x.x, -127.f), max_nan(x.y, -127.f));
+  const float2 big = make_float2(12582912.f, 12582912.f), neg = make_float2(-12582912.f, -12582912.f);
+  const float2 t = add2(x, big);
+  const float2 whole = add2(t, neg);
+  const float2 f = fma2(whole, make_float2(-1.f, -1.f), x);
+  float2 p = fma2(f, make_float2(0.009582852944731712f, 0.009582852944731712f), make_float2(0.055906426161527634f, 0.055906426161527634f));
+  p = fma2(p, f, make_float2(0.24024099111557007f, 0.24024099111557007f));
+  p = fma2(p, f, make_float2(0.6931241750717163f, 0.6931241750717163f));
+  p = fma2(p, f, make_float2(1.f, 1.f));
+  return make_float2(__int_as_float(__float_as_int(p.x) + (__float_as_int(t.x) << 23)),
+                     __int_as_float(__float_as_int(p.y) + (__float_as_int(t.y) << 23)));
+}
+// A bounded wait that looks at the clock only after it has failed for a while (reading it takes longer than most waits).
+__device__ __forceinline__ bool wait_bounded(uint64_t *bar, uint32_t parity, volatile int *abort_flag) {
+#pragma unroll 1
+  for (int i = 0; i < 16; ++i)
+    if (mbar_try_wait(bar, parity)) return true;
+  return mbar_wait(bar, parity, abort_flag);
 }
 // D += A B with A in tensor memory (16-bit pairs of one row in a 32-bit column)
 __device__ __forceinline__ void tc_mma_ts(uint32_t tmem_d, uint32_t tmem_a, uint64_t desc_b, uint32_t idesc, uint32_t accumulate) {
@@ -129,6 +177,11 @@ __device__ __forceinline__ uint64_t smem_desc(uint32_t saddr, uint32_t lbo, uint
          (static_cast<uint64_t>(sbo >> 4) << 32) | (static_cast<uint64_t>(1) << 46) | (static_cast<uint64_t>(2) << 61);
 }
 constexpr uint32_t kIdescBMajorMN = 1u << 16;
+__device__ __forceinline__ bool elect_one() {
+  uint32_t one;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(one));
+  return one != 0;
+}
 
 __device__ __forceinline__ void tma_load_3d(const CUtensorMap *map, uint64_t *bar, uint32_t dst, int c0, int c1, int c2) {
   asm volatile(
@@ -186,8 +239,8 @@ __device__ __forceinline__ int cut_tile(long long x, bool single, int seen) {
 // ---- the kernel ----------------------------------------------------------------------------------------
 template <int HD> struct Shared {
   uint64_t q_full[2], q_empty[2], kv_full[AttSmem<HD>::kStages], kv_empty[AttSmem<HD>::kStages];
-  uint64_t s_full[2], p_ready[2], pv_done[2], item_full[kItemRing], item_empty[kItemRing];
-  uint64_t look[2], join[2], drain;
+  uint64_t s_full[2], p_half[2], p_ready[2], pv_done[2], item_full[kItemRing], item_empty[kItemRing];
+  uint64_t look[2], join[2], drain[2];
   Item items[kItemRing];
   int bad_page[kItemRing];
   int bad_value[2];                 // step (+ 1) of a stream whose P V the threads add themselves
@@ -282,8 +335,10 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
   if (threadIdx.x == 0) {
     for (int i = 0; i < 2; ++i) {
       mbar_init(&sh.q_full[i], 1);
-      mbar_init(&sh.q_empty[i], 1);
+      mbar_init(&sh.q_empty[i], 2);
+      mbar_init(&sh.drain[i], 1);
       mbar_init(&sh.s_full[i], 1);
+      mbar_init(&sh.p_half[i], 4);
       mbar_init(&sh.p_ready[i], 4);
       mbar_init(&sh.pv_done[i], 1);
       mbar_init(&sh.look[i], 4);
@@ -292,13 +347,12 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
     }
     for (int i = 0; i < M::kStages; ++i) {
       mbar_init(&sh.kv_full[i], 1);
-      mbar_init(&sh.kv_empty[i], 1);
+      mbar_init(&sh.kv_empty[i], 2);
     }
     for (int i = 0; i < kItemRing; ++i) {
       mbar_init(&sh.item_full[i], 1);
-      mbar_init(&sh.item_empty[i], 9);
+      mbar_init(&sh.item_empty[i], 10);
     }
-    mbar_init(&sh.drain, 1);
     sh.abort_flag = 0;
     mbar_fence_init();
   }
@@ -315,13 +369,13 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
   if (warp >= 8) asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
   else asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
   // waits of a whole warp, whose lanes go on or give up together
-  auto wait = [&](uint64_t *bar, int parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity & 1, abort_flag)) != 0; };
+  auto wait = [&](uint64_t *bar, int parity) { return __all_sync(0xffffffffu, wait_bounded(bar, parity & 1, abort_flag)) != 0; };
 
   if (warp == 9) {
     // ---------------------------------------------------------------- items and copies
     PartRecord rec = {};
     int n_items = 0;                            // published
-    int q_uses[2] = {0, 0}, next_slot = 0;
+    int q_uses0 = 0, q_uses1 = 0, next_slot = 0;
     int kv_at = 0;                              // position in the ring: stage kv_at % kStages
     bool ok = true;
     const uint32_t q_s = smem_u32(smem + M::kQ), kv_s = smem_u32(smem + M::kKV);
@@ -339,7 +393,8 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
       ++n_items;
     };
     auto load_q = [&](const Item &it, int slot, int tile) {
-      if (ok && q_uses[slot] > 0) ok = wait(&sh.q_empty[slot], q_uses[slot] - 1);
+      const int uses = slot ? q_uses1 : q_uses0;
+      if (ok && uses > 0) ok = wait(&sh.q_empty[slot], uses - 1);
       if (!ok) return;
       if (lane == 0) {
         mbar_expect_tx(&sh.q_full[slot], q_bytes);
@@ -349,7 +404,8 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                       it.row0 + tile * a.tile_tok);
       }
       __syncwarp();
-      ++q_uses[slot];
+      if (slot) ++q_uses1;
+      else ++q_uses0;
     };
     if (sh.first_seq >= 0) {
       long long left = x_end - x_begin, y = x_begin - sh.start;      // cost left to do; place within the sequence
@@ -477,138 +533,114 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
     if (!ok) {
       // give up: let the copies that are under way land before the shared memory goes
       if (lane == 0) {
-        for (int i = 0; i < 2; ++i)
-          if (q_uses[i] > 0) mbar_drain(&sh.q_full[i], (q_uses[i] - 1) & 1);
+        if (q_uses0 > 0) mbar_drain(&sh.q_full[0], (q_uses0 - 1) & 1);
+        if (q_uses1 > 0) mbar_drain(&sh.q_full[1], (q_uses1 - 1) & 1);
         for (int i = max(0, kv_at - M::kStages); i < kv_at; ++i) mbar_drain(&sh.kv_full[i % M::kStages], (i / M::kStages) & 1);
       }
       __syncwarp();
     }
   } else if (warp >= 8) {
     // ---------------------------------------------------------------- MMA issue
-    if (warp == 8 && lane == 0) {
-      const uint32_t idesc_s = idesc_operands(instr_desc_bf16(kKeys), HALF);
-      const uint32_t idesc_o = idesc_operands(instr_desc_bf16(HD), HALF) | kIdescBMajorMN;
+    // A warp for each stream, so that one's waits and bookkeeping run under the other's products (one warp for both left
+    // the tensor cores idle for half of the time).  The whole warp takes every step and one elected lane issues: operands
+    // that are the same for all lanes are in uniform registers when an MMA needs them there; with one lane walking alone
+    // an MMA took 100 to 150 cycles to issue, twice as long as it runs.
+    if (warp == 8 || warp == 10) {
+      const int w = warp == 8 ? 0 : 1;
+      constexpr uint32_t idesc_s = idesc_operands(instr_desc_bf16(kKeys), HALF);
+      constexpr uint32_t idesc_o = idesc_operands(instr_desc_bf16(HD), HALF) | kIdescBMajorMN;
+      constexpr uint32_t idesc_half = idesc_operands(instr_desc_bf16(64), HALF);
+      constexpr int kStages = M::kStages;
       const uint32_t q_s = smem_u32(smem + M::kQ), kv_s = smem_u32(smem + M::kKV);
-      int q_item = -1, q_step = 0, q_steps = 0, q_tile0 = 0, q_tiles = 0, q_slot = 0, next_slot = 0;      // S = Q K^T
-      int p_item = -1, p_step = 0, p_steps = 0, p_tile0 = 0, p_tiles = 0;                                 // O += P V
-      bool q_paired = false, p_paired = false, q_end = false, ok = true;
-      int q_uses[2] = {0, 0};
-      int gq = 0, gp = 0, stream_steps[2] = {0, 0};
-      int first_of[2] = {0, 0};                                       // streams that have begun the item
-      // Waits without blocking where there is other work to issue.
-      auto ready = [&](uint64_t *bar, uint32_t parity, bool block) {
-        if (mbar_try_wait(bar, parity)) return true;
-        if (!block) return false;
-        if (!mbar_wait(bar, parity, abort_flag)) ok = false;
-        return ok;
-      };
-      // the items whose S has been begun, as far as they have no steps left
-      auto next_p = [&]() {
-        while (p_step == p_steps && p_item < q_item) {
-          p_tile0 += p_tiles;
-          ++p_item;
-          const Item &it = sh.items[p_item % kItemRing];
-          p_step = 0;
-          p_paired = it.flags & kPaired;
-          p_tiles = it.t1 - it.t0;
-          p_steps = p_paired ? 2 * p_tiles : p_tiles;
-          first_of[0] = first_of[1] = 1;
-          if (p_steps == 0) mbar_arrive(&sh.item_empty[p_item % kItemRing]);
+      const uint32_t t_s = tmem + w * 128, t_o = tmem + 256 + w * 128;
+      uint64_t *s_full = &sh.s_full[w], *p_half = &sh.p_half[w], *p_ready = &sh.p_ready[w], *pv_done = &sh.pv_done[w];
+      bool ok = true;
+      int next_slot = 0, stage = 0, phase = 0, step = 0;
+      uint32_t q_uses = 0;                                            // parity of each query tile's use
+      for (int n = 0; ok; ++n) {
+        const int slot = n % kItemRing;
+        ok = wait(&sh.item_full[slot], n / kItemRing);
+        if (!ok) break;
+        const int flags = __shfl_sync(0xffffffffu, sh.items[slot].flags, 0);
+        if (flags & kEnd) break;
+        const int t0 = __shfl_sync(0xffffffffu, sh.items[slot].t0, 0), t1 = __shfl_sync(0xffffffffu, sh.items[slot].t1, 0);
+        const int pos0 = __shfl_sync(0xffffffffu, sh.items[slot].pos0, 0);
+        const bool paired = (flags & kPaired) != 0;
+        const int qs = paired ? w : next_slot;
+        // keys of a tile that end behind the first row's position: from this tile on
+        const int first_masked = ((pos0 + (paired ? w * a.tile_tok : 0) + 1 - (paired ? kKeys : 64 * (w + 1))) >> 7) + 1;
+        const uint64_t dq = smem_desc(q_s + qs * M::kQTile, 16, 1024);
+        const uint32_t idesc = paired ? idesc_s : idesc_half, half = paired ? 0 : w;
+        if (t0 < t1) {                                                // (both tiles' uses are seen by both warps)
+          if (paired) ok = wait(&sh.q_full[0], q_uses & 1) && wait(&sh.q_full[1], q_uses >> 1);
+          else ok = wait(&sh.q_full[qs], q_uses >> qs);
         }
-      };
-      while (ok) {
-        next_p();
-        if (!q_end && gq < gp + 2) {
-          const bool block = gq == gp;
-          bool go = true;
-          while (go && q_step == q_steps) {                           // next item
-            const int n = q_item + 1, slot = n % kItemRing;
-            if (!ready(&sh.item_full[slot], (n / kItemRing) & 1, block)) {
-              go = false;
-              break;
-            }
-            const int flags = sh.items[slot].flags;
-            if (flags & kEnd) {
-              q_end = true;
-              break;
-            }
-            q_tile0 += q_tiles;
-            q_item = n;
-            q_step = 0;
-            q_paired = flags & kPaired;
-            q_tiles = sh.items[slot].t1 - sh.items[slot].t0;
-            q_steps = q_paired ? 2 * q_tiles : q_tiles;
-            next_p();
-            if (q_steps == 0) continue;
-            q_slot = 0;
-            if (!q_paired) {
-              q_slot = next_slot;
-              next_slot ^= 1;
-            }
-          }
+        for (int t = t0; ok && t < t1; ++t) {
+          ok = wait(&sh.kv_full[stage], phase);
           if (!ok) break;
-          if (go && !q_end) {
-            const int row_tile = q_paired ? q_step & 1 : 0, tile = q_paired ? q_step >> 1 : q_step;
-            const int qs = q_paired ? row_tile : q_slot;
-            const int at = 2 * (q_tile0 + tile), stage = at % M::kStages;
-            const bool first_use = !q_paired || row_tile == 0, last_use = !q_paired || row_tile == 1;
-            if (q_step < (q_paired ? 2 : 1)) go = ready(&sh.q_full[qs], q_uses[qs] & 1, block);
-            if (go && first_use) go = ready(&sh.kv_full[stage], (at / M::kStages) & 1, block);
-            if (!ok) break;
-            if (go) {
-              const int w = gq & 1;
-              tc_fence_after();
-#pragma unroll
-              for (int k = 0; k < HD / 16; ++k) {
-                const uint64_t da = smem_desc(q_s + qs * M::kQTile + (k >> 2) * 16384 + (k & 3) * 32, 16, 1024);
-                const uint64_t db = smem_desc(kv_s + stage * M::kStage + (k >> 2) * 1024 + (k & 3) * 32, 16, HD * 16);
-                tc_mma_bf16(tmem + w * 128, da, db, idesc_s, k > 0);
-              }
-              tc_commit(&sh.s_full[w]);
-              if (last_use) tc_commit(&sh.kv_empty[stage]);
-              if (q_step >= q_steps - (q_paired ? 2 : 1)) {
-                tc_commit(&sh.q_empty[qs]);
-                ++q_uses[qs];
-              }
-              ++q_step;
-              ++gq;
-              continue;
-            }
-          }
-        }
-        if (gp == gq) {
-          if (q_end) break;
-          continue;
-        }
-        {
-          const int w = gp & 1, tile = p_paired ? p_step >> 1 : p_step;
-          const int at = 2 * (p_tile0 + tile) + 1, stage = at % M::kStages;
-          const bool first_use = !p_paired || (p_step & 1) == 0, last_use = !p_paired || (p_step & 1) == 1;
-          if (first_use && !ready(&sh.kv_full[stage], (at / M::kStages) & 1, true)) break;
-          if (!ready(&sh.p_ready[w], stream_steps[w] & 1, true)) break;
           tc_fence_after();
-          if (*const_cast<volatile int *>(&sh.bad_value[w]) != stream_steps[w] + 1) {
+          if (elect_one()) {
+            const uint64_t db = smem_desc(kv_s + stage * M::kStage + half * (64 * HD * 2), 16, HD * 16);
 #pragma unroll
-            for (int k = 0; k < kKeys / 16; ++k) {
-              const uint64_t db = smem_desc(kv_s + stage * M::kStage + k * (HD * 32), 1024, HD * 16);
-              tc_mma_ts(tmem + 256 + w * 128, tmem + w * 128 + k * 8, db, idesc_o, !(first_of[w] && k == 0));
+            for (int k = 0; k < HD / 16; ++k)
+              tc_mma_bf16(t_s, dq + (k >> 2) * (16384 >> 4) + (k & 3) * 2, db + (k >> 2) * (1024 >> 4) + (k & 3) * 2, idesc, k > 0);
+            tc_commit(s_full);
+            tc_commit(&sh.kv_empty[stage]);
+            if (t + 1 == t1) {                                        // (both of a pair's tiles wait for both warps, as both see them)
+              tc_commit(&sh.q_empty[qs]);
+              if (paired) tc_commit(&sh.q_empty[qs ^ 1]);
             }
           }
-          first_of[w] = 0;
-          tc_commit(&sh.pv_done[w]);
-          if (last_use) tc_commit(&sh.kv_empty[stage]);
-          ++stream_steps[w];
-          ++gp;
-          if (++p_step == p_steps) mbar_arrive(&sh.item_empty[p_item % kItemRing]);
+          __syncwarp();
+          if (++stage == kStages) {
+            stage = 0;
+            phase ^= 1;
+          }
+          const uint64_t dv = smem_desc(kv_s + stage * M::kStage + half * (64 * HD * 2), 1024, HD * 16);
+          ok = wait(&sh.kv_full[stage], phase) && wait(p_half, step);
+          if (!ok) break;
+          tc_fence_after();
+          bool by_mma = true;
+          if (t >= first_masked) by_mma = __shfl_sync(0xffffffffu, *const_cast<volatile int *>(&sh.bad_value[w]), 0) != step + 1;
+          if (by_mma && elect_one()) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) tc_mma_ts(t_o, t_s + k * 8, dv + k * (HD * 32 >> 4), idesc_o, k > 0 || t != t0);
+          }
+          __syncwarp();
+          ok = wait(p_ready, step);
+          if (!ok) break;
+          tc_fence_after();
+          if (elect_one()) {
+            if (by_mma && paired) {
+#pragma unroll
+              for (int k = 4; k < 8; ++k) tc_mma_ts(t_o, t_s + k * 8, dv + k * (HD * 32 >> 4), idesc_o, true);
+            }
+            tc_commit(pv_done);
+            tc_commit(&sh.kv_empty[stage]);
+          }
+          __syncwarp();
+          ++step;
+          if (++stage == kStages) {
+            stage = 0;
+            phase ^= 1;
+          }
         }
+        if (!ok) break;
+        if (t0 < t1) {
+          q_uses ^= paired ? 3u : 1u << qs;
+          if (!paired) next_slot ^= 1;
+        }
+        if (lane == 0) mbar_arrive(&sh.item_empty[slot]);
       }
       if (!ok) {
         *abort_flag = 1;
-        tc_commit(&sh.drain);                    // everything issued has ended before tensor memory is freed
-        mbar_drain(&sh.drain, 0);
+        if (elect_one()) {
+          tc_commit(&sh.drain[w]);               // everything issued has ended before tensor memory is freed
+          mbar_drain(&sh.drain[w], 0);
+        }
+        __syncwarp();
       }
     }
-    __syncwarp();
   } else {
     // ---------------------------------------------------------------- softmax and results
     const int w = warp >> 2, row = (warp & 3) * 32 + lane, wg_tid = threadIdx.x & 127;
@@ -616,7 +648,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
     const uint32_t t_s = tmem + lanes + w * 128, t_o = tmem + lanes + 256 + w * 128;
     const float c = a.scale_log2;
     const int tok = row / a.group, rep = row % a.group;
-    int n_item = 0, steps_done = 0 /* of this stream */, g0 = 0 /* steps of both before the item */, tile0 = 0, looks = 0, joins = 0;
+    int n_item = 0, steps_done = 0, looks = 0, joins = 0;        // (steps: key tiles of all items so far)
     bool ok = true;
     while (ok) {
       const int slot = n_item % kItemRing;
@@ -625,93 +657,110 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
       const Item it = sh.items[slot];
       if (it.flags & kEnd) break;
       const bool paired = it.flags & kPaired;
-      const int tiles = it.t1 - it.t0, n_steps = paired ? 2 * tiles : tiles, i0 = (w - g0) & 1;
-      const int row_tile = paired ? i0 : 0;
+      const int row_tile = paired ? w : 0, key_off = paired ? 0 : 64 * w, n_keys = paired ? kKeys : 64;
       const int tok0 = row_tile * a.tile_tok, n_tok = min(a.tile_tok, it.n_tok - tok0);      // (may be <= 0: no rows)
       const int pos_first = it.pos0 + tok0, pos = pos_first + tok;
       const bool mine = row < n_tok * a.group, warp_mine = (warp & 3) * 32 < n_tok * a.group;
       float m = -INFINITY, l = 0.f;              // reference (score units) and sum
-      for (int i = i0; i < n_steps; i += 2) {
-        const int t = it.t0 + (paired ? i >> 1 : i), key0 = t * kKeys;
+      for (int t = it.t0; t < it.t1; ++t) {
+        const int key0 = t * kKeys + key_off;
         ok = wait(&sh.s_full[w], steps_done);
         if (!ok) break;
         tc_fence_after();
-        const bool masked = key0 + kKeys > pos_first + 1;             // some row does not see all of the tile
+        const bool masked = key0 + n_keys > pos_first + 1;            // some row does not see all of these keys
         if (warp_mine) {
-          uint32_t s[4][32];
-#pragma unroll
-          for (int b = 0; b < 4; ++b) tc_ld32(t_s + b * 32, s[b]);
+          uint32_t s[4][32];                     // (blocks 2 and 3 with 128 keys only)
+          tc_ld32(t_s, s[0]);
+          tc_ld32(t_s + 32, s[1]);
+          if (paired) {
+            tc_ld32(t_s + 64, s[2]);
+            tc_ld32(t_s + 96, s[3]);
+          }
           tc_wait_ld();
 #pragma unroll
           for (int b = 0; b < 4; ++b) after_wait(s[b]);
-          if (masked) {
-            const int last = pos - key0;
-#pragma unroll
-            for (int b = 0; b < 4; ++b)
+          const int last = pos - key0;           // the row sees elements 0 .. last
+          float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+          auto mask_and_max = [&](int b) {
+            if (masked) {
 #pragma unroll
               for (int e = 0; e < 32; ++e)
                 if (b * 32 + e > last) s[b][e] = 0xff800000u;
+            }
+#pragma unroll
+            for (int e = 0; e < 32; e += 2)
+              top[(e >> 1) & 3] = max3_nan(top[(e >> 1) & 3], __uint_as_float(s[b][e]), __uint_as_float(s[b][e + 1]));
+          };
+          mask_and_max(0);
+          mask_and_max(1);
+          if (paired) {
+            mask_and_max(2);
+            mask_and_max(3);
           }
-          float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-          for (int e = 0; e < 32; ++e)
-#pragma unroll
-            for (int b = 0; b < 4; ++b) top[b] = fmaxf(top[b], __uint_as_float(s[b][e]));
-          const float now = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
-          const bool move = mine && now > m && !((now - m) * c <= kMoveReference);
+          const float now = max_nan(max3_nan(top[0], top[1], top[2]), top[3]);
+          const bool move = mine && !(now <= m || (now - m) * c <= kMoveReference);      // (NaN moves)
           if (__any_sync(0xffffffffu, move)) {
-            const float to = fmaxf(m, now);
+            const float to = max_nan(m, now);
             const float fix = to == m ? 1.0f : ex2((m - to) * c);     // (m = -inf: 0)
             m = to;
             l *= fix;
-            if (i != i0) {
+            if (t != it.t0) {
               ok = wait(&sh.pv_done[w], steps_done - 1);
               if (!ok) break;
               tc_fence_after();
 #pragma unroll
-              for (int b = 0; b < HD / 32; ++b) {
-                uint32_t o[32];
-                tc_ld32(t_o + b * 32, o);
+              for (int b = 0; b < HD / 16; ++b) {
+                uint32_t o[16];
+                tc_ld16(t_o + b * 16, o);
                 tc_wait_ld();
                 after_wait(o);
 #pragma unroll
-                for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * fix);
-                tc_st32(t_o + b * 32, o);
+                for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * fix);
+                tc_st16(t_o + b * 16, o);
               }
             }
           }
-          const float base = m == -INFINITY ? 0.f : -m * c;
+          const float base = m == -INFINITY ? 0.f : m == INFINITY ? NAN : -m * c;
           const float2 c2 = make_float2(c, c), b2 = make_float2(base, base);
           float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
+          auto probabilities = [&](int h) {      // of keys 64 h .. 64 h + 63
             uint32_t p[32];
 #pragma unroll
             for (int e = 0; e < 32; ++e) {
               const int b = 2 * h + (e >> 4), j = 2 * (e & 15);
               const float2 x = fma2(make_float2(__uint_as_float(s[b][j]), __uint_as_float(s[b][j + 1])), c2, b2);
-              const float2 y = make_float2(ex2(x.x), ex2(x.y));
+              const float2 y = (e & 7) < kFmaShare ? exp2_by_fma(x) : make_float2(ex2(x.x), ex2(x.y));
               sum[e & 1] = add2(sum[e & 1], y);
               p[e] = cvt16x2(y.x, y.y, HALF);
             }
             tc_st32(t_s + h * 32, p);
+          };
+          probabilities(0);
+          if (paired) {
+            if (!masked) {                       // the products of the first 64 keys may begin
+              tc_wait_st();
+              tc_fence_before();
+              __syncwarp();
+              if (lane == 0) mbar_arrive(&sh.p_half[w]);
+            }
+            probabilities(1);
           }
           l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
           tc_wait_st();
         }
         // keys that some row of the tile does not see: their values must be finite, or kept out of the products
-        const int ks = max(0, pos_first + 1 - key0), ke = min(kKeys, it.seen_end - key0);
+        const int ks = max(0, pos_first + 1 - key0), ke = min(n_keys, it.seen_end - key0);
         const int ke16 = (ke + 15) & ~15;
         bool slow = false;
-        if (masked && (ks < ke || ke < ke16)) {
-          const int at = 2 * (tile0 + t - it.t0) + 1, stage = at % M::kStages;
+        if (masked && ke > 0 && (ks < ke || ke < ke16)) {
+          const int at = 2 * steps_done + 1, stage = at % M::kStages;
           ok = wait(&sh.kv_full[stage], at / M::kStages);
           if (!ok) break;
           uint8_t *v = smem + M::kKV + stage * M::kStage;
           const int u0 = min(ks, ke) * (HD / 8), u1 = ke16 * (HD / 8);
           bool bad = false;
           for (int u = u0 + wg_tid; u < u1; u += 128) {
-            uint4 *unit = reinterpret_cast<uint4 *>(v + kv_unit<HD>(u / (HD / 8), u % (HD / 8)));
+            uint4 *unit = reinterpret_cast<uint4 *>(v + kv_unit<HD>(key_off + u / (HD / 8), u % (HD / 8)));
             if (u / (HD / 8) < ke) bad |= any_undefined<HALF>(*unit);
             else *unit = make_uint4(0u, 0u, 0u, 0u);                  // no row of the item sees it
           }
@@ -726,27 +775,27 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             slow = *const_cast<volatile int *>(&sh.bad_value[w]) == steps_done + 1;
           }
           if (slow && warp_mine) {
-            if (i != i0) ok = wait(&sh.pv_done[w], steps_done - 1);
+            if (t != it.t0) ok = wait(&sh.pv_done[w], steps_done - 1);
             if (!ok) break;
             tc_fence_after();
-            const int last = min(pos - key0, kKeys - 1);
+            const int last = pos - key0;
 #pragma unroll 1
             for (int b = 0; b < HD / 32; ++b) {
               uint32_t o[32];
               tc_ld32(t_o + b * 32, o);
               tc_wait_ld();
               after_wait(o);
-              if (i == i0)
+              if (t == it.t0)
 #pragma unroll
                 for (int e = 0; e < 32; ++e) o[e] = 0u;
 #pragma unroll 1
-              for (int key = 0; key < kKeys; ++key) {
+              for (int key = 0; key < n_keys; ++key) {
                 const float2 pp = widen16x2(tc_ld1(t_s + (key >> 1)), HALF);
                 const float p = (key & 1) ? pp.y : pp.x;
                 __syncwarp();
 #pragma unroll
                 for (int u = 0; u < 4 && key <= last; ++u) {
-                  const uint4 q = *reinterpret_cast<const uint4 *>(v + kv_unit<HD>(key, b * 4 + u));
+                  const uint4 q = *reinterpret_cast<const uint4 *>(v + kv_unit<HD>(key_off + key, b * 4 + u));
                   const uint32_t words[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
                   for (int e = 0; e < 4; ++e) {
@@ -764,12 +813,15 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
         }
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&sh.p_ready[w]);
+        if (lane == 0) {
+          if (masked || !warp_mine || !paired) mbar_arrive(&sh.p_half[w]);
+          mbar_arrive(&sh.p_ready[w]);
+        }
         ++steps_done;
       }
       if (!ok) break;
       // ---- the item's result: whole rows, or a part for the joining launch
-      if (i0 < n_steps) {
+      if (it.t0 < it.t1) {
         ok = wait(&sh.pv_done[w], steps_done - 1);
         if (!ok) break;
       }
@@ -778,7 +830,8 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
       float my_ref = m == -INFINITY ? -INFINITY : m * c, scale0 = 1.f, scale1 = 0.f;
       int col0 = 0, col1 = HD;
       uint32_t o_main = t_o, o_other = t_o;
-      bool has_main = i0 < n_steps, has_other = false;
+      const bool has_main = it.t0 < it.t1;
+      bool has_other = false;
       if (!paired) {
         // both streams hold a share of the keys: each warpgroup joins half of the columns
         sh.ml[w][row] = make_float2(my_ref, l);
@@ -796,8 +849,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
         my_ref = ref;
         o_main = tmem + lanes + 256;
         o_other = o_main + 128;
-        has_main = ((0 - g0) & 1) < n_steps;
-        has_other = ((1 - g0) & 1) < n_steps;
+        has_other = has_main;
         col0 = w * (HD / 2);
         col1 = col0 + HD / 2;
       }
@@ -862,8 +914,6 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
       __syncwarp();
       if (lane == 0) mbar_arrive(&sh.item_empty[slot]);
       ++n_item;
-      g0 += n_steps;
-      tile0 += tiles;
     }
     if (!ok) *abort_flag = 1;
   }

@@ -209,6 +209,9 @@ def test_attention_of_ragged_chunks(B, heads, dtype):
     ((12, 2, 64), [(700, 1024), (64, 640)]),
     ((4, 2, 64), [(1, n) for n in range(1, 290, 7)]),         # many sequences of one token
     ((16, 8, 128), [(n, 2 * n) for n in range(1, 60)]),
+    ((8, 8, 128), [(1, 20000)] * 6 + [(2, 17)]),              # dozens of tiles in a row for each CTA
+    ((16, 8, 128), [(300, 6300), (1, 9000), (259, 4500)]),
+    ((8, 8, 64), [(1, 30000)] * 5 + [(150, 9000)]),
 ])
 def test_attention_of_long_caches_and_odd_groups(B, heads, seqs, dtype):
     got, want, spread, scores, keys, top = _attention_case(B, heads, dtype, seqs, seed=3)
