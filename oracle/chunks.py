@@ -52,12 +52,12 @@ def attend(pool, q, row_starts, kv_lens, page_table, out):
             kv = pool[page_table[s, : -(-int(kv_lens[s]) // page)].astype(np.int64)].astype(np.float64)
             gathered = {s: kv.transpose(1, 2, 0, 3, 4).reshape(Hkv, 2, -1, hd)}
         k, v = gathered[s][:, 0, : t + 1], gathered[s][:, 1, : t + 1]
-        z = np.einsum("hgd,hkd->hgk", q[row].astype(np.float64).reshape(Hkv, group, hd), k) / np.sqrt(hd)
+        z = np.matmul(q[row].astype(np.float64).reshape(Hkv, group, hd), k.transpose(0, 2, 1)) / np.sqrt(hd)
         with np.errstate(invalid="ignore"):
             p = np.exp(z - z.max(axis=2, keepdims=True))
             p /= p.sum(axis=2, keepdims=True)
-            out[row] = np.einsum("hgk,hkd->hgd", p, v).reshape(-1, hd)
-            spread[row] = np.einsum("hgk,hkd->hgd", p, np.abs(v)).reshape(-1, hd)
+            out[row] = np.matmul(p, v).reshape(-1, hd)
+            spread[row] = np.matmul(p, np.abs(v)).reshape(-1, hd)
             qa = np.abs(q[row].astype(np.float64)).reshape(Hkv, group, hd)
-            scores[row] = (np.einsum("hgd,hkd->hgk", qa, np.abs(k)) / np.sqrt(hd)).max(axis=2).reshape(-1)
+            scores[row] = (np.matmul(qa, np.abs(k).transpose(0, 2, 1)) / np.sqrt(hd)).max(axis=2).reshape(-1)
     return out, spread, scores

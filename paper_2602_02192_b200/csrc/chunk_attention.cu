@@ -52,7 +52,7 @@ constexpr int kPages = kKeys / kChunkPage;
 constexpr int kAttThreads = 384;
 constexpr int kMaxCtas = 148;                  // CTAs of a launch: sizes the workspace
 constexpr int kItemRing = 4;
-constexpr int kFmaShare = 3;                   // of 8 pairs of exponentials, those that the FMA units compute
+constexpr int kFmaShare = 1;                   // of 8 pairs of exponentials, those that the FMA units compute
 constexpr float kMoveReference = 8.0f;         // log2 of how far a maximum may run ahead of the reference
 
 // Costs that the shares are cut by, in keys of a single item.  A paired item's tile keeps the tensor cores twice as long.
@@ -127,6 +127,26 @@ __device__ __forceinline__ uint32_t tc_ld1(uint32_t taddr) {
   asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];\n\ttcgen05.wait::ld.sync.aligned;" : "=r"(v) : "r"(taddr) : "memory");
   return v;
 }
+// 64 columns of a thread's row, the wait for them included
+__device__ __forceinline__ void tc_ld64_wait(uint32_t taddr, uint32_t *r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x64.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, "
+      "%32, %33, %34, %35, %36, %37, %38, %39, %40, %41, %42, %43, %44, %45, %46, %47, "
+      "%48, %49, %50, %51, %52, %53, %54, %55, %56, %57, %58, %59, %60, %61, %62, %63}, [%64];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+        "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+        "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31]),
+        "=r"(r[32]), "=r"(r[33]), "=r"(r[34]), "=r"(r[35]), "=r"(r[36]), "=r"(r[37]), "=r"(r[38]), "=r"(r[39]),
+        "=r"(r[40]), "=r"(r[41]), "=r"(r[42]), "=r"(r[43]), "=r"(r[44]), "=r"(r[45]), "=r"(r[46]), "=r"(r[47]),
+        "=r"(r[48]), "=r"(r[49]), "=r"(r[50]), "=r"(r[51]), "=r"(r[52]), "=r"(r[53]), "=r"(r[54]), "=r"(r[55]),
+        "=r"(r[56]), "=r"(r[57]), "=r"(r[58]), "=r"(r[59]), "=r"(r[60]), "=r"(r[61]), "=r"(r[62]), "=r"(r[63])
+      : "r"(taddr)
+      : "memory");
+}
 // ties a loaded block of registers to the wait before it
 template <int N> __device__ __forceinline__ void after_wait(uint32_t (&r)[N]) {
 #pragma unroll
@@ -154,12 +174,23 @@ __device__ __forceinline__ float2 exp2_by_fma(float2 x) {
   return make_float2(__int_as_float(__float_as_int(p.x) + (__float_as_int(t.x) << 23)),
                      __int_as_float(__float_as_int(p.y) + (__float_as_int(t.y) << 23)));
 }
-// A bounded wait that looks at the clock only after it has failed for a while (reading it takes longer than most waits).
-__device__ __forceinline__ bool wait_bounded(uint64_t *bar, uint32_t parity, volatile int *abort_flag) {
+// A whole warp's bounded wait; its lanes go on or give up together.  Votes keep the loop free of divergence, and the clock
+// is read now and then only: a wait that has nothing to wait for takes 60 cycles, four times less than with a clock and a
+// branch of each lane's own.
+__device__ __forceinline__ bool warp_wait(uint64_t *bar, uint32_t parity, volatile int *abort_flag) {
+  if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+  uint64_t t0 = 0;
 #pragma unroll 1
-  for (int i = 0; i < 16; ++i)
-    if (mbar_try_wait(bar, parity)) return true;
-  return mbar_wait(bar, parity, abort_flag);
+  for (uint32_t i = 1;; ++i) {
+    if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+    if ((i & 255u) == 0) {
+      const uint64_t now = global_timer_ns();
+      if (t0 == 0) t0 = now;
+      if (__any_sync(0xffffffffu, *abort_flag != 0 || now - t0 > kWaitLimitNs)) break;
+    }
+  }
+  *abort_flag = 1;
+  return false;
 }
 // D += A B with A in tensor memory (16-bit pairs of one row in a 32-bit column)
 __device__ __forceinline__ void tc_mma_ts(uint32_t tmem_d, uint32_t tmem_a, uint64_t desc_b, uint32_t idesc, uint32_t accumulate) {
@@ -239,8 +270,8 @@ __device__ __forceinline__ int cut_tile(long long x, bool single, int seen) {
 // ---- the kernel ----------------------------------------------------------------------------------------
 template <int HD> struct Shared {
   uint64_t q_full[2], q_empty[2], kv_full[AttSmem<HD>::kStages], kv_empty[AttSmem<HD>::kStages];
-  uint64_t s_full[2], p_half[2], p_ready[2], pv_done[2], item_full[kItemRing], item_empty[kItemRing];
-  uint64_t look[2], join[2], drain[2];
+  uint64_t s_full[2], p_ready[2], pv_done[2], item_full[kItemRing], item_empty[kItemRing];
+  uint64_t look[2], join[2], turn[2], drain[2];
   Item items[kItemRing];
   int bad_page[kItemRing];
   int bad_value[2];                 // step (+ 1) of a stream whose P V the threads add themselves
@@ -338,7 +369,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
       mbar_init(&sh.q_empty[i], 2);
       mbar_init(&sh.drain[i], 1);
       mbar_init(&sh.s_full[i], 1);
-      mbar_init(&sh.p_half[i], 4);
+      mbar_init(&sh.turn[i], 1);
       mbar_init(&sh.p_ready[i], 4);
       mbar_init(&sh.pv_done[i], 1);
       mbar_init(&sh.look[i], 4);
@@ -369,7 +400,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
   if (warp >= 8) asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
   else asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
   // waits of a whole warp, whose lanes go on or give up together
-  auto wait = [&](uint64_t *bar, int parity) { return __all_sync(0xffffffffu, wait_bounded(bar, parity & 1, abort_flag)) != 0; };
+  auto wait = [&](uint64_t *bar, int parity) { return warp_wait(bar, parity & 1, abort_flag); };
 
   if (warp == 9) {
     // ---------------------------------------------------------------- items and copies
@@ -542,9 +573,11 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
   } else if (warp >= 8) {
     // ---------------------------------------------------------------- MMA issue
     // A warp for each stream, so that one's waits and bookkeeping run under the other's products (one warp for both left
-    // the tensor cores idle for half of the time).  The whole warp takes every step and one elected lane issues: operands
-    // that are the same for all lanes are in uniform registers when an MMA needs them there; with one lane walking alone
-    // an MMA took 100 to 150 cycles to issue, twice as long as it runs.
+    // the tensor cores idle for half of the time).  They issue in turn: two streams whose products mix on the tensor cores
+    // finish them at the same time, form their probabilities at the same time, and each pipe idles while the other works.
+    // The whole warp takes every step and one elected lane issues: operands that are the same for all lanes are in uniform
+    // registers when an MMA needs them there; with one lane walking alone an MMA took 100 to 150 cycles to issue, twice as
+    // long as it runs.
     if (warp == 8 || warp == 10) {
       const int w = warp == 8 ? 0 : 1;
       constexpr uint32_t idesc_s = idesc_operands(instr_desc_bf16(kKeys), HALF);
@@ -553,9 +586,8 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
       constexpr int kStages = M::kStages;
       const uint32_t q_s = smem_u32(smem + M::kQ), kv_s = smem_u32(smem + M::kKV);
       const uint32_t t_s = tmem + w * 128, t_o = tmem + 256 + w * 128;
-      uint64_t *s_full = &sh.s_full[w], *p_half = &sh.p_half[w], *p_ready = &sh.p_ready[w], *pv_done = &sh.pv_done[w];
       bool ok = true;
-      int next_slot = 0, stage = 0, phase = 0, step = 0;
+      int next_slot = 0, stage = 0, phase = 0, step = 0, batch = 0;
       uint32_t q_uses = 0;                                            // parity of each query tile's use
       for (int n = 0; ok; ++n) {
         const int slot = n % kItemRing;
@@ -575,54 +607,60 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
           if (paired) ok = wait(&sh.q_full[0], q_uses & 1) && wait(&sh.q_full[1], q_uses >> 1);
           else ok = wait(&sh.q_full[qs], q_uses >> qs);
         }
-        for (int t = t0; ok && t < t1; ++t) {
-          ok = wait(&sh.kv_full[stage], phase);
+        int v_stage = 0;
+        bool by_mma = true;
+        // batch t: the products P V of tile t - 1, then S = Q K^T of tile t
+        for (int t = t0; ok && t0 < t1 && t <= t1; ++t) {
+          if (t < t1) ok = wait(&sh.kv_full[stage], phase);
+          if (ok && t > t0) {
+            ok = wait(&sh.p_ready[w], step);
+            if (ok && t - 1 >= first_masked) by_mma = __shfl_sync(0xffffffffu, *const_cast<volatile int *>(&sh.bad_value[w]), 0) != step + 1;
+            ++step;
+          }
+          if (ok) ok = wait(&sh.turn[w], batch - (w == 0 ? 1 : 0));
           if (!ok) break;
+          ++batch;
           tc_fence_after();
           if (elect_one()) {
-            const uint64_t db = smem_desc(kv_s + stage * M::kStage + half * (64 * HD * 2), 16, HD * 16);
+            if (t > t0) {
+              if (by_mma) {
+                const uint64_t dv = smem_desc(kv_s + v_stage * M::kStage + half * (64 * HD * 2), 1024, HD * 16);
 #pragma unroll
-            for (int k = 0; k < HD / 16; ++k)
-              tc_mma_bf16(t_s, dq + (k >> 2) * (16384 >> 4) + (k & 3) * 2, db + (k >> 2) * (1024 >> 4) + (k & 3) * 2, idesc, k > 0);
-            tc_commit(s_full);
-            tc_commit(&sh.kv_empty[stage]);
-            if (t + 1 == t1) {                                        // (both of a pair's tiles wait for both warps, as both see them)
-              tc_commit(&sh.q_empty[qs]);
-              if (paired) tc_commit(&sh.q_empty[qs ^ 1]);
+                for (int k = 0; k < 4; ++k) tc_mma_ts(t_o, t_s + k * 8, dv + k * (HD * 32 >> 4), idesc_o, k > 0 || t - 1 != t0);
+                if (paired) {
+#pragma unroll
+                  for (int k = 4; k < 8; ++k) tc_mma_ts(t_o, t_s + k * 8, dv + k * (HD * 32 >> 4), idesc_o, true);
+                }
+              }
+              tc_commit(&sh.pv_done[w]);
+              tc_commit(&sh.kv_empty[v_stage]);
             }
-          }
-          __syncwarp();
-          if (++stage == kStages) {
-            stage = 0;
-            phase ^= 1;
-          }
-          const uint64_t dv = smem_desc(kv_s + stage * M::kStage + half * (64 * HD * 2), 1024, HD * 16);
-          ok = wait(&sh.kv_full[stage], phase) && wait(p_half, step);
-          if (!ok) break;
-          tc_fence_after();
-          bool by_mma = true;
-          if (t >= first_masked) by_mma = __shfl_sync(0xffffffffu, *const_cast<volatile int *>(&sh.bad_value[w]), 0) != step + 1;
-          if (by_mma && elect_one()) {
+            if (t < t1) {
+              const uint64_t db = smem_desc(kv_s + stage * M::kStage + half * (64 * HD * 2), 16, HD * 16);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) tc_mma_ts(t_o, t_s + k * 8, dv + k * (HD * 32 >> 4), idesc_o, k > 0 || t != t0);
-          }
-          __syncwarp();
-          ok = wait(p_ready, step);
-          if (!ok) break;
-          tc_fence_after();
-          if (elect_one()) {
-            if (by_mma && paired) {
-#pragma unroll
-              for (int k = 4; k < 8; ++k) tc_mma_ts(t_o, t_s + k * 8, dv + k * (HD * 32 >> 4), idesc_o, true);
+              for (int k = 0; k < HD / 16; ++k)
+                tc_mma_bf16(t_s, dq + (k >> 2) * (16384 >> 4) + (k & 3) * 2, db + (k >> 2) * (1024 >> 4) + (k & 3) * 2, idesc, k > 0);
+              tc_commit(&sh.s_full[w]);
+              tc_commit(&sh.kv_empty[stage]);
+              if (t + 1 == t1) {                                      // (both of a pair's tiles wait for both warps, as both see them)
+                tc_commit(&sh.q_empty[qs]);
+                if (paired) tc_commit(&sh.q_empty[qs ^ 1]);
+              }
             }
-            tc_commit(pv_done);
-            tc_commit(&sh.kv_empty[stage]);
+            mbar_arrive(&sh.turn[w ^ 1]);
           }
           __syncwarp();
-          ++step;
-          if (++stage == kStages) {
-            stage = 0;
-            phase ^= 1;
+          if (t < t1) {                                               // on to the tile's V, and the next K
+            if (++stage == kStages) {
+              stage = 0;
+              phase ^= 1;
+            }
+            ok = wait(&sh.kv_full[stage], phase);
+            v_stage = stage;
+            if (++stage == kStages) {
+              stage = 0;
+              phase ^= 1;
+            }
           }
         }
         if (!ok) break;
@@ -669,27 +707,20 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
         tc_fence_after();
         const bool masked = key0 + n_keys > pos_first + 1;            // some row does not see all of these keys
         if (warp_mine) {
-          uint32_t s[4][32];                     // (blocks 2 and 3 with 128 keys only)
-          tc_ld32(t_s, s[0]);
-          tc_ld32(t_s + 32, s[1]);
-          if (paired) {
-            tc_ld32(t_s + 64, s[2]);
-            tc_ld32(t_s + 96, s[3]);
-          }
-          tc_wait_ld();
-#pragma unroll
-          for (int b = 0; b < 4; ++b) after_wait(s[b]);
+          uint32_t s[128];                       // (the second half with 128 keys only)
+          tc_ld64_wait(t_s, s);
+          if (paired) tc_ld64_wait(t_s + 64, s + 64);
           const int last = pos - key0;           // the row sees elements 0 .. last
           float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
           auto mask_and_max = [&](int b) {
             if (masked) {
 #pragma unroll
               for (int e = 0; e < 32; ++e)
-                if (b * 32 + e > last) s[b][e] = 0xff800000u;
+                if (b * 32 + e > last) s[b * 32 + e] = 0xff800000u;
             }
 #pragma unroll
             for (int e = 0; e < 32; e += 2)
-              top[(e >> 1) & 3] = max3_nan(top[(e >> 1) & 3], __uint_as_float(s[b][e]), __uint_as_float(s[b][e + 1]));
+              top[(e >> 1) & 3] = max3_nan(top[(e >> 1) & 3], __uint_as_float(s[b * 32 + e]), __uint_as_float(s[b * 32 + e + 1]));
           };
           mask_and_max(0);
           mask_and_max(1);
@@ -723,27 +754,23 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
           const float base = m == -INFINITY ? 0.f : m == INFINITY ? NAN : -m * c;
           const float2 c2 = make_float2(c, c), b2 = make_float2(base, base);
           float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-          auto probabilities = [&](int h) {      // of keys 64 h .. 64 h + 63
-            uint32_t p[32];
+          auto probabilities = [&](int from) {   // of 32 keys
+            uint32_t p[16];
 #pragma unroll
-            for (int e = 0; e < 32; ++e) {
-              const int b = 2 * h + (e >> 4), j = 2 * (e & 15);
-              const float2 x = fma2(make_float2(__uint_as_float(s[b][j]), __uint_as_float(s[b][j + 1])), c2, b2);
+            for (int e = 0; e < 16; ++e) {
+              const int j = from + 2 * e;
+              const float2 x = fma2(make_float2(__uint_as_float(s[j]), __uint_as_float(s[j + 1])), c2, b2);
               const float2 y = (e & 7) < kFmaShare ? exp2_by_fma(x) : make_float2(ex2(x.x), ex2(x.y));
               sum[e & 1] = add2(sum[e & 1], y);
               p[e] = cvt16x2(y.x, y.y, HALF);
             }
-            tc_st32(t_s + h * 32, p);
+            tc_st16(t_s + from / 2, p);
           };
           probabilities(0);
+          probabilities(32);
           if (paired) {
-            if (!masked) {                       // the products of the first 64 keys may begin
-              tc_wait_st();
-              tc_fence_before();
-              __syncwarp();
-              if (lane == 0) mbar_arrive(&sh.p_half[w]);
-            }
-            probabilities(1);
+            probabilities(64);
+            probabilities(96);
           }
           l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
           tc_wait_st();
@@ -813,10 +840,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
         }
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) {
-          if (masked || !warp_mine || !paired) mbar_arrive(&sh.p_half[w]);
-          mbar_arrive(&sh.p_ready[w]);
-        }
+        if (lane == 0) mbar_arrive(&sh.p_ready[w]);
         ++steps_done;
       }
       if (!ok) break;

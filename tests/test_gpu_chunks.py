@@ -212,6 +212,7 @@ def test_attention_of_ragged_chunks(B, heads, dtype):
     ((8, 8, 128), [(1, 20000)] * 6 + [(2, 17)]),              # dozens of tiles in a row for each CTA
     ((16, 8, 128), [(300, 6300), (1, 9000), (259, 4500)]),
     ((8, 8, 64), [(1, 30000)] * 5 + [(150, 9000)]),
+    ((64, 8, 128), [(130, 130), (70, 200)] * 5),             # many short items
 ])
 def test_attention_of_long_caches_and_odd_groups(B, heads, seqs, dtype):
     got, want, spread, scores, keys, top = _attention_case(B, heads, dtype, seqs, seed=3)
