@@ -22,8 +22,9 @@
 // fp32 partial results (unnormalised O, maximum, sum) in the workspace, in places that only depend on the CTA, and a second
 // launch joins them in key order: no atomics, equal inputs give equal outputs.
 //
-// A row's reference (the maximum that its exponents are relative to) moves only when the maximum has grown by more than
-// 2^8, so that O is hardly ever rescaled; probabilities then reach 256, which both formats hold.
+// A row's reference (what its exponents are relative to) is its maximum over the item's first tile.  It moves when a tile's
+// probabilities, relative to it, add up to more than 2^13: the maximum has then grown.  So O is hardly ever rescaled, most
+// tiles need no maxima, and a probability is at most 2^13, which both formats hold.
 //
 // What a row does not see has no part in it: masked scores are replaced, not added to.  A masked probability is 0, but
 // 0 times an undefined value would not be: where a tile has keys that only some of its rows see, their values are looked
@@ -53,7 +54,7 @@ constexpr int kAttThreads = 384;
 constexpr int kMaxCtas = 148;                  // CTAs of a launch: sizes the workspace
 constexpr int kItemRing = 4;
 constexpr int kFmaShare = 1;                   // of 8 pairs of exponentials, those that the FMA units compute
-constexpr float kMoveReference = 8.0f;         // log2 of how far a maximum may run ahead of the reference
+constexpr float kMostSum = 8192.0f;            // of a row's probabilities in a tile, before its reference has to move
 
 // Costs that the shares are cut by, in keys of a single item.  A paired item's tile keeps the tensor cores twice as long.
 constexpr int kSingleStart = 256, kPairWeight = 2, kPairStart = 512;
@@ -94,7 +95,7 @@ struct AttendArgs {
 };
 
 // ---- tensor memory and descriptors -----------------------------------------------------------------
-__device__ __forceinline__ void tc_st32(uint32_t taddr, const uint32_t (&r)[32]) {
+__device__ __forceinline__ void tc_st32(uint32_t taddr, const uint32_t *r) {
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
       "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
@@ -103,22 +104,6 @@ __device__ __forceinline__ void tc_st32(uint32_t taddr, const uint32_t (&r)[32])
         "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
         "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
         "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(taddr)
-      : "memory");
-}
-__device__ __forceinline__ void tc_ld16(uint32_t taddr, uint32_t (&r)[16]) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
-      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
-        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-      : "r"(taddr));
-}
-__device__ __forceinline__ void tc_st16(uint32_t taddr, const uint32_t (&r)[16]) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], "
-      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};"
-      ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
-        "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(taddr)
       : "memory");
 }
 __device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
@@ -707,72 +692,75 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
         tc_fence_after();
         const bool masked = key0 + n_keys > pos_first + 1;            // some row does not see all of these keys
         if (warp_mine) {
-          uint32_t s[128];                       // (the second half with 128 keys only)
-          tc_ld64_wait(t_s, s);
-          if (paired) tc_ld64_wait(t_s + 64, s + 64);
+          uint32_t p[64];                        // pairs of probabilities (the second half with 128 keys only)
+          float2 sum[2];
           const int last = pos - key0;           // the row sees elements 0 .. last
-          float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-          auto mask_and_max = [&](int b) {
+          // With the reference as it is, unless the row has none yet: maxima take a quarter of a step's time, and a
+          // reference that is too low shows in the sum.  Where it does, once more with maxima.
+          bool careful = __any_sync(0xffffffffu, mine && m == -INFINITY);
+          auto scores = [&](int half, uint32_t *s) {                   // of 64 keys
+            tc_ld64_wait(t_s + 64 * half, s);
             if (masked) {
 #pragma unroll
-              for (int e = 0; e < 32; ++e)
-                if (b * 32 + e > last) s[b * 32 + e] = 0xff800000u;
+              for (int e = 0; e < 64; ++e)
+                if (64 * half + e > last) s[e] = 0xff800000u;
             }
-#pragma unroll
-            for (int e = 0; e < 32; e += 2)
-              top[(e >> 1) & 3] = max3_nan(top[(e >> 1) & 3], __uint_as_float(s[b * 32 + e]), __uint_as_float(s[b * 32 + e + 1]));
           };
-          mask_and_max(0);
-          mask_and_max(1);
-          if (paired) {
-            mask_and_max(2);
-            mask_and_max(3);
-          }
-          const float now = max_nan(max3_nan(top[0], top[1], top[2]), top[3]);
-          const bool move = mine && !(now <= m || (now - m) * c <= kMoveReference);      // (NaN moves)
-          if (__any_sync(0xffffffffu, move)) {
-            const float to = max_nan(m, now);
-            const float fix = to == m ? 1.0f : ex2((m - to) * c);     // (m = -inf: 0)
-            m = to;
-            l *= fix;
-            if (t != it.t0) {
-              ok = wait(&sh.pv_done[w], steps_done - 1);
-              if (!ok) break;
-              tc_fence_after();
+          while (true) {
+            if (careful) {
+              float to = m;
+#pragma unroll 1
+              for (int half = 0; half < (paired ? 2 : 1); ++half) {
+                uint32_t s[64];
+                scores(half, s);
+                float top[4] = {to, to, to, to};
 #pragma unroll
-              for (int b = 0; b < HD / 16; ++b) {
-                uint32_t o[16];
-                tc_ld16(t_o + b * 16, o);
-                tc_wait_ld();
-                after_wait(o);
+                for (int e = 0; e < 64; e += 2) top[(e >> 1) & 3] = max3_nan(top[(e >> 1) & 3], __uint_as_float(s[e]), __uint_as_float(s[e + 1]));
+                to = max_nan(max3_nan(top[0], top[1], top[2]), top[3]);
+              }
+              const float fix = to == m ? 1.0f : ex2((m - to) * c);   // (m = -inf: 0)
+              m = to;
+              l *= fix;
+              if (t != it.t0) {
+                ok = wait(&sh.pv_done[w], steps_done - 1);
+                if (!ok) break;
+                tc_fence_after();
+#pragma unroll 1
+                for (int b = 0; b < HD / 32; ++b) {
+                  uint32_t o[32];
+                  tc_ld32(t_o + b * 32, o);
+                  tc_wait_ld();
+                  after_wait(o);
 #pragma unroll
-                for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * fix);
-                tc_st16(t_o + b * 16, o);
+                  for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * fix);
+                  tc_st32(t_o + b * 32, o);
+                }
               }
             }
-          }
-          const float base = m == -INFINITY ? 0.f : m == INFINITY ? NAN : -m * c;
-          const float2 c2 = make_float2(c, c), b2 = make_float2(base, base);
-          float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-          auto probabilities = [&](int from) {   // of 32 keys
-            uint32_t p[16];
+            const float base = m == -INFINITY ? 0.f : m == INFINITY ? NAN : -m * c;
+            const float2 c2 = make_float2(c, c), b2 = make_float2(base, base);
+            sum[0] = sum[1] = make_float2(0.f, 0.f);
+            auto probabilities = [&](int half) {
+              uint32_t s[64];
+              scores(half, s);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              const int j = from + 2 * e;
-              const float2 x = fma2(make_float2(__uint_as_float(s[j]), __uint_as_float(s[j + 1])), c2, b2);
-              const float2 y = (e & 7) < kFmaShare ? exp2_by_fma(x) : make_float2(ex2(x.x), ex2(x.y));
-              sum[e & 1] = add2(sum[e & 1], y);
-              p[e] = cvt16x2(y.x, y.y, HALF);
-            }
-            tc_st16(t_s + from / 2, p);
-          };
-          probabilities(0);
-          probabilities(32);
-          if (paired) {
-            probabilities(64);
-            probabilities(96);
+              for (int e = 0; e < 32; ++e) {
+                const float2 x = fma2(make_float2(__uint_as_float(s[2 * e]), __uint_as_float(s[2 * e + 1])), c2, b2);
+                const float2 y = (e & 7) < kFmaShare ? exp2_by_fma(x) : make_float2(ex2(x.x), ex2(x.y));
+                sum[e & 1] = add2(sum[e & 1], y);
+                p[32 * half + e] = cvt16x2(y.x, y.y, HALF);
+              }
+            };
+            probabilities(0);
+            if (paired) probabilities(1);
+            sum[0].x = (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
+            if (careful || !__any_sync(0xffffffffu, mine && !(sum[0].x <= kMostSum))) break;
+            careful = true;
           }
-          l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
+          if (!ok) break;
+          l += sum[0].x;
+          tc_st32(t_s, p);
+          if (paired) tc_st32(t_s + 32, p + 32);
           tc_wait_st();
         }
         // keys that some row of the tile does not see: their values must be finite, or kept out of the products
