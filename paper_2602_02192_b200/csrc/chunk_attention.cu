@@ -14,10 +14,12 @@
 //   single items   one row tile; the streams take 64 keys each of every tile, and their two results are joined at the end
 //                  (few rows: what counts is to keep the copies running)
 // Either way both streams take every key tile in order, so that a barrier's phase is never more than one away from what is
-// waited for.
+// waited for.  A step of a stream is 64 keys, and its S has room for two: S of the next step is formed while this one's
+// probabilities are (with one S of 128 keys the streams' chains bounded everything: 462 us for 2048 tokens over 14336).
 //
-// Work.  An item is (sequence, kv head, pair of row tiles or last single one) with its keys.  Items have very different
-// lengths and the lengths are in device memory, so every CTA (one to an SM) adds up all items' costs, takes its equal share
+// Work.  An item is (sequence, pair of row tiles or last single one, kv head) with its keys, in this order: the CTAs that
+// work on one head's row tiles then do so at about the same time, and its keys come from HBM once (with the heads outside,
+// 40 chunks of 16 to 400 tokens over 200 to 5000 took 413 us).  Items have very different lengths and the lengths are in device memory, so every CTA (one to an SM) adds up all items' costs, takes its equal share
 // of the total, and walks the items in it; an item that crosses a border is cut between two key tiles.  Cut items leave
 // fp32 partial results (unnormalised O, maximum, sum) in the workspace, in places that only depend on the CTA, and a second
 // launch joins them in key order: no atomics, equal inputs give equal outputs.
@@ -53,19 +55,25 @@ constexpr int kPages = kKeys / kChunkPage;
 constexpr int kAttThreads = 384;
 constexpr int kMaxCtas = 148;                  // CTAs of a launch: sizes the workspace
 constexpr int kItemRing = 4;
-constexpr int kFmaShare = 2;                   // of 8 pairs of exponentials, those that the FMA units compute
+constexpr int kFmaShare = 1;                   // of 8 pairs of exponentials, those that the FMA units compute
 constexpr float kMostSum = 8192.0f;            // of a row's probabilities in a tile, before its reference has to move
 
 // Costs that the shares are cut by, in keys of a single item.  A paired item's tile keeps the tensor cores twice as long.
 constexpr int kSingleStart = 256, kPairWeight = 2, kPairStart = 512;
 constexpr int kLeastPart = 1;                  // key tiles
 
-template <int HD> struct AttSmem {
-  static constexpr int kQTile = 128 * HD * 2;
+// FEW: no item has more than 32 rows.  Its query tiles are stored as far as they have rows (what an MMA reads behind them
+// makes rows that nobody reads), and the copies get a stage more.
+constexpr int kFewRows = 32;
+template <int HD, bool FEW> struct AttSmem {
+  static constexpr int kQRows = FEW ? kFewRows : 128;
+  static constexpr int kQHalf = kQRows * 128;                         // 64 elements of every row
+  static constexpr int kQTile = HD / 64 * kQHalf;
   static constexpr int kStage = kKeys * HD * 2;
-  static constexpr int kStages = HD == 128 ? 5 : 8;
-  static constexpr int kQ = 0, kKV = 2 * kQTile, kBars = kKV + kStages * kStage;
-  static constexpr int kTotal = kBars + 3072;
+  static constexpr int kStages = HD == 128 ? (FEW ? 6 : 5) : (FEW ? 11 : 9);
+  static constexpr int kKV = 0, kQ = kStages * kStage, kBars = kQ + 2 * kQTile;      // (an MMA's rows behind Q: no KV stage in use)
+  static constexpr int kReach = kQ + 2 * kQTile - kQHalf + 16384;     // end of what an MMA reads as Q
+  static constexpr int kTotal = (kBars + 3072 > kReach ? kBars + 3072 : kReach);
   static_assert(kTotal <= 227 * 1024, "shared memory");
 };
 
@@ -90,7 +98,7 @@ struct AttendArgs {
   float *part_o;                    // [cta][2][rows_cap][hd]
   float2 *part_ml;                  // [cta][2][rows_cap]: reference in log2 units, sum
   PartRecord *records;
-  int Hq, Hkv, group, tile_tok, n_pages, rows_cap;
+  int Hq, Hkv, group, tile_tok, load_tok /* of a query tile's tokens, those that are loaded */, n_pages, rows_cap;
   bool wide_stores;                 // out begins on a 32-byte boundary
   float scale_log2;
 };
@@ -233,7 +241,7 @@ struct SeqCost {
     if (i == n_items) c += cost(n_items - 1);
     return c;
   }
-  __device__ __forceinline__ long long head() const { return n_items ? before(n_items) : 0; }
+  __device__ __forceinline__ long long all() const { return n_items ? before(n_items) : 0; }
 };
 __device__ __forceinline__ SeqCost seq_cost(const SeqSpan &p, int tile_tok) {
   SeqCost k;
@@ -254,13 +262,14 @@ __device__ __forceinline__ int cut_tile(long long x, bool single, int seen) {
 }
 
 // ---- the kernel ----------------------------------------------------------------------------------------
-template <int HD> struct Shared {
-  uint64_t q_full[2], q_empty[2], kv_full[AttSmem<HD>::kStages], kv_empty[AttSmem<HD>::kStages];
-  uint64_t s_full[2], p_ready[2], pv_done[2], item_full[kItemRing], item_empty[kItemRing];
+template <int HD, bool FEW> struct Shared {
+  uint64_t q_full[2], q_empty[2], kv_full[AttSmem<HD, FEW>::kStages], kv_empty[AttSmem<HD, FEW>::kStages];
+  uint64_t s_full[2][2], p_ready[2][2], pv_done[2],                   // [stream][half of its S] 
+      item_full[kItemRing], item_empty[kItemRing];
   uint64_t look[2], join[2], turn[2], drain[2];
   Item items[kItemRing];
   int bad_page[kItemRing];
-  int bad_value[2];                 // step (+ 1) of a stream whose P V the threads add themselves
+  int bad_value[2][2];              // [stream][half]: step (+ 1) whose P V the threads add themselves
   uint32_t tmem;
   int abort_flag;
   long long total, start;           // plan: cost of everything; cost in front of the CTA's first sequence
@@ -295,14 +304,14 @@ template <int HD> __device__ __forceinline__ uint32_t kv_unit(int key, int c) {
 }
 
 // The total cost, and where this CTA's share begins.
-template <int HD> __device__ __forceinline__ void make_plan(const AttendArgs &a, Shared<HD> &sh) {
+template <int HD, bool FEW> __device__ __forceinline__ void make_plan(const AttendArgs &a, Shared<HD, FEW> &sh) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   constexpr int kWarps = kAttThreads / 32;
   auto cost_of = [&](int s, bool report) -> long long {
     if (s >= a.c.S) return 0;
     const SeqSpan p = seq_span(a.c, s);
     if (report && !p.ok) atomicMax(a.c.status, STATUS_BAD_CHUNK);
-    return seq_cost(p, a.tile_tok).head() * a.Hkv;
+    return seq_cost(p, a.tile_tok).all() * a.Hkv;
   };
   long long mine = 0, first = 0;
   for (int s = threadIdx.x; s < a.c.S; s += kAttThreads) {
@@ -350,14 +359,14 @@ template <int HD> __device__ __forceinline__ void make_plan(const AttendArgs &a,
   }
 }
 
-template <int HD, bool HALF>
+template <int HD, bool HALF, bool FEW>
 __global__ void __launch_bounds__(kAttThreads, 1)
 chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_kv,
                        const __grid_constant__ AttendArgs a) {
-  using M = AttSmem<HD>;
+  using M = AttSmem<HD, FEW>;
   extern __shared__ __align__(1024) uint8_t smem[];
-  Shared<HD> &sh = *reinterpret_cast<Shared<HD> *>(smem + M::kBars);
-  static_assert(sizeof(Shared<HD>) <= 3072, "barriers");
+  Shared<HD, FEW> &sh = *reinterpret_cast<Shared<HD, FEW> *>(smem + M::kBars);
+  static_assert(sizeof(Shared<HD, FEW>) <= 3072, "barriers");
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   volatile int *abort_flag = &sh.abort_flag;
   if (smem_u32(smem) & 1023) {                 // (swizzled tiles need it; a dynamic array alone begins there)
@@ -370,13 +379,15 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
       mbar_init(&sh.q_full[i], 1);
       mbar_init(&sh.q_empty[i], 2);
       mbar_init(&sh.drain[i], 1);
-      mbar_init(&sh.s_full[i], 1);
       mbar_init(&sh.turn[i], 1);
-      mbar_init(&sh.p_ready[i], 4);
+      for (int b = 0; b < 2; ++b) {
+        mbar_init(&sh.s_full[i][b], 1);
+        mbar_init(&sh.p_ready[i][b], 4);
+        sh.bad_value[i][b] = 0;
+      }
       mbar_init(&sh.pv_done[i], 1);
       mbar_init(&sh.look[i], 4);
       mbar_init(&sh.join[i], 8);
-      sh.bad_value[i] = 0;
     }
     for (int i = 0; i < M::kStages; ++i) {
       mbar_init(&sh.kv_full[i], 1);
@@ -391,16 +402,13 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
   }
   if (warp == 8) tc_alloc(&sh.tmem, 512);
   early_start_sync();
-  make_plan<HD>(a, sh);
+  make_plan<HD, FEW>(a, sh);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = sh.tmem;               // S of the streams at columns 0 and 128, O at 256 and 384
   const long long x_begin = sh.total * blockIdx.x / gridDim.x, x_end = sh.total * (blockIdx.x + 1) / gridDim.x;
 
-  // 168 registers a thread at launch (64512 in all): 208 for the two softmax warpgroups, 80 for the third
-  if (warp >= 8) asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
-  else asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
   // waits of a whole warp, whose lanes go on or give up together
   auto wait = [&](uint64_t *bar, int parity) { return warp_wait(bar, parity & 1, abort_flag); };
 
@@ -412,7 +420,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
     int kv_at = 0;                              // position in the ring: stage kv_at % kStages
     bool ok = true;
     const uint32_t q_s = smem_u32(smem + M::kQ), kv_s = smem_u32(smem + M::kKV);
-    const int q_bytes = 2 * HD * a.group * a.tile_tok;
+    const int q_bytes = 2 * HD * a.group * a.load_tok;
     auto publish = [&](const Item &it) {
       const int slot = n_items % kItemRing;
       if (n_items >= kItemRing) ok = wait(&sh.item_empty[slot], (n_items / kItemRing) - 1);
@@ -433,7 +441,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
         mbar_expect_tx(&sh.q_full[slot], q_bytes);
 #pragma unroll
         for (int h = 0; h < HD / 64; ++h)
-          tma_load_3d(&tm_q, &sh.q_full[slot], q_s + slot * M::kQTile + h * 16384, 64 * h, it.head * a.group,
+          tma_load_3d(&tm_q, &sh.q_full[slot], q_s + slot * M::kQTile + h * M::kQHalf, 64 * h, it.head * a.group,
                       it.row0 + tile * a.tile_tok);
       }
       __syncwarp();
@@ -464,20 +472,19 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
           y = 0;
           continue;
         }
-        const long long head_cost = k.head();
-        int head = static_cast<int>(y / head_cost);
-        y -= head * head_cost;
-        // last item that starts at or before y
+        // the last pair of row tiles whose items start at or before y, and the head
         int lo = 0, hi = k.n_items;
         while (hi - lo > 1) {
           const int step = (hi - lo + 31) / 32, at = lo + lane * step;
-          const unsigned m = __ballot_sync(0xffffffffu, at < hi && k.before(at) <= y);
+          const unsigned m = __ballot_sync(0xffffffffu, at < hi && k.before(at) * a.Hkv <= y);
           lo += (31 - __clz(m)) * step;
           hi = min(hi, lo + step);
         }
-        y -= k.before(lo);
+        y -= k.before(lo) * a.Hkv;
+        int head = static_cast<int>(y / k.cost(lo));
+        y -= head * k.cost(lo);
         const int32_t *pages = a.c.page_table + static_cast<int64_t>(seq) * a.c.pt_width;
-        for (int i = lo; head < a.Hkv && left > 0 && ok;) {
+        for (int i = lo; i < k.n_items && left > 0 && ok;) {
           const bool single = k.single(i);
           const long long cost = k.cost(i), take = min(left, cost - y);
           const int seen = k.seen(i), tiles = (seen + kKeys - 1) / kKeys;
@@ -548,9 +555,9 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
           }
           left -= take;
           y = 0;
-          if (++i == k.n_items) {
-            i = 0;
-            ++head;
+          if (++head == a.Hkv) {
+            head = 0;
+            ++i;
           }
         }
         ++seq;
@@ -582,15 +589,22 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
     // long as it runs.
     if (warp == 8 || warp == 10) {
       const int w = warp == 8 ? 0 : 1;
-      constexpr uint32_t idesc_s = idesc_operands(instr_desc_bf16(kKeys), HALF);
+      constexpr uint32_t idesc_s = idesc_operands(instr_desc_bf16(64), HALF);
       constexpr uint32_t idesc_o = idesc_operands(instr_desc_bf16(HD), HALF) | kIdescBMajorMN;
-      constexpr uint32_t idesc_half = idesc_operands(instr_desc_bf16(64), HALF);
       constexpr int kStages = M::kStages;
       const uint32_t q_s = smem_u32(smem + M::kQ), kv_s = smem_u32(smem + M::kKV);
       const uint32_t t_s = tmem + w * 128, t_o = tmem + 256 + w * 128;
       bool ok = true;
-      int next_slot = 0, stage = 0, phase = 0, step = 0, batch = 0;
+      int next_slot = 0, k_stage = 0, k_phase = 0, v_stage = 1, v_phase = 0, step = 0, batch = 0;
       uint32_t q_uses = 0;                                            // parity of each query tile's use
+      // the other stage of the same kind (K, V, K, V, ...)
+      auto next = [&](int &stage, int &phase) {
+        stage += 2;
+        if (stage >= kStages) {
+          stage -= kStages;
+          phase ^= 1;
+        }
+      };
       for (int n = 0; ok; ++n) {
         const int slot = n % kItemRing;
         ok = wait(&sh.item_full[slot], n / kItemRing);
@@ -599,52 +613,54 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
         if (flags & kEnd) break;
         const int t0 = __shfl_sync(0xffffffffu, sh.items[slot].t0, 0), t1 = __shfl_sync(0xffffffffu, sh.items[slot].t1, 0);
         const int pos0 = __shfl_sync(0xffffffffu, sh.items[slot].pos0, 0);
-        const bool paired = (flags & kPaired) != 0;
-        const int qs = paired ? w : next_slot;
-        // keys of a tile that end behind the first row's position: from this tile on
-        const int first_masked = ((pos0 + (paired ? w * a.tile_tok : 0) + 1 - (paired ? kKeys : 64 * (w + 1))) >> 7) + 1;
+        const bool paired = !FEW && (flags & kPaired) != 0;
+        const int qs = paired ? w : next_slot, steps = paired ? 2 * (t1 - t0) : t1 - t0;
+        // the first step with keys behind the first row's position
+        const int clear = pos0 + (paired ? w * a.tile_tok : 0) + 1 - t0 * kKeys - (paired ? 0 : 64 * w);
+        const int first_masked = paired ? clear >> 6 : clear < 64 ? 0 : ((clear - 64) >> 7) + 1;
         const uint64_t dq = smem_desc(q_s + qs * M::kQTile, 16, 1024);
-        const uint32_t idesc = paired ? idesc_s : idesc_half, half = paired ? 0 : w;
-        if (t0 < t1) {                                                // (both tiles' uses are seen by both warps)
+        if (steps > 0) {                                              // (both tiles' uses are seen by both warps)
           if (paired) ok = wait(&sh.q_full[0], q_uses & 1) && wait(&sh.q_full[1], q_uses >> 1);
           else ok = wait(&sh.q_full[qs], q_uses >> qs);
         }
-        int v_stage = 0;
-        bool by_mma = true;
-        // batch t: the products P V of tile t - 1, then S = Q K^T of tile t
-        for (int t = t0; ok && t0 < t1 && t <= t1; ++t) {
-          if (t < t1) ok = wait(&sh.kv_full[stage], phase);
-          if (ok && t > t0) {
-            ok = wait(&sh.p_ready[w], step);
-            if (ok && t - 1 >= first_masked) by_mma = __shfl_sync(0xffffffffu, *const_cast<volatile int *>(&sh.bad_value[w]), 0) != step + 1;
-            ++step;
+        // batch i: the products P V of step i - ahead, then S = Q K^T of step i.  (Single items wait for memory: a K tile that
+        // is needed early would have to be loaded in place of a later one.)
+        const int ahead = paired ? 2 : 1;
+        for (int i = 0; ok && steps > 0 && i < steps + ahead; ++i) {
+          const int half = paired ? i & 1 : w;                        // (of pairs, steps i and i - 2 are the same half)
+          const bool open = !paired || half == 0, close = !paired || half == 1;      // first and last use of a tile
+          if (i < steps && open) ok = wait(&sh.kv_full[k_stage], k_phase);
+          bool by_mma = true;
+          if (ok && i >= ahead) {
+            if (open) ok = wait(&sh.kv_full[v_stage], v_phase);
+            if (ok) ok = wait(&sh.p_ready[w][step & 1], step >> 1);
+            if (ok && i - ahead >= first_masked)
+              by_mma = __shfl_sync(0xffffffffu, *const_cast<volatile int *>(&sh.bad_value[w][step & 1]), 0) != step + 1;
           }
           if (ok) ok = wait(&sh.turn[w], batch - (w == 0 ? 1 : 0));
           if (!ok) break;
           ++batch;
           tc_fence_after();
+          const int q_buf = (i < ahead ? step + i : step + ahead) & 1;
+          const uint32_t t_p = t_s + (step & 1) * 64, t_q = t_s + q_buf * 64;
           if (elect_one()) {
-            if (t > t0) {
+            if (i >= ahead) {
               if (by_mma) {
                 const uint64_t dv = smem_desc(kv_s + v_stage * M::kStage + half * (64 * HD * 2), 1024, HD * 16);
 #pragma unroll
-                for (int k = 0; k < 4; ++k) tc_mma_ts(t_o, t_s + k * 8, dv + k * (HD * 32 >> 4), idesc_o, k > 0 || t - 1 != t0);
-                if (paired) {
-#pragma unroll
-                  for (int k = 4; k < 8; ++k) tc_mma_ts(t_o, t_s + k * 8, dv + k * (HD * 32 >> 4), idesc_o, true);
-                }
+                for (int k = 0; k < 4; ++k) tc_mma_ts(t_o, t_p + k * 8, dv + k * (HD * 32 >> 4), idesc_o, k > 0 || i != ahead);
               }
               tc_commit(&sh.pv_done[w]);
-              tc_commit(&sh.kv_empty[v_stage]);
+              if (close) tc_commit(&sh.kv_empty[v_stage]);
             }
-            if (t < t1) {
-              const uint64_t db = smem_desc(kv_s + stage * M::kStage + half * (64 * HD * 2), 16, HD * 16);
+            if (i < steps) {
+              const uint64_t db = smem_desc(kv_s + k_stage * M::kStage + half * (64 * HD * 2), 16, HD * 16);
 #pragma unroll
               for (int k = 0; k < HD / 16; ++k)
-                tc_mma_bf16(t_s, dq + (k >> 2) * (16384 >> 4) + (k & 3) * 2, db + (k >> 2) * (1024 >> 4) + (k & 3) * 2, idesc, k > 0);
-              tc_commit(&sh.s_full[w]);
-              tc_commit(&sh.kv_empty[stage]);
-              if (t + 1 == t1) {                                      // (both of a pair's tiles wait for both warps, as both see them)
+                tc_mma_bf16(t_q, dq + (k >> 2) * (M::kQHalf >> 4) + (k & 3) * 2, db + (k >> 2) * (1024 >> 4) + (k & 3) * 2, idesc_s, k > 0);
+              tc_commit(&sh.s_full[w][q_buf]);
+              if (close) tc_commit(&sh.kv_empty[k_stage]);
+              if (i + 1 == steps) {                                   // (both of a pair's tiles wait for both warps, as both see them)
                 tc_commit(&sh.q_empty[qs]);
                 if (paired) tc_commit(&sh.q_empty[qs ^ 1]);
               }
@@ -652,21 +668,14 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             mbar_arrive(&sh.turn[w ^ 1]);
           }
           __syncwarp();
-          if (t < t1) {                                               // on to the tile's V, and the next K
-            if (++stage == kStages) {
-              stage = 0;
-              phase ^= 1;
-            }
-            ok = wait(&sh.kv_full[stage], phase);
-            v_stage = stage;
-            if (++stage == kStages) {
-              stage = 0;
-              phase ^= 1;
-            }
+          if (i >= ahead) {
+            ++step;
+            if (close) next(v_stage, v_phase);
           }
+          if (i < steps && close) next(k_stage, k_phase);
         }
         if (!ok) break;
-        if (t0 < t1) {
+        if (steps > 0) {
           q_uses ^= paired ? 3u : 1u << qs;
           if (!paired) next_slot ^= 1;
         }
@@ -685,10 +694,10 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
     // ---------------------------------------------------------------- softmax and results
     const int w = warp >> 2, row = (warp & 3) * 32 + lane, wg_tid = threadIdx.x & 127;
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
-    const uint32_t t_s = tmem + lanes + w * 128, t_o = tmem + lanes + 256 + w * 128;
+    const uint32_t t_s0 = tmem + lanes + w * 128, t_o = tmem + lanes + 256 + w * 128;
     const float c = a.scale_log2;
     const int tok = row / a.group, rep = row % a.group;
-    int n_item = 0, steps_done = 0, looks = 0, joins = 0;        // (steps: key tiles of all items so far)
+    int n_item = 0, steps_done = 0, tiles_done = 0, looks = 0, joins = 0;
     bool ok = true;
     while (ok) {
       const int slot = n_item % kItemRing;
@@ -696,49 +705,43 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
       if (!ok) break;
       const Item it = sh.items[slot];
       if (it.flags & kEnd) break;
-      const bool paired = it.flags & kPaired;
-      const int row_tile = paired ? w : 0, key_off = paired ? 0 : 64 * w, n_keys = paired ? kKeys : 64;
+      const bool paired = !FEW && (it.flags & kPaired);
+      const int row_tile = paired ? w : 0, steps = (it.t1 - it.t0) * (paired ? 2 : 1);
       const int tok0 = row_tile * a.tile_tok, n_tok = min(a.tile_tok, it.n_tok - tok0);      // (may be <= 0: no rows)
       const int pos_first = it.pos0 + tok0, pos = pos_first + tok;
       const bool mine = row < n_tok * a.group, warp_mine = (warp & 3) * 32 < n_tok * a.group;
       float m = -INFINITY, l = 0.f;              // reference (score units) and sum
-      for (int t = it.t0; t < it.t1; ++t) {
-        const int key0 = t * kKeys + key_off;
-        ok = wait(&sh.s_full[w], steps_done);
+      for (int i = 0; i < steps; ++i) {          // of 64 keys
+        const int tile = paired ? i >> 1 : i, key_off = 64 * (paired ? i & 1 : w), key0 = (it.t0 + tile) * kKeys + key_off;
+        const int buf = steps_done & 1;
+        const uint32_t t_s = t_s0 + 64 * buf;
+        ok = wait(&sh.s_full[w][buf], steps_done >> 1);
         if (!ok) break;
         tc_fence_after();
-        const bool masked = key0 + n_keys > pos_first + 1;            // some row does not see all of these keys
+        const bool masked = key0 + 64 > pos_first + 1;                // some row does not see all of these keys
         if (warp_mine) {
-          uint32_t p[64];                        // pairs of probabilities (the second half with 128 keys only)
+          uint32_t s[64], p[32];
           float2 sum[2];
-          const int last = pos - key0;           // the row sees elements 0 .. last
+          tc_ld64_wait(t_s, s);
+          if (masked) {
+            const int last = pos - key0;         // the row sees elements 0 .. last
+#pragma unroll
+            for (int e = 0; e < 64; ++e)
+              if (e > last) s[e] = 0xff800000u;
+          }
           // With the reference as it is, unless the row has none yet: maxima take a quarter of a step's time, and a
           // reference that is too low shows in the sum.  Where it does, once more with maxima.
           bool careful = __any_sync(0xffffffffu, mine && m == -INFINITY);
-          auto scores = [&](int half, uint32_t *s) {                   // of 64 keys
-            tc_ld64_wait(t_s + 64 * half, s);
-            if (masked) {
-#pragma unroll
-              for (int e = 0; e < 64; ++e)
-                if (64 * half + e > last) s[e] = 0xff800000u;
-            }
-          };
           while (true) {
             if (careful) {
-              float to = m;
-#pragma unroll 1
-              for (int half = 0; half < (paired ? 2 : 1); ++half) {
-                uint32_t s[64];
-                scores(half, s);
-                float top[4] = {to, to, to, to};
+              float top[4] = {m, m, m, m};
 #pragma unroll
-                for (int e = 0; e < 64; e += 2) top[(e >> 1) & 3] = max3_nan(top[(e >> 1) & 3], __uint_as_float(s[e]), __uint_as_float(s[e + 1]));
-                to = max_nan(max3_nan(top[0], top[1], top[2]), top[3]);
-              }
+              for (int e = 0; e < 64; e += 2) top[(e >> 1) & 3] = max3_nan(top[(e >> 1) & 3], __uint_as_float(s[e]), __uint_as_float(s[e + 1]));
+              const float to = max_nan(max3_nan(top[0], top[1], top[2]), top[3]);
               const float fix = to == m ? 1.0f : ex2((m - to) * c);   // (m = -inf: 0)
               m = to;
               l *= fix;
-              if (t != it.t0) {
+              if (i > 0) {
                 ok = wait(&sh.pv_done[w], steps_done - 1);
                 if (!ok) break;
                 tc_fence_after();
@@ -757,19 +760,13 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             const float base = m == -INFINITY ? 0.f : m == INFINITY ? NAN : -m * c;
             const float2 c2 = make_float2(c, c), b2 = make_float2(base, base);
             sum[0] = sum[1] = make_float2(0.f, 0.f);
-            auto probabilities = [&](int half) {
-              uint32_t s[64];
-              scores(half, s);
 #pragma unroll
-              for (int e = 0; e < 32; ++e) {
-                const float2 x = fma2(make_float2(__uint_as_float(s[2 * e]), __uint_as_float(s[2 * e + 1])), c2, b2);
-                const float2 y = (e & 7) < kFmaShare ? exp2_by_fma(x) : make_float2(ex2(x.x), ex2(x.y));
-                sum[e & 1] = add2(sum[e & 1], y);
-                p[32 * half + e] = cvt16x2(y.x, y.y, HALF);
-              }
-            };
-            probabilities(0);
-            if (paired) probabilities(1);
+            for (int e = 0; e < 32; ++e) {
+              const float2 x = fma2(make_float2(__uint_as_float(s[2 * e]), __uint_as_float(s[2 * e + 1])), c2, b2);
+              const float2 y = (e & 7) < kFmaShare ? exp2_by_fma(x) : make_float2(ex2(x.x), ex2(x.y));
+              sum[e & 1] = add2(sum[e & 1], y);
+              p[e] = cvt16x2(y.x, y.y, HALF);
+            }
             sum[0].x = (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
             if (careful || !__any_sync(0xffffffffu, mine && !(sum[0].x <= kMostSum))) break;
             careful = true;
@@ -777,15 +774,14 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
           if (!ok) break;
           l += sum[0].x;
           tc_st32(t_s, p);
-          if (paired) tc_st32(t_s + 32, p + 32);
           tc_wait_st();
         }
         // keys that some row of the tile does not see: their values must be finite, or kept out of the products
-        const int ks = max(0, pos_first + 1 - key0), ke = min(n_keys, it.seen_end - key0);
+        const int ks = max(0, pos_first + 1 - key0), ke = min(64, it.seen_end - key0);
         const int ke16 = (ke + 15) & ~15;
         bool slow = false;
         if (masked && ke > 0 && (ks < ke || ke < ke16)) {
-          const int at = 2 * steps_done + 1, stage = at % M::kStages;
+          const int at = 2 * (tiles_done + tile) + 1, stage = at % M::kStages;
           ok = wait(&sh.kv_full[stage], at / M::kStages);
           if (!ok) break;
           uint8_t *v = smem + M::kKV + stage * M::kStage;
@@ -798,16 +794,16 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
           }
           fence_proxy_async();
           if (ks < ke) {
-            if (bad) *const_cast<volatile int *>(&sh.bad_value[w]) = steps_done + 1;
+            if (bad) *const_cast<volatile int *>(&sh.bad_value[w][buf]) = steps_done + 1;
             __syncwarp();
             if (lane == 0) mbar_arrive(&sh.look[w]);
             ok = wait(&sh.look[w], looks);
             if (!ok) break;
             ++looks;
-            slow = *const_cast<volatile int *>(&sh.bad_value[w]) == steps_done + 1;
+            slow = *const_cast<volatile int *>(&sh.bad_value[w][buf]) == steps_done + 1;
           }
           if (slow && warp_mine) {
-            if (t != it.t0) ok = wait(&sh.pv_done[w], steps_done - 1);
+            if (i > 0) ok = wait(&sh.pv_done[w], steps_done - 1);
             if (!ok) break;
             tc_fence_after();
             const int last = pos - key0;
@@ -817,11 +813,11 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
               tc_ld32(t_o + b * 32, o);
               tc_wait_ld();
               after_wait(o);
-              if (t == it.t0)
+              if (i == 0)
 #pragma unroll
                 for (int e = 0; e < 32; ++e) o[e] = 0u;
 #pragma unroll 1
-              for (int key = 0; key < n_keys; ++key) {
+              for (int key = 0; key < 64; ++key) {
                 const float2 pp = widen16x2(tc_ld1(t_s + (key >> 1)), HALF);
                 const float p = (key & 1) ? pp.y : pp.x;
                 __syncwarp();
@@ -845,13 +841,15 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
         }
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&sh.p_ready[w]);
+        if (lane == 0) mbar_arrive(&sh.p_ready[w][buf]);
         ++steps_done;
       }
       if (!ok) break;
       // ---- the item's result: whole rows, or a part for the joining launch
       if (it.t0 < it.t1) {
-        ok = wait(&sh.pv_done[w], steps_done - 1);
+        // one after the other: the products of the last two steps may both be under way, and a phase is known by its parity
+        if (steps > 1) ok = wait(&sh.pv_done[w], steps_done - 2);
+        if (ok) ok = wait(&sh.pv_done[w], steps_done - 1);
         if (!ok) break;
       }
       tc_fence_after();
@@ -936,6 +934,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
       __syncwarp();
       if (lane == 0) mbar_arrive(&sh.item_empty[slot]);
       ++n_item;
+      tiles_done += it.t1 - it.t0;
     }
     if (!ok) *abort_flag = 1;
   }
@@ -1014,12 +1013,12 @@ int rows_cap(int max_chunk, int group) {
   return max_chunk > tile_tok ? 256 : (max_chunk * group + 7) / 8 * 8;
 }
 
-template <int HD, bool HALF>
+template <int HD, bool HALF, bool FEW>
 cudaError_t launch_attend(const CUtensorMap &tm_q, const CUtensorMap &tm_kv, const AttendArgs &a, int ctas, cudaStream_t s) {
-  cudaError_t e = cudaFuncSetAttribute(chunk_attention_kernel<HD, HALF>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                       AttSmem<HD>::kTotal);
+  constexpr int smem = AttSmem<HD, FEW>::kTotal;
+  cudaError_t e = cudaFuncSetAttribute(chunk_attention_kernel<HD, HALF, FEW>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
-  e = launch_early(chunk_attention_kernel<HD, HALF>, dim3(ctas), dim3(kAttThreads), AttSmem<HD>::kTotal, s, tm_q, tm_kv, a);
+  e = launch_early(chunk_attention_kernel<HD, HALF, FEW>, dim3(ctas), dim3(kAttThreads), smem, s, tm_q, tm_kv, a);
   if (e != cudaSuccess) return e;
   return launch_early(join_parts_kernel<HD, HALF>, dim3(ctas, a.rows_cap / 8), dim3(256), 0, s, a, ctas);
 }
@@ -1062,6 +1061,8 @@ int echo_chunk_attention(const void *q, int64_t q_stride, const void *kv_pool, i
   a.group = Hq / Hkv;
   a.wide_stores = (reinterpret_cast<uintptr_t>(out) & 31) == 0;
   a.tile_tok = 128 / a.group;
+  const bool few = static_cast<int64_t>(a.c.max_chunk) * a.group <= kFewRows;
+  a.load_tok = few ? kFewRows / a.group : a.tile_tok;
   a.n_pages = n_pages;
   a.rows_cap = rows_cap(a.c.max_chunk, a.group);
   a.scale_log2 = 1.4426950408889634f / std::sqrt(static_cast<float>(hd));
@@ -1078,7 +1079,7 @@ int echo_chunk_attention(const void *q, int64_t q_stride, const void *kv_pool, i
   // queries: 64 elements of a head x the heads of a group x the tokens of a tile
   const cuuint64_t qd[3] = {static_cast<cuuint64_t>(hd), static_cast<cuuint64_t>(Hq), static_cast<cuuint64_t>(a.c.n_rows)};
   const cuuint64_t qst[2] = {static_cast<cuuint64_t>(hd) * 2, static_cast<cuuint64_t>(q_stride) * 2};
-  const cuuint32_t qb[3] = {64, static_cast<cuuint32_t>(a.group), static_cast<cuuint32_t>(a.tile_tok)};
+  const cuuint32_t qb[3] = {64, static_cast<cuuint32_t>(a.group), static_cast<cuuint32_t>(a.load_tok)};
   // the pool in groups of eight rows, each read as 64-element halves: 64 elements x 8 rows x halves x the two groups of a
   // page's K (or V) lie in shared memory as [group][half][row], so that operands have one stride from group to group
   const cuuint64_t kd[4] = {64, 8, static_cast<cuuint64_t>(hd / 64), static_cast<cuuint64_t>(n_pages) * Hkv * 4};
@@ -1087,8 +1088,11 @@ int echo_chunk_attention(const void *q, int64_t q_stride, const void *kv_pool, i
   if (!make_map(&tm_q, 3, q, half, qd, qst, qb) || !make_map(&tm_kv, 4, kv_pool, half, kd, kst, kb)) return ECHO_ERR_CUDA;
   const int ctas = std::min(sms, kMaxCtas);
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-  const cudaError_t e = hd == 128 ? (half ? launch_attend<128, true>(tm_q, tm_kv, a, ctas, s) : launch_attend<128, false>(tm_q, tm_kv, a, ctas, s))
-                                  : (half ? launch_attend<64, true>(tm_q, tm_kv, a, ctas, s) : launch_attend<64, false>(tm_q, tm_kv, a, ctas, s));
+  const auto launch = hd == 128 ? (half ? (few ? launch_attend<128, true, true> : launch_attend<128, true, false>)
+                                        : (few ? launch_attend<128, false, true> : launch_attend<128, false, false>))
+                                : (half ? (few ? launch_attend<64, true, true> : launch_attend<64, true, false>)
+                                        : (few ? launch_attend<64, false, true> : launch_attend<64, false, false>));
+  const cudaError_t e = launch(tm_q, tm_kv, a, ctas, s);
   return e == cudaSuccess ? ECHO_OK : ECHO_ERR_CUDA;
 }
 
