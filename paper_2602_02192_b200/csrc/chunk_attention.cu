@@ -17,9 +17,9 @@
 // waited for.  A step of a stream is 64 keys, and its S has room for two: S of the next step is formed while this one's
 // probabilities are (with one S of 128 keys the streams' chains bounded everything: 462 us for 2048 tokens over 14336).
 //
-// Work.  An item is (sequence, pair of row tiles or last single one, kv head) with its keys, in this order: the CTAs that
-// work on one head's row tiles then do so at about the same time, and its keys come from HBM once (with the heads outside,
-// 40 chunks of 16 to 400 tokens over 200 to 5000 took 413 us).  Items have very different lengths and the lengths are in device memory, so every CTA (one to an SM) adds up all items' costs, takes its equal share
+// Work.  An item is (sequence, kv head, pair of row tiles or last single one) with its keys.  Every other item of a head
+// takes its key tiles from the last to the first: they are the ones that L2 still holds, where the caches that 148 CTAs
+// read at once do not fit (40 chunks of 16 to 400 tokens over 200 to 5000).  Items have very different lengths and the lengths are in device memory, so every CTA (one to an SM) adds up all items' costs, takes its equal share
 // of the total, and walks the items in it; an item that crosses a border is cut between two key tiles.  Cut items leave
 // fp32 partial results (unnormalised O, maximum, sum) in the workspace, in places that only depend on the CTA, and a second
 // launch joins them in key order: no atomics, equal inputs give equal outputs.
@@ -82,6 +82,7 @@ struct Item {
   int t0, t1, seen_end, flags;      // key tiles [t0, t1); no row sees key seen_end or a later one
 };
 constexpr int kPaired = 1, kEnd = 2, kPartLater = 4, kPartFirst = 8;      // parts of a cut item: a later one, the first
+constexpr int kBackwards = 16;                                            // the tiles from the last to the first
 
 // What a CTA says of its (at most two) partial results to the joining launch.
 struct PartRecord {
@@ -241,7 +242,7 @@ struct SeqCost {
     if (i == n_items) c += cost(n_items - 1);
     return c;
   }
-  __device__ __forceinline__ long long all() const { return n_items ? before(n_items) : 0; }
+  __device__ __forceinline__ long long head() const { return n_items ? before(n_items) : 0; }
 };
 __device__ __forceinline__ SeqCost seq_cost(const SeqSpan &p, int tile_tok) {
   SeqCost k;
@@ -311,7 +312,7 @@ template <int HD, bool FEW> __device__ __forceinline__ void make_plan(const Atte
     if (s >= a.c.S) return 0;
     const SeqSpan p = seq_span(a.c, s);
     if (report && !p.ok) atomicMax(a.c.status, STATUS_BAD_CHUNK);
-    return seq_cost(p, a.tile_tok).all() * a.Hkv;
+    return seq_cost(p, a.tile_tok).head() * a.Hkv;
   };
   long long mine = 0, first = 0;
   for (int s = threadIdx.x; s < a.c.S; s += kAttThreads) {
@@ -401,6 +402,10 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
     mbar_fence_init();
   }
   if (warp == 8) tc_alloc(&sh.tmem, 512);
+  if (warp == 9 && lane == 0) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tm_q)) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tm_kv)) : "memory");
+  }
   early_start_sync();
   make_plan<HD, FEW>(a, sh);
   tc_fence_before();
@@ -417,7 +422,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
     PartRecord rec = {};
     int n_items = 0;                            // published
     int q_uses0 = 0, q_uses1 = 0, next_slot = 0;
-    int kv_at = 0;                              // position in the ring: stage kv_at % kStages
+    int kv_at = 0, ring = 0, ring_use = 0;      // stages loaded; the next one, and how often it was used
     bool ok = true;
     const uint32_t q_s = smem_u32(smem + M::kQ), kv_s = smem_u32(smem + M::kKV);
     const int q_bytes = 2 * HD * a.group * a.load_tok;
@@ -437,7 +442,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
       const int uses = slot ? q_uses1 : q_uses0;
       if (ok && uses > 0) ok = wait(&sh.q_empty[slot], uses - 1);
       if (!ok) return;
-      if (lane == 0) {
+      if (elect_one()) {
         mbar_expect_tx(&sh.q_full[slot], q_bytes);
 #pragma unroll
         for (int h = 0; h < HD / 64; ++h)
@@ -472,19 +477,20 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
           y = 0;
           continue;
         }
-        // the last pair of row tiles whose items start at or before y, and the head
+        const long long head_cost = k.head();
+        int head = static_cast<int>(y / head_cost);
+        y -= head * head_cost;
+        // last item that starts at or before y
         int lo = 0, hi = k.n_items;
         while (hi - lo > 1) {
           const int step = (hi - lo + 31) / 32, at = lo + lane * step;
-          const unsigned m = __ballot_sync(0xffffffffu, at < hi && k.before(at) * a.Hkv <= y);
+          const unsigned m = __ballot_sync(0xffffffffu, at < hi && k.before(at) <= y);
           lo += (31 - __clz(m)) * step;
           hi = min(hi, lo + step);
         }
-        y -= k.before(lo) * a.Hkv;
-        int head = static_cast<int>(y / k.cost(lo));
-        y -= head * k.cost(lo);
+        y -= k.before(lo);
         const int32_t *pages = a.c.page_table + static_cast<int64_t>(seq) * a.c.pt_width;
-        for (int i = lo; i < k.n_items && left > 0 && ok;) {
+        for (int i = lo; head < a.Hkv && left > 0 && ok;) {
           const bool single = k.single(i);
           const long long cost = k.cost(i), take = min(left, cost - y);
           const int seen = k.seen(i), tiles = (seen + kKeys - 1) / kKeys;
@@ -496,7 +502,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
           it.head = head;
           it.pos0 = k.base + i * k.step;
           it.seen_end = seen;
-          it.flags = single ? 0 : kPaired;
+          it.flags = (single ? 0 : kPaired) | (i & 1 ? kBackwards : 0);
           if (it.t0 > 0) it.flags |= kPartLater;
           else if (it.t1 < tiles) it.flags |= kPartFirst;
           const bool none = tiles == 0 && y == 0;                    // rows that see nothing: zeros
@@ -520,14 +526,16 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                 load_q(it, 0, 0);
                 load_q(it, 1, 1);
               }
+              const bool back = it.flags & kBackwards;
               int ids = 0, ids_next = 0, block = -1;
               const int n_need = (seen + kChunkPage - 1) / kChunkPage;
-              auto fetch = [&](int b) { return 32 * b + lane < n_need ? pages[32 * b + lane] : -1; };
-              for (int t = it.t0; t < it.t1 && ok; ++t) {
+              auto fetch = [&](int b) { return b >= 0 && 32 * b + lane < n_need ? pages[32 * b + lane] : -1; };
+              for (int n = it.t0; n < it.t1 && ok; ++n) {
+                const int t = back ? it.t0 + it.t1 - 1 - n : n;
                 if (block != t / 4) {
                   ids = block < 0 ? fetch(t / 4) : ids_next;
                   block = t / 4;
-                  ids_next = fetch(block + 1);
+                  ids_next = fetch(back ? block - 1 : block + 1);
                 }
                 const int id = __shfl_sync(0xffffffffu, ids, (t & 3) * 8 + (lane & 7));
                 const bool need = t * kPages + (lane & 7) < n_need, valid = need && id >= 0 && id < a.n_pages;
@@ -537,27 +545,36 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                 }
                 // a page that nothing sees, or that does not exist, reads as zeros
                 const int unit = valid ? (id * a.Hkv + it.head) * 4 : a.n_pages * a.Hkv * 4;
+                // one lane issues, from coordinates that all lanes hold: copies from eight lanes' own coordinates take
+                // three times as long to issue, and then bound the whole (1900 cycles a tile)
+                int units[kPages];
+#pragma unroll
+                for (int j = 0; j < kPages; ++j) units[j] = __shfl_sync(0xffffffffu, unit, j);
 #pragma unroll
                 for (int kv = 0; kv < 2; ++kv) {
-                  const int stage = kv_at % M::kStages, use = kv_at / M::kStages;
-                  if (use > 0) ok = wait(&sh.kv_empty[stage], use - 1);
+                  if (ring_use > 0) ok = wait(&sh.kv_empty[ring], ring_use - 1);
                   if (!ok) break;
-                  if (lane == 0) mbar_expect_tx(&sh.kv_full[stage], M::kStage);
-                  __syncwarp();
-                  if (lane < 8)
-                    tma_load_4d(&tm_kv, &sh.kv_full[stage], kv_s + stage * M::kStage + lane * (M::kStage / kPages), 0, 0, 0,
-                                unit + 2 * kv);
+                  if (elect_one()) {
+                    mbar_expect_tx(&sh.kv_full[ring], M::kStage);
+#pragma unroll
+                    for (int j = 0; j < kPages; ++j)
+                      tma_load_4d(&tm_kv, &sh.kv_full[ring], kv_s + ring * M::kStage + j * (M::kStage / kPages), 0, 0, 0, units[j] + 2 * kv);
+                  }
                   __syncwarp();
                   ++kv_at;
+                  if (++ring == M::kStages) {
+                    ring = 0;
+                    ++ring_use;
+                  }
                 }
               }
             }
           }
           left -= take;
           y = 0;
-          if (++head == a.Hkv) {
-            head = 0;
-            ++i;
+          if (++i == k.n_items) {
+            i = 0;
+            ++head;
           }
         }
         ++seq;
@@ -615,9 +632,12 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
         const int pos0 = __shfl_sync(0xffffffffu, sh.items[slot].pos0, 0);
         const bool paired = !FEW && (flags & kPaired) != 0;
         const int qs = paired ? w : next_slot, steps = paired ? 2 * (t1 - t0) : t1 - t0;
-        // the first step with keys behind the first row's position
-        const int clear = pos0 + (paired ? w * a.tile_tok : 0) + 1 - t0 * kKeys - (paired ? 0 : 64 * w);
-        const int first_masked = paired ? clear >> 6 : clear < 64 ? 0 : ((clear - 64) >> 7) + 1;
+        // of the stream's steps, those that may be added by the threads: with keys behind the first row's position
+        const int pos_first = pos0 + (paired ? w * a.tile_tok : 0);
+        auto masked = [&](int i) {
+          const int tile = paired ? i >> 1 : i, key0 = (flags & kBackwards ? t1 - 1 - tile : t0 + tile) * kKeys + 64 * (paired ? i & 1 : w);
+          return key0 + 64 > pos_first + 1;
+        };
         const uint64_t dq = smem_desc(q_s + qs * M::kQTile, 16, 1024);
         if (steps > 0) {                                              // (both tiles' uses are seen by both warps)
           if (paired) ok = wait(&sh.q_full[0], q_uses & 1) && wait(&sh.q_full[1], q_uses >> 1);
@@ -634,7 +654,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
           if (ok && i >= ahead) {
             if (open) ok = wait(&sh.kv_full[v_stage], v_phase);
             if (ok) ok = wait(&sh.p_ready[w][step & 1], step >> 1);
-            if (ok && i - ahead >= first_masked)
+            if (ok && masked(i - ahead))
               by_mma = __shfl_sync(0xffffffffu, *const_cast<volatile int *>(&sh.bad_value[w][step & 1]), 0) != step + 1;
           }
           if (ok) ok = wait(&sh.turn[w], batch - (w == 0 ? 1 : 0));
@@ -712,7 +732,8 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
       const bool mine = row < n_tok * a.group, warp_mine = (warp & 3) * 32 < n_tok * a.group;
       float m = -INFINITY, l = 0.f;              // reference (score units) and sum
       for (int i = 0; i < steps; ++i) {          // of 64 keys
-        const int tile = paired ? i >> 1 : i, key_off = 64 * (paired ? i & 1 : w), key0 = (it.t0 + tile) * kKeys + key_off;
+        const int tile = paired ? i >> 1 : i, key_off = 64 * (paired ? i & 1 : w);
+        const int key0 = (it.flags & kBackwards ? it.t1 - 1 - tile : it.t0 + tile) * kKeys + key_off;
         const int buf = steps_done & 1;
         const uint32_t t_s = t_s0 + 64 * buf;
         ok = wait(&sh.s_full[w][buf], steps_done >> 1);
