@@ -32,7 +32,9 @@
 // 0 times an undefined value would not be: where a tile has keys that only some of its rows see, their values are looked
 // at, and a tile with an infinity or a NaN among them is accumulated by the threads instead (slow, and nothing else).
 //
-// Roles: warps 0-3 and 4-7 the two streams' softmax, warps 8 and 10 issue their MMAs, warp 9 walks the items and loads.
+// Roles: warps 0-7 and 8-15 the two streams' softmax, warps 16 and 18 issue their MMAs, warp 17 walks the items and loads.
+// A softmax warp has 16 rows, four threads to a row: with 32 rows to a warp and a thread to a row two warps shared a
+// scheduler, and what one waited for the other could not fill (2048 tokens over 14336: 447 us).
 
 #include <algorithm>
 #include <cmath>
@@ -52,28 +54,28 @@ namespace {
 
 constexpr int kKeys = 128;                     // keys of a tile
 constexpr int kPages = kKeys / kChunkPage;
-constexpr int kAttThreads = 384;
+constexpr int kSoftWarps = 16;
+constexpr int kAttThreads = 32 * (kSoftWarps + 4);
 constexpr int kMaxCtas = 148;                  // CTAs of a launch: sizes the workspace
 constexpr int kItemRing = 4;
 constexpr int kFmaShare = 1;                   // of 8 pairs of exponentials, those that the FMA units compute
 constexpr float kMostSum = 8192.0f;            // of a row's probabilities in a tile, before its reference has to move
 
-// Costs that the shares are cut by, in keys of a single item.  A paired item's tile keeps the tensor cores twice as long.
-constexpr int kSingleStart = 256, kPairWeight = 2, kPairStart = 512;
+// Costs that the shares are cut by: of a key, and of an item's beginning and end.
+constexpr int kSingleWeight = 6, kPairWeight = 8, kSingleStart = 2048, kPairStart = 3072;
 constexpr int kLeastPart = 1;                  // key tiles
 
-// FEW: no item has more than 32 rows.  Its query tiles are stored as far as they have rows (what an MMA reads behind them
-// makes rows that nobody reads), and the copies get a stage more.
-constexpr int kFewRows = 32;
+// FEW: no item has more than 64 rows.  Its query tiles are stored as far as they have rows (what an MMA reads behind them,
+// keys, makes rows that nobody reads), and the copies get a stage more.
+constexpr int kFewRows = 64;
 template <int HD, bool FEW> struct AttSmem {
   static constexpr int kQRows = FEW ? kFewRows : 128;
   static constexpr int kQHalf = kQRows * 128;                         // 64 elements of every row
   static constexpr int kQTile = HD / 64 * kQHalf;
   static constexpr int kStage = kKeys * HD * 2;
   static constexpr int kStages = HD == 128 ? (FEW ? 6 : 5) : (FEW ? 11 : 9);
-  static constexpr int kKV = 0, kQ = kStages * kStage, kBars = kQ + 2 * kQTile;      // (an MMA's rows behind Q: no KV stage in use)
-  static constexpr int kReach = kQ + 2 * kQTile - kQHalf + 16384;     // end of what an MMA reads as Q
-  static constexpr int kTotal = (kBars + 3072 > kReach ? kBars + 3072 : kReach);
+  static constexpr int kQ = 0, kKV = 2 * kQTile, kBars = kKV + kStages * kStage;
+  static constexpr int kTotal = kBars + 3072;
   static_assert(kTotal <= 227 * 1024, "shared memory");
 };
 
@@ -100,53 +102,59 @@ struct AttendArgs {
   float2 *part_ml;                  // [cta][2][rows_cap]: reference in log2 units, sum
   PartRecord *records;
   int Hq, Hkv, group, tile_tok, load_tok /* of a query tile's tokens, those that are loaded */, n_pages, rows_cap;
-  bool wide_stores;                 // out begins on a 32-byte boundary
   float scale_log2;
 };
 
 // ---- tensor memory and descriptors -----------------------------------------------------------------
-__device__ __forceinline__ void tc_st32(uint32_t taddr, const uint32_t *r) {
+// A warp reads 16 rows (lanes): thread t holds of row t / 4, and of row t / 4 + 8, two neighbouring columns of every eight
+// (r[4 b], r[4 b + 1]; r[4 b + 2], r[4 b + 3]).  Loads include their wait.
+__device__ __forceinline__ void tc_ld_64cols(uint32_t taddr, uint32_t (&r)[32]) {
   asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
+      "tcgen05.ld.sync.aligned.16x256b.x8.b32 "
       "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};"
-      ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
-        "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
-        "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
-        "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(taddr)
-      : "memory");
-}
-__device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-__device__ __forceinline__ uint32_t tc_ld1(uint32_t taddr) {
-  uint32_t v;
-  asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];\n\ttcgen05.wait::ld.sync.aligned;" : "=r"(v) : "r"(taddr) : "memory");
-  return v;
-}
-// 64 columns of a thread's row, the wait for them included
-__device__ __forceinline__ void tc_ld64_wait(uint32_t taddr, uint32_t *r) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x64.b32 "
-      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, "
-      "%32, %33, %34, %35, %36, %37, %38, %39, %40, %41, %42, %43, %44, %45, %46, %47, "
-      "%48, %49, %50, %51, %52, %53, %54, %55, %56, %57, %58, %59, %60, %61, %62, %63}, [%64];\n\t"
-      "tcgen05.wait::ld.sync.aligned;"
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      "\n\ttcgen05.wait::ld.sync.aligned;"
       : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
         "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
         "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
-        "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31]),
-        "=r"(r[32]), "=r"(r[33]), "=r"(r[34]), "=r"(r[35]), "=r"(r[36]), "=r"(r[37]), "=r"(r[38]), "=r"(r[39]),
-        "=r"(r[40]), "=r"(r[41]), "=r"(r[42]), "=r"(r[43]), "=r"(r[44]), "=r"(r[45]), "=r"(r[46]), "=r"(r[47]),
-        "=r"(r[48]), "=r"(r[49]), "=r"(r[50]), "=r"(r[51]), "=r"(r[52]), "=r"(r[53]), "=r"(r[54]), "=r"(r[55]),
-        "=r"(r[56]), "=r"(r[57]), "=r"(r[58]), "=r"(r[59]), "=r"(r[60]), "=r"(r[61]), "=r"(r[62]), "=r"(r[63])
+        "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
       : "r"(taddr)
       : "memory");
 }
-// ties a loaded block of registers to the wait before it
-template <int N> __device__ __forceinline__ void after_wait(uint32_t (&r)[N]) {
-#pragma unroll
-  for (int i = 0; i < N; ++i) asm volatile("" : "+r"(r[i]));
+__device__ __forceinline__ void tc_ld_32cols(uint32_t taddr, uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.16x256b.x4.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      "\n\ttcgen05.wait::ld.sync.aligned;"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr)
+      : "memory");
 }
+__device__ __forceinline__ void tc_st_32cols(uint32_t taddr, const uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.16x256b.x4.b32 [%16], "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};"
+      ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+        "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(taddr)
+      : "memory");
+}
+// The same rows with one column of every four to a thread: 16-bit numbers in pairs, as the columns above.
+__device__ __forceinline__ void tc_st_64keys(uint32_t taddr, const uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.16x128b.x8.b32 [%16], "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};"
+      ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+        "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void tc_ld_8keys(uint32_t taddr, uint32_t (&r)[2]) {
+  asm volatile("tcgen05.ld.sync.aligned.16x128b.x1.b32 {%0, %1}, [%2];\n\ttcgen05.wait::ld.sync.aligned;"
+               : "=r"(r[0]), "=r"(r[1])
+               : "r"(taddr)
+               : "memory");
+}
+__device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 // largest of three; NaN wins
 __device__ __forceinline__ float max3_nan(float a, float b, float c) {
   float d;
@@ -231,7 +239,7 @@ struct SeqCost {
   __device__ __forceinline__ int seen(int i) const { return max(0, base + min(n, (i + 1) * step)); }
   __device__ __forceinline__ bool single(int i) const { return i == n_items - 1 && last_single; }
   __device__ __forceinline__ long long cost(int i) const {
-    return single(i) ? kSingleStart + static_cast<long long>(seen(i)) : kPairStart + static_cast<long long>(kPairWeight) * seen(i);
+    return single(i) ? kSingleStart + static_cast<long long>(kSingleWeight) * seen(i) : kPairStart + static_cast<long long>(kPairWeight) * seen(i);
   }
   // cost of the items before i
   __device__ __forceinline__ long long before(int i) const {
@@ -257,7 +265,7 @@ __device__ __forceinline__ SeqCost seq_cost(const SeqSpan &p, int tile_tok) {
 // key tile at which an item is cut, x into its cost
 __device__ __forceinline__ int cut_tile(long long x, bool single, int seen) {
   const int tiles = (seen + kKeys - 1) / kKeys;
-  const long long y = x - (single ? kSingleStart : kPairStart), per = single ? kKeys : kPairWeight * kKeys;
+  const long long y = x - (single ? kSingleStart : kPairStart), per = (single ? kSingleWeight : kPairWeight) * kKeys;
   const int t = y <= 0 ? 0 : static_cast<int>(min(static_cast<long long>(tiles), (y + per - 1) / per));
   return t < kLeastPart ? 0 : tiles - t < kLeastPart ? tiles : t;
 }
@@ -279,20 +287,20 @@ template <int HD, bool FEW> struct Shared {
   float2 ml[2][128];
 };
 
-// A row's stores touch a line of its own for each thread, so that their number counts: 32 bytes at a time where the output
-// begins on such a boundary (8 x 1024 tokens at 64/8 heads: 237 us with 16 bytes, 223 with 32).
-__device__ __forceinline__ void store_64_bytes(void *dst, const uint32_t *v, bool wide) {
+// Four threads of a row hold a word each of four 16-byte units (v[i]: unit i); afterwards thread j of them holds unit j.
+__device__ __forceinline__ void units_of_quad(uint32_t (&v)[4], int lane) {
+  const bool odd = lane & 1, high = lane & 2;
 #pragma unroll
-  for (int h = 0; h < 16; h += 8) {
-    uint32_t *q = static_cast<uint32_t *>(dst) + h;
-    if (wide) {
-      asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(q), "r"(v[h]), "r"(v[h + 1]), "r"(v[h + 2]),
-                   "r"(v[h + 3]), "r"(v[h + 4]), "r"(v[h + 5]), "r"(v[h + 6]), "r"(v[h + 7])
-                   : "memory");
-    } else {
-      reinterpret_cast<uint4 *>(q)[0] = make_uint4(v[h], v[h + 1], v[h + 2], v[h + 3]);
-      reinterpret_cast<uint4 *>(q)[1] = make_uint4(v[h + 4], v[h + 5], v[h + 6], v[h + 7]);
-    }
+  for (int i = 0; i < 4; i += 2) {
+    const uint32_t got = __shfl_xor_sync(0xffffffffu, odd ? v[i] : v[i + 1], 1);
+    if (odd) v[i] = got;
+    else v[i + 1] = got;
+  }
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const uint32_t got = __shfl_xor_sync(0xffffffffu, high ? v[i] : v[i + 2], 2);
+    if (high) v[i] = got;
+    else v[i + 2] = got;
   }
 }
 template <bool HALF> __device__ __forceinline__ bool any_undefined(uint4 v) {
@@ -369,6 +377,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
   Shared<HD, FEW> &sh = *reinterpret_cast<Shared<HD, FEW> *>(smem + M::kBars);
   static_assert(sizeof(Shared<HD, FEW>) <= 3072, "barriers");
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  constexpr int kMma0 = kSoftWarps, kLoad = kSoftWarps + 1, kMma1 = kSoftWarps + 2;
   volatile int *abort_flag = &sh.abort_flag;
   if (smem_u32(smem) & 1023) {                 // (swizzled tiles need it; a dynamic array alone begins there)
     if (threadIdx.x == 0) atomicMax(a.c.status, STATUS_WAIT_TIMEOUT);
@@ -383,12 +392,12 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
       mbar_init(&sh.turn[i], 1);
       for (int b = 0; b < 2; ++b) {
         mbar_init(&sh.s_full[i][b], 1);
-        mbar_init(&sh.p_ready[i][b], 4);
+        mbar_init(&sh.p_ready[i][b], kSoftWarps / 2);
         sh.bad_value[i][b] = 0;
       }
       mbar_init(&sh.pv_done[i], 1);
-      mbar_init(&sh.look[i], 4);
-      mbar_init(&sh.join[i], 8);
+      mbar_init(&sh.look[i], kSoftWarps / 2);
+      mbar_init(&sh.join[i], kSoftWarps);
     }
     for (int i = 0; i < M::kStages; ++i) {
       mbar_init(&sh.kv_full[i], 1);
@@ -396,13 +405,13 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
     }
     for (int i = 0; i < kItemRing; ++i) {
       mbar_init(&sh.item_full[i], 1);
-      mbar_init(&sh.item_empty[i], 10);
+      mbar_init(&sh.item_empty[i], kSoftWarps + 2);
     }
     sh.abort_flag = 0;
     mbar_fence_init();
   }
-  if (warp == 8) tc_alloc(&sh.tmem, 512);
-  if (warp == 9 && lane == 0) {
+  if (warp == kMma0) tc_alloc(&sh.tmem, 512);
+  if (warp == kLoad && lane == 0) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tm_q)) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tm_kv)) : "memory");
   }
@@ -417,7 +426,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
   // waits of a whole warp, whose lanes go on or give up together
   auto wait = [&](uint64_t *bar, int parity) { return warp_wait(bar, parity & 1, abort_flag); };
 
-  if (warp == 9) {
+  if (warp == kLoad) {
     // ---------------------------------------------------------------- items and copies
     PartRecord rec = {};
     int n_items = 0;                            // published
@@ -596,7 +605,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
       }
       __syncwarp();
     }
-  } else if (warp >= 8) {
+  } else if (warp >= kSoftWarps) {
     // ---------------------------------------------------------------- MMA issue
     // A warp for each stream, so that one's waits and bookkeeping run under the other's products (one warp for both left
     // the tensor cores idle for half of the time).  They issue in turn: two streams whose products mix on the tensor cores
@@ -604,8 +613,8 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
     // The whole warp takes every step and one elected lane issues: operands that are the same for all lanes are in uniform
     // registers when an MMA needs them there; with one lane walking alone an MMA took 100 to 150 cycles to issue, twice as
     // long as it runs.
-    if (warp == 8 || warp == 10) {
-      const int w = warp == 8 ? 0 : 1;
+    if (warp == kMma0 || warp == kMma1) {
+      const int w = warp == kMma0 ? 0 : 1;
       constexpr uint32_t idesc_s = idesc_operands(instr_desc_bf16(64), HALF);
       constexpr uint32_t idesc_o = idesc_operands(instr_desc_bf16(HD), HALF) | kIdescBMajorMN;
       constexpr int kStages = M::kStages;
@@ -712,11 +721,12 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
     }
   } else {
     // ---------------------------------------------------------------- softmax and results
-    const int w = warp >> 2, row = (warp & 3) * 32 + lane, wg_tid = threadIdx.x & 127;
-    const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
+    const int w = warp >> 3, lane0 = (warp & 3) * 32 + (warp & 4) * 4, stream_tid = threadIdx.x & 255;
+    const uint32_t lanes = static_cast<uint32_t>(lane0) << 16;
     const uint32_t t_s0 = tmem + lanes + w * 128, t_o = tmem + lanes + 256 + w * 128;
     const float c = a.scale_log2;
-    const int tok = row / a.group, rep = row % a.group;
+    const int row_a = lane0 + (lane >> 2), row_b = row_a + 8, col = 2 * (lane & 3);      // of every eight columns: col, col + 1
+    const int tok_a = row_a / a.group, tok_b = row_b / a.group;
     int n_item = 0, steps_done = 0, tiles_done = 0, looks = 0, joins = 0;
     bool ok = true;
     while (ok) {
@@ -727,10 +737,11 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
       if (it.flags & kEnd) break;
       const bool paired = !FEW && (it.flags & kPaired);
       const int row_tile = paired ? w : 0, steps = (it.t1 - it.t0) * (paired ? 2 : 1);
-      const int tok0 = row_tile * a.tile_tok, n_tok = min(a.tile_tok, it.n_tok - tok0);      // (may be <= 0: no rows)
-      const int pos_first = it.pos0 + tok0, pos = pos_first + tok;
-      const bool mine = row < n_tok * a.group, warp_mine = (warp & 3) * 32 < n_tok * a.group;
-      float m = -INFINITY, l = 0.f;              // reference (score units) and sum
+      const int tok0 = row_tile * a.tile_tok, n_rows = min(a.tile_tok, it.n_tok - tok0) * a.group;
+      const int pos_first = it.pos0 + tok0, pos_a = pos_first + tok_a, pos_b = pos_first + tok_b;
+      const bool mine_a = row_a < n_rows, mine_b = row_b < n_rows, warp_mine = lane0 < n_rows;
+      float m_a = -INFINITY, m_b = -INFINITY;                         // references (score units)
+      float l_a = 0.f, l_b = 0.f;                                     // sums of this thread's columns
       for (int i = 0; i < steps; ++i) {          // of 64 keys
         const int tile = paired ? i >> 1 : i, key_off = 64 * (paired ? i & 1 : w);
         const int key0 = (it.flags & kBackwards ? it.t1 - 1 - tile : it.t0 + tile) * kKeys + key_off;
@@ -741,66 +752,84 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
         tc_fence_after();
         const bool masked = key0 + 64 > pos_first + 1;                // some row does not see all of these keys
         if (warp_mine) {
-          uint32_t s[64], p[32];
-          float2 sum[2];
-          tc_ld64_wait(t_s, s);
+          uint32_t s[32], p[16];
+          float2 sum_a, sum_b;
+          tc_ld_64cols(t_s, s);
           if (masked) {
-            const int last = pos - key0;         // the row sees elements 0 .. last
+            const int last_a = pos_a - key0 - col, last_b = pos_b - key0 - col;
 #pragma unroll
-            for (int e = 0; e < 64; ++e)
-              if (e > last) s[e] = 0xff800000u;
+            for (int b = 0; b < 8; ++b) {
+              if (8 * b > last_a) s[4 * b] = 0xff800000u;
+              if (8 * b + 1 > last_a) s[4 * b + 1] = 0xff800000u;
+              if (8 * b > last_b) s[4 * b + 2] = 0xff800000u;
+              if (8 * b + 1 > last_b) s[4 * b + 3] = 0xff800000u;
+            }
           }
-          // With the reference as it is, unless the row has none yet: maxima take a quarter of a step's time, and a
-          // reference that is too low shows in the sum.  Where it does, once more with maxima.
-          bool careful = __any_sync(0xffffffffu, mine && m == -INFINITY);
+          // With the references as they are, unless a row has none yet: maxima take a quarter of a step's time, and a
+          // reference that is too low shows in the sum.  Where one does, once more with maxima.
+          bool careful = __any_sync(0xffffffffu, (mine_a && m_a == -INFINITY) || (mine_b && m_b == -INFINITY));
           while (true) {
             if (careful) {
-              float top[4] = {m, m, m, m};
+              float to_a = m_a, to_b = m_b;
 #pragma unroll
-              for (int e = 0; e < 64; e += 2) top[(e >> 1) & 3] = max3_nan(top[(e >> 1) & 3], __uint_as_float(s[e]), __uint_as_float(s[e + 1]));
-              const float to = max_nan(max3_nan(top[0], top[1], top[2]), top[3]);
-              const float fix = to == m ? 1.0f : ex2((m - to) * c);   // (m = -inf: 0)
-              m = to;
-              l *= fix;
+              for (int b = 0; b < 8; ++b) {
+                to_a = max3_nan(to_a, __uint_as_float(s[4 * b]), __uint_as_float(s[4 * b + 1]));
+                to_b = max3_nan(to_b, __uint_as_float(s[4 * b + 2]), __uint_as_float(s[4 * b + 3]));
+              }
+#pragma unroll
+              for (int o = 1; o < 4; o <<= 1) {
+                to_a = max_nan(to_a, __shfl_xor_sync(0xffffffffu, to_a, o));
+                to_b = max_nan(to_b, __shfl_xor_sync(0xffffffffu, to_b, o));
+              }
+              const float fix_a = to_a == m_a ? 1.0f : ex2((m_a - to_a) * c);      // (from -inf: 0)
+              const float fix_b = to_b == m_b ? 1.0f : ex2((m_b - to_b) * c);
+              m_a = to_a;
+              m_b = to_b;
+              l_a *= fix_a;
+              l_b *= fix_b;
               if (i > 0) {
                 ok = wait(&sh.pv_done[w], steps_done - 1);
                 if (!ok) break;
                 tc_fence_after();
 #pragma unroll 1
                 for (int b = 0; b < HD / 32; ++b) {
-                  uint32_t o[32];
-                  tc_ld32(t_o + b * 32, o);
-                  tc_wait_ld();
-                  after_wait(o);
+                  uint32_t o[16];
+                  tc_ld_32cols(t_o + b * 32, o);
 #pragma unroll
-                  for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * fix);
-                  tc_st32(t_o + b * 32, o);
+                  for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * ((e & 2) ? fix_b : fix_a));
+                  tc_st_32cols(t_o + b * 32, o);
                 }
               }
             }
-            const float base = m == -INFINITY ? 0.f : m == INFINITY ? NAN : -m * c;
-            const float2 c2 = make_float2(c, c), b2 = make_float2(base, base);
-            sum[0] = sum[1] = make_float2(0.f, 0.f);
+            const float base_a = m_a == -INFINITY ? 0.f : m_a == INFINITY ? NAN : -m_a * c;
+            const float base_b = m_b == -INFINITY ? 0.f : m_b == INFINITY ? NAN : -m_b * c;
+            const float2 c2 = make_float2(c, c), base2_a = make_float2(base_a, base_a), base2_b = make_float2(base_b, base_b);
+            sum_a = sum_b = make_float2(0.f, 0.f);
 #pragma unroll
-            for (int e = 0; e < 32; ++e) {
-              const float2 x = fma2(make_float2(__uint_as_float(s[2 * e]), __uint_as_float(s[2 * e + 1])), c2, b2);
-              const float2 y = (e & 7) < kFmaShare ? exp2_by_fma(x) : make_float2(ex2(x.x), ex2(x.y));
-              sum[e & 1] = add2(sum[e & 1], y);
-              p[e] = cvt16x2(y.x, y.y, HALF);
+            for (int b = 0; b < 8; ++b) {
+              const float2 x = fma2(make_float2(__uint_as_float(s[4 * b]), __uint_as_float(s[4 * b + 1])), c2, base2_a);
+              const float2 y = fma2(make_float2(__uint_as_float(s[4 * b + 2]), __uint_as_float(s[4 * b + 3])), c2, base2_b);
+              const float2 px = (2 * b & 7) < kFmaShare ? exp2_by_fma(x) : make_float2(ex2(x.x), ex2(x.y));
+              const float2 py = (2 * b + 1 & 7) < kFmaShare ? exp2_by_fma(y) : make_float2(ex2(y.x), ex2(y.y));
+              sum_a = add2(sum_a, px);
+              sum_b = add2(sum_b, py);
+              p[2 * b] = cvt16x2(px.x, px.y, HALF);
+              p[2 * b + 1] = cvt16x2(py.x, py.y, HALF);
             }
-            sum[0].x = (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
-            if (careful || !__any_sync(0xffffffffu, mine && !(sum[0].x <= kMostSum))) break;
+            sum_a.x += sum_a.y;
+            sum_b.x += sum_b.y;
+            if (careful || !__any_sync(0xffffffffu, (mine_a && !(sum_a.x <= kMostSum / 4)) || (mine_b && !(sum_b.x <= kMostSum / 4)))) break;
             careful = true;
           }
           if (!ok) break;
-          l += sum[0].x;
-          tc_st32(t_s, p);
+          l_a += sum_a.x;
+          l_b += sum_b.x;
+          tc_st_64keys(t_s, p);
           tc_wait_st();
         }
         // keys that some row of the tile does not see: their values must be finite, or kept out of the products
         const int ks = max(0, pos_first + 1 - key0), ke = min(64, it.seen_end - key0);
         const int ke16 = (ke + 15) & ~15;
-        bool slow = false;
         if (masked && ke > 0 && (ks < ke || ke < ke16)) {
           const int at = 2 * (tiles_done + tile) + 1, stage = at % M::kStages;
           ok = wait(&sh.kv_full[stage], at / M::kStages);
@@ -808,12 +837,13 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
           uint8_t *v = smem + M::kKV + stage * M::kStage;
           const int u0 = min(ks, ke) * (HD / 8), u1 = ke16 * (HD / 8);
           bool bad = false;
-          for (int u = u0 + wg_tid; u < u1; u += 128) {
+          for (int u = u0 + stream_tid; u < u1; u += 256) {
             uint4 *unit = reinterpret_cast<uint4 *>(v + kv_unit<HD>(key_off + u / (HD / 8), u % (HD / 8)));
             if (u / (HD / 8) < ke) bad |= any_undefined<HALF>(*unit);
             else *unit = make_uint4(0u, 0u, 0u, 0u);                  // no row of the item sees it
           }
           fence_proxy_async();
+          bool slow = false;
           if (ks < ke) {
             if (bad) *const_cast<volatile int *>(&sh.bad_value[w][buf]) = steps_done + 1;
             __syncwarp();
@@ -827,35 +857,39 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             if (i > 0) ok = wait(&sh.pv_done[w], steps_done - 1);
             if (!ok) break;
             tc_fence_after();
-            const int last = pos - key0;
 #pragma unroll 1
             for (int b = 0; b < HD / 32; ++b) {
-              uint32_t o[32];
-              tc_ld32(t_o + b * 32, o);
-              tc_wait_ld();
-              after_wait(o);
+              uint32_t o[16];
+              tc_ld_32cols(t_o + b * 32, o);
               if (i == 0)
 #pragma unroll
-                for (int e = 0; e < 32; ++e) o[e] = 0u;
+                for (int e = 0; e < 16; ++e) o[e] = 0u;
 #pragma unroll 1
               for (int key = 0; key < 64; ++key) {
-                const float2 pp = widen16x2(tc_ld1(t_s + (key >> 1)), HALF);
-                const float p = (key & 1) ? pp.y : pp.x;
-                __syncwarp();
+                uint32_t p[2];
+                if ((key & 7) == 0) __syncwarp();
+                tc_ld_8keys(t_s + (key >> 3) * 4, p);
+                const int from = (lane & ~3) | ((key & 7) >> 1);
+                const float2 qa = widen16x2(__shfl_sync(0xffffffffu, p[0], from), HALF);
+                const float2 qb = widen16x2(__shfl_sync(0xffffffffu, p[1], from), HALF);
+                const float pa = (key & 1) ? qa.y : qa.x, pb = (key & 1) ? qb.y : qb.x;
+                const bool see_a = key <= pos_a - key0, see_b = key <= pos_b - key0;
 #pragma unroll
-                for (int u = 0; u < 4 && key <= last; ++u) {
-                  const uint4 q = *reinterpret_cast<const uint4 *>(v + kv_unit<HD>(key_off + key, b * 4 + u));
-                  const uint32_t words[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-                  for (int e = 0; e < 4; ++e) {
-                    const float2 f = widen16x2(words[e], HALF);
-                    o[u * 8 + 2 * e] = __float_as_uint(fmaf(p, f.x, __uint_as_float(o[u * 8 + 2 * e])));
-                    o[u * 8 + 2 * e + 1] = __float_as_uint(fmaf(p, f.y, __uint_as_float(o[u * 8 + 2 * e + 1])));
+                for (int e = 0; e < 4; ++e) {
+                  const uint32_t vv = *reinterpret_cast<const uint32_t *>(v + kv_unit<HD>(key_off + key, b * 4 + e) + 2 * col);
+                  const float2 f = widen16x2(vv, HALF);
+                  if (see_a) {
+                    o[4 * e] = __float_as_uint(fmaf(pa, f.x, __uint_as_float(o[4 * e])));
+                    o[4 * e + 1] = __float_as_uint(fmaf(pa, f.y, __uint_as_float(o[4 * e + 1])));
+                  }
+                  if (see_b) {
+                    o[4 * e + 2] = __float_as_uint(fmaf(pb, f.x, __uint_as_float(o[4 * e + 2])));
+                    o[4 * e + 3] = __float_as_uint(fmaf(pb, f.y, __uint_as_float(o[4 * e + 3])));
                   }
                 }
+                __syncwarp();
               }
-              __syncwarp();
-              tc_st32(t_o + b * 32, o);
+              tc_st_32cols(t_o + b * 32, o);
             }
             tc_wait_st();
           }
@@ -867,7 +901,8 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
       }
       if (!ok) break;
       // ---- the item's result: whole rows, or a part for the joining launch
-      if (it.t0 < it.t1) {
+      const bool any = it.t0 < it.t1;
+      if (any) {
         // one after the other: the products of the last two steps may both be under way, and a phase is known by its parity
         if (steps > 1) ok = wait(&sh.pv_done[w], steps_done - 2);
         if (ok) ok = wait(&sh.pv_done[w], steps_done - 1);
@@ -875,76 +910,94 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
       }
       tc_fence_after();
       const bool spoiled = *const_cast<volatile int *>(&sh.bad_page[slot]) != 0;
-      float my_ref = m == -INFINITY ? -INFINITY : m * c, scale0 = 1.f, scale1 = 0.f;
+#pragma unroll
+      for (int o = 1; o < 4; o <<= 1) {
+        l_a += __shfl_xor_sync(0xffffffffu, l_a, o);
+        l_b += __shfl_xor_sync(0xffffffffu, l_b, o);
+      }
+      float ref_a = m_a * c, ref_b = m_b * c, a0 = 1.f, a1 = 0.f, b0 = 1.f, b1 = 0.f;      // scales of the streams' O
       int col0 = 0, col1 = HD;
       uint32_t o_main = t_o, o_other = t_o;
-      const bool has_main = it.t0 < it.t1;
-      bool has_other = false;
       if (!paired) {
-        // both streams hold a share of the keys: each warpgroup joins half of the columns
-        sh.ml[w][row] = make_float2(my_ref, l);
+        // both streams hold a share of the keys: each joins half of the columns
+        if ((lane & 3) == 0) {
+          sh.ml[w][row_a] = make_float2(ref_a, l_a);
+          sh.ml[w][row_b] = make_float2(ref_b, l_b);
+        }
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(&sh.join[0]);
         ok = wait(&sh.join[0], joins);
         if (!ok) break;
         tc_fence_after();
-        const float2 m0 = sh.ml[0][row], m1 = sh.ml[1][row];
-        const float ref = fmaxf(m0.x, m1.x);
-        scale0 = m0.x == -INFINITY ? 0.f : ex2(m0.x - ref);
-        scale1 = m1.x == -INFINITY ? 0.f : ex2(m1.x - ref);
-        l = m0.y * scale0 + m1.y * scale1;
-        my_ref = ref;
+        auto join = [&](int row, float &ref, float &sum, float &x0, float &x1) {
+          const float2 m0 = sh.ml[0][row], m1 = sh.ml[1][row];
+          ref = max_nan(m0.x, m1.x);
+          x0 = m0.x == -INFINITY ? 0.f : ex2(m0.x - ref);
+          x1 = m1.x == -INFINITY ? 0.f : ex2(m1.x - ref);
+          sum = m0.y * x0 + m1.y * x1;
+        };
+        join(row_a, ref_a, l_a, a0, a1);
+        join(row_b, ref_b, l_b, b0, b1);
         o_main = tmem + lanes + 256;
         o_other = o_main + 128;
-        has_other = has_main;
         col0 = w * (HD / 2);
         col1 = col0 + HD / 2;
       }
       if (warp_mine) {
         const bool part = it.flags & (kPartFirst | kPartLater);
-        const int part_row = row_tile * 128 + row;
-        const int64_t part_at = (static_cast<int64_t>(blockIdx.x) * 2 + (it.flags & kPartFirst ? 1 : 0)) * a.rows_cap + part_row;
-        if (spoiled) l = NAN;
-        if (part && mine && col0 == 0) a.part_ml[part_at] = make_float2(spoiled ? 0.f : my_ref, l);
-        const float norm = part ? 1.f : spoiled ? NAN : pos < 0 ? 0.f : 1.0f / l;
-        uint16_t *dst = a.out + (static_cast<int64_t>(it.row0 + tok0 + tok) * a.Hq + it.head * a.group + rep) * HD;
+        const int64_t part_at = (static_cast<int64_t>(blockIdx.x) * 2 + (it.flags & kPartFirst ? 1 : 0)) * a.rows_cap + row_tile * 128;
+        if (spoiled) {                           // whatever else the row holds, it is undefined
+          l_a = l_b = NAN;
+          ref_a = ref_b = 0.f;
+        }
+        if (part && col0 == 0 && (lane & 3) == 0) {
+          if (mine_a) a.part_ml[part_at + row_a] = make_float2(ref_a, l_a);
+          if (mine_b) a.part_ml[part_at + row_b] = make_float2(ref_b, l_b);
+        }
+        const float norm_a = 1.0f / l_a, norm_b = 1.0f / l_b;
+        const int64_t tok_first = it.row0 + tok0;
+        uint16_t *dst_a = a.out + ((tok_first + tok_a) * a.Hq + it.head * a.group + row_a % a.group) * HD + 8 * (lane & 3);
+        uint16_t *dst_b = a.out + ((tok_first + tok_b) * a.Hq + it.head * a.group + row_b % a.group) * HD + 8 * (lane & 3);
 #pragma unroll 1
-        for (int col = col0; col < col1; col += 32) {
-          float f[32];
+        for (int c0 = col0; c0 < col1; c0 += 32) {
+          float f[16];
 #pragma unroll
-          for (int e = 0; e < 32; ++e) f[e] = 0.f;
-          if (has_main) {
-            uint32_t o[32];
-            tc_ld32(o_main + col, o);
-            tc_wait_ld();
-            after_wait(o);
+          for (int e = 0; e < 16; ++e) f[e] = 0.f;
+          if (any) {
+            uint32_t o[16];
+            tc_ld_32cols(o_main + c0, o);
 #pragma unroll
-            for (int e = 0; e < 32; ++e) f[e] = __uint_as_float(o[e]) * scale0;
+            for (int e = 0; e < 16; ++e) f[e] = __uint_as_float(o[e]) * ((e & 2) ? b0 : a0);
+            if (!paired) {
+              tc_ld_32cols(o_other + c0, o);
+#pragma unroll
+              for (int e = 0; e < 16; ++e) f[e] = fmaf(__uint_as_float(o[e]), (e & 2) ? b1 : a1, f[e]);
+            }
           }
-          if (has_other) {
-            uint32_t o[32];
-            tc_ld32(o_other + col, o);
-            tc_wait_ld();
-            after_wait(o);
+          if (part) {
 #pragma unroll
-            for (int e = 0; e < 32; ++e) f[e] = fmaf(__uint_as_float(o[e]), scale1, f[e]);
-          }
-          if (mine && part) {
-            float4 *q = reinterpret_cast<float4 *>(a.part_o + part_at * HD + col);
+            for (int e = 0; e < 4; ++e) {
+              if (mine_a) *reinterpret_cast<float2 *>(a.part_o + (part_at + row_a) * HD + c0 + 8 * e + col) = make_float2(f[4 * e], f[4 * e + 1]);
+              if (mine_b) *reinterpret_cast<float2 *>(a.part_o + (part_at + row_b) * HD + c0 + 8 * e + col) = make_float2(f[4 * e + 2], f[4 * e + 3]);
+            }
+          } else {                               // (rows that see nothing: 0)
+            uint32_t va[4], vb[4];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) q[e] = make_float4(f[4 * e], f[4 * e + 1], f[4 * e + 2], f[4 * e + 3]);
-          } else if (mine) {
-            uint32_t pk[16];
-#pragma unroll
-            for (int k = 0; k < 16; ++k) pk[k] = pos < 0 ? 0u : cvt16x2(f[2 * k] * norm, f[2 * k + 1] * norm, HALF);
-            store_64_bytes(dst + col, pk, a.wide_stores);
+            for (int e = 0; e < 4; ++e) {
+              va[e] = pos_a < 0 ? 0u : cvt16x2(f[4 * e] * norm_a, f[4 * e + 1] * norm_a, HALF);
+              vb[e] = pos_b < 0 ? 0u : cvt16x2(f[4 * e + 2] * norm_b, f[4 * e + 3] * norm_b, HALF);
+            }
+            units_of_quad(va, lane);
+            units_of_quad(vb, lane);
+            if (mine_a) *reinterpret_cast<uint4 *>(dst_a + c0) = make_uint4(va[0], va[1], va[2], va[3]);
+            if (mine_b) *reinterpret_cast<uint4 *>(dst_b + c0) = make_uint4(vb[0], vb[1], vb[2], vb[3]);
           }
           __syncwarp();
         }
       }
       if (!paired) {
-        // the other warpgroup has read this stream's O before it is written again
+        // the other stream's warps have read this one's O before it is written again
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(&sh.join[1]);
@@ -961,7 +1014,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
   }
   __syncthreads();
   if (threadIdx.x == 0 && sh.abort_flag) atomicMax(a.c.status, STATUS_WAIT_TIMEOUT);
-  if (warp == 8) {
+  if (warp == kMma0) {
     tc_fence_after();
     tc_dealloc(tmem, 512);
   }
@@ -1080,7 +1133,6 @@ int echo_chunk_attention(const void *q, int64_t q_stride, const void *kv_pool, i
   a.Hq = Hq;
   a.Hkv = Hkv;
   a.group = Hq / Hkv;
-  a.wide_stores = (reinterpret_cast<uintptr_t>(out) & 31) == 0;
   a.tile_tok = 128 / a.group;
   const bool few = static_cast<int64_t>(a.c.max_chunk) * a.group <= kFewRows;
   a.load_tok = few ? kFewRows / a.group : a.tile_tok;
