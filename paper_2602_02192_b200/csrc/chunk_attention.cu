@@ -63,6 +63,7 @@ constexpr float kMostSum = 8192.0f;            // of a row's probabilities in a 
 
 // Costs that the shares are cut by: of a key, and of an item's beginning and end.
 constexpr int kSingleWeight = 6, kPairWeight = 8, kSingleStart = 2048, kPairStart = 3072;
+constexpr int kLeastShare = 1024;              // of a CTA: little work goes to few CTAs, for whoever joins its parts
 constexpr int kLeastPart = 1;                  // key tiles
 
 // FEW: no item has more than 64 rows.  Its query tiles are stored as far as they have rows (what an MMA reads behind them,
@@ -267,13 +268,13 @@ __device__ __forceinline__ int cut_tile(long long x, bool single, int seen) {
   const int tiles = (seen + kKeys - 1) / kKeys;
   const long long y = x - (single ? kSingleStart : kPairStart), per = (single ? kSingleWeight : kPairWeight) * kKeys;
   const int t = y <= 0 ? 0 : static_cast<int>(min(static_cast<long long>(tiles), (y + per - 1) / per));
-  return t < kLeastPart ? 0 : tiles - t < kLeastPart ? tiles : t;
+  return t == tiles ? t : t < kLeastPart ? 0 : tiles - t < kLeastPart ? tiles : t;
 }
 
 // ---- the kernel ----------------------------------------------------------------------------------------
 template <int HD, bool FEW> struct Shared {
   uint64_t q_full[2], q_empty[2], kv_full[AttSmem<HD, FEW>::kStages], kv_empty[AttSmem<HD, FEW>::kStages];
-  uint64_t s_full[2][2], p_ready[2][2], pv_done[2],                   // [stream][half of its S] 
+  uint64_t s_full[2][2], p_ready[2][2], pv_done[2][2],                // [stream][parity of its step]
       item_full[kItemRing], item_empty[kItemRing];
   uint64_t look[2], join[2], turn[2], drain[2];
   Item items[kItemRing];
@@ -281,9 +282,9 @@ template <int HD, bool FEW> struct Shared {
   int bad_value[2][2];              // [stream][half]: step (+ 1) whose P V the threads add themselves
   uint32_t tmem;
   int abort_flag;
-  long long total, start;           // plan: cost of everything; cost in front of the CTA's first sequence
+  long long x0, x1, start;          // plan: the CTA's share of the cost; cost in front of its first sequence
   int first_seq;
-  long long warp_sum[kAttThreads / 32];
+  long long warp_sum[2][kAttThreads / 32];
   float2 ml[2][128];
 };
 
@@ -312,7 +313,8 @@ template <int HD> __device__ __forceinline__ uint32_t kv_unit(int key, int c) {
   return (key >> 3) * (HD * 16) + (c >> 3) * 1024 + (key & 7) * 128 + (((c & 7) ^ (key & 7)) << 4);
 }
 
-// The total cost, and where this CTA's share begins.
+// The CTA's share of the total cost, [x0, x1), and the sequence that it begins in.  Every thread takes a sequence (and one
+// of the next kAttThreads ...): prefix sums over the warp, then over the warps.
 template <int HD, bool FEW> __device__ __forceinline__ void make_plan(const AttendArgs &a, Shared<HD, FEW> &sh) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   constexpr int kWarps = kAttThreads / 32;
@@ -322,49 +324,67 @@ template <int HD, bool FEW> __device__ __forceinline__ void make_plan(const Atte
     if (report && !p.ok) atomicMax(a.c.status, STATUS_BAD_CHUNK);
     return seq_cost(p, a.tile_tok).head() * a.Hkv;
   };
-  long long mine = 0, first = 0;
-  for (int s = threadIdx.x; s < a.c.S; s += kAttThreads) {
-    const long long c = cost_of(s, blockIdx.x == 0);
-    if (s < kAttThreads) first = c;
-    mine += c;
-  }
-#pragma unroll
-  for (int o = 16; o; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
-  if (lane == 0) sh.warp_sum[warp] = mine;
-  if (threadIdx.x == 0) sh.first_seq = -1;
-  __syncthreads();
-  long long total = 0;
-#pragma unroll
-  for (int w = 0; w < kWarps; ++w) total += sh.warp_sum[w];
-  const long long x0 = total * blockIdx.x / gridDim.x, x1 = total * (blockIdx.x + 1) / gridDim.x;
-  if (threadIdx.x == 0) sh.total = total;
-  __syncthreads();
-  if (x0 == x1) return;                          // nothing to do (first_seq stays -1)
-  long long before = 0;
-  for (int s0 = 0; s0 < a.c.S; s0 += kAttThreads) {
-    const int s = s0 + threadIdx.x;
-    const long long c = s0 == 0 ? first : cost_of(s, false);
-    long long run = c;
+  // costs up to and with this thread's, of this warp
+  auto scan = [&](long long run) {
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const long long up = __shfl_up_sync(0xffffffffu, run, o);
       if (lane >= o) run += up;
     }
-    if (lane == 31) sh.warp_sum[warp] = run;
+    return run;
+  };
+  const long long first = cost_of(threadIdx.x, blockIdx.x == 0), first_run = scan(first);
+  long long rest = 0;
+  if (a.c.S > kAttThreads) {
+    for (int s = threadIdx.x + kAttThreads; s < a.c.S; s += kAttThreads) rest += cost_of(s, blockIdx.x == 0);
+    rest = scan(rest);
+  }
+  if (lane == 31) {
+    sh.warp_sum[0][warp] = first_run;
+    sh.warp_sum[1][warp] = rest;
+  }
+  if (threadIdx.x == 0) sh.first_seq = -1;
+  __syncthreads();
+  long long before = 0, firsts = 0, rests = 0;
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) {
+    if (w < warp) before += sh.warp_sum[0][w];
+    firsts += sh.warp_sum[0][w];
+    rests += sh.warp_sum[1][w];
+  }
+  const long long total = firsts + rests;
+  const unsigned ctas = static_cast<unsigned>(max(1ll, min(static_cast<long long>(gridDim.x), total / kLeastShare)));
+  const long long each = total / ctas, more = total - each * ctas;      // (the first `more` CTAs take one more)
+  const long long c = min(blockIdx.x, ctas);
+  const long long x0 = each * c + min(c, more), x1 = blockIdx.x < ctas ? x0 + each + (c < more) : x0;
+  if (threadIdx.x == 0) {
+    sh.x0 = x0;
+    sh.x1 = x1;
+  }
+  if (x0 == x1) return;                          // nothing to do (first_seq stays -1)
+  before += first_run - first;
+  if (first > 0 && x0 >= before && x0 < before + first) {
+    sh.first_seq = threadIdx.x;
+    sh.start = before;
+  }
+  if (x0 < firsts) return;
+  before = firsts;                               // among the later ones
+  for (int s0 = kAttThreads; s0 < a.c.S; s0 += kAttThreads) {
+    const long long cost = cost_of(s0 + threadIdx.x, false), run = scan(cost);
     __syncthreads();
-    long long mine_before = before;
+    if (lane == 31) sh.warp_sum[0][warp] = run;
+    __syncthreads();
+    long long mine = before + run - cost;
 #pragma unroll
     for (int w = 0; w < kWarps; ++w) {
-      if (w < warp) mine_before += sh.warp_sum[w];
-      before += sh.warp_sum[w];
+      if (w < warp) mine += sh.warp_sum[0][w];
+      before += sh.warp_sum[0][w];
     }
-    mine_before += run - c;
-    if (c > 0 && x0 >= mine_before && x0 < mine_before + c) {
-      sh.first_seq = s;
-      sh.start = mine_before;
+    if (cost > 0 && x0 >= mine && x0 < mine + cost) {
+      sh.first_seq = s0 + threadIdx.x;
+      sh.start = mine;
     }
-    __syncthreads();
-    if (sh.first_seq >= 0) break;
+    if (x0 < before) break;
   }
 }
 
@@ -392,10 +412,10 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
       mbar_init(&sh.turn[i], 1);
       for (int b = 0; b < 2; ++b) {
         mbar_init(&sh.s_full[i][b], 1);
+        mbar_init(&sh.pv_done[i][b], 1);
         mbar_init(&sh.p_ready[i][b], kSoftWarps / 2);
         sh.bad_value[i][b] = 0;
       }
-      mbar_init(&sh.pv_done[i], 1);
       mbar_init(&sh.look[i], kSoftWarps / 2);
       mbar_init(&sh.join[i], kSoftWarps);
     }
@@ -421,7 +441,6 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = sh.tmem;               // S of the streams at columns 0 and 128, O at 256 and 384
-  const long long x_begin = sh.total * blockIdx.x / gridDim.x, x_end = sh.total * (blockIdx.x + 1) / gridDim.x;
 
   // waits of a whole warp, whose lanes go on or give up together
   auto wait = [&](uint64_t *bar, int parity) { return warp_wait(bar, parity & 1, abort_flag); };
@@ -463,7 +482,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
       else ++q_uses0;
     };
     if (sh.first_seq >= 0) {
-      long long left = x_end - x_begin, y = x_begin - sh.start;      // cost left to do; place within the sequence
+      long long left = sh.x1 - sh.x0, y = sh.x0 - sh.start;        // cost left to do; place within the sequence
       int window = sh.first_seq & ~31;
       SeqSpan span = {};
       int seq = sh.first_seq;
@@ -679,7 +698,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
 #pragma unroll
                 for (int k = 0; k < 4; ++k) tc_mma_ts(t_o, t_p + k * 8, dv + k * (HD * 32 >> 4), idesc_o, k > 0 || i != ahead);
               }
-              tc_commit(&sh.pv_done[w]);
+              tc_commit(&sh.pv_done[w][step & 1]);
               if (close) tc_commit(&sh.kv_empty[v_stage]);
             }
             if (i < steps) {
@@ -729,6 +748,9 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
     const int tok_a = row_a / a.group, tok_b = row_b / a.group;
     int n_item = 0, steps_done = 0, tiles_done = 0, looks = 0, joins = 0;
     bool ok = true;
+    // Barriers by the parity of the step, since two steps' products may be under way: a barrier that had both would be a
+    // phase before or behind the one that is waited for, and a phase is known by its parity alone.
+    auto products_done = [&](int step) { return wait(&sh.pv_done[w][step & 1], step >> 1); };
     while (ok) {
       const int slot = n_item % kItemRing;
       ok = wait(&sh.item_full[slot], n_item / kItemRing);
@@ -788,7 +810,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
               l_a *= fix_a;
               l_b *= fix_b;
               if (i > 0) {
-                ok = wait(&sh.pv_done[w], steps_done - 1);
+                ok = products_done(steps_done - 1);
                 if (!ok) break;
                 tc_fence_after();
 #pragma unroll 1
@@ -854,7 +876,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             slow = *const_cast<volatile int *>(&sh.bad_value[w][buf]) == steps_done + 1;
           }
           if (slow && warp_mine) {
-            if (i > 0) ok = wait(&sh.pv_done[w], steps_done - 1);
+            if (i > 0) ok = products_done(steps_done - 1);
             if (!ok) break;
             tc_fence_after();
 #pragma unroll 1
@@ -903,9 +925,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
       // ---- the item's result: whole rows, or a part for the joining launch
       const bool any = it.t0 < it.t1;
       if (any) {
-        // one after the other: the products of the last two steps may both be under way, and a phase is known by its parity
-        if (steps > 1) ok = wait(&sh.pv_done[w], steps_done - 2);
-        if (ok) ok = wait(&sh.pv_done[w], steps_done - 1);
+        ok = products_done(steps_done - 1);
         if (!ok) break;
       }
       tc_fence_after();
@@ -1020,43 +1040,60 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
   }
 }
 
-// Joins the parts of the items that were cut, in key order: CTA (b, g) the item whose first part CTA b left, rows g * 8 ..
-// A warp to a row.
+// Joins the parts of the items that were cut, in key order: CTA (b, g) the item whose first part CTA b left, rows 8 g ..
+// A warp to a row; its lanes look up 32 CTAs' records and partial sums at once.
 template <int HD, bool HALF>
 __global__ void __launch_bounds__(256) join_parts_kernel(const __grid_constant__ AttendArgs a, int n_ctas) {
   early_start_sync();
   const int b = blockIdx.x, lane = threadIdx.x & 31;
-  if (!a.records[b].first) return;
+  // lane i: the part of CTA b + i
+  PartRecord mine = {};
+  if (b + lane < n_ctas) mine = a.records[b + lane];
+  if (!__shfl_sync(0xffffffffu, mine.first, 0)) return;
   const Item it = a.records[b].item;
   const int row = blockIdx.y * 8 + (threadIdx.x >> 5);
   const int tile = row >> 7, r = row & 127, tok = tile * a.tile_tok + r / a.group;
   if (r >= a.tile_tok * a.group || tok >= it.n_tok) return;
-  // the reference of all parts, then their sums
-  const int64_t stride = 2 * static_cast<int64_t>(a.rows_cap), at0 = b * stride + a.rows_cap + row;
-  float ref = a.part_ml[at0].x;
-  int end = b + 1;                               // CTAs b + 1 .. end - 1 hold the later parts
-  for (bool more = true; more && end < n_ctas; ++end) {
-    const PartRecord &rec = a.records[end];
-    if (!rec.later) continue;
-    ref = fmaxf(ref, a.part_ml[end * stride + row].x);
-    more = !rec.later_ends;
-  }
-  float l = 0.f, o[HD / 32];
+  const int64_t stride = 2 * static_cast<int64_t>(a.rows_cap);
+  constexpr int kCols = HD / 32;                 // of a lane
+  float ref = -INFINITY, l = 0.f, o[kCols];
 #pragma unroll
-  for (int e = 0; e < HD / 32; ++e) o[e] = 0.f;
-  for (int k = b; k < end; ++k) {
-    if (k > b && !a.records[k].later) continue;
-    const int64_t at = k == b ? at0 : k * stride + row;
-    const float2 ml = a.part_ml[at];
+  for (int e = 0; e < kCols; ++e) o[e] = 0.f;
+  for (int k0 = b; k0 < n_ctas; k0 += 32) {
+    if (k0 > b) mine = k0 + lane < n_ctas ? a.records[k0 + lane] : PartRecord{};
+    const unsigned ends = __ballot_sync(0xffffffffu, (k0 > b || lane > 0) && mine.later && mine.later_ends);
+    const int n = ends ? __ffs(ends) : 32;       // lanes that belong to the item
+    const bool part = lane < n && (k0 + lane == b || mine.later);
+    const int64_t at = (k0 + lane) * stride + (k0 + lane == b ? a.rows_cap : 0) + row;
+    const float2 ml = part ? a.part_ml[at] : make_float2(-INFINITY, 0.f);
+    float to = fmaxf(ref, ml.x);
+#pragma unroll
+    for (int d = 16; d; d >>= 1) to = fmaxf(to, __shfl_xor_sync(0xffffffffu, to, d));
+    if (to != ref) {                             // (from -inf: nothing yet)
+      const float fix = ref == -INFINITY ? 0.f : ex2(ref - to);
+      l *= fix;
+#pragma unroll
+      for (int e = 0; e < kCols; ++e) o[e] *= fix;
+      ref = to;
+    }
     const float scale = ml.x == -INFINITY ? 0.f : ex2(ml.x - ref);
-    l += ml.y * scale;
+    float sum = ml.y * scale;
 #pragma unroll
-    for (int e = 0; e < HD / 32; ++e) o[e] += a.part_o[at * HD + lane * (HD / 32) + e] * scale;
+    for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+    l += sum;
+    for (unsigned left = __ballot_sync(0xffffffffu, part); left; left &= left - 1) {
+      const int k = __ffs(left) - 1;
+      const float *p = a.part_o + __shfl_sync(0xffffffffu, at, k) * HD + lane * kCols;
+      const float s = __shfl_sync(0xffffffffu, scale, k);
+#pragma unroll
+      for (int e = 0; e < kCols; ++e) o[e] = fmaf(p[e], s, o[e]);
+    }
+    if (ends) break;
   }
-  const float norm = it.pos0 + tok < 0 ? 0.f : 1.0f / l;
-  uint16_t *dst = a.out + (static_cast<int64_t>(it.row0 + tok) * a.Hq + it.head * a.group + r % a.group) * HD + lane * (HD / 32);
+  const float norm = 1.0f / l;
+  uint16_t *dst = a.out + (static_cast<int64_t>(it.row0 + tok) * a.Hq + it.head * a.group + r % a.group) * HD + lane * kCols;
 #pragma unroll
-  for (int e = 0; e < HD / 32; e += 2)
+  for (int e = 0; e < kCols; e += 2)
     *reinterpret_cast<uint32_t *>(dst + e) = it.pos0 + tok < 0 ? 0u : cvt16x2(o[e] * norm, o[e + 1] * norm, HALF);
 }
 
