@@ -14,9 +14,11 @@
 namespace echo {
 namespace {
 
-constexpr int kAppThreads = 256;
-constexpr int kAppRows = 8;                     // most rows of a CTA
-constexpr int kAppItems = 2;                    // work items a thread holds in registers at once
+// What hides HBM's latency is the number of warps: one item in a thread's registers, 40 registers, and CTAs of 128 threads
+// where there are many rows (16 x 1024 rows at 64/8 heads, bf16: 119 us, 0.86 of the copy rate; two items a thread 144).  Where
+// there are few, a row's items at once (384 threads are the 48 heads of 128 of one row).
+constexpr int kAppThreads = 128, kAppFewThreads = 384;
+constexpr int kAppRows = 2;                     // most rows of a CTA
 
 struct AppendArgs {
   const void *q, *k, *v;                        // q may be null
@@ -75,7 +77,7 @@ __device__ __forceinline__ int find_sequence(const ChunkArgs &c, int row) {
 }
 
 template <int IN, bool VEC>
-__global__ void __launch_bounds__(kAppThreads)
+__global__ void __launch_bounds__(kAppFewThreads, 4)
 append_kv_kernel(const __grid_constant__ AppendArgs a) {
   __shared__ int s_pos[kAppRows];
   __shared__ long long s_slot[kAppRows];            // element of the pool where head 0's key goes; -1: nowhere
@@ -85,37 +87,24 @@ append_kv_kernel(const __grid_constant__ AppendArgs a) {
   const int row0 = static_cast<int>(blockIdx.x) * a.rows_per_cta, rows = min(a.rows_per_cta, a.c.n_rows - row0);
   const int items = rows * units * per_unit;
   const int warp = threadIdx.x >> 5;
-  for (int begin = 0; begin < items; begin += kAppThreads * kAppItems) {
-    float x[kAppItems][8], y[kAppItems][8];
-    int unit[kAppItems], row[kAppItems], at[kAppItems];
-#pragma unroll
-    for (int j = 0; j < kAppItems; ++j) {
-      const int item = begin + j * kAppThreads + threadIdx.x;
-      const int u = item / per_unit;
-      at[j] = (item % per_unit) * 8;
-      row[j] = u / units;
-      unit[j] = item < items ? u % units : -1;
-      if (unit[j] < 0) continue;
-      const int64_t r = row0 + row[j];
-      const void *src;
-      int64_t off;
-      if (unit[j] < a.Hq) {
-        src = a.q;
-        off = r * a.q_stride + unit[j] * a.hd + at[j];
-      } else if (unit[j] < a.Hq + a.Hkv) {
-        src = a.k;
-        off = r * a.k_stride + (unit[j] - a.Hq) * a.hd + at[j];
-      } else {
-        src = a.v;
-        off = r * a.v_stride + (unit[j] - a.Hq - a.Hkv) * a.hd + at[j];
-      }
-      load8<IN, VEC>(src, off, x[j]);
-      load8<IN, VEC>(src, off + half, y[j]);
+  const int threads = blockDim.x;
+  for (int item = threadIdx.x, begin = 0; begin < items; item += threads, begin += threads) {
+    const int u = item / per_unit, at = (item % per_unit) * 8, row = u / units, unit = item < items ? u % units : -1;
+    const bool value = unit >= a.Hq + a.Hkv;
+    float x[8], y[8];
+    if (unit >= 0) {
+      const int64_t r = row0 + row;
+      const void *src = value ? a.v : unit < a.Hq ? a.q : a.k;
+      const int64_t off = value           ? r * a.v_stride + (unit - a.Hq - a.Hkv) * a.hd
+                          : unit < a.Hq ? r * a.q_stride + unit * a.hd
+                                          : r * a.k_stride + (unit - a.Hq) * a.hd;
+      load8<IN, VEC>(src, off + at, x);
+      load8<IN, VEC>(src, off + at + half, y);
     }
     if (begin == 0) {
       // every sequence's lengths are looked at once, by the first CTA
       if (blockIdx.x == 0)
-        for (int s = threadIdx.x; s < a.c.S; s += kAppThreads) {
+        for (int s = threadIdx.x; s < a.c.S; s += threads) {
           const SeqSpan p = seq_span(a.c, s);
           if (!p.ok || p.kv < p.n) atomicMax(a.c.status, STATUS_BAD_CHUNK);
         }
@@ -141,7 +130,7 @@ append_kv_kernel(const __grid_constant__ AppendArgs a) {
         }
       }
       __syncthreads();
-      for (int i = threadIdx.x; i < rows * half; i += kAppThreads) {
+      for (int i = threadIdx.x; i < rows * half; i += threads) {
         const int r = i / half, j = i % half;
         const double turns = static_cast<double>(s_pos[r]) * a.rate[j];
         float sn, cs;
@@ -150,31 +139,27 @@ append_kv_kernel(const __grid_constant__ AppendArgs a) {
       }
       __syncthreads();
     }
+    if (unit < 0 || s_pos[row] < 0) continue;
+    if (!value) {
 #pragma unroll
-    for (int j = 0; j < kAppItems; ++j) {
-      if (unit[j] < 0 || s_pos[row[j]] < 0) continue;
-      const bool value = unit[j] >= a.Hq + a.Hkv;
-      if (!value) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float2 t = s_turn[row[j]][at[j] + e];
-          const float lo = x[j][e] * t.x - y[j][e] * t.y, hi = y[j][e] * t.x + x[j][e] * t.y;
-          x[j][e] = lo;
-          y[j][e] = hi;
-        }
+      for (int e = 0; e < 8; ++e) {
+        const float2 t = s_turn[row][at + e];
+        const float lo = x[e] * t.x - y[e] * t.y, hi = y[e] * t.x + x[e] * t.y;
+        x[e] = lo;
+        y[e] = hi;
       }
-      uint16_t *dst;
-      if (unit[j] < a.Hq) {
-        dst = a.out_q + (static_cast<int64_t>(row0 + row[j]) * a.Hq + unit[j]) * a.hd + at[j];
-      } else {
-        const long long slot = s_slot[row[j]];
-        if (slot < 0) continue;
-        const int head = unit[j] - a.Hq - (value ? a.Hkv : 0);
-        dst = a.pool + slot + static_cast<long long>(head * 2 + (value ? 1 : 0)) * kChunkPage * a.hd + at[j];
-      }
-      *reinterpret_cast<uint4 *>(dst) = pack8(x[j], a.half_out);
-      *reinterpret_cast<uint4 *>(dst + half) = pack8(y[j], a.half_out);
     }
+    uint16_t *dst;
+    if (unit < a.Hq) {
+      dst = a.out_q + (static_cast<int64_t>(row0 + row) * a.Hq + unit) * a.hd + at;
+    } else {
+      const long long slot = s_slot[row];
+      if (slot < 0) continue;
+      const int head = unit - a.Hq - (value ? a.Hkv : 0);
+      dst = a.pool + slot + static_cast<long long>(head * 2 + (value ? 1 : 0)) * kChunkPage * a.hd + at;
+    }
+    *reinterpret_cast<uint4 *>(dst) = pack8(x, a.half_out);
+    *reinterpret_cast<uint4 *>(dst + half) = pack8(y, a.half_out);
   }
 }
 
@@ -231,14 +216,14 @@ extern "C" int echo_append_kv(const void *q, const void *k, const void *v, int32
   a.half_out = kv_format == 1;
   for (int j = 0; j < hd / 2; ++j)
     a.rate[j] = std::pow(static_cast<double>(rope_theta), -2.0 * j / hd) / 6.283185307179586476925286766559;
-  // a row to a CTA while that makes fewer than eight CTAs an SM; more rows share the look-ups' latency
-  int rows = 1;
-  while (rows < kAppRows && a.c.n_rows / (2 * rows) >= 8 * 148) rows *= 2;
+  // few rows (fewer than eight CTAs an SM): a row to a CTA; otherwise two rows share the look-ups' latency
+  const bool few = a.c.n_rows < 8 * 148;
+  const int rows = few ? 1 : kAppRows;
   a.rows_per_cta = rows;
   const auto kernel = in_format == 0   ? (vec ? append_kv_kernel<0, true> : append_kv_kernel<0, false>)
                       : in_format == 1 ? (vec ? append_kv_kernel<1, true> : append_kv_kernel<1, false>)
                                        : (vec ? append_kv_kernel<2, true> : append_kv_kernel<2, false>);
-  const cudaError_t e = launch_early(kernel, dim3((static_cast<unsigned>(a.c.n_rows) + rows - 1) / rows), dim3(kAppThreads), 0,
+  const cudaError_t e = launch_early(kernel, dim3((static_cast<unsigned>(a.c.n_rows) + rows - 1) / rows), dim3(few ? kAppFewThreads : kAppThreads), 0,
                                      static_cast<cudaStream_t>(cuda_stream), a);
   return e == cudaSuccess ? ECHO_OK : ECHO_ERR_CUDA;
 }

@@ -37,6 +37,7 @@
 // scheduler, and what one waited for the other could not fill (2048 tokens over 14336: 447 us).
 
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 
 #include "chunks.cuh"
@@ -58,6 +59,7 @@ constexpr int kSoftWarps = 16;
 constexpr int kAttThreads = 32 * (kSoftWarps + 4);
 constexpr int kMaxCtas = 148;                  // CTAs of a launch: sizes the workspace
 constexpr int kItemRing = 4;
+constexpr int kDevices = 64;                   // whose properties are remembered
 constexpr int kFmaShare = 1;                   // of 8 pairs of exponentials, those that the FMA units compute
 constexpr float kMostSum = 8192.0f;            // of a row's probabilities in a tile, before its reference has to move
 
@@ -1124,12 +1126,25 @@ int rows_cap(int max_chunk, int group) {
   return max_chunk > tile_tok ? 256 : (max_chunk * group + 7) / 8 * 8;
 }
 
+// SMs of the current device (0: unknown), looked up once.
+int sm_count(int dev) {
+  static std::atomic<int> known[kDevices];
+  int n = dev < kDevices ? known[dev].load(std::memory_order_relaxed) : 0;
+  if (n == 0 && cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess && dev < kDevices)
+    known[dev].store(n, std::memory_order_relaxed);
+  return n;
+}
+
 template <int HD, bool HALF, bool FEW>
-cudaError_t launch_attend(const CUtensorMap &tm_q, const CUtensorMap &tm_kv, const AttendArgs &a, int ctas, cudaStream_t s) {
+cudaError_t launch_attend(const CUtensorMap &tm_q, const CUtensorMap &tm_kv, const AttendArgs &a, int dev, int ctas, cudaStream_t s) {
   constexpr int smem = AttSmem<HD, FEW>::kTotal;
-  cudaError_t e = cudaFuncSetAttribute(chunk_attention_kernel<HD, HALF, FEW>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-  if (e != cudaSuccess) return e;
-  e = launch_early(chunk_attention_kernel<HD, HALF, FEW>, dim3(ctas), dim3(kAttThreads), smem, s, tm_q, tm_kv, a);
+  static std::atomic<bool> allowed[kDevices];      // the kernel's shared memory, on a device
+  if (dev >= kDevices || !allowed[dev].load(std::memory_order_acquire)) {
+    const cudaError_t e = cudaFuncSetAttribute(chunk_attention_kernel<HD, HALF, FEW>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != cudaSuccess) return e;
+    if (dev < kDevices) allowed[dev].store(true, std::memory_order_release);
+  }
+  const cudaError_t e = launch_early(chunk_attention_kernel<HD, HALF, FEW>, dim3(ctas), dim3(kAttThreads), smem, s, tm_q, tm_kv, a);
   if (e != cudaSuccess) return e;
   return launch_early(join_parts_kernel<HD, HALF>, dim3(ctas, a.rows_cap / 8), dim3(256), 0, s, a, ctas);
 }
@@ -1181,9 +1196,10 @@ int echo_chunk_attention(const void *q, int64_t q_stride, const void *kv_pool, i
   ws += kMaxCtas * kRecordBytes;
   a.part_o = reinterpret_cast<float *>(ws);
   a.part_ml = reinterpret_cast<float2 *>(ws + static_cast<size_t>(kMaxCtas) * 2 * a.rows_cap * hd * sizeof(float));
-  int dev = 0, sms = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
-    return ECHO_ERR_CUDA;
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return ECHO_ERR_CUDA;
+  const int ctas = std::min(sm_count(dev), kMaxCtas);
+  if (ctas < 1) return ECHO_ERR_CUDA;
   const bool half = format == 1;
   CUtensorMap tm_q, tm_kv;
   // queries: 64 elements of a head x the heads of a group x the tokens of a tile
@@ -1196,13 +1212,12 @@ int echo_chunk_attention(const void *q, int64_t q_stride, const void *kv_pool, i
   const cuuint64_t kst[3] = {static_cast<cuuint64_t>(hd) * 2, 128, static_cast<cuuint64_t>(hd) * 16};
   const cuuint32_t kb[4] = {64, 8, static_cast<cuuint32_t>(hd / 64), 2};
   if (!make_map(&tm_q, 3, q, half, qd, qst, qb) || !make_map(&tm_kv, 4, kv_pool, half, kd, kst, kb)) return ECHO_ERR_CUDA;
-  const int ctas = std::min(sms, kMaxCtas);
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
   const auto launch = hd == 128 ? (half ? (few ? launch_attend<128, true, true> : launch_attend<128, true, false>)
                                         : (few ? launch_attend<128, false, true> : launch_attend<128, false, false>))
                                 : (half ? (few ? launch_attend<64, true, true> : launch_attend<64, true, false>)
                                         : (few ? launch_attend<64, false, true> : launch_attend<64, false, false>));
-  const cudaError_t e = launch(tm_q, tm_kv, a, ctas, s);
+  const cudaError_t e = launch(tm_q, tm_kv, a, dev, ctas, s);
   return e == cudaSuccess ? ECHO_OK : ECHO_ERR_CUDA;
 }
 
