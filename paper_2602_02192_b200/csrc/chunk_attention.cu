@@ -60,7 +60,6 @@ constexpr int kAttThreads = 32 * (kSoftWarps + 4);
 constexpr int kMaxCtas = 148;                  // CTAs of a launch: sizes the workspace
 constexpr int kItemRing = 4;
 constexpr int kDevices = 64;                   // whose properties are remembered
-constexpr int kFmaShare = 1;                   // of 8 pairs of exponentials, those that the FMA units compute
 constexpr float kMostSum = 8192.0f;            // of a row's probabilities in a tile, before its reference has to move
 
 // Costs that the shares are cut by: of a key, and of an item's beginning and end.
@@ -73,6 +72,7 @@ constexpr int kLeastPart = 1;                  // key tiles
 constexpr int kFewRows = 64;
 template <int HD, bool FEW> struct AttSmem {
   static constexpr int kQRows = FEW ? kFewRows : 128;
+  static constexpr int kRowWarps = kQRows / 16;                       // softmax warps of a stream that can have rows
   static constexpr int kQHalf = kQRows * 128;                         // 64 elements of every row
   static constexpr int kQTile = HD / 64 * kQHalf;
   static constexpr int kStage = kKeys * HD * 2;
@@ -163,22 +163,6 @@ __device__ __forceinline__ float max3_nan(float a, float b, float c) {
   float d;
   asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
   return d;
-}
-// 2^x of two numbers on the fused multiply-add units: whole part by adding 1.5 2^23, which rounds it into the low bits of the
-// sum; 2^f on [-1/2, 1/2] by a polynomial of degree 4 with constant term 1, fitted here to the least largest relative error
-// (2^-18.4); the whole part goes to the exponent.  Exactly 0 from 2^-127 down; x up to 127.
-__device__ __forceinline__ float2 exp2_by_fma(float2 x) {
-  x = make_float2(max_nan(x.x, -127.f), max_nan(x.y, -127.f));
-  const float2 big = make_float2(12582912.f, 12582912.f), neg = make_float2(-12582912.f, -12582912.f);
-  const float2 t = add2(x, big);
-  const float2 whole = add2(t, neg);
-  const float2 f = fma2(whole, make_float2(-1.f, -1.f), x);
-  float2 p = fma2(f, make_float2(0.009582852944731712f, 0.009582852944731712f), make_float2(0.055906426161527634f, 0.055906426161527634f));
-  p = fma2(p, f, make_float2(0.24024099111557007f, 0.24024099111557007f));
-  p = fma2(p, f, make_float2(0.6931241750717163f, 0.6931241750717163f));
-  p = fma2(p, f, make_float2(1.f, 1.f));
-  return make_float2(__int_as_float(__float_as_int(p.x) + (__float_as_int(t.x) << 23)),
-                     __int_as_float(__float_as_int(p.y) + (__float_as_int(t.y) << 23)));
 }
 // A whole warp's bounded wait; its lanes go on or give up together.  Votes keep the loop free of divergence, and the clock
 // is read now and then only: a wait that has nothing to wait for takes 60 cycles, four times less than with a clock and a
@@ -415,11 +399,11 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
       for (int b = 0; b < 2; ++b) {
         mbar_init(&sh.s_full[i][b], 1);
         mbar_init(&sh.pv_done[i][b], 1);
-        mbar_init(&sh.p_ready[i][b], kSoftWarps / 2);
+        mbar_init(&sh.p_ready[i][b], M::kRowWarps);
         sh.bad_value[i][b] = 0;
       }
-      mbar_init(&sh.look[i], kSoftWarps / 2);
-      mbar_init(&sh.join[i], kSoftWarps);
+      mbar_init(&sh.look[i], M::kRowWarps);
+      mbar_init(&sh.join[i], 2 * M::kRowWarps);
     }
     for (int i = 0; i < M::kStages; ++i) {
       mbar_init(&sh.kv_full[i], 1);
@@ -427,7 +411,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
     }
     for (int i = 0; i < kItemRing; ++i) {
       mbar_init(&sh.item_full[i], 1);
-      mbar_init(&sh.item_empty[i], kSoftWarps + 2);
+      mbar_init(&sh.item_empty[i], 2 * M::kRowWarps + 2);
     }
     sh.abort_flag = 0;
     mbar_fence_init();
@@ -742,7 +726,9 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
     }
   } else {
     // ---------------------------------------------------------------- softmax and results
-    const int w = warp >> 3, lane0 = (warp & 3) * 32 + (warp & 4) * 4, stream_tid = threadIdx.x & 255;
+    const int w = warp >> 3, lane0 = (warp & 3) * 32 + (warp & 4) * 4;
+    // thread of the stream's 32 kRowWarps; a warp whose rows no item has takes no part (its waits would only cost power)
+    const int stream_tid = FEW ? ((warp & 4) >> 1 | (warp & 1)) * 32 + lane : threadIdx.x & 255;
     const uint32_t lanes = static_cast<uint32_t>(lane0) << 16;
     const uint32_t t_s0 = tmem + lanes + w * 128, t_o = tmem + lanes + 256 + w * 128;
     const float c = a.scale_log2;
@@ -753,7 +739,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
     // Barriers by the parity of the step, since two steps' products may be under way: a barrier that had both would be a
     // phase before or behind the one that is waited for, and a phase is known by its parity alone.
     auto products_done = [&](int step) { return wait(&sh.pv_done[w][step & 1], step >> 1); };
-    while (ok) {
+    while (ok && lane0 < M::kQRows) {
       const int slot = n_item % kItemRing;
       ok = wait(&sh.item_full[slot], n_item / kItemRing);
       if (!ok) break;
@@ -833,8 +819,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             for (int b = 0; b < 8; ++b) {
               const float2 x = fma2(make_float2(__uint_as_float(s[4 * b]), __uint_as_float(s[4 * b + 1])), c2, base2_a);
               const float2 y = fma2(make_float2(__uint_as_float(s[4 * b + 2]), __uint_as_float(s[4 * b + 3])), c2, base2_b);
-              const float2 px = (2 * b & 7) < kFmaShare ? exp2_by_fma(x) : make_float2(ex2(x.x), ex2(x.y));
-              const float2 py = (2 * b + 1 & 7) < kFmaShare ? exp2_by_fma(y) : make_float2(ex2(y.x), ex2(y.y));
+              const float2 px = make_float2(ex2(x.x), ex2(x.y)), py = make_float2(ex2(y.x), ex2(y.y));
               sum_a = add2(sum_a, px);
               sum_b = add2(sum_b, py);
               p[2 * b] = cvt16x2(px.x, px.y, HALF);
@@ -861,7 +846,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
           uint8_t *v = smem + M::kKV + stage * M::kStage;
           const int u0 = min(ks, ke) * (HD / 8), u1 = ke16 * (HD / 8);
           bool bad = false;
-          for (int u = u0 + stream_tid; u < u1; u += 256) {
+          for (int u = u0 + stream_tid; u < u1; u += 32 * M::kRowWarps) {
             uint4 *unit = reinterpret_cast<uint4 *>(v + kv_unit<HD>(key_off + u / (HD / 8), u % (HD / 8)));
             if (u / (HD / 8) < ke) bad |= any_undefined<HALF>(*unit);
             else *unit = make_uint4(0u, 0u, 0u, 0u);                  // no row of the item sees it
