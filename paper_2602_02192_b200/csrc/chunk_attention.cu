@@ -67,8 +67,8 @@ constexpr int kSingleWeight = 6, kPairWeight = 8, kSingleStart = 2048, kPairStar
 constexpr int kLeastShare = 1024;              // of a CTA: little work goes to few CTAs, for whoever joins its parts
 constexpr int kLeastPart = 1;                  // key tiles
 
-// FEW: no item has more than 64 rows.  Its query tiles are stored as far as they have rows (what an MMA reads behind them,
-// keys, makes rows that nobody reads), and the copies get a stage more.
+// FEW: no item has more than 64 rows.  MMAs of 64 rows, which take less power (a decode step is bound by HBM in a burst and by
+// power in a run), and smaller query tiles, so that the copies get a stage more.
 constexpr int kFewRows = 64;
 template <int HD, bool FEW> struct AttSmem {
   static constexpr int kQRows = FEW ? kFewRows : 128;
@@ -198,6 +198,10 @@ __device__ __forceinline__ uint64_t smem_desc(uint32_t saddr, uint32_t lbo, uint
          (static_cast<uint64_t>(sbo >> 4) << 32) | (static_cast<uint64_t>(1) << 46) | (static_cast<uint64_t>(2) << 61);
 }
 constexpr uint32_t kIdescBMajorMN = 1u << 16;
+// M = 128, or 64: rows 16 i .. 16 i + 15 are then the first 16 lanes of warp quarter i
+__host__ __device__ constexpr uint32_t idesc_rows(uint32_t idesc, int rows) {
+  return (idesc & ~(31u << 24)) | (static_cast<uint32_t>(rows >> 4) << 24);
+}
 __device__ __forceinline__ bool elect_one() {
   uint32_t one;
   asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(one));
@@ -620,8 +624,8 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
     // long as it runs.
     if (warp == kMma0 || warp == kMma1) {
       const int w = warp == kMma0 ? 0 : 1;
-      constexpr uint32_t idesc_s = idesc_operands(instr_desc_bf16(64), HALF);
-      constexpr uint32_t idesc_o = idesc_operands(instr_desc_bf16(HD), HALF) | kIdescBMajorMN;
+      constexpr uint32_t idesc_s = idesc_operands(idesc_rows(instr_desc_bf16(64), M::kQRows), HALF);
+      constexpr uint32_t idesc_o = idesc_operands(idesc_rows(instr_desc_bf16(HD), M::kQRows), HALF) | kIdescBMajorMN;
       constexpr int kStages = M::kStages;
       const uint32_t q_s = smem_u32(smem + M::kQ), kv_s = smem_u32(smem + M::kKV);
       const uint32_t t_s = tmem + w * 128, t_o = tmem + 256 + w * 128;
@@ -726,20 +730,22 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
     }
   } else {
     // ---------------------------------------------------------------- softmax and results
-    const int w = warp >> 3, lane0 = (warp & 3) * 32 + (warp & 4) * 4;
-    // thread of the stream's 32 kRowWarps; a warp whose rows no item has takes no part (its waits would only cost power)
-    const int stream_tid = FEW ? ((warp & 4) >> 1 | (warp & 1)) * 32 + lane : threadIdx.x & 255;
+    // 16 rows: of 128, the first or the second 16 lanes of the warp's quarter of tensor memory; of 64, its first 16 (the
+    // other warp of the quarter takes no part)
+    const int w = warp >> 3, high = (warp >> 2) & 1, quarter = warp & 3;
+    const int lane0 = quarter * 32 + high * 16, row0 = FEW ? quarter * 16 : lane0;
+    const int stream_tid = (FEW ? quarter : warp & 7) * 32 + lane;
     const uint32_t lanes = static_cast<uint32_t>(lane0) << 16;
     const uint32_t t_s0 = tmem + lanes + w * 128, t_o = tmem + lanes + 256 + w * 128;
     const float c = a.scale_log2;
-    const int row_a = lane0 + (lane >> 2), row_b = row_a + 8, col = 2 * (lane & 3);      // of every eight columns: col, col + 1
+    const int row_a = row0 + (lane >> 2), row_b = row_a + 8, col = 2 * (lane & 3);      // of every eight columns: col, col + 1
     const int tok_a = row_a / a.group, tok_b = row_b / a.group;
     int n_item = 0, steps_done = 0, tiles_done = 0, looks = 0, joins = 0;
     bool ok = true;
     // Barriers by the parity of the step, since two steps' products may be under way: a barrier that had both would be a
     // phase before or behind the one that is waited for, and a phase is known by its parity alone.
     auto products_done = [&](int step) { return wait(&sh.pv_done[w][step & 1], step >> 1); };
-    while (ok && lane0 < M::kQRows) {
+    while (ok && !(FEW && high)) {
       const int slot = n_item % kItemRing;
       ok = wait(&sh.item_full[slot], n_item / kItemRing);
       if (!ok) break;
@@ -749,7 +755,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
       const int row_tile = paired ? w : 0, steps = (it.t1 - it.t0) * (paired ? 2 : 1);
       const int tok0 = row_tile * a.tile_tok, n_rows = min(a.tile_tok, it.n_tok - tok0) * a.group;
       const int pos_first = it.pos0 + tok0, pos_a = pos_first + tok_a, pos_b = pos_first + tok_b;
-      const bool mine_a = row_a < n_rows, mine_b = row_b < n_rows, warp_mine = lane0 < n_rows;
+      const bool mine_a = row_a < n_rows, mine_b = row_b < n_rows, warp_mine = row0 < n_rows;
       float m_a = -INFINITY, m_b = -INFINITY;                         // references (score units)
       float l_a = 0.f, l_b = 0.f;                                     // sums of this thread's columns
       for (int i = 0; i < steps; ++i) {          // of 64 keys
