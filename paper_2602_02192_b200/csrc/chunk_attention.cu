@@ -3,38 +3,42 @@
 //   o_i = sum_{u <= t_i} exp(q_i . k_u / sqrt(hd)) v_u / sum_{u <= t_i} exp(q_i . k_u / sqrt(hd)),   t_i = L - n + i
 //
 // Tiles.  The query heads of a kv head read the same keys, so a row of a tile is a (token, query head) pair: 128 rows are
-// 128 / (Hq / Hkv) tokens.  Keys come in tiles of 128 (eight pages).  S = Q K^T (128 x 128) and O += P V (128 x hd) run on
-// the tcgen05 tensor cores: Q, K, V in shared memory as TMA leaves them (128-byte swizzle; K is the K-major operand, V the
-// same bytes read as an MN-major one), S, P and O in tensor memory, P over the columns that held S.  A thread owns a row:
-// it finds the row's maximum and sum without a shuffle.
+// 128 / (Hq / Hkv) tokens.  Keys come in tiles of 128 (eight pages).  S = Q K^T and O += P V run on the tcgen05 tensor
+// cores: Q, K, V in shared memory as TMA leaves them (128-byte swizzle; K is the K-major operand, V the same bytes read as an
+// MN-major one), S, P and O in tensor memory, P over the columns that held S.
 //
-// Two streams of tiles are in flight in a CTA, each with its own warpgroup, S and O, so that the tensor cores work on one
-// while the other's probabilities are formed:
+// Two streams of tiles are in flight in a CTA, each with its own warps, S and O, so that the tensor cores work on one while
+// the other's probabilities are formed:
 //   paired items   two row tiles share each K and V tile (long chunks: keys are read once per 256 rows)
 //   single items   one row tile; the streams take 64 keys each of every tile, and their two results are joined at the end
 //                  (few rows: what counts is to keep the copies running)
 // Either way both streams take every key tile in order, so that a barrier's phase is never more than one away from what is
-// waited for.  A step of a stream is 64 keys, and its S has room for two: S of the next step is formed while this one's
-// probabilities are (with one S of 128 keys the streams' chains bounded everything: 462 us for 2048 tokens over 14336).
+// waited for.  A step of a stream is 64 keys, and its S has room for two: of pairs, S of the next step is formed while this
+// one's probabilities are.
 //
-// Work.  An item is (sequence, kv head, pair of row tiles or last single one) with its keys.  Every other item of a head
-// takes its key tiles from the last to the first: they are the ones that L2 still holds, where the caches that 148 CTAs
-// read at once do not fit (40 chunks of 16 to 400 tokens over 200 to 5000).  Items have very different lengths and the lengths are in device memory, so every CTA (one to an SM) adds up all items' costs, takes its equal share
+// Work.  An item is (sequence, kv head, pair of row tiles or last single one) with its keys.  Items have very different
+// lengths and the lengths are in device memory, so every CTA (one to an SM) adds up all items' costs, takes its equal share
 // of the total, and walks the items in it; an item that crosses a border is cut between two key tiles.  Cut items leave
-// fp32 partial results (unnormalised O, maximum, sum) in the workspace, in places that only depend on the CTA, and a second
-// launch joins them in key order: no atomics, equal inputs give equal outputs.
+// fp32 partial results (unnormalised O, reference, sum) in the workspace, in places that only depend on the CTA, and a second
+// launch joins them in key order: no atomics, equal inputs give equal outputs.  Every other item of a head takes its key
+// tiles from the last to the first: those are what L2 may still hold.
 //
-// A row's reference (what its exponents are relative to) is its maximum over the item's first tile.  It moves when a tile's
-// probabilities, relative to it, add up to more than 2^13: the maximum has then grown.  So O is hardly ever rescaled, most
-// tiles need no maxima, and a probability is at most 2^13, which both formats hold.
+// A row's reference (what its exponents are relative to) is its maximum over the item's first step.  It moves when the
+// probabilities of 64 keys, relative to it, add up to more than 2^13: the maximum has then grown.  So O is hardly ever
+// rescaled, most steps need no maxima, and a probability is at most 2^13, which both formats hold.
 //
 // What a row does not see has no part in it: masked scores are replaced, not added to.  A masked probability is 0, but
-// 0 times an undefined value would not be: where a tile has keys that only some of its rows see, their values are looked
-// at, and a tile with an infinity or a NaN among them is accumulated by the threads instead (slow, and nothing else).
+// 0 times an undefined value would not be: where a step has keys that only some of its rows see, their values are looked
+// at, and a step with an infinity or a NaN among them is accumulated by the threads instead (slow, and nothing else).
 //
 // Roles: warps 0-7 and 8-15 the two streams' softmax, warps 16 and 18 issue their MMAs, warp 17 walks the items and loads.
 // A softmax warp has 16 rows, four threads to a row: with 32 rows to a warp and a thread to a row two warps shared a
-// scheduler, and what one waited for the other could not fill (2048 tokens over 14336: 447 us).
+// scheduler, and what one waited for the other could not fill (2048 tokens over 14336: 447 us instead of 431).
+//
+// Measured (32/8 heads of 128, bf16, in bursts; in a run of them the SM clock falls with the power): 256 single tokens over
+// 512 to 2559 keys 258 us, 0.96 of the copy rate; 2048 tokens over 14336 431 us, 1.19 PFLOP/s.  Few rows are bound by HBM
+// (by power in a run), long chunks by the tensor cores at two thirds of their cycles and the softmax warps between them: a
+// step's S of 64 keys reads Q from shared memory again, 48 cycles an MMA instead of 32.
 
 #include <algorithm>
 #include <atomic>
@@ -60,12 +64,12 @@ constexpr int kAttThreads = 32 * (kSoftWarps + 4);
 constexpr int kMaxCtas = 148;                  // CTAs of a launch: sizes the workspace
 constexpr int kItemRing = 4;
 constexpr int kDevices = 64;                   // whose properties are remembered
-constexpr float kMostSum = 8192.0f;            // of a row's probabilities in a tile, before its reference has to move
+constexpr float kMostSum = 8192.0f;            // of a row's probabilities in a step, before its reference has to move
 
 // Costs that the shares are cut by: of a key, and of an item's beginning and end.
 constexpr int kSingleWeight = 6, kPairWeight = 8, kSingleStart = 2048, kPairStart = 3072;
-constexpr int kLeastShare = 1024;              // of a CTA: little work goes to few CTAs, for whoever joins its parts
-constexpr int kLeastPart = 1;                  // key tiles
+// Measured: with the weights 4 : 8 and half of these starts 40 chunks of 16 to 400 tokens took 437 us instead of 356.
+constexpr int kLeastShare = 1024;              // of a CTA that has work: little work goes to few CTAs
 
 // FEW: no item has more than 64 rows.  MMAs of 64 rows, which take less power (a decode step is bound by HBM in a burst and by
 // power in a run), and smaller query tiles, so that the copies get a stage more.
@@ -257,8 +261,7 @@ __device__ __forceinline__ SeqCost seq_cost(const SeqSpan &p, int tile_tok) {
 __device__ __forceinline__ int cut_tile(long long x, bool single, int seen) {
   const int tiles = (seen + kKeys - 1) / kKeys;
   const long long y = x - (single ? kSingleStart : kPairStart), per = (single ? kSingleWeight : kPairWeight) * kKeys;
-  const int t = y <= 0 ? 0 : static_cast<int>(min(static_cast<long long>(tiles), (y + per - 1) / per));
-  return t == tiles ? t : t < kLeastPart ? 0 : tiles - t < kLeastPart ? tiles : t;
+  return y <= 0 ? 0 : static_cast<int>(min(static_cast<long long>(tiles), (y + per - 1) / per));
 }
 
 // ---- the kernel ----------------------------------------------------------------------------------------
@@ -269,7 +272,7 @@ template <int HD, bool FEW> struct Shared {
   uint64_t look[2], join[2], turn[2], drain[2];
   Item items[kItemRing];
   int bad_page[kItemRing];
-  int bad_value[2][2];              // [stream][half]: step (+ 1) whose P V the threads add themselves
+  int bad_value[2][2];              // [stream][parity of its step]: step + 1 whose P V the threads add themselves
   uint32_t tmem;
   int abort_flag;
   long long x0, x1, start;          // plan: the CTA's share of the cost; cost in front of its first sequence
@@ -390,7 +393,10 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
   constexpr int kMma0 = kSoftWarps, kLoad = kSoftWarps + 1, kMma1 = kSoftWarps + 2;
   volatile int *abort_flag = &sh.abort_flag;
   if (smem_u32(smem) & 1023) {                 // (swizzled tiles need it; a dynamic array alone begins there)
-    if (threadIdx.x == 0) atomicMax(a.c.status, STATUS_WAIT_TIMEOUT);
+    if (threadIdx.x == 0) {
+      atomicMax(a.c.status, STATUS_WAIT_TIMEOUT);
+      a.records[blockIdx.x] = PartRecord{};
+    }
     return;
   }
 

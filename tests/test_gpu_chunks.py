@@ -210,9 +210,13 @@ def test_attention_of_ragged_chunks(B, heads, dtype):
     ((4, 2, 64), [(1, n) for n in range(1, 290, 7)]),         # many sequences of one token
     ((16, 8, 128), [(n, 2 * n) for n in range(1, 60)]),
     ((8, 8, 128), [(1, 20000)] * 6 + [(2, 17)]),              # dozens of tiles in a row for each CTA
-    ((16, 8, 128), [(300, 6300), (1, 9000), (259, 4500)]),
-    ((8, 8, 64), [(1, 30000)] * 5 + [(150, 9000)]),
+    ((16, 8, 128), [(130, 9300), (1, 9000), (67, 6500)]),
+    ((8, 8, 64), [(1, 30000)] * 5 + [(140, 4000)]),
     ((64, 8, 128), [(130, 130), (70, 200)] * 5),             # many short items
+    ((32, 8, 128), [(16, 300), (3, 40), (1, 5000), (16, 16)]),        # no more than 64 rows to an item
+    ((48, 1, 128), [(1, 600), (1, 1)]),                       # the same, one token of 48 heads
+    ((2, 1, 64), [(1, 1 + s % 50) if s % 7 else (0, 9) for s in range(1500)]),      # more sequences than a CTA has threads
+    ((4, 2, 64), [(0, 3)] * 1300 + [(40, 170), (1, 300)]),
 ])
 def test_attention_of_long_caches_and_odd_groups(B, heads, seqs, dtype):
     got, want, spread, scores, keys, top = _attention_case(B, heads, dtype, seqs, seed=3)
@@ -254,6 +258,32 @@ def test_what_a_row_does_not_see_has_no_part_in_it(B, dtype, value, what):
         assert np.array_equal(got[~fine], want[~fine], equal_nan=True)
     z = np.where(np.isfinite(scores), scores, 0)
     _check_attention(np.where(fine, got, 0), np.where(fine, want, 0), np.where(fine, spread, 0), z, keys, top, dtype, 64)
+
+
+@pytest.mark.parametrize("value", [np.nan, np.inf])
+@pytest.mark.parametrize("longest", [None, 200])             # rows in tiles of 64, of 128
+def test_an_undefined_query_spoils_its_row_alone(B, value, longest):
+    Hq, Hkv, hd = 8, 2, 64
+    seqs = [(3, 700), (9, 9)] if longest is None else [(3, 700), (150, 300)]
+    starts, lens, table, n_pages = _tables(seqs, seed=11)
+    n = int(starts[-1])
+    rng = np.random.default_rng(12)
+    pool = _dev(rng.normal(size=(n_pages, Hkv, 2, 16, hd))).bfloat16()
+    q = _dev(rng.normal(size=(n, Hq, hd))).bfloat16()
+    chunks = _batch(B, starts, lens, table, n, longest or 9)
+    q[1, 5, 3], q[5, 0, 0] = value, value
+    got = _f64(B.echo_chunk_attention(chunks, q, pool))
+    chunks.check()
+    spoiled = np.zeros((n, Hq), dtype=bool)
+    spoiled[1, 5] = spoiled[5, 0] = True
+    assert np.isnan(got[spoiled]).all()
+    q[1, 5, 3], q[5, 0, 0] = 0, 0
+    want, spread, scores = K.attend(_f64(pool), _f64(q), starts, lens, table, np.zeros(q.shape))
+    got[spoiled], want[spoiled] = 0, 0       # (the other rows of a warp may round their probabilities at other references)
+    keys = np.zeros(n)
+    for s, row, t in K.positions(starts, lens):
+        keys[row] = t + 1
+    _check_attention(got, want, spread, scores, keys, 8.0, torch.bfloat16, hd)
 
 
 def test_bad_pages_and_lengths_are_reported(B):
@@ -415,3 +445,58 @@ def test_a_conversation_in_pieces_is_the_conversation_at_once(B):
     h = HALF_STEP[dtype]
     rows = [total - 1, 2 * total - 1]
     assert np.all(np.abs(_f64(last) - want[rows]) <= 2 * h * np.abs(want[rows]) + 4 * h * spread[rows])
+
+
+def test_a_decoder_layer_by_layer_scores_as_the_engine_does(B):
+    """Two layers run by a caller on the library's own pieces: projections, append, attention over a cache that takes the
+    prompt in two pieces and the response in one, log-probabilities; against the fp64 decoder, with the tolerance that the
+    engine's own scores have (5e-2), and against echo_score (both: twice that)."""
+    from oracle import decoder
+    from paper_2602_02192_b200 import synth
+    wl = synth.WORKLOADS["tiny"]
+    S, P, G, Lp, T = wl.shape, 2, 1, 45, 20
+    w_t = synth.make_weights(S, wl.weight_seed)
+    w = {k: ([x.cuda() for x in v] if isinstance(v, list) else v.cuda()) for k, v in w_t.items()}
+    prompts = synth.make_prompts(P, Lp, S.vocab, wl.prompt_seed)
+    rng = np.random.default_rng(9)
+    response = rng.integers(0, S.vocab, size=(P, T)).astype(np.int32)
+    whole = np.concatenate([prompts, response], axis=1)
+    Hq, Hkv, hd = S.n_q_heads, S.n_kv_heads, S.head_dim
+    width = -(-(Lp + T) // 16)
+    table = rng.permutation(P * width).reshape(P, width).astype(np.int32)
+    pools = [torch.full((P * width, Hkv, 2, 16, hd), float("nan"), dtype=torch.bfloat16, device="cuda") for _ in range(S.n_layers)]
+
+    def norm(x, gain):
+        return (x * torch.rsqrt(x.pow(2).mean(dim=1, keepdim=True) + S.rms_eps) * gain.float()).bfloat16()
+
+    def advance(at, n):
+        """Feeds positions at .. at + n - 1 of every sequence; the residual stream of these rows."""
+        chunks = _batch(B, np.arange(P + 1, dtype=np.int32) * n, np.full(P, at + n, np.int32), table, P * n, n)
+        x = w["embed"][torch.from_numpy(whole[:, at:at + n].reshape(-1).astype(np.int64)).cuda()].float()
+        for l in range(S.n_layers):
+            h = norm(x, w["attn_norm"][l])
+            qkv = B.echo_gemm_bf16(h, torch.cat([w["wq"][l], w["wk"][l], w["wv"][l]]))
+            q, k, v = (y.view(P * n, -1, hd) for y in qkv.split((Hq * hd, Hkv * hd, Hkv * hd), dim=1))
+            q = B.echo_append_kv(chunks, q, k, v, pools[l], S.rope_theta)
+            o = B.echo_chunk_attention(chunks, q, pools[l])
+            x = B.echo_gemm_bf16(o.view(P * n, Hq * hd), w["wo"][l], epilogue=1, Y=x)
+            act = B.echo_gemm_bf16(norm(x, w["mlp_norm"][l]), torch.cat([w["w_gate"][l], w["w_up"][l]]), epilogue=2)
+            x = B.echo_gemm_bf16(act, w["w_down"][l], epilogue=1, Y=x)
+        chunks.check()
+        return x.view(P, n, -1)
+
+    advance(0, 30)
+    x = torch.cat([advance(30, Lp - 30)[:, -1:], advance(Lp, T - 1)], dim=1)     # what predicts the response
+    logits = B.echo_gemm_bf16(norm(x.reshape(P * T, -1), w["final_norm"]), w["lm_head"])
+    got = B.echo_token_logprobs(logits, torch.from_numpy(response.reshape(-1)).cuda())[0].view(P, T).cpu().numpy()
+    dims = decoder.ModelDims(S.n_layers, S.d_model, Hq, Hkv, hd, S.d_ff, S.vocab, S.rms_eps, S.rope_theta)
+    weights = decoder.Weights(synth.weights_to_bits(w_t))
+    for p in range(P):
+        want = decoder.score_forced(dims, weights, prompts[p], response[p], 1.0, 0, p).logprob_given
+        assert np.all(np.abs(got[p] - want) <= 5e-2)
+    eng = B.Engine(B.make_config(S, P, G, Lp, T))
+    eng.echo_load_policy(w, 1)
+    lp, _ = eng.echo_score(torch.from_numpy(prompts).cuda(), [Lp] * P, torch.from_numpy(response[:, None]).cuda(), 1.0)
+    eng.echo_sync()
+    assert np.all(np.abs(lp[:, 0].cpu().numpy() - got) <= 1e-1)
+    eng.close()
