@@ -1039,61 +1039,68 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
   }
 }
 
-// Joins the parts of the items that were cut, in key order: CTA (b, g) the item whose first part CTA b left, rows 8 g ..
-// A warp to a row; its lanes look up 32 CTAs' records and partial sums at once.
+// Joins the parts of the items that were cut, in key order: CTA (b, g) the item whose first part CTA b left, rows 16 g ..
+// Half a warp to a row; its lanes look up 16 CTAs' records and partial sums at once.
 template <int HD, bool HALF>
 __global__ void __launch_bounds__(256) join_parts_kernel(const __grid_constant__ AttendArgs a, int n_ctas) {
   early_start_sync();
-  const int b = blockIdx.x, lane = threadIdx.x & 31;
+  const int b = blockIdx.x, lane = threadIdx.x & 15, upper = threadIdx.x & 16;
   // lane i: the part of CTA b + i
   PartRecord mine = {};
   if (b + lane < n_ctas) mine = a.records[b + lane];
   if (!__shfl_sync(0xffffffffu, mine.first, 0)) return;
   const Item it = a.records[b].item;
-  const int row = blockIdx.y * 8 + (threadIdx.x >> 5);
+  const int row = blockIdx.y * 16 + (threadIdx.x >> 4);
   const int tile = row >> 7, r = row & 127, tok = tile * a.tile_tok + r / a.group;
-  if (r >= a.tile_tok * a.group || tok >= it.n_tok) return;
+  const bool there = row < a.rows_cap && r < a.tile_tok * a.group && tok < it.n_tok;
   const int64_t stride = 2 * static_cast<int64_t>(a.rows_cap);
-  constexpr int kCols = HD / 32;                 // of a lane
+  constexpr int kCols = HD / 16;                 // of a lane
   float ref = -INFINITY, l = 0.f, o[kCols];
 #pragma unroll
   for (int e = 0; e < kCols; ++e) o[e] = 0.f;
-  for (int k0 = b; k0 < n_ctas; k0 += 32) {
+  for (int k0 = b; k0 < n_ctas; k0 += 16) {
     if (k0 > b) mine = k0 + lane < n_ctas ? a.records[k0 + lane] : PartRecord{};
-    const unsigned ends = __ballot_sync(0xffffffffu, (k0 > b || lane > 0) && mine.later && mine.later_ends);
-    const int n = ends ? __ffs(ends) : 32;       // lanes that belong to the item
+    const unsigned ends = __ballot_sync(0xffffffffu, (k0 > b || lane > 0) && mine.later && mine.later_ends) & 0xffffu;
+    const int n = ends ? __ffs(ends) : 16;       // lanes that belong to the item
     const bool part = lane < n && (k0 + lane == b || mine.later);
     const int64_t at = (k0 + lane) * stride + (k0 + lane == b ? a.rows_cap : 0) + row;
-    const float2 ml = part ? a.part_ml[at] : make_float2(-INFINITY, 0.f);
+    const float2 ml = part && there ? a.part_ml[at] : make_float2(-INFINITY, 0.f);
     float to = fmaxf(ref, ml.x);
 #pragma unroll
-    for (int d = 16; d; d >>= 1) to = fmaxf(to, __shfl_xor_sync(0xffffffffu, to, d));
-    if (to != ref) {                             // (from -inf: nothing yet)
-      const float fix = ref == -INFINITY ? 0.f : ex2(ref - to);
-      l *= fix;
+    for (int d = 8; d; d >>= 1) to = fmaxf(to, __shfl_xor_sync(0xffffffffu, to, d));
+    const float fix = to == ref ? 1.f : ref == -INFINITY ? 0.f : ex2(ref - to);      // (from -inf: nothing yet)
+    l *= fix;
 #pragma unroll
-      for (int e = 0; e < kCols; ++e) o[e] *= fix;
-      ref = to;
-    }
+    for (int e = 0; e < kCols; ++e) o[e] *= fix;
+    ref = to;
     const float scale = ml.x == -INFINITY ? 0.f : ex2(ml.x - ref);
     float sum = ml.y * scale;
 #pragma unroll
-    for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+    for (int d = 8; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
     l += sum;
-    for (unsigned left = __ballot_sync(0xffffffffu, part); left; left &= left - 1) {
-      const int k = __ffs(left) - 1;
+    for (unsigned left = __ballot_sync(0xffffffffu, part) & 0xffffu; left; left &= left - 1) {
+      const int k = upper + __ffs(left) - 1;
       const float *p = a.part_o + __shfl_sync(0xffffffffu, at, k) * HD + lane * kCols;
       const float s = __shfl_sync(0xffffffffu, scale, k);
+      if (!there) continue;
 #pragma unroll
-      for (int e = 0; e < kCols; ++e) o[e] = fmaf(p[e], s, o[e]);
+      for (int e = 0; e < kCols; e += 4) {
+        const float4 x = *reinterpret_cast<const float4 *>(p + e);
+        o[e] = fmaf(x.x, s, o[e]);
+        o[e + 1] = fmaf(x.y, s, o[e + 1]);
+        o[e + 2] = fmaf(x.z, s, o[e + 2]);
+        o[e + 3] = fmaf(x.w, s, o[e + 3]);
+      }
     }
     if (ends) break;
   }
+  if (!there) return;
   const float norm = 1.0f / l;
   uint16_t *dst = a.out + (static_cast<int64_t>(it.row0 + tok) * a.Hq + it.head * a.group + r % a.group) * HD + lane * kCols;
 #pragma unroll
-  for (int e = 0; e < kCols; e += 2)
-    *reinterpret_cast<uint32_t *>(dst + e) = it.pos0 + tok < 0 ? 0u : cvt16x2(o[e] * norm, o[e + 1] * norm, HALF);
+  for (int e = 0; e < kCols; e += 4)
+    *reinterpret_cast<uint2 *>(dst + e) =
+        it.pos0 + tok < 0 ? make_uint2(0u, 0u) : make_uint2(cvt16x2(o[e] * norm, o[e + 1] * norm, HALF), cvt16x2(o[e + 2] * norm, o[e + 3] * norm, HALF));
 }
 
 // ---- host ------------------------------------------------------------------------------------------------
@@ -1143,7 +1150,7 @@ cudaError_t launch_attend(const CUtensorMap &tm_q, const CUtensorMap &tm_kv, con
   }
   const cudaError_t e = launch_early(chunk_attention_kernel<HD, HALF, FEW>, dim3(ctas), dim3(kAttThreads), smem, s, tm_q, tm_kv, a);
   if (e != cudaSuccess) return e;
-  return launch_early(join_parts_kernel<HD, HALF>, dim3(ctas, a.rows_cap / 8), dim3(256), 0, s, a, ctas);
+  return launch_early(join_parts_kernel<HD, HALF>, dim3(ctas, (a.rows_cap + 15) / 16), dim3(256), 0, s, a, ctas);
 }
 
 }  // namespace
