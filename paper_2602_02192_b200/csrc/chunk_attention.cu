@@ -33,12 +33,14 @@
 //
 // Roles: warps 0-7 and 8-15 the two streams' softmax, warps 16 and 18 issue their MMAs, warp 17 walks the items and loads.
 // A softmax warp has 16 rows, four threads to a row: with 32 rows to a warp and a thread to a row two warps shared a
-// scheduler, and what one waited for the other could not fill (2048 tokens over 14336: 447 us instead of 431).
+// scheduler, and what one waited for the other could not fill (2048 tokens over 14336: 447 us, with 16 rows 431).
 //
 // Measured (32/8 heads of 128, bf16, in bursts; in a run of them the SM clock falls with the power): 256 single tokens over
-// 512 to 2559 keys 258 us, 0.96 of the copy rate; 2048 tokens over 14336 431 us, 1.19 PFLOP/s.  Few rows are bound by HBM
-// (by power in a run), long chunks by the tensor cores at two thirds of their cycles and the softmax warps between them: a
-// step's S of 64 keys reads Q from shared memory again, 48 cycles an MMA instead of 32.
+// 512 to 2559 keys 258 us, 0.96 of the copy rate; 2048 tokens over 14336 421 us, 1.22 PFLOP/s.  Few rows are bound by HBM
+// (by power in a run), long chunks of heads of 128 by the issue of MMAs: 12 to a step, about 64 cycles each, where the eight of
+// Q K^T with their 64 keys have half the work of the four of P V.  S of 128 keys would halve their number, but with two O
+// there is room for one such S a stream, and then its products wait for its softmax (452 us with S of 128, 499 with S of
+// 128 whose probabilities go in halves).  Heads of 64 are bound by the softmax warps' chain: wait, load, exponentials, store.
 
 #include <algorithm>
 #include <atomic>
@@ -849,9 +851,9 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
           tc_wait_st();
         }
         // keys that some row of the tile does not see: their values must be finite, or kept out of the products
-        const int ks = max(0, pos_first + 1 - key0), ke = min(64, it.seen_end - key0);
-        const int ke16 = (ke + 15) & ~15;
-        if (masked && ke > 0 && (ks < ke || ke < ke16)) {
+        if (masked && it.seen_end > key0) {
+          const int ks = max(0, pos_first + 1 - key0), ke = min(64, it.seen_end - key0);
+          const int ke16 = (ke + 15) & ~15;
           const int at = 2 * (tiles_done + tile) + 1, stage = at % M::kStages;
           ok = wait(&sh.kv_full[stage], at / M::kStages);
           if (!ok) break;
