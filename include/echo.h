@@ -442,7 +442,9 @@ typedef struct echo_kv_chunks {
                                  1 a page id outside the pool, 3 a bounded wait ran out, 4 lengths outside the
                                  limits: the batch's, or more than 16 pt_width keys)                          */
   int32_t n_seqs;             /* 0: nothing is done                                                           */
-  int32_t n_rows;             /* rows of the arrays; those of no sequence are left as they are                */
+  int32_t n_rows;             /* rows of the arrays; those of no sequence are left as they are.  0: nothing is
+                                 done (with either 0 the tables, q, k, v, the outputs and the workspace may be
+                                 NULL, and pt_width and max_chunk 0)                                          */
   int32_t pt_width;           /* at most 2^26                                                                 */
   int32_t max_chunk;          /* no chunk is longer (sizes workspaces, chooses tiles)                         */
 } echo_kv_chunks;

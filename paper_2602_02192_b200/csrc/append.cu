@@ -177,7 +177,8 @@ extern "C" int echo_append_kv(const void *q, const void *k, const void *v, int32
   if (!q) Hq = 0;
   const int rc = chunk_args(chunks, Hq, Hkv, hd, kv_pool, n_pages, kv_format, &a.c);
   if (rc != ECHO_OK) return rc;
-  if (!k || !v || in_format < 0 || in_format > 2 || !(rope_theta > 0.f) || !std::isfinite(rope_theta)) return ECHO_ERR_INVALID;
+  const bool none = a.c.S == 0 || a.c.n_rows == 0;
+  if ((!none && (!k || !v)) || in_format < 0 || in_format > 2 || !(rope_theta > 0.f) || !std::isfinite(rope_theta)) return ECHO_ERR_INVALID;
   if ((q && q_stride < static_cast<int64_t>(Hq) * hd) || k_stride < static_cast<int64_t>(Hkv) * hd ||
       v_stride < static_cast<int64_t>(Hkv) * hd)
     return ECHO_ERR_INVALID;
@@ -186,7 +187,7 @@ extern "C" int echo_append_kv(const void *q, const void *k, const void *v, int32
   const int64_t strides[3] = {q_stride, k_stride, v_stride};
   const int64_t widths[3] = {static_cast<int64_t>(Hq) * hd, static_cast<int64_t>(Hkv) * hd, static_cast<int64_t>(Hkv) * hd};
   if (reinterpret_cast<uintptr_t>(out_q) & 15) return ECHO_ERR_INVALID;
-  if (a.c.S == 0 || a.c.n_rows == 0) return ECHO_OK;
+  if (none) return ECHO_OK;
   bool vec = true;
   const uint64_t pool = pool_bytes(n_pages, Hkv, hd), outs = static_cast<uint64_t>(a.c.n_rows) * Hq * hd * 2;
   if (ranges_meet(kv_pool, pool, out_q, outs)) return ECHO_ERR_INVALID;

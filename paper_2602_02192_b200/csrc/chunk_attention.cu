@@ -69,7 +69,7 @@ constexpr int kDevices = 64;                   // whose properties are remembere
 constexpr float kMostSum = 8192.0f;            // of a row's probabilities in a step, before its reference has to move
 
 // Costs that the shares are cut by: of a key, and of an item's beginning and end.
-constexpr int kSingleWeight = 6, kPairWeight = 8, kSingleStart = 2048, kPairStart = 3072;
+constexpr int kSingleWeight = 6, kPairWeight = 8, kSingleStart = 2 * 1024, kPairStart = 3 * 1024;
 // Measured: with the weights 4 : 8 and half of these starts 40 chunks of 16 to 400 tokens took 437 us instead of 356.
 constexpr int kLeastShare = 1024;              // of a CTA that has work: little work goes to few CTAs
 
@@ -84,7 +84,7 @@ template <int HD, bool FEW> struct AttSmem {
   static constexpr int kStage = kKeys * HD * 2;
   static constexpr int kStages = HD == 128 ? (FEW ? 6 : 5) : (FEW ? 11 : 9);
   static constexpr int kQ = 0, kKV = 2 * kQTile, kBars = kKV + kStages * kStage;
-  static constexpr int kTotal = kBars + 3072;
+  static constexpr int kBarBytes = 3 * 1024, kTotal = kBars + kBarBytes;
   static_assert(kTotal <= 227 * 1024, "shared memory");
 };
 
@@ -390,7 +390,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
   using M = AttSmem<HD, FEW>;
   extern __shared__ __align__(1024) uint8_t smem[];
   Shared<HD, FEW> &sh = *reinterpret_cast<Shared<HD, FEW> *>(smem + M::kBars);
-  static_assert(sizeof(Shared<HD, FEW>) <= 3072, "barriers");
+  static_assert(sizeof(Shared<HD, FEW>) <= M::kBarBytes, "barriers");
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   constexpr int kMma0 = kSoftWarps, kLoad = kSoftWarps + 1, kMma1 = kSoftWarps + 2;
   volatile int *abort_flag = &sh.abort_flag;
@@ -1175,13 +1175,14 @@ int echo_chunk_attention(const void *q, int64_t q_stride, const void *kv_pool, i
   const int rc = chunk_args(chunks, Hq, Hkv, hd, kv_pool, n_pages, format, &a.c);
   if (rc != ECHO_OK) return rc;
   const int64_t width = static_cast<int64_t>(Hq) * hd;
-  if (!q || !out || Hq < 1 || q_stride < width || q_stride % 8 || q_stride > (1 << 30)) return ECHO_ERR_INVALID;
+  const bool none = a.c.S == 0 || a.c.n_rows == 0;
+  if ((!none && (!q || !out)) || Hq < 1 || q_stride < width || q_stride % 8 || q_stride > (1 << 30)) return ECHO_ERR_INVALID;
   for (const void *p : {q, const_cast<const void *>(out), const_cast<const void *>(workspace)})
     if (reinterpret_cast<uintptr_t>(p) & 15) return ECHO_ERR_INVALID;
   if (Hq / Hkv > 128 || static_cast<int64_t>(n_pages) * Hkv > (1 << 26)) return ECHO_ERR_UNSUPPORTED;
   const size_t need = echo_chunk_attention_workspace_bytes(a.c.max_chunk, Hq, Hkv, hd);
+  if (none) return ECHO_OK;
   if (!workspace || workspace_bytes < need) return ECHO_ERR_INVALID;
-  if (a.c.S == 0 || a.c.n_rows == 0) return ECHO_OK;
   const uint64_t qs = (static_cast<uint64_t>(a.c.n_rows - 1) * q_stride + width) * 2, outs = a.c.n_rows * static_cast<uint64_t>(width) * 2;
   if (ranges_meet(out, outs, q, qs) || ranges_meet(out, outs, kv_pool, pool_bytes(n_pages, Hkv, hd)) ||
       ranges_meet(out, outs, workspace, need) || ranges_meet(workspace, need, q, qs) ||

@@ -17,8 +17,10 @@ struct ChunkArgs {
 // Host checks that both calls share.  heads: Hq may be 0 (no queries in the call).
 inline int chunk_args(const echo_kv_chunks *c, int32_t Hq, int32_t Hkv, int32_t hd, const void *pool, int32_t n_pages,
                       int32_t format, ChunkArgs *out) {
-  if (!c || c->n_seqs < 0 || c->n_rows < 0 || c->pt_width < 1 || c->max_chunk < 1) return ECHO_ERR_INVALID;
-  if (!c->row_starts || !c->kv_lens || !c->page_table || !c->status) return ECHO_ERR_INVALID;
+  if (!c || c->n_seqs < 0 || c->n_rows < 0 || c->pt_width < 0 || c->max_chunk < 0) return ECHO_ERR_INVALID;
+  const bool none = c->n_seqs == 0 || c->n_rows == 0;      // nothing to do, and arrays of nothing may have no address
+  if (!none && (c->pt_width < 1 || c->max_chunk < 1 || !c->row_starts || !c->kv_lens || !c->page_table || !c->status))
+    return ECHO_ERR_INVALID;
   for (const void *p : {static_cast<const void *>(c->row_starts), static_cast<const void *>(c->kv_lens),
                         static_cast<const void *>(c->page_table), static_cast<const void *>(c->status)})
     if (reinterpret_cast<uintptr_t>(p) & 3) return ECHO_ERR_INVALID;

@@ -500,3 +500,16 @@ def test_a_decoder_layer_by_layer_scores_as_the_engine_does(B):
     eng.echo_sync()
     assert np.all(np.abs(lp[:, 0].cpu().numpy() - got) <= 1e-1)
     eng.close()
+
+
+@pytest.mark.parametrize("S", [0, 3])
+def test_a_batch_without_new_tokens(B, S):
+    chunks = B.KVChunks(torch.zeros(S + 1, dtype=torch.int32, device="cuda"), torch.full((S,), 5, dtype=torch.int32, device="cuda"),
+                        torch.zeros((S, 1), dtype=torch.int32, device="cuda"), 0, 0)
+    pool = torch.ones((2, 2, 2, 16, 64), dtype=torch.bfloat16, device="cuda")
+    q, k, v = (torch.empty((0, h, 64), dtype=torch.bfloat16, device="cuda") for h in (4, 2, 2))
+    assert B.echo_append_kv(chunks, q, k, v, pool).shape == q.shape
+    assert B.echo_append_kv(chunks, None, k, v, pool) is None
+    assert B.echo_chunk_attention(chunks, q, pool).shape == q.shape
+    chunks.check()
+    assert bool((pool == 1).all())

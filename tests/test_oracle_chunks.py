@@ -102,6 +102,17 @@ def test_batches_that_are_refused(lib, call):
     assert call(lib, _chunks(lib, n_seqs=0)) == 0 and call(lib, _chunks(lib, n_rows=0)) == 0
 
 
+@pytest.mark.parametrize("change", [dict(n_seqs=0), dict(n_rows=0)])
+def test_a_batch_of_nothing_needs_no_arrays(lib, change):
+    f = dict(row_starts=None, kv_lens=None, page_table=None, status=None, pt_width=0, max_chunk=0, **change)
+    for q in (P, None):
+        assert _append(lib, _chunks(lib, **f), q=q, k=None, v=None, out_q=q and 32 * P) == 0
+        assert _attend(lib, _chunks(lib, **f), q=q, out=None, workspace=None, workspace_bytes=0) == 0
+    assert _append(lib, _chunks(lib, **f), Hkv=0) == INVALID and _attend(lib, _chunks(lib, **f), q_stride=504) == INVALID
+    f["max_chunk"] = -1
+    assert _append(lib, _chunks(lib, **f)) == INVALID and _attend(lib, _chunks(lib, **f)) == INVALID
+
+
 @pytest.mark.parametrize("call", [_append, _attend])
 def test_shapes_and_pools_that_are_refused(lib, call):
     for change in (dict(Hkv=0), dict(Hq=5), dict(Hq=-2), dict(hd=0), dict(kv_pool=None), dict(kv_pool=64 * P + 8),
