@@ -36,7 +36,7 @@
 // scheduler, and what one waited for the other could not fill (2048 tokens over 14336: 447 us, with 16 rows 431).
 //
 // Measured (32/8 heads of 128, bf16, in bursts; in a run of them the SM clock falls with the power): 256 single tokens over
-// 512 to 2559 keys 258 us, 0.96 of the copy rate; 2048 tokens over 14336 421 us, 1.22 PFLOP/s.  Few rows are bound by HBM
+// 512 to 2559 keys 258 us, 0.96 of the copy rate; 2048 tokens over 14336 424 us, 1.21 PFLOP/s.  Few rows are bound by HBM
 // (by power in a run), long chunks of heads of 128 by the issue of MMAs: 12 to a step, about 64 cycles each, where the eight of
 // Q K^T with their 64 keys have half the work of the four of P V.  S of 128 keys would halve their number, but with two O
 // there is room for one such S a stream, and then its products wait for its softmax (452 us with S of 128, 499 with S of
