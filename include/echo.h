@@ -468,7 +468,7 @@ int echo_append_kv(const void *q, const void *k, const void *v, int32_t in_forma
  *   out = sum_{u <= t} exp(q . k_u / sqrt(hd)) v_u / sum_{u <= t} exp(q . k_u / sqrt(hd))
  * (the row's own key is among them: append first).  A row with t < 0 (a chunk longer than its cache) sees nothing: 0.
  * Keys and values behind a row's position have no part in it, whatever they hold.  Fp32 softmax and accumulation;
- * probabilities enter the products in the cache's format.
+ * probabilities enter the products in the cache's format (in half to 2^-31 of the row's largest where that is coarser).
  *   q           dev rows of [Hq][hd] in `format` (0 bf16, 1 half; the cache's), q_stride elements from row to row (a
  *               multiple of 8, up to 2^30), 16-byte aligned; rotated (echo_append_kv)
  *   kv_pool     dev, 16-byte aligned

@@ -24,8 +24,9 @@
 // tiles from the last to the first: those are what L2 may still hold.
 //
 // A row's reference (what its exponents are relative to) is its maximum over the item's first step.  It moves when the
-// probabilities of 64 keys, relative to it, add up to more than 2^13: the maximum has then grown.  So O is hardly ever
-// rescaled, most steps need no maxima, and a probability is at most 2^13, which both formats hold.
+// probabilities of 64 keys, relative to it, add up to more than 2^13 (half: 2^17, of 2^6 for the reference): the maximum
+// has then grown.  So O is hardly ever rescaled, most steps need no maxima, and a probability that is used is at most 2^13
+// (2^15), which the formats hold.
 //
 // What a row does not see has no part in it: masked scores are replaced, not added to.  A masked probability is 0, but
 // 0 times an undefined value would not be: where a step has keys that only some of its rows see, their values are looked
@@ -66,7 +67,11 @@ constexpr int kAttThreads = 32 * (kSoftWarps + 4);
 constexpr int kMaxCtas = 148;                  // CTAs of a launch: sizes the workspace
 constexpr int kItemRing = 4;
 constexpr int kDevices = 64;                   // whose properties are remembered
-constexpr float kMostSum = 8192.0f;            // of a row's probabilities in a step, before its reference has to move
+// Probabilities are relative to 2^kShift for a score that equals the reference.  Half precision ends at 2^-24 below: with 1
+// for the largest, 100,000 keys whose scores lie 18 below it would lose all that they add up to (bf16 ends at 2^-133).
+constexpr int shift_of(bool half) { return half ? 6 : 0; }
+// of a row's probabilities in a step, a quarter of them in a thread, before its reference has to move (half: 65504 ends it)
+constexpr float most_sum(bool half) { return half ? 131072.0f : 8192.0f; }
 
 // Costs that the shares are cut by: of a key, and of an item's beginning and end.
 constexpr int kSingleWeight = 6, kPairWeight = 8, kSingleStart = 2 * 1024, kPairStart = 3 * 1024;
@@ -746,6 +751,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
     const uint32_t lanes = static_cast<uint32_t>(lane0) << 16;
     const uint32_t t_s0 = tmem + lanes + w * 128, t_o = tmem + lanes + 256 + w * 128;
     const float c = a.scale_log2;
+    constexpr float kShift = shift_of(HALF), kMost = most_sum(HALF) / 4;
     const int row_a = row0 + (lane >> 2), row_b = row_a + 8, col = 2 * (lane & 3);      // of every eight columns: col, col + 1
     const int tok_a = row_a / a.group, tok_b = row_b / a.group;
     int n_item = 0, steps_done = 0, tiles_done = 0, looks = 0, joins = 0;
@@ -825,8 +831,8 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                 }
               }
             }
-            const float base_a = m_a == -INFINITY ? 0.f : m_a == INFINITY ? NAN : -m_a * c;
-            const float base_b = m_b == -INFINITY ? 0.f : m_b == INFINITY ? NAN : -m_b * c;
+            const float base_a = m_a == -INFINITY ? 0.f : m_a == INFINITY ? NAN : kShift - m_a * c;
+            const float base_b = m_b == -INFINITY ? 0.f : m_b == INFINITY ? NAN : kShift - m_b * c;
             const float2 c2 = make_float2(c, c), base2_a = make_float2(base_a, base_a), base2_b = make_float2(base_b, base_b);
             sum_a = sum_b = make_float2(0.f, 0.f);
 #pragma unroll
@@ -841,7 +847,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             }
             sum_a.x += sum_a.y;
             sum_b.x += sum_b.y;
-            if (careful || !__any_sync(0xffffffffu, (mine_a && !(sum_a.x <= kMostSum / 4)) || (mine_b && !(sum_b.x <= kMostSum / 4)))) break;
+            if (careful || !__any_sync(0xffffffffu, (mine_a && !(sum_a.x <= kMost)) || (mine_b && !(sum_b.x <= kMost)))) break;
             careful = true;
           }
           if (!ok) break;

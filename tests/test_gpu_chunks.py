@@ -513,3 +513,27 @@ def test_a_batch_without_new_tokens(B, S):
     assert B.echo_chunk_attention(chunks, q, pool).shape == q.shape
     chunks.check()
     assert bool((pool == 1).all())
+
+
+@pytest.mark.parametrize("n", [1, 66])
+def test_many_small_probabilities_beside_a_large_one(B, n):
+    """One key whose score is 17.6 above those of all others: each of these has a probability of 2^-25.4, below half of
+    half precision's smallest number, and together they are all that the result holds.  Relative to 2^6 for the largest
+    they are rounded by at most 2^-31 of it each; everything else is as in the attention's bound above."""
+    S, kv, hd = 150, 30000, 64
+    pages = -(-kv // 16)
+    pool = torch.zeros((pages, 1, 2, 16, hd), dtype=torch.float16, device="cuda")
+    pool[:, :, 1] = 1
+    q = torch.zeros((S * n, 2, hd), dtype=torch.float16, device="cuda")
+    q[..., 0] = pool[0, 0, 0, 0, 0] = 11.866
+    pool[0, 0, 1, 0] = 0
+    starts, lens = np.arange(S + 1, dtype=np.int32) * n, np.full(S, kv, np.int32)
+    table = np.tile(np.random.default_rng(0).permutation(pages).astype(np.int32), (S, 1))
+    table[:, np.flatnonzero(table[0] == 0)[0]], table[:, 0] = table[0, 0], 0          # the large one first
+    chunks = _batch(B, starts, lens, table, S * n, n)
+    got = _f64(B.echo_chunk_attention(chunks, q, pool)).reshape(S, n, 2, hd)
+    chunks.check()
+    want, *_ = K.attend(_f64(pool), _f64(q[:n]), starts[:2], lens[:1], table[:1], np.zeros((n, 2, hd)))
+    z = 11.866 ** 2 / 8
+    bound = np.abs(want) * (2 * HALF_STEP[torch.float16] + 2 * E * kv + 4 * E * (hd + 8) * z) + kv * TINY[torch.float16] / 64
+    assert np.all(want > 6e-4) and np.all(np.abs(got - want[None]) <= bound[None])
