@@ -540,6 +540,11 @@ int echo_probe_read_bandwidth(const void *buf, size_t bytes, int32_t repeats, vo
  * NULL).  scratch: dev, 16 bytes, 8-byte aligned.  Synchronises the stream. */
 int echo_debug_wait_limit(uint64_t limit_ns, void *scratch, uint64_t *waited_ns, void *cuda_stream);
 
+/* The limit of the waits inside the kernels of later echo_chunk_attention calls of this process, 1 ns to one second
+ * (0: the second again).  A wait that takes longer than a short limit gives up as one that would never end does: status 3,
+ * outputs undefined, the device as before.  For tests of that way out alone. */
+int echo_debug_chunk_wait_limit(uint64_t limit_ns);
+
 /* The KV page plan of a rollout, computed on the host without a context or a GPU (the same
  * routine echo_rollout uses).  prompt_lens host int32 [P].  Writes out_table (host int32
  * [(P*G + P)][*width], capacity in elements): rows 0..P*G-1 are the sequences' page tables

@@ -116,7 +116,8 @@ def _load() -> C.CDLL:
     lib.echo_set_sequence_base.argtypes = [vp, u32]
     lib.echo_debug_capture.argtypes = [vp, i32, vp, vp, vp, vp]
     lib.echo_debug_wait_limit.argtypes = [u64, vp, C.POINTER(u64), vp]
-    for name in ("echo_set_sequence_base", "echo_debug_capture", "echo_debug_wait_limit"):
+    lib.echo_debug_chunk_wait_limit.argtypes = [u64]
+    for name in ("echo_set_sequence_base", "echo_debug_capture", "echo_debug_wait_limit", "echo_debug_chunk_wait_limit"):
         getattr(lib, name).restype = C.c_int
     lib.echo_debug_noise.argtypes = [u64, u32, u32, u32, u32, vp, vp, vp]
     lib.echo_sample.argtypes = [vp, i32, i32, i32, vp, u32, f32, u64, vp, vp, vp, vp]
@@ -192,7 +193,7 @@ EXPORTED = ["echo_arena_bytes", "echo_create", "echo_destroy", "echo_load_policy
             "echo_gemm_bf16_noalloc_status", "echo_probe_read_bandwidth", "echo_peer_score", "echo_chain_assemble",
             "echo_chain_arrival_time", "echo_score", "echo_turn_mask", "echo_score_detail", "echo_token_logprobs",
             "echo_token_logprobs_backward", "echo_grpo_gradient", "echo_adamw_step", "echo_adamw_unpack", "echo_append_kv",
-            "echo_chunk_attention_workspace_bytes", "echo_chunk_attention"]
+            "echo_chunk_attention_workspace_bytes", "echo_chunk_attention", "echo_debug_chunk_wait_limit"]
 
 
 def _stream_ptr(stream: Optional[torch.cuda.Stream]) -> int:
@@ -835,6 +836,11 @@ def echo_debug_wait_limit(limit_ns: int):
     scratch = torch.zeros(2, dtype=torch.int64, device="cuda")
     rc = lib.echo_debug_wait_limit(int(limit_ns), scratch.data_ptr(), C.byref(waited), _stream_ptr(None))
     return rc, int(waited.value)
+
+
+def echo_debug_chunk_wait_limit(limit_ns: int):
+    """Limit of the waits inside later echo_chunk_attention calls (0: one second again); for tests."""
+    _check(lib.echo_debug_chunk_wait_limit(int(limit_ns)))
 
 
 def echo_debug_noise(seed: int, s: int, j: int, v0: int, n: int, device="cuda"):

@@ -109,8 +109,14 @@ struct PartRecord {
 constexpr int kRecordBytes = 64;
 static_assert(sizeof(PartRecord) <= kRecordBytes, "record");
 
+struct WaitLimit {
+  uint64_t ns;                      // of a wait
+  uint32_t look;                    // the clock is read every look + 1 tries (a power of two)
+};
+
 struct AttendArgs {
   ChunkArgs c;
+  WaitLimit limit;
   uint16_t *out;
   float *part_o;                    // [cta][2][rows_cap][hd]
   float2 *part_ml;                  // [cta][2][rows_cap]: reference in log2 units, sum
@@ -178,16 +184,16 @@ __device__ __forceinline__ float max3_nan(float a, float b, float c) {
 // A whole warp's bounded wait; its lanes go on or give up together.  Votes keep the loop free of divergence, and the clock
 // is read now and then only: a wait that has nothing to wait for takes 60 cycles, four times less than with a clock and a
 // branch of each lane's own.
-__device__ __forceinline__ bool warp_wait(uint64_t *bar, uint32_t parity, volatile int *abort_flag) {
+__device__ __forceinline__ bool warp_wait(uint64_t *bar, uint32_t parity, volatile int *abort_flag, const WaitLimit &limit) {
   if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
   uint64_t t0 = 0;
 #pragma unroll 1
   for (uint32_t i = 1;; ++i) {
     if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
-    if ((i & 255u) == 0) {
+    if ((i & limit.look) == 0) {
       const uint64_t now = global_timer_ns();
       if (t0 == 0) t0 = now;
-      if (__any_sync(0xffffffffu, *abort_flag != 0 || now - t0 > kWaitLimitNs)) break;
+      if (__any_sync(0xffffffffu, *abort_flag != 0 || now - t0 > limit.ns)) break;
     }
   }
   *abort_flag = 1;
@@ -282,6 +288,7 @@ template <int HD, bool FEW> struct Shared {
   int bad_value[2][2];              // [stream][parity of its step]: step + 1 whose P V the threads add themselves
   uint32_t tmem;
   int abort_flag;
+  int kv_loads, q_loads[2];         // copies issued: of key and value tiles, into each query tile
   long long x0, x1, start;          // plan: the CTA's share of the cost; cost in front of its first sequence
   int first_seq;
   long long warp_sum[2][kAttThreads / 32];
@@ -446,7 +453,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
   const uint32_t tmem = sh.tmem;               // S of the streams at columns 0 and 128, O at 256 and 384
 
   // waits of a whole warp, whose lanes go on or give up together
-  auto wait = [&](uint64_t *bar, int parity) { return warp_wait(bar, parity & 1, abort_flag); };
+  auto wait = [&](uint64_t *bar, int parity) { return warp_wait(bar, parity & 1, abort_flag, a.limit); };
 
   if (warp == kLoad) {
     // ---------------------------------------------------------------- items and copies
@@ -617,15 +624,11 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
       end.flags = kEnd;
       publish(end);
     }
-    if (lane == 0) a.records[blockIdx.x] = rec;
-    if (!ok) {
-      // give up: let the copies that are under way land before the shared memory goes
-      if (lane == 0) {
-        if (q_uses0 > 0) mbar_drain(&sh.q_full[0], (q_uses0 - 1) & 1);
-        if (q_uses1 > 0) mbar_drain(&sh.q_full[1], (q_uses1 - 1) & 1);
-        for (int i = max(0, kv_at - M::kStages); i < kv_at; ++i) mbar_drain(&sh.kv_full[i % M::kStages], (i / M::kStages) & 1);
-      }
-      __syncwarp();
+    if (lane == 0) {
+      a.records[blockIdx.x] = rec;
+      sh.kv_loads = kv_at;
+      sh.q_loads[0] = q_uses0;
+      sh.q_loads[1] = q_uses1;
     }
   } else if (warp >= kSoftWarps) {
     // ---------------------------------------------------------------- MMA issue
@@ -731,14 +734,6 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
           if (!paired) next_slot ^= 1;
         }
         if (lane == 0) mbar_arrive(&sh.item_empty[slot]);
-      }
-      if (!ok) {
-        *abort_flag = 1;
-        if (elect_one()) {
-          tc_commit(&sh.drain[w]);               // everything issued has ended before tensor memory is freed
-          mbar_drain(&sh.drain[w], 0);
-        }
-        __syncwarp();
       }
     }
   } else {
@@ -1037,10 +1032,25 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
       ++n_item;
       tiles_done += it.t1 - it.t0;
     }
-    if (!ok) *abort_flag = 1;
   }
   __syncthreads();
-  if (threadIdx.x == 0 && sh.abort_flag) atomicMax(a.c.status, STATUS_WAIT_TIMEOUT);
+  if (sh.abort_flag) {
+    // A wait ran out.  Whichever it was, copies and products may be under way that nobody waited for, since the warps that did
+    // not wait in vain have gone on or ended: they land before shared and tensor memory go.
+    if (threadIdx.x == 0) atomicMax(a.c.status, STATUS_WAIT_TIMEOUT);
+    if (warp == kLoad && lane == 0) {
+      for (int i = 0; i < 2; ++i)
+        if (sh.q_loads[i] > 0) mbar_drain(&sh.q_full[i], (sh.q_loads[i] - 1) & 1);
+      for (int i = max(0, sh.kv_loads - M::kStages); i < sh.kv_loads; ++i)
+        mbar_drain(&sh.kv_full[i % M::kStages], (i / M::kStages) & 1);
+    }
+    if ((warp == kMma0 || warp == kMma1) && elect_one()) {
+      uint64_t *bar = &sh.drain[warp == kMma0 ? 0 : 1];
+      tc_commit(bar);
+      mbar_drain(bar, 0);
+    }
+    __syncthreads();
+  }
   if (warp == kMma0) {
     tc_fence_after();
     tc_dealloc(tmem, 512);
@@ -1132,6 +1142,8 @@ bool make_map(CUtensorMap *out, int rank, const void *base, bool half, const cuu
                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+std::atomic<uint64_t> g_wait_limit_ns{kWaitLimitNs};
+
 // rows of an item's partial result
 int rows_cap(int max_chunk, int group) {
   const int tile_tok = 128 / group;
@@ -1194,6 +1206,8 @@ int echo_chunk_attention(const void *q, int64_t q_stride, const void *kv_pool, i
       ranges_meet(out, outs, workspace, need) || ranges_meet(workspace, need, q, qs) ||
       ranges_meet(workspace, need, kv_pool, pool_bytes(n_pages, Hkv, hd)))
     return ECHO_ERR_INVALID;
+  a.limit.ns = g_wait_limit_ns.load(std::memory_order_relaxed);
+  a.limit.look = a.limit.ns < kWaitLimitNs ? 0 : 255;
   a.out = static_cast<uint16_t *>(out);
   a.Hq = Hq;
   a.Hkv = Hkv;
@@ -1232,6 +1246,12 @@ int echo_chunk_attention(const void *q, int64_t q_stride, const void *kv_pool, i
                                         : (few ? launch_attend<64, false, true> : launch_attend<64, false, false>));
   const cudaError_t e = launch(tm_q, tm_kv, a, dev, ctas, s);
   return e == cudaSuccess ? ECHO_OK : ECHO_ERR_CUDA;
+}
+
+int echo_debug_chunk_wait_limit(uint64_t limit_ns) {
+  if (limit_ns > kWaitLimitNs) return ECHO_ERR_INVALID;
+  g_wait_limit_ns.store(limit_ns ? limit_ns : kWaitLimitNs, std::memory_order_relaxed);
+  return ECHO_OK;
 }
 
 }  // extern "C"

@@ -1,0 +1,62 @@
+"""GPU tests of the caller's paged cache where its inputs leave the ordinary: bad pages that only some rows see, scores near
+the ends of their format, calls on other streams, caches so long that a lost tile of keys is small beside the roundings."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import chunks as K
+from test_gpu_chunks import HALF_STEP, TINY, E, _batch, _check_attention, _dev, _f64, _tables
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def B():
+    from paper_2602_02192_b200 import binding
+    return binding
+
+
+def _positions(starts, lens, rows):
+    """Position of every row; -1 for rows of no sequence."""
+    t = np.full(rows, -1)
+    for _, row, at in K.positions(starts, lens):
+        t[row] = at
+    return t
+
+
+# ---- waits ----------------------------------------------------------------------------------------
+@pytest.mark.parametrize("heads,seqs", [
+    ((32, 8, 128), [(16, 300)] * 40),                        # 64 rows to a tile
+    ((32, 8, 128), [(30, 500)] * 40),                        # one tile of 128 rows
+    ((32, 8, 128), [(64, 900), (130, 5000)] * 8),            # two
+    ((8, 8, 64), [(128, 400), (3, 9000)] * 12),
+])
+def test_a_wait_that_runs_out_is_reported_and_leaves_the_device_as_it_was(B, heads, seqs):
+    """With a limit of a nanosecond a wait that takes some microseconds is one that runs out: the tensor cores' warps wait for
+    probabilities while the others add a step with undefined values key by key.  What was under way lands, the status says
+    so, and the next call is as any other."""
+    Hq, Hkv, hd = heads
+    starts, lens, table, n_pages = _tables(seqs, seed=33)
+    n = int(starts[-1])
+    g = torch.Generator(device="cuda").manual_seed(34)
+    pool = torch.randn((n_pages, Hkv, 2, 16, hd), generator=g, device="cuda").bfloat16()
+    for s, (new, kv) in enumerate(seqs):
+        for t in (kv - 1, kv - new // 2):                    # behind some row of the chunk
+            pool[int(table[s, t // 16]), :, 1, t % 16, ::7] = float("nan")
+    q = torch.randn((n, Hq, hd), generator=g, device="cuda").bfloat16()
+    chunks = _batch(B, starts, lens, table, n, max(c for c, _ in seqs))
+    good = B.echo_chunk_attention(chunks, q, pool)
+    chunks.check()
+    try:
+        B.echo_debug_chunk_wait_limit(1)
+        for _ in range(5):
+            B.echo_chunk_attention(chunks, q, pool)
+            with pytest.raises(B.EchoError, match="ECHO_ERR_TIMEOUT"):
+                chunks.check()
+    finally:
+        B.echo_debug_chunk_wait_limit(0)
+    for _ in range(3):
+        assert torch.equal(torch.nan_to_num(B.echo_chunk_attention(chunks, q, pool)), torch.nan_to_num(good))
+    chunks.check()
+    with pytest.raises(B.EchoError, match="ECHO_ERR_INVALID"):
+        B.echo_debug_chunk_wait_limit(1_000_000_001)
