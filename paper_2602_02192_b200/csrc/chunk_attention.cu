@@ -45,6 +45,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <climits>
 #include <cmath>
 
 #include "chunks.cuh"
@@ -284,7 +285,7 @@ template <int HD, bool FEW> struct Shared {
       item_full[kItemRing], item_empty[kItemRing];
   uint64_t look[2], join[2], turn[2], drain[2];
   Item items[kItemRing];
-  int bad_page[kItemRing];
+  int bad_key[kItemRing];           // first key of the item's first page whose id is outside the pool
   int bad_value[2][2];              // [stream][parity of its step]: step + 1 whose P V the threads add themselves
   uint32_t tmem;
   int abort_flag;
@@ -470,7 +471,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
       if (!ok) return;
       if (lane == 0) {
         sh.items[slot] = it;
-        sh.bad_page[slot] = 0;
+        sh.bad_key[slot] = INT_MAX;
         mbar_arrive(&sh.item_full[slot]);
       }
       __syncwarp();
@@ -577,9 +578,13 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                 }
                 const int id = __shfl_sync(0xffffffffu, ids, (t & 3) * 8 + (lane & 7));
                 const bool need = t * kPages + (lane & 7) < n_need, valid = need && id >= 0 && id < a.n_pages;
-                if (lane < 8 && need && !valid) {
-                  sh.bad_page[slot] = 1;
-                  atomicMax(a.c.status, STATUS_BAD_PAGE);
+                const unsigned bad = __ballot_sync(0xffffffffu, need && !valid) & 0xffu;
+                if (bad) {
+                  if (lane == 0) {
+                    sh.bad_key[slot] = min(sh.bad_key[slot], (t * kPages + __ffs(bad) - 1) * kChunkPage);
+                    atomicMax(a.c.status, STATUS_BAD_PAGE);
+                  }
+                  __syncwarp();                  // before the copy that the others wait for is issued
                 }
                 // a page that nothing sees, or that does not exist, reads as zeros
                 const int unit = valid ? (id * a.Hkv + it.head) * 4 : a.n_pages * a.Hkv * 4;
@@ -931,7 +936,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
         if (!ok) break;
       }
       tc_fence_after();
-      const bool spoiled = *const_cast<volatile int *>(&sh.bad_page[slot]) != 0;
+      const int bad_key = *const_cast<volatile int *>(&sh.bad_key[slot]);
 #pragma unroll
       for (int o = 1; o < 4; o <<= 1) {
         l_a += __shfl_xor_sync(0xffffffffu, l_a, o);
@@ -969,9 +974,13 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
       if (warp_mine) {
         const bool part = it.flags & (kPartFirst | kPartLater);
         const int64_t part_at = (static_cast<int64_t>(blockIdx.x) * 2 + (it.flags & kPartFirst ? 1 : 0)) * a.rows_cap + row_tile * 128;
-        if (spoiled) {                           // whatever else the row holds, it is undefined
-          l_a = l_b = NAN;
-          ref_a = ref_b = 0.f;
+        if (pos_a >= bad_key) {                  // the row needs the page: whatever else it holds, it is undefined
+          l_a = NAN;
+          ref_a = 0.f;
+        }
+        if (pos_b >= bad_key) {
+          l_b = NAN;
+          ref_b = 0.f;
         }
         if (part && col0 == 0 && (lane & 3) == 0) {
           if (mine_a) a.part_ml[part_at + row_a] = make_float2(ref_a, l_a);

@@ -24,6 +24,42 @@ def _positions(starts, lens, rows):
     return t
 
 
+# ---- bad pages ------------------------------------------------------------------------------------
+@pytest.mark.parametrize("heads,seqs,s,bad", [
+    ((4, 1, 64), [(3, 40), (16, 24)], 1, [1]),               # 64 rows to a tile
+    ((8, 2, 128), [(1, 9), (30, 30), (2, 50)], 1, [1]),      # one tile of 128 rows
+    ((8, 2, 128), [(64, 64), (5, 70)], 0, [2]),              # two
+    ((8, 2, 64), [(200, 300), (1, 1)], 0, [14, 9]),          # several items, every other one from its last keys to its first
+    ((32, 8, 128), [(10, 9000)], 0, [562]),                  # long caches, cut among the CTAs
+    ((32, 8, 128), [(20, 9000), (1, 700)], 0, [562]),
+    ((32, 8, 128), [(40, 9000)], 0, [562, 561]),
+    ((32, 8, 128), [(40, 9000)], 0, [3]),                    # a page that every row needs
+    ((8, 2, 128), [(100, 40)], 0, [1]),                      # rows that see nothing
+])
+def test_a_bad_page_spoils_the_rows_that_need_it(B, heads, seqs, s, bad):
+    Hq, Hkv, hd = heads
+    starts, lens, table, n_pages = _tables(seqs, seed=21)
+    n = int(starts[-1])
+    rng = np.random.default_rng(22)
+    pool = _dev(rng.normal(size=(n_pages, Hkv, 2, 16, hd))).bfloat16()
+    q = _dev(rng.normal(size=(n, Hq, hd))).bfloat16()
+    want, spread, scores = K.attend(_f64(pool), _f64(q), starts, lens, table, np.zeros(q.shape))
+    t = _positions(starts, lens, n)
+    needs = np.zeros(n, dtype=bool)
+    needs[starts[s]:starts[s + 1]] = t[starts[s]:starts[s + 1]] >= 16 * min(bad)
+    assert needs.any()
+    for page in (-1, n_pages):
+        spoiled = table.copy()
+        spoiled[s, bad] = page
+        chunks = _batch(B, starts, lens, spoiled, n, max(c for c, _ in seqs))
+        got = _f64(B.echo_chunk_attention(chunks, q, pool))
+        with pytest.raises(B.EchoError, match="a page id"):
+            chunks.check()
+        assert np.isnan(got[needs]).all()
+        keep = ~needs
+        _check_attention(got[keep], want[keep], spread[keep], scores[keep], np.maximum(t[keep] + 1, 0), 8.0, torch.bfloat16, hd)
+
+
 # ---- waits ----------------------------------------------------------------------------------------
 @pytest.mark.parametrize("heads,seqs", [
     ((32, 8, 128), [(16, 300)] * 40),                        # 64 rows to a tile
