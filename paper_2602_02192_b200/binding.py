@@ -746,9 +746,11 @@ class KVChunks:
     def check(self):
         """Waits for the GPU; raises where a kernel found page ids or lengths out of range (EchoError -7) or gave up
         waiting (-8) since the status was last zero, and zeroes it."""
+        torch.cuda.synchronize(self.device)                  # (the calls may be on other streams than the current one)
         found = int(self.status.item())
         if found:
             self.status.zero_()
+            torch.cuda.synchronize(self.device)
             raise EchoError(-8 if found == 3 else -7, {1: "a page id outside the pool", 4: "lengths outside the limits"}.get(found, ""))
 
 

@@ -60,6 +60,23 @@ def test_a_bad_page_spoils_the_rows_that_need_it(B, heads, seqs, s, bad):
         _check_attention(got[keep], want[keep], spread[keep], scores[keep], np.maximum(t[keep] + 1, 0), 8.0, torch.bfloat16, hd)
 
 
+# ---- status ---------------------------------------------------------------------------------------
+def test_check_waits_for_calls_on_other_streams(B):
+    pool = torch.zeros((2, 1, 2, 16, 64), dtype=torch.bfloat16, device="cuda")
+    k, v = (torch.ones((1, 1, 64), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    one, start = np.array([1], np.int32), np.array([0, 1], np.int32)
+    chunks = _batch(B, start, one, np.array([[9]], np.int32), 1, 1)
+    side = torch.cuda.Stream()
+    for sleep in (0, 200_000_000):                           # (the first time the kernels are loaded); a tenth of a second
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(sleep)
+            B.echo_append_kv(chunks, None, k, v, pool)
+        with pytest.raises(B.EchoError, match="a page id"):
+            chunks.check()
+        chunks.check()
+
+
 # ---- waits ----------------------------------------------------------------------------------------
 @pytest.mark.parametrize("heads,seqs", [
     ((32, 8, 128), [(16, 300)] * 40),                        # 64 rows to a tile
