@@ -74,6 +74,10 @@ constexpr int shift_of(bool half) { return half ? 6 : 0; }
 // of a row's probabilities in a step, a quarter of them in a thread, before its reference has to move (half: 65504 ends it)
 constexpr float most_sum(bool half) { return half ? 131072.0f : 8192.0f; }
 
+// References beyond this (of q . k) are taken off the scores before these are scaled, which is exact where it counts: relative
+// to a rounded product of the two a probability of 1 would be off by 2^(2^-24 times the product), and end in infinity or 0.
+constexpr float kFar = 4194304.0f;
+
 // Costs that the shares are cut by: of a key, and of an item's beginning and end.
 constexpr int kSingleWeight = 6, kPairWeight = 8, kSingleStart = 2 * 1024, kPairStart = 3 * 1024;
 // Measured: with the weights 4 : 8 and half of these starts 40 chunks of 16 to 400 tokens took 437 us instead of 356.
@@ -772,6 +776,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
       const bool mine_a = row_a < n_rows, mine_b = row_b < n_rows, warp_mine = row0 < n_rows;
       float m_a = -INFINITY, m_b = -INFINITY;                         // references (score units)
       float l_a = 0.f, l_b = 0.f;                                     // sums of this thread's columns
+      bool far = false;                                               // a row of the warp has had a far reference
       for (int i = 0; i < steps; ++i) {          // of 64 keys
         const int tile = paired ? i >> 1 : i, key_off = 64 * (paired ? i & 1 : w);
         const int key0 = (it.flags & kBackwards ? it.t1 - 1 - tile : it.t0 + tile) * kKeys + key_off;
@@ -795,9 +800,9 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
               if (8 * b + 1 > last_b) s[4 * b + 3] = 0xff800000u;
             }
           }
-          // With the references as they are, unless a row has none yet: maxima take a quarter of a step's time, and a
-          // reference that is too low shows in the sum.  Where one does, once more with maxima.
-          bool careful = __any_sync(0xffffffffu, (mine_a && m_a == -INFINITY) || (mine_b && m_b == -INFINITY));
+          // With the references as they are, unless a row has none yet or a far one: maxima take a quarter of a step's
+          // time, and a reference that is too low shows in the sum.  Where one does, once more with maxima.
+          bool careful = __any_sync(0xffffffffu, (mine_a && m_a == -INFINITY) || (mine_b && m_b == -INFINITY)) || far;
           while (true) {
             if (careful) {
               float to_a = m_a, to_b = m_b;
@@ -829,6 +834,27 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                   for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * ((e & 2) ? fix_b : fix_a));
                   tc_st_32cols(t_o + b * 32, o);
                 }
+              }
+              const bool far_a = fabsf(m_a) > kFar && fabsf(m_a) < INFINITY, far_b = fabsf(m_b) > kFar && fabsf(m_b) < INFINITY;
+              if (__any_sync(0xffffffffu, far_a || far_b)) {
+                // (in place of the block below, which this leaves as fast as it is; every further step comes here too)
+                far = true;
+                const float off_a = far_a ? m_a : 0.f, off_b = far_b ? m_b : 0.f;
+                const float base_a = far_a ? kShift : m_a == -INFINITY ? 0.f : m_a == INFINITY ? NAN : kShift - m_a * c;
+                const float base_b = far_b ? kShift : m_b == -INFINITY ? 0.f : m_b == INFINITY ? NAN : kShift - m_b * c;
+                sum_a = sum_b = make_float2(0.f, 0.f);
+#pragma unroll
+                for (int b = 0; b < 8; ++b) {
+                  const float ax = ex2(fmaf(__uint_as_float(s[4 * b]) - off_a, c, base_a));
+                  const float ay = ex2(fmaf(__uint_as_float(s[4 * b + 1]) - off_a, c, base_a));
+                  const float bx = ex2(fmaf(__uint_as_float(s[4 * b + 2]) - off_b, c, base_b));
+                  const float by = ex2(fmaf(__uint_as_float(s[4 * b + 3]) - off_b, c, base_b));
+                  sum_a.x += ax + ay;
+                  sum_b.x += bx + by;
+                  p[2 * b] = cvt16x2(ax, ay, HALF);
+                  p[2 * b + 1] = cvt16x2(bx, by, HALF);
+                }
+                break;
               }
             }
             const float base_a = m_a == -INFINITY ? 0.f : m_a == INFINITY ? NAN : kShift - m_a * c;

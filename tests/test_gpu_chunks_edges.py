@@ -77,6 +77,45 @@ def test_check_waits_for_calls_on_other_streams(B):
         chunks.check()
 
 
+# ---- scores near the ends of their format ---------------------------------------------------------
+@pytest.mark.parametrize("heads,seqs", [
+    ((4, 2, 64), [(5, 300), (9, 9)]),                        # 64 rows to a tile
+    ((8, 2, 128), [(30, 1000), (1, 70)]),
+    ((8, 2, 128), [(150, 700)]),
+    ((8, 2, 64), [(130, 130), (40, 9000)]),
+])
+@pytest.mark.parametrize("dtype,size", [(torch.float16, 60000.0), (torch.float16, 20000.0), (torch.bfloat16, 1.5e19), (torch.bfloat16, 1e13),
+                                        (torch.bfloat16, 5e4)])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+def test_scores_near_the_ends_of_their_format(B, heads, seqs, dtype, size, sign):
+    """One element of q and k makes the score, so that it is a product that fp32 holds to a rounding; neighbouring keys'
+    scores lie so far apart that a row's largest has all of the probability: its value comes out as it is.  Every third row
+    has ordinary queries beside them, whose scores are 0 here: it has the mean of the values."""
+    Hq, Hkv, hd = heads
+    starts, lens, table, n_pages = _tables(seqs, seed=23)
+    n = int(starts[-1])
+    rng = np.random.default_rng(24)
+    pool = np.zeros((n_pages, Hkv, 2, 16, hd))
+    pool[:, :, 1] = rng.normal(size=pool[:, :, 1].shape)
+    # 64 sizes, a 128th of the largest apart; each position's at random
+    pool[:, :, 0, :, 3] = sign * size * (1 - rng.integers(0, 64, size=pool[:, :, 0, :, 3].shape) / 128)
+    pool = _dev(pool).to(dtype)
+    q = torch.zeros((n, Hq, hd), dtype=dtype, device="cuda")
+    q[..., 3] = size
+    flat = np.arange(n) % 3 == 2
+    q[torch.from_numpy(flat).cuda()] = 0
+    chunks = _batch(B, starts, lens, table, n, max(c for c, _ in seqs))
+    got = _f64(B.echo_chunk_attention(chunks, q, pool))
+    chunks.check()
+    want, spread, scores = K.attend(_f64(pool), _f64(q), starts, lens, table, np.zeros(q.shape))
+    t = _positions(starts, lens, n)
+    assert np.isfinite(want).all()
+    # equal probabilities (of equal scores) are equal numbers of the format, at most 2^-8 apart from their fp32 values
+    h = HALF_STEP[dtype]
+    tol = h * np.abs(want) + spread * (1 + h) * (h + 2 * E * (t[:, None, None] + 17)) + 2 * TINY[dtype]
+    assert np.all(np.abs(got - want) <= tol), np.argwhere(~(np.abs(got - want) <= tol))[:5]
+
+
 # ---- waits ----------------------------------------------------------------------------------------
 @pytest.mark.parametrize("heads,seqs", [
     ((32, 8, 128), [(16, 300)] * 40),                        # 64 rows to a tile
