@@ -445,8 +445,8 @@ typedef struct echo_kv_chunks {
   int32_t n_rows;             /* rows of the arrays; those of no sequence are left as they are.  0: nothing is
                                  done (with either 0 the tables, q, k, v, the outputs and the workspace may be
                                  NULL, and pt_width and max_chunk 0)                                          */
-  int32_t pt_width;           /* at most 2^26                                                                 */
-  int32_t max_chunk;          /* no chunk is longer (sizes workspaces, chooses tiles)                         */
+  int32_t pt_width;           /* 1 to 2^26                                                                    */
+  int32_t max_chunk;          /* at least 1; no chunk is longer (sizes workspaces, chooses tiles)             */
 } echo_kv_chunks;
 
 /* Appends the chunks' keys and values, with the position rotation on the way (rotate-half pairs (j, j + hd/2), angle

@@ -725,8 +725,8 @@ class KVChunks:
     row_starts int32 [n_seqs + 1], kv_lens int32 [n_seqs] (keys once the new tokens are appended), page_table int32
     [n_seqs][width]: contiguous tensors of one GPU, read by the kernels when they run, so that a captured step follows
     what is written into them.  n_rows: rows of q, k, v and the outputs (those behind the last sequence are left as they
-    are); max_chunk: no sequence brings more new tokens.  status: int32 tensor of one element that receives what the
-    kernels find (its own, zeroed, by default): see check()."""
+    are); max_chunk: no sequence brings more new tokens (0, of a batch that has none, is as 1).  status: int32 tensor of one
+    element that receives what the kernels find (its own, zeroed, by default): see check()."""
 
     def __init__(self, row_starts: torch.Tensor, kv_lens: torch.Tensor, page_table: torch.Tensor, n_rows: int, max_chunk: int,
                  status: Optional[torch.Tensor] = None):
@@ -737,7 +737,8 @@ class KVChunks:
         assert page_table.dim() == 2 and page_table.shape[0] == n
         for x in (row_starts, kv_lens, page_table, status):
             assert x.is_cuda and x.device == kv_lens.device and x.dtype is torch.int32 and x.is_contiguous()
-        self.device, self.n_rows, self.max_chunk, self.status = kv_lens.device, int(n_rows), int(max_chunk), status
+        self.device, self.n_rows, self.status = kv_lens.device, int(n_rows), status
+        self.max_chunk = int(max_chunk) or 1     # (the library wants at least 1 where there are rows)
         self._keep = (row_starts, kv_lens, page_table)
         self.table = EchoKVChunks(row_starts.data_ptr(), kv_lens.data_ptr(), page_table.data_ptr(), status.data_ptr(), n,
                                   self.n_rows, page_table.shape[1], self.max_chunk)

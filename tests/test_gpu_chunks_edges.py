@@ -77,6 +77,19 @@ def test_check_waits_for_calls_on_other_streams(B):
         chunks.check()
 
 
+def test_a_batch_that_says_no_new_tokens(B):
+    """max_chunk = 0 with rows that no sequence has: nothing to do, and no error, nor a finding."""
+    i32 = dict(dtype=torch.int32, device="cuda")
+    chunks = B.KVChunks(torch.zeros(4, **i32), torch.full((3,), 5, **i32), torch.zeros((3, 1), **i32), 7, 0)
+    pool = torch.ones((2, 2, 2, 16, 64), dtype=torch.bfloat16, device="cuda")
+    q, k, v = (torch.ones((7, h, 64), dtype=torch.bfloat16, device="cuda") for h in (4, 2, 2))
+    out = torch.full_like(q, 7.0)
+    assert B.echo_append_kv(chunks, q, k, v, pool, out=out) is out and bool((out == 7).all())
+    assert B.echo_chunk_attention(chunks, q, pool, out=out) is out and bool((out == 7).all())
+    chunks.check()
+    assert bool((pool == 1).all())
+
+
 # ---- scores near the ends of their format ---------------------------------------------------------
 @pytest.mark.parametrize("heads,seqs", [
     ((4, 2, 64), [(5, 300), (9, 9)]),                        # 64 rows to a tile
