@@ -472,9 +472,10 @@ int echo_append_kv(const void *q, const void *k, const void *v, int32_t in_forma
  *   q           dev rows of [Hq][hd] in `format` (0 bf16, 1 half; the cache's), q_stride elements from row to row (a
  *               multiple of 8, up to 2^30), 16-byte aligned; rotated (echo_append_kv)
  *   kv_pool     dev, 16-byte aligned
- *   out         dev [n_rows][Hq][hd] in `format`, 16-byte aligned; may not overlap q, the pool or the workspace
+ *   out         dev [n_rows][Hq][hd] in `format`, 16-byte aligned
  *   workspace   dev, echo_chunk_attention_workspace_bytes(...) bytes, 16-byte aligned: partial results of long caches.
  *               Only this call's kernels use it: calls that may overlap on the GPU need one each.
+ * Nothing that is written (out, the workspace, the status) may overlap anything else (ECHO_ERR_INVALID).
  * hd 64 or 128, at most 128 query heads to a kv head, n_pages Hkv at most 2^26 (else ECHO_ERR_UNSUPPORTED).  Sequences
  * with lengths outside the limits are passed over (status 4); rows that need a page whose id is outside the pool become
  * NaN (status 1). */

@@ -190,13 +190,14 @@ extern "C" int echo_append_kv(const void *q, const void *k, const void *v, int32
   if (none) return ECHO_OK;
   bool vec = true;
   const uint64_t pool = pool_bytes(n_pages, Hkv, hd), outs = static_cast<uint64_t>(a.c.n_rows) * Hq * hd * 2;
-  if (ranges_meet(kv_pool, pool, out_q, outs)) return ECHO_ERR_INVALID;
+  if (ranges_meet(kv_pool, pool, out_q, outs) || meets_tables(a.c, kv_pool, pool) || meets_tables(a.c, out_q, outs) || status_in_tables(a.c))
+    return ECHO_ERR_INVALID;
   for (int i = 0; i < 3; ++i) {
     if (!given[i]) continue;
     const uintptr_t p = reinterpret_cast<uintptr_t>(given[i]);
     if (p % eb || strides[i] > (int64_t(1) << 30)) return ECHO_ERR_INVALID;
     const uint64_t bytes = (static_cast<uint64_t>(a.c.n_rows - 1) * strides[i] + widths[i]) * eb;
-    if (ranges_meet(given[i], bytes, kv_pool, pool)) return ECHO_ERR_INVALID;
+    if (ranges_meet(given[i], bytes, kv_pool, pool) || ranges_meet(given[i], bytes, a.c.status, 4)) return ECHO_ERR_INVALID;
     // the rotated queries may replace the given ones, element for element
     const bool same = i == 0 && q == out_q && in_format == kv_format && (q_stride == widths[0] || a.c.n_rows == 1);
     if (!same && ranges_meet(given[i], bytes, out_q, outs)) return ECHO_ERR_INVALID;

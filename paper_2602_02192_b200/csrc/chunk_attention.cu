@@ -1241,6 +1241,9 @@ int echo_chunk_attention(const void *q, int64_t q_stride, const void *kv_pool, i
       ranges_meet(out, outs, workspace, need) || ranges_meet(workspace, need, q, qs) ||
       ranges_meet(workspace, need, kv_pool, pool_bytes(n_pages, Hkv, hd)))
     return ECHO_ERR_INVALID;
+  if (meets_tables(a.c, out, outs) || meets_tables(a.c, workspace, need) || status_in_tables(a.c) ||
+      ranges_meet(a.c.status, 4, q, qs) || ranges_meet(a.c.status, 4, kv_pool, pool_bytes(n_pages, Hkv, hd)))
+    return ECHO_ERR_INVALID;
   a.limit.ns = g_wait_limit_ns.load(std::memory_order_relaxed);
   a.limit.look = a.limit.ns < kWaitLimitNs ? 0 : 255;
   a.out = static_cast<uint16_t *>(out);

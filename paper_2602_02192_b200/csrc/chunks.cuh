@@ -38,6 +38,18 @@ inline bool ranges_meet(const void *a, uint64_t na, const void *b, uint64_t nb) 
   const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
   return a && b && na && nb && x < y + nb && y < x + na;
 }
+// An array that a call writes, and the batch's tables and status.
+inline bool meets_tables(const ChunkArgs &c, const void *p, uint64_t bytes) {
+  const uint64_t seqs = static_cast<uint64_t>(c.S);
+  return ranges_meet(p, bytes, c.row_starts, (seqs + 1) * 4) || ranges_meet(p, bytes, c.kv_lens, seqs * 4) ||
+         ranges_meet(p, bytes, c.page_table, seqs * c.pt_width * 4) || ranges_meet(p, bytes, c.status, 4);
+}
+// The status, which every call writes, and the tables.
+inline bool status_in_tables(const ChunkArgs &c) {
+  ChunkArgs tables = c;
+  tables.status = nullptr;
+  return meets_tables(tables, c.status, 4);
+}
 
 #ifdef __CUDACC__
 struct SeqSpan {
