@@ -129,6 +129,135 @@ def test_scores_near_the_ends_of_their_format(B, heads, seqs, dtype, size, sign)
     assert np.all(np.abs(got - want) <= tol), np.argwhere(~(np.abs(got - want) <= tol))[:5]
 
 
+# ---- every tile of keys, once ---------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("heads,seqs,q_size", [
+    ((2, 1, 64), [(1, 33333)], 1.0),
+    ((8, 8, 64), [(1, 30000)] * 3 + [(140, 4000)], 0.1),
+    ((8, 8, 128), [(1, 20000)] * 4 + [(2, 17)], 1.0),
+    ((8, 2, 64), [(20, 33000)], 0.1),                        # 80 rows
+    ((8, 2, 128), [(70, 12000), (100, 5000)], 0.1),          # two tiles of rows, every other pair from the last keys to the first
+    ((4, 4, 64), [(260, 9000)], 1.0),
+])
+def test_no_tile_of_a_long_cache_is_lost_or_taken_twice(B, heads, seqs, q_size, dtype):
+    """The values of the 128 keys of a tile are 1 in one column, another for each tile (hd tiles long), and 0 elsewhere: a
+    column of the result is the probability of its few tiles, and all roundings are relative to that.  What one tile adds is
+    well above them, which is asserted."""
+    Hq, Hkv, hd = heads
+    starts, lens, table, n_pages = _tables(seqs, seed=25)
+    n = int(starts[-1])
+    rng = np.random.default_rng(26)
+    pool = torch.zeros((n_pages, Hkv, 2, 16, hd), dtype=dtype, device="cuda")
+    pool[:, :, 0] = _dev(rng.normal(size=(n_pages, Hkv, 16, hd))).to(dtype)
+    for s, (_, kv) in enumerate(seqs):
+        for p in range(-(-kv // 16)):
+            pool[int(table[s, p]), :, 1, :, (p // 8) % hd] = 1
+    q = _dev(rng.normal(size=(n, Hq, hd)) * q_size).to(dtype)
+    chunks = _batch(B, starts, lens, table, n, max(c for c, _ in seqs))
+    got = _f64(B.echo_chunk_attention(chunks, q, pool))
+    chunks.check()
+    h, row = HALF_STEP[dtype], 0
+    k64, q64 = pool[:, :, 0].double(), q.double()
+    for s, (c, kv) in enumerate(seqs):
+        k = k64[torch.from_numpy(table[s, :-(-kv // 16)]).long().cuda()].transpose(0, 1).reshape(Hkv, -1, hd)[:, :kv]
+        rows = q64[row:row + c].view(c, Hkv, -1, hd)
+        seen = torch.arange(kv, device="cuda")[None] <= torch.arange(kv - c, kv, device="cuda")[:, None]
+        z = torch.einsum("nhgd,hkd->nhgk", rows, k) / hd ** 0.5
+        size = torch.einsum("nhgd,hkd->nhgk", rows.abs(), k.abs()) / hd ** 0.5
+        p = torch.softmax(z.masked_fill(~seen[:, None, None], -np.inf), dim=-1)
+        pad = -kv % 128
+        tiles = torch.nn.functional.pad(p, (0, pad)).view(c, Hkv, -1, (kv + pad) // 128, 128).sum(dim=-1)
+        want = torch.zeros((c, Hkv, Hq // Hkv, hd), dtype=torch.float64, device="cuda")
+        want.index_add_(3, torch.arange(tiles.shape[3], device="cuda") % hd, tiles)
+        d = 2 * E * (hd + 8) * size.amax(dim=-1, keepdim=True)
+        tol = h * want + (1 + h) * want * (h + 2 * d + 2 * E * (kv + 16)) + TINY[dtype]
+        if dtype == torch.float16:
+            tol += p.amax(dim=-1, keepdim=True) * kv * 2.0 ** -31
+        err = (torch.from_numpy(got[row:row + c]).cuda().view(want.shape) - want).abs()
+        assert bool((err <= tol).all()), (s, (~(err <= tol)).nonzero()[:5])
+        whole = tiles[..., :max((kv - c + 1) // 128, 0)]             # tiles that all rows see
+        bound = tol.gather(3, (torch.arange(whole.shape[3], device="cuda") % hd).expand(whole.shape))
+        assert whole.shape[3] == 0 or bool((whole > 2 * bound).double().mean() > 0.999)
+        row += c
+
+
+@pytest.mark.parametrize("heads,seqs", [
+    ((4, 2, 64), [(1, 1), (5, 700), (12, 129)]),
+    ((32, 8, 128), [(1, 9000), (16, 300)]),
+    ((10, 2, 64), [(40, 2000), (130, 130), (1, 1001)]),
+    ((64, 8, 128), [(70, 1500), (3, 129)]),
+])
+@pytest.mark.parametrize("size", [0.01, 1.0, 5.0])
+def test_small_probabilities_in_half_precision(B, heads, seqs, size):
+    """A probability is rounded by half of the format's step, or where it is below the normal numbers by 2^-25 of a scale on
+    which the row's largest is at least 2^6: 2^-31 of that.  The other roundings are relative, as in the tests of the chunks."""
+    Hq, Hkv, hd = heads
+    starts, lens, table, n_pages = _tables(seqs, seed=35)
+    n = int(starts[-1])
+    rng = np.random.default_rng(36)
+    pool = _dev(rng.normal(size=(n_pages, Hkv, 2, 16, hd))).half()
+    q = _dev(rng.normal(size=(n, Hq, hd)) * size).half()
+    chunks = _batch(B, starts, lens, table, n, max(c for c, _ in seqs))
+    got = _f64(B.echo_chunk_attention(chunks, q, pool))
+    chunks.check()
+    want, spread, scores = K.attend(_f64(pool), _f64(q), starts, lens, table, np.zeros(q.shape))
+    keys = _positions(starts, lens, n)[:, None, None] + 1
+    h, top = HALF_STEP[torch.float16], float(pool.abs().max())
+    d = 2 * E * (hd + 8) * scores[:, :, None]
+    tol = h * np.abs(want) + (1 + h) * spread * (h + 2 * d + 2 * E * (keys + 16)) + TINY[torch.float16] + keys * 2.0 ** -31 * top
+    assert np.all(np.abs(got - want) <= tol), np.argwhere(~(np.abs(got - want) <= tol))[:5]
+
+
+
+# ---- workspaces -----------------------------------------------------------------------------------
+@pytest.mark.parametrize("heads,longest", [
+    ((32, 8, 128), 1), ((32, 8, 128), 16), ((32, 8, 128), 17), ((32, 8, 128), 32), ((32, 8, 128), 33),       # 64 rows, 128, two tiles
+    ((10, 2, 64), 1), ((10, 2, 64), 12), ((10, 2, 64), 13), ((10, 2, 64), 25), ((10, 2, 64), 26),
+    ((128, 1, 64), 1), ((128, 1, 64), 2), ((48, 1, 128), 2), ((48, 1, 128), 3), ((7, 1, 128), 9),
+])
+def test_a_workspace_of_the_stated_size_is_enough(B, heads, longest):
+    Hq, Hkv, hd = heads
+    seqs = [(longest, 9000), (1, 1), (longest, longest + 2000), (longest, longest)]
+    starts, lens, table, n_pages = _tables(seqs, seed=27)
+    n = int(starts[-1])
+    g = torch.Generator(device="cuda").manual_seed(28)
+    pool = torch.randn((n_pages, Hkv, 2, 16, hd), generator=g, device="cuda").bfloat16()
+    q = torch.randn((n, Hq, hd), generator=g, device="cuda").bfloat16()
+    chunks = _batch(B, starts, lens, table, n, longest)
+    want = B.echo_chunk_attention(chunks, q, pool)
+    need = B.lib.echo_chunk_attention_workspace_bytes(longest, Hq, Hkv, hd)
+    assert need % 4 == 0
+    guard = 4096
+    whole = torch.full((need + 2 * guard,), 0xA5, dtype=torch.uint8, device="cuda")
+    got = B.echo_chunk_attention(chunks, q, pool, workspace=whole[guard:guard + need])
+    chunks.check()
+    assert torch.equal(got, want)
+    assert bool((whole[:guard] == 0xA5).all()) and bool((whole[guard + need:] == 0xA5).all())
+    assert bool((whole[guard:guard + need] != 0xA5).any())               # it was used
+    with pytest.raises(B.EchoError, match="ECHO_ERR_INVALID"):
+        B.echo_chunk_attention(chunks, q, pool, workspace=whole[guard:guard + need - 1], out=torch.empty_like(q))
+
+
+def test_rows_in_front_of_the_first_sequence(B):
+    """row_starts may begin behind row 0: the rows before are left as they are."""
+    Hq, Hkv, hd, front = 8, 2, 64, 5
+    starts, lens, table, n_pages = _tables([(3, 40), (0, 9), (70, 90)], seed=29)
+    n = int(starts[-1])
+    g = torch.Generator(device="cuda").manual_seed(30)
+    pool = torch.randn((n_pages, Hkv, 2, 16, hd), generator=g, device="cuda").bfloat16()
+    q, k, v = (torch.randn((n + front, H, hd), generator=g, device="cuda").bfloat16() for H in (Hq, Hkv, Hkv))
+    pools = [pool.clone(), pool.clone()]
+    plain, moved = _batch(B, starts, lens, table, n, 70), _batch(B, starts + front, lens, table, n + front, 70)
+    a = B.echo_append_kv(plain, q[front:], k[front:], v[front:], pools[0])
+    b = B.echo_append_kv(moved, q, k, v, pools[1], out=torch.full_like(q, 7.0))
+    assert torch.equal(pools[0], pools[1]) and torch.equal(a, b[front:]) and bool((b[:front] == 7).all())
+    x = B.echo_chunk_attention(plain, a, pools[0])
+    y = B.echo_chunk_attention(moved, b, pools[0], out=torch.full_like(q, 7.0))
+    assert torch.equal(x, y[front:]) and bool((y[:front] == 7).all())
+    plain.check()
+    moved.check()
+
+
 # ---- waits ----------------------------------------------------------------------------------------
 @pytest.mark.parametrize("heads,seqs", [
     ((32, 8, 128), [(16, 300)] * 40),                        # 64 rows to a tile
