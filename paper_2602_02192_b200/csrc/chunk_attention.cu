@@ -835,7 +835,8 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                   tc_st_32cols(t_o + b * 32, o);
                 }
               }
-              const bool far_a = fabsf(m_a) > kFar && fabsf(m_a) < INFINITY, far_b = fabsf(m_b) > kFar && fabsf(m_b) < INFINITY;
+              const bool far_a = mine_a && fabsf(m_a) > kFar && fabsf(m_a) < INFINITY;      // (other rows hold anything)
+              const bool far_b = mine_b && fabsf(m_b) > kFar && fabsf(m_b) < INFINITY;
               if (__any_sync(0xffffffffu, far_a || far_b)) {
                 // (in place of the block below, which this leaves as fast as it is; every further step comes here too)
                 far = true;

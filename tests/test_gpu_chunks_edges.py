@@ -129,6 +129,26 @@ def test_scores_near_the_ends_of_their_format(B, heads, seqs, dtype, size, sign)
     assert np.all(np.abs(got - want) <= tol), np.argwhere(~(np.abs(got - want) <= tol))[:5]
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_rows_of_a_tile_that_hold_nothing_have_no_part_in_the_others(B, dtype):
+    """100 query heads to a kv head leave 28 rows of each tile as an earlier call left them: with queries of any size in
+    them, the results are the same bit for bit."""
+    S, kv, hd, n = 200, 300, 128, 3
+    starts, lens = np.arange(S + 1, dtype=np.int32) * n, np.full(S, kv, np.int32)
+    pages = -(-kv // 16)
+    rng = np.random.default_rng(37)
+    table = rng.permutation(S * pages).reshape(S, pages).astype(np.int32)
+    pool = _dev(rng.normal(size=(S * pages, 1, 2, 16, hd)) * 20).to(dtype)
+    q = _dev(rng.normal(size=(S * n, 100, hd)) / 20).to(dtype)
+    chunks = _batch(B, starts, lens, table, S * n, n)
+    got = []
+    for size in (0.0, 1e3, 6e4, float("inf")):               # scores of 0, 10^5, 10^7 and infinities
+        B.echo_chunk_attention(chunks, torch.full((S * n, 128, hd), size, dtype=dtype, device="cuda"), pool)
+        got.append(B.echo_chunk_attention(chunks, q, pool))
+    chunks.check()
+    assert all(torch.equal(got[0], x) for x in got[1:])
+
+
 # ---- every tile of keys, once ---------------------------------------------------------------------
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
 @pytest.mark.parametrize("heads,seqs,q_size", [
