@@ -476,6 +476,9 @@ int echo_append_kv(const void *q, const void *k, const void *v, int32_t in_forma
  *   workspace   dev, echo_chunk_attention_workspace_bytes(...) bytes, 16-byte aligned: partial results of long caches.
  *               Only this call's kernels use it: calls that may overlap on the GPU need one each.
  * Nothing that is written (out, the workspace, the status) may overlap anything else (ECHO_ERR_INVALID).
+ * Sequences may name the same pages, and each reads them for itself: single tokens of samples that share their prompt are
+ * echo_decode_attention's, which reads it once for a group.  max_chunk chooses the tiles of the whole batch: many single
+ * tokens beside a long chunk are better a call of their own.
  * hd 64 or 128, at most 128 query heads to a kv head, n_pages Hkv at most 2^26 (else ECHO_ERR_UNSUPPORTED).  Sequences
  * with lengths outside the limits are passed over (status 4); rows that need a page whose id is outside the pool become
  * NaN (status 1). */

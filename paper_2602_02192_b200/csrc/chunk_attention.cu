@@ -23,10 +23,16 @@
 // launch joins them in key order: no atomics, equal inputs give equal outputs.  Every other item of a head takes its key
 // tiles from the last to the first: those are what L2 may still hold.
 //
-// A row's reference (what its exponents are relative to) is its maximum over the item's first step.  It moves when the
-// probabilities of 64 keys, relative to it, add up to more than 2^13 (half: 2^17, of 2^6 for the reference): the maximum
-// has then grown.  So O is hardly ever rescaled, most steps need no maxima, and a probability that is used is at most 2^13
-// (2^15), which the formats hold.
+// A row's reference (what its exponents are relative to) is its maximum over the item's first step.  It moves when a
+// step's probabilities, relative to it, add up to more than 2^11 (half: 2^15, of 2^6 for the reference) in one of the
+// row's four threads, which have sixteen each: the maximum has then grown.  So O is hardly ever rescaled, most steps need no
+// maxima, and a probability that is used is at most 2^11 (2^15), which the formats hold.
+//
+// Probabilities are rounded to the cache's format: the second product wants both operands in it, and V is the caller's.  The
+// row's sum is that of the fp32 values.  Measured, the distance to the 64-bit result is 1.1 to 1.7 times that of fp32
+// probabilities (of 131001 keys, bf16: 0.0019 to 0.0027 of the result's norm, where rounding the result alone makes 0.0016).
+// The sum of the rounded values instead would take 1 to 11 % off that distance, and 2048 tokens over 14336 453 us (422).  A
+// second product, of what the rounding leaves, would turn a visible infinite value into NaN (0 times it).
 //
 // What a row does not see has no part in it: masked scores are replaced, not added to.  A masked probability is 0, but
 // 0 times an undefined value would not be: where a step has keys that only some of its rows see, their values are looked
@@ -37,7 +43,7 @@
 // scheduler, and what one waited for the other could not fill (2048 tokens over 14336: 447 us, with 16 rows 431).
 //
 // Measured (32/8 heads of 128, bf16, in bursts; in a run of them the SM clock falls with the power): 256 single tokens over
-// 512 to 2559 keys 258 us, 0.96 of the copy rate; 2048 tokens over 14336 424 us, 1.21 PFLOP/s.  Few rows are bound by HBM
+// 512 to 2559 keys 257 us, 0.96 of the copy rate; 2048 tokens over 14336 422 us, 1.22 PFLOP/s.  Few rows are bound by HBM
 // (by power in a run), long chunks of heads of 128 by the issue of MMAs: 12 to a step, about 64 cycles each, where the eight of
 // Q K^T with their 64 keys have half the work of the four of P V.  S of 128 keys would halve their number, but with two O
 // there is room for one such S a stream, and then its products wait for its softmax (452 us with S of 128, 499 with S of
@@ -71,8 +77,8 @@ constexpr int kDevices = 64;                   // whose properties are remembere
 // Probabilities are relative to 2^kShift for a score that equals the reference.  Half precision ends at 2^-24 below: with 1
 // for the largest, 100,000 keys whose scores lie 18 below it would lose all that they add up to (bf16 ends at 2^-133).
 constexpr int shift_of(bool half) { return half ? 6 : 0; }
-// of a row's probabilities in a step, a quarter of them in a thread, before its reference has to move (half: 65504 ends it)
-constexpr float most_sum(bool half) { return half ? 131072.0f : 8192.0f; }
+// of a thread's sixteen probabilities of a row's step before its reference has to move (half: 65504 ends it)
+constexpr float most_sum(bool half) { return half ? 32768.0f : 2048.0f; }
 
 // References beyond this (of q . k) are taken off the scores before these are scaled, which is exact where it counts: relative
 // to a rounded product of the two a probability of 1 would be off by 2^(2^-24 times the product), and end in infinity or 0.
@@ -80,7 +86,8 @@ constexpr float kFar = 4194304.0f;
 
 // Costs that the shares are cut by: of a key, and of an item's beginning and end.
 constexpr int kSingleWeight = 6, kPairWeight = 8, kSingleStart = 2 * 1024, kPairStart = 3 * 1024;
-// Measured: with the weights 4 : 8 and half of these starts 40 chunks of 16 to 400 tokens took 437 us instead of 356.
+// Measured with heads of 128: with the weights 4 : 8 and half of these starts 40 chunks of 16 to 400 tokens took 437 us instead
+// of 356.  Heads of 64 and tiles of 64 rows, whose keys cost less, are cut by the same ratio: shares are then less even.
 constexpr int kLeastShare = 1024;              // of a CTA that has work: little work goes to few CTAs
 
 // FEW: no item has more than 64 rows.  MMAs of 64 rows, which take less power (a decode step is bound by HBM in a burst and by
@@ -755,7 +762,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
     const uint32_t lanes = static_cast<uint32_t>(lane0) << 16;
     const uint32_t t_s0 = tmem + lanes + w * 128, t_o = tmem + lanes + 256 + w * 128;
     const float c = a.scale_log2;
-    constexpr float kShift = shift_of(HALF), kMost = most_sum(HALF) / 4;
+    constexpr float kShift = shift_of(HALF), kMost = most_sum(HALF);
     const int row_a = row0 + (lane >> 2), row_b = row_a + 8, col = 2 * (lane & 3);      // of every eight columns: col, col + 1
     const int tok_a = row_a / a.group, tok_b = row_b / a.group;
     int n_item = 0, steps_done = 0, tiles_done = 0, looks = 0, joins = 0;
